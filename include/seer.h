@@ -21,8 +21,8 @@
  *     the products then only read.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All
  *     device work is enqueued on it.  seer_spmv, seer_spmv_auto, seer_spmv_model and
- *     seer_spmv_prepared return without waiting; seer_features, seer_spmv_prepare and
- *     seer_spmv_plan wait for their own result because they return host values.
+ *     seer_spmv_prepared return without waiting, and so do all calls of a routed layer (seer_route to
+ *     seer_grad_clip); seer_features, seer_spmv_prepare and seer_spmv_plan wait for their own result because they return host values.
  *   - Every call returns SEER_OK (0) or a negative seer_status; on error no output
  *     is written.  Nothing throws or aborts.  Matrix contents (monotone row_ptr,
  *     column range) are NOT validated: they are the caller's contract.
@@ -55,7 +55,8 @@ typedef enum {
     SEER_EWORKSPACE = -4, /* workspace missing, misaligned or too small               */
     SEER_EHIP = -5,       /* a HIP runtime call failed; see seer_last_hip_error()     */
     SEER_ELIMIT = -6      /* seer_spmv_auto_static: the matrix needs more scratch than
-                             the library's built-in array holds                         */
+                             the library's built-in array holds; seer_route, seer_i8_product:
+                             more experts or columns than they take                     */
 } seer_status;
 
 /* Kernel ids: the CSR rows of Table II ("load balancing schedules"), in its order. */
@@ -501,6 +502,127 @@ int seer_gather_sum(const int32_t *idx, const float *val, size_t n, const float 
  * and stores the mean wall-clock nanoseconds per decision in *ns.  HOST only. */
 int seer_model_host_ns(const seer_model *model, int32_t rows, int32_t cols, int32_t nnz, int32_t reps,
                        double *ns);
+
+/* ---------------------------------------------------------------------------------------
+ * A routed layer: every token is sent to a few of many experts, each expert multiplies the rows
+ * it is sent, and the results come back to the tokens, weighted.  The router's choices are a
+ * sparse (experts x tokens) matrix with rows as uneven as any above; sorting the tokens by expert
+ * writes its CSR form, and bringing rows to the experts and back are products of it and of its
+ * transpose with a dense matrix.  The same rules as above hold: caller's memory, asynchronous on
+ * `stream`, capturable, a status and no output on an error.  Contents (the entries of a routing
+ * or of group offsets) are the caller's contract, as a matrix's are, where not said otherwise.
+ * Outputs must not overlap inputs or one another (SEER_EINVAL) where not said otherwise. */
+
+typedef enum {
+    SEER_F32 = 0,
+    SEER_BF16 = 1,
+    SEER_F16 = 2,
+    SEER_I8 = 3,
+    SEER_I32 = 4,
+    SEER_I64 = 5
+} seer_type;
+
+/* A dense matrix: element (i, j) at data[i * ld + j], ld >= cols counted in elements.  data:
+ * DEVICE, a multiple of the element size (16-byte aligned rows are faster); it may be NULL if
+ * there are no elements.  rows and cols below 2^31. */
+typedef struct {
+    void *data;
+    int64_t rows, cols, ld;
+    int32_t type; /* seer_type */
+} seer_dense;
+
+/* The order of tokens * choices choices by expert.  Choice c = t * choices + k is the k-th choice
+ * of token t; a slot is a place in the order.  All pointers DEVICE, caller-owned. */
+#define SEER_MAX_EXPERTS 4096
+typedef struct {
+    int32_t tokens, choices, experts; /* experts in 1 .. SEER_MAX_EXPERTS, tokens * choices < 2^31 */
+    int32_t *expert_ptr;  /* [experts + 1]: expert e has the slots expert_ptr[e] .. expert_ptr[e + 1] - 1: the
+                             row_ptr of the (experts x tokens) matrix                                     */
+    int32_t *slot_choice; /* [tokens * choices]: the choice in each slot: by expert, then by number; choices
+                             that are no expert's lie behind expert_ptr[experts], by number               */
+    int32_t *choice_slot; /* [tokens * choices]: the slot p of each choice, as p, or as -1 - p for a choice
+                             that is no expert's                                                          */
+} seer_routing;
+
+/* Sorts the choices by expert: fills r's three arrays.  expert: DEVICE [tokens][choices], of index_type
+ * SEER_I32 or SEER_I64; an entry outside [0, experts) (-1 for padding, say) is no expert's.  A token may
+ * choose an expert more than once.  The order is stable, and the same on every run.
+ * workspace: >= seer_route_workspace_bytes(tokens, choices, experts) (0 for small ones, then it may be
+ * NULL).  SEER_ELIMIT for more than SEER_MAX_EXPERTS experts. */
+int seer_route(const void *expert, int32_t index_type, const seer_routing *r, void *workspace,
+               size_t workspace_bytes, void *stream);
+size_t seer_route_workspace_bytes(int32_t tokens, int32_t choices, int32_t experts);
+
+/* Rows to the experts: out[p] = weight[c] * x[c / choices] for the choice c in slot p, and a row of zeros in
+ * the slots that are no expert's.  x: tokens rows, out: tokens * choices rows, as many columns, one
+ * type of SEER_F32, SEER_BF16, SEER_F16.  weight: DEVICE fp32 [tokens][choices], or NULL for ones (then
+ * rows are copied bit by bit).  Its gradients: that of x is seer_route_combine of out's gradient
+ * with the same weight; that of weight is what seer_route_grad writes to dweight for dy = x and z = out's gradient. */
+int seer_route_gather(const seer_routing *r, const seer_dense *x, const float *weight, const seer_dense *out,
+                      void *stream);
+
+/* Rows back to the tokens: y[t] = sum over k of weight[t][k] * z[slot of choice (t, k)], in the order of k, over
+ * the choices that are an expert's; a token without one gets zeros, and rows in other slots are not read.  Summed in
+ * fp32, rounded once.  z: tokens * choices rows, y: tokens rows; types as above. */
+int seer_route_combine(const seer_routing *r, const seer_dense *z, const float *weight, const seer_dense *y,
+                       void *stream);
+
+/* The gradients of seer_route_combine: for the choice c in slot p, dz[p] = weight[c] * dy[c / choices] and
+ * dweight[c] = sum over j of dy[c / choices][j] * z[p][j] (fp32 sums); zeros for choices that are no
+ * expert's (their rows of z are not read).  dz may be NULL, and so may dweight (then z may be,
+ * too); dweight: DEVICE fp32 [tokens][choices]. */
+int seer_route_grad(const seer_routing *r, const seer_dense *dy, const seer_dense *z, const float *weight,
+                    const seer_dense *dz, float *dweight, void *stream);
+
+/* Rows in 8-bit integers with a scale each: scale[i] = max_j |x[i][j]| / 127 (an fp32 division) and
+ * q[i][j] = x[i][j] / scale[i] (an fp32 division) to the nearest integer, ties to even, in -127 .. 127; 0 where scale is 0.
+ * A row with an infinity or a NaN has it as its scale, whose products then are not finite, either; its
+ * q are 0 (infinity) or unspecified.  q (SEER_I8) has x's rows and columns; where its rows are further apart, the columns up to the
+ * next multiple of 16 (not beyond ld) are set to 0.  scale: DEVICE fp32 [rows]. */
+int seer_i8_quantize(const seer_dense *x, const seer_dense *q, float *scale, void *stream);
+
+/* seer_route_gather without weights into 8-bit integers: q and scale have tokens * choices rows; rows of slots
+ * that are no expert's are 0 with scale 0. */
+int seer_route_gather_i8(const seer_routing *r, const seer_dense *x, const seer_dense *q, float *scale,
+                         void *stream);
+
+/* Products of 8-bit integers with a scale for each token (row of a) and each channel (row of a b):
+ *   out[i][n] = a_scale[i] * b_scale[g][n] * sum_k a[i][k] * b[g][n][k]
+ * for the rows i of group g, group_ptr[g] <= i < group_ptr[g + 1]; rows from group_ptr[groups] on are set to zero.
+ * The sums are exact (32-bit integers: at most SEER_I8_MAX_K columns, else SEER_ELIMIT).
+ * a: SEER_I8.  b: SEER_I8 with groups * channels rows, the channels of group 0 first, and a's columns.
+ * out: a's rows, `channels` = out's columns; SEER_F32, SEER_BF16 or SEER_F16.
+ * a_scale: DEVICE fp32 [a.rows].  b_scale: DEVICE fp32 [groups][channels].  group_ptr: DEVICE int32 [groups + 1],
+ * non-decreasing from 0 (entries outside 0 .. a.rows are taken as the nearer end), an expert_ptr for
+ * instance; NULL with groups == 1: all rows.
+ * workspace: >= seer_i8_product_workspace_bytes(a.rows, out.cols, a.cols, groups) (may be 0). */
+#define SEER_I8_MAX_K 131071
+int seer_i8_product(const seer_dense *a, const float *a_scale, const seer_dense *b, const float *b_scale,
+                    const int32_t *group_ptr, int32_t groups, const seer_dense *out, void *workspace,
+                    size_t workspace_bytes, void *stream);
+size_t seer_i8_product_workspace_bytes(int64_t rows, int64_t channels, int64_t columns, int32_t groups);
+
+/* One of the many tensors whose gradient is clipped: n contiguous elements. */
+typedef struct {
+    const void *grad; /* DEVICE */
+    void *out;        /* DEVICE: where the clipped gradient goes: grad itself, or memory apart from every grad.
+                         seer_grad_norm does not look at it                                       */
+    int64_t n;
+    int32_t type;     /* SEER_F32, SEER_BF16 or SEER_F16, for both */
+} seer_grad;
+
+/* norm[0] = the square root of the sum of the squares of all elements of all tensors, summed in fp64 in an
+ * order that the sizes alone decide, rounded to fp32 once.  tensors: HOST [count], read before the
+ * call returns.  norm: DEVICE fp32 [1].  workspace: >= seer_grad_workspace_bytes(). */
+int seer_grad_norm(const seer_grad *tensors, int32_t count, float *norm, void *workspace,
+                   size_t workspace_bytes, void *stream);
+size_t seer_grad_workspace_bytes(void);
+
+/* seer_grad_norm, then out = grad * c for every tensor, c = max_norm / (norm + 1e-6) in fp32 where that is
+ * less than 1 (or NaN), else 1; products in fp32, rounded once.  An infinity or a NaN among the gradients
+ * makes c 0 or NaN: norm says so.  max_norm >= 0 (SEER_EINVAL). */
+int seer_grad_clip(const seer_grad *tensors, int32_t count, float max_norm, float *norm, void *workspace,
+                   size_t workspace_bytes, void *stream);
 
 int seer_num_kernels(void);
 const char *seer_kernel_name(int kernel_id); /* "CSR,TM" ...; NULL if out of range  */

@@ -10,3 +10,9 @@ from .binding import (  # noqa: F401
     seer_spmv_plan, seer_spmv_prepare, seer_spmv_prepared, seer_csr_check, seer_gather_sum, seer_stream_copy, seer_stream_sum, set_tuning,
     spmv_auto_workspace_bytes, spmv_prepared_workspace_bytes, spmv_workspace_bytes, strerror,
 )
+from .routed import (  # noqa: F401
+    I8_MAX_K, MAX_EXPERTS, GradTensors, Routing,
+    grad_workspace_bytes, i8_product_workspace_bytes, route_workspace_bytes,
+    seer_grad_clip, seer_grad_norm, seer_i8_product, seer_i8_quantize,
+    seer_route, seer_route_combine, seer_route_gather, seer_route_gather_i8, seer_route_grad,
+)

@@ -171,6 +171,8 @@ def lib():
         L.seer_strerror.argtypes = [C.c_int]
         L.seer_strerror.restype = C.c_char_p
         L.seer_last_hip_error.restype = C.c_int
+        from .routed import bind
+        bind(L)
         _bind_marshal(L)
         _lib = L
     return _lib

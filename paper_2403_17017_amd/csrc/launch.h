@@ -9,6 +9,8 @@
 
 namespace seer {
 
+int hip_fail(hipError_t e);       // records e for seer_last_hip_error and gives SEER_EHIP
+
 constexpr int kBmMaxRows = 2048;  // most rows one CSR,BM workgroup owns (8 per lane, bounds in registers)
 constexpr int kAutoBmMaxRows = 1024;   // ... inside the combined kernel (4 per lane: keeps it at eight waves per SIMD)
 constexpr int kBmChunk = 2048;    // products staged in LDS per CSR,BM pass (4096 is the other choice)

@@ -1,0 +1,434 @@
+// A routed layer's rows: the choices sorted by expert, rows brought to the experts and back, and
+// the gradients of both.  The choices are a sparse (experts x tokens) matrix: the sort writes its CSR
+// form, `gather` multiplies by it and `combine` by its transpose, with dense rows as operands.
+#include "dense.hiph"
+#include "dense_launch.h"
+
+namespace seer {
+
+// ------------------------------------------------------------------ sort
+//
+// A stable counting sort with one bucket per expert and one behind them for choices that are
+// no expert's.  Each wave counts a run of consecutive choices, 64 at a time: the lanes with equal keys find
+// each other with one ballot per key bit, a lane's rank among them is the set bits below it, and the run's
+// counters lie in LDS.  A choice's slot is then
+//   entries of lower keys + entries of its key in earlier workgroups + ... in earlier waves + its rank in the run
+// where the rank is left in choice_slot between the two passes over the choices.
+constexpr int kSortWaves = 16;
+constexpr uint32_t kSortMaxGroups = 128;
+
+template <class I>
+__device__ __forceinline__ uint32_t key_of(const I *expert, uint32_t c, uint32_t experts)
+{
+    const I e = expert[c];
+    return e >= 0 && e < (I)experts ? (uint32_t)e : experts;
+}
+
+// Ranks in the run [begin, end) of the calling wave; cnt [buckets] of this wave, zeroed before.
+template <class I>
+__device__ __forceinline__ void count_run(const I *expert, uint32_t begin, uint32_t end, uint32_t experts, int key_bits,
+                                          uint32_t *cnt, int32_t *rank_out)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    for (uint32_t at = begin; at < end; at += 64) {
+        const uint32_t c = at + lane;
+        const bool in = c < end;
+        const uint32_t key = in ? key_of(expert, c, experts) : 0;
+        uint64_t peers = __ballot(in);
+        for (int b = 0; b < key_bits; ++b) {
+            const uint64_t set = __ballot(key >> b & 1);
+            peers &= (key >> b & 1) ? set : ~set;
+        }
+        // the first lane of each key counts them all
+        const int first = __ffsll((unsigned long long)peers) - 1;
+        uint32_t before = 0;
+        if (in && first == (int)lane) before = atomicAdd(&cnt[key], (uint32_t)__popcll(peers));
+        before = __shfl(before, first, 64);
+        if (in) rank_out[c] = (int32_t)(before + (uint32_t)__popcll(peers & ((1ull << lane) - 1)));
+    }
+}
+
+// One workgroup's share of the sort: choices [begin, end) in `waves` runs.  base [buckets + 1] in LDS: where each key's
+// entries of this workgroup begin.
+template <class I>
+__device__ void place_choices(const I *expert, uint32_t begin, uint32_t end, uint32_t per_wave, uint32_t experts,
+                              const uint32_t *cnt, const uint32_t *base, int32_t *slot_choice, int32_t *choice_slot)
+{
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63, buckets = experts + 1;
+    const uint32_t from = begin + wave * per_wave, to = min(end, from + per_wave);
+    for (uint32_t at = from; at < to; at += 64) {
+        const uint32_t c = at + lane;
+        if (c < to) {
+            const uint32_t key = key_of(expert, c, experts);
+            const uint32_t p = base[key] + cnt[wave * buckets + key] + (uint32_t)choice_slot[c];
+            slot_choice[p] = (int32_t)c;
+            choice_slot[c] = key < experts ? (int32_t)p : -1 - (int32_t)p;
+        }
+    }
+}
+
+// Exclusive prefix sum over v[0 .. n) in LDS by the whole workgroup, the total in v[n].
+__device__ void scan_lds(uint32_t *v, uint32_t n, uint32_t *s_wave)
+{
+    const uint32_t threads = blockDim.x, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    uint32_t carry = 0;
+    for (uint32_t at = 0; at < n; at += threads) {
+        const uint32_t i = at + threadIdx.x;
+        const uint32_t mine = i < n ? v[i] : 0;
+        uint32_t sum = mine;
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t other = __shfl_up(sum, d, 64);
+            if ((int)lane >= d) sum += other;
+        }
+        if (lane == 63) s_wave[wave] = sum;
+        __syncthreads();
+        uint32_t before = carry, all = 0;
+        for (uint32_t w = 0; w < threads / 64; ++w) {
+            if (w < wave) before += s_wave[w];
+            all += s_wave[w];
+        }
+        if (i < n) v[i] = before + sum - mine;
+        carry += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) v[n] = carry;
+    __syncthreads();
+}
+
+struct SortArgs {
+    const void *expert;
+    uint32_t count, experts, per_wave, groups;
+    int key_bits;
+    int32_t *expert_ptr, *slot_choice, *choice_slot;
+    uint32_t *counts;       // [groups][buckets], in the workspace; null with one workgroup
+};
+
+// pass 0: everything in one workgroup; 1: counts of each workgroup's share; 2: the slots.
+// LDS: cnt [waves][buckets], base [buckets + 1].
+template <class I, int PASS>
+__global__ __launch_bounds__(kSortWaves * 64) void route_kernel(SortArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+    __shared__ uint32_t s_wave[kSortWaves];
+    const uint32_t waves = blockDim.x / 64, wave = threadIdx.x / 64, buckets = a.experts + 1;
+    uint32_t *cnt = lds, *base = lds + waves * buckets;
+    const I *expert = static_cast<const I *>(a.expert);
+    const uint32_t begin = blockIdx.x * waves * a.per_wave, end = min(a.count, begin + waves * a.per_wave);
+    if constexpr (PASS == 0 || PASS == 1) {
+        for (uint32_t i = threadIdx.x; i < waves * buckets; i += blockDim.x) cnt[i] = 0;
+        __syncthreads();
+        const uint32_t from = min(end, begin + wave * a.per_wave);
+        count_run(expert, from, min(end, from + a.per_wave), a.experts, a.key_bits, cnt + wave * buckets, a.choice_slot);
+        __syncthreads();
+        // each wave's counters become the entries of the key in earlier waves, base the workgroup's
+        for (uint32_t k = threadIdx.x; k < buckets; k += blockDim.x) {
+            uint32_t sum = 0;
+            for (uint32_t w = 0; w < waves; ++w) {
+                const uint32_t n = cnt[w * buckets + k];
+                if (PASS == 0) cnt[w * buckets + k] = sum;
+                sum += n;
+            }
+            if (PASS == 0) base[k] = sum;
+            else a.counts[(size_t)blockIdx.x * buckets + k] = sum;
+        }
+        if constexpr (PASS == 1) return;
+        __syncthreads();
+        scan_lds(base, buckets, s_wave);
+    } else {
+        // the counters of the waves again, without ranks, and the counts of all workgroups
+        for (uint32_t i = threadIdx.x; i < waves * buckets; i += blockDim.x) cnt[i] = 0;
+        for (uint32_t k = threadIdx.x; k < buckets; k += blockDim.x) {
+            uint32_t sum = 0;
+            for (uint32_t g = 0; g < a.groups; ++g) sum += a.counts[(size_t)g * buckets + k];
+            base[k] = sum;
+        }
+        __syncthreads();
+        const uint32_t from = min(end, begin + wave * a.per_wave), to = min(end, from + a.per_wave);
+        for (uint32_t c = from + (threadIdx.x & 63); c < to; c += 64)
+            atomicAdd(&cnt[wave * buckets + key_of(expert, c, a.experts)], 1u);
+        scan_lds(base, buckets, s_wave);
+        if (blockIdx.x == 0)
+            for (uint32_t k = threadIdx.x; k <= a.experts; k += blockDim.x) a.expert_ptr[k] = (int32_t)base[k];
+        __syncthreads();
+        for (uint32_t k = threadIdx.x; k < buckets; k += blockDim.x) {
+            uint32_t sum = 0;
+            for (uint32_t w = 0; w < waves; ++w) {
+                const uint32_t n = cnt[w * buckets + k];
+                cnt[w * buckets + k] = sum;
+                sum += n;
+            }
+            for (uint32_t g = 0; g < blockIdx.x; ++g) base[k] += a.counts[(size_t)g * buckets + k];
+        }
+        __syncthreads();
+    }
+    if constexpr (PASS == 0)
+        for (uint32_t k = threadIdx.x; k <= a.experts; k += blockDim.x) a.expert_ptr[k] = (int32_t)base[k];
+    place_choices(expert, begin, end, a.per_wave, a.experts, cnt, base, a.slot_choice, a.choice_slot);
+}
+
+// Waves whose counters fit the LDS beside the bases.
+static uint32_t sort_waves(uint32_t experts)
+{
+    return experts <= 1024 ? kSortWaves : experts <= 2048 ? kSortWaves / 2 : kSortWaves / 4;
+}
+
+// Choices that one workgroup sorts on its own, and those of each workgroup where there are more.
+constexpr uint32_t kSortAlone = 4096, kSortShare = 4096;
+
+static uint32_t sort_groups(uint32_t count, uint32_t experts, uint32_t *per_wave)
+{
+    const uint32_t waves = sort_waves(experts);
+    uint32_t groups = count <= kSortAlone ? 1 : std::min((count + kSortShare - 1) / kSortShare, kSortMaxGroups);
+    const uint32_t share = (count + groups - 1) / groups;
+    *per_wave = std::max(64u, ((share + waves - 1) / waves + 63) & ~63u);
+    return (count + waves * *per_wave - 1) / (waves * *per_wave);
+}
+
+size_t route_workspace_bytes(uint32_t count, uint32_t experts)
+{
+    uint32_t per_wave;
+    const uint32_t groups = sort_groups(count, experts, &per_wave);
+    return groups > 1 ? (((size_t)groups * (experts + 1) * 4 + 255) & ~(size_t)255) : 0;
+}
+
+template <class I>
+static void launch_route_of(SortArgs a, uint32_t waves, hipStream_t st)
+{
+    const size_t lds = ((size_t)waves * (a.experts + 1) + a.experts + 2) * 4;
+    if (a.groups <= 1) {
+        hipLaunchKernelGGL((route_kernel<I, 0>), dim3(1), dim3(waves * 64), lds, st, a);
+        return;
+    }
+    hipLaunchKernelGGL((route_kernel<I, 1>), dim3(a.groups), dim3(waves * 64), lds, st, a);
+    hipLaunchKernelGGL((route_kernel<I, 2>), dim3(a.groups), dim3(waves * 64), lds, st, a);
+}
+
+void launch_route(const void *expert, bool wide, uint32_t count, uint32_t experts, int32_t *expert_ptr, int32_t *slot_choice,
+                  int32_t *choice_slot, void *workspace, hipStream_t st)
+{
+    SortArgs a{};
+    a.expert = expert;
+    a.count = count;
+    a.experts = experts;
+    a.groups = sort_groups(count, experts, &a.per_wave);
+    for (a.key_bits = 1; (experts >> a.key_bits) != 0; ++a.key_bits) {}
+    a.expert_ptr = expert_ptr;
+    a.slot_choice = slot_choice;
+    a.choice_slot = choice_slot;
+    a.counts = static_cast<uint32_t *>(workspace);
+    if (wide) launch_route_of<int64_t>(a, sort_waves(experts), st);
+    else launch_route_of<int32_t>(a, sort_waves(experts), st);
+}
+
+// ------------------------------------------------------------------ rows to the experts and back
+//
+// All three kernels go by token: a token's row is read (or written) once, and its choices' rows, each
+// contiguous, once.  Bound by bytes.
+
+constexpr uint32_t kMaxGrid = 1u << 20;     // workgroups; more work is looped over
+
+template <class T, bool WEIGHTED>
+__global__ __launch_bounds__(kWG) void gather_kernel(RouteRows r, const float *__restrict__ weight, const T *__restrict__ x,
+                                                     int64_t ldx, T *__restrict__ out, int64_t ldo)
+{
+    constexpr int E = Unit<T>::kElems;
+    for (uint32_t t = blockIdx.y; t < r.tokens; t += gridDim.y)
+    for (uint32_t col = (blockIdx.x * kWG + threadIdx.x) * E; col < r.cols; col += gridDim.x * kWG * E) {
+        const int n = (int)min((uint32_t)E, r.cols - col);
+        const Unit<T> u = load_some(x + (int64_t)t * ldx + col, n);
+        for (uint32_t k = 0; k < r.choices; ++k) {
+            const uint32_t c = t * r.choices + k;
+            const int32_t slot = r.choice_slot[c];
+            Unit<T> v = u;
+            if constexpr (WEIGHTED) {
+                const float s = weight[c];
+#pragma unroll
+                for (int j = 0; j < E; ++j) v.v[j] = (T)(s * (float)u.v[j]);
+            }
+            if (slot < 0) v = zero_unit<T>();
+            store_some(out + (int64_t)(slot < 0 ? -1 - slot : slot) * ldo + col, v, n);
+        }
+    }
+}
+
+template <class T, bool WEIGHTED>
+__global__ __launch_bounds__(kWG) void combine_kernel(RouteRows r, const float *__restrict__ weight, const T *__restrict__ z,
+                                                      int64_t ldz, T *__restrict__ y, int64_t ldy)
+{
+    constexpr int E = Unit<T>::kElems;
+    for (uint32_t t = blockIdx.y; t < r.tokens; t += gridDim.y)
+    for (uint32_t col = (blockIdx.x * kWG + threadIdx.x) * E; col < r.cols; col += gridDim.x * kWG * E) {
+        const int n = (int)min((uint32_t)E, r.cols - col);
+        float acc[E] = {};
+        for (uint32_t k = 0; k < r.choices; ++k) {
+            const uint32_t c = t * r.choices + k;
+            const int32_t slot = r.choice_slot[c];
+            if (slot < 0) continue;
+            const Unit<T> u = load_some(z + (int64_t)slot * ldz + col, n);
+            const float s = WEIGHTED ? weight[c] : 1.0f;
+#pragma unroll
+            for (int j = 0; j < E; ++j) acc[j] += s * (float)u.v[j];
+        }
+        Unit<T> v;
+#pragma unroll
+        for (int j = 0; j < E; ++j) v.v[j] = (T)acc[j];
+        store_some(y + (int64_t)t * ldy + col, v, n);
+    }
+}
+
+// One workgroup per token.
+template <class T>
+__global__ __launch_bounds__(kWG) void route_grad_kernel(RouteRows r, const float *__restrict__ weight, const T *__restrict__ dy,
+                                                         int64_t lddy, const T *__restrict__ z, int64_t ldz, T *__restrict__ dz,
+                                                         int64_t lddz, float *__restrict__ dweight)
+{
+    constexpr int E = Unit<T>::kElems;
+    __shared__ float s_dot[kWG / kWave];
+    for (uint32_t t = blockIdx.x; t < r.tokens; t += gridDim.x) {
+        for (uint32_t k = 0; k < r.choices; ++k) {
+            const uint32_t c = t * r.choices + k;
+            const int32_t slot = r.choice_slot[c];
+            const int64_t p = slot < 0 ? -1 - slot : slot;
+            const float s = weight ? weight[c] : 1.0f;
+            float dot = 0;
+            for (uint32_t col = threadIdx.x * E; col < r.cols; col += kWG * E) {
+                const int n = (int)min((uint32_t)E, r.cols - col);
+                const Unit<T> g = load_some(dy + (int64_t)t * lddy + col, n);
+                if (dweight && slot >= 0) {
+                    const Unit<T> u = load_some(z + p * ldz + col, n);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) dot += (float)g.v[j] * (float)u.v[j];
+                }
+                if (dz) {
+                    Unit<T> v = zero_unit<T>();
+                    if (slot >= 0) {
+#pragma unroll
+                        for (int j = 0; j < E; ++j) v.v[j] = (T)(s * (float)g.v[j]);
+                    }
+                    store_some(dz + p * lddz + col, v, n);
+                }
+            }
+            if (dweight) {
+                dot = lanes_fold(dot, [](float a, float b) { return a + b; });
+                if ((threadIdx.x & 63) == 0) s_dot[threadIdx.x / 64] = dot;
+                __syncthreads();
+                if (threadIdx.x == 0) dweight[c] = (s_dot[0] + s_dot[1]) + (s_dot[2] + s_dot[3]);
+                __syncthreads();
+            }
+        }
+    }
+}
+
+// A row's largest magnitude comes from the bits: they order as the magnitudes do, and a NaN's are above
+// infinity's, so a NaN anywhere is found.
+__device__ __forceinline__ float quantised(float x, float scale)
+{
+    const float v = rintf(x / scale);
+    return scale > 0 ? fminf(fmaxf(v, -127.0f), 127.0f) : 0.0f;
+}
+
+// One workgroup per row of x; routed: its copies go to the slots of its choices.
+template <class T, bool ROUTED>
+__global__ __launch_bounds__(kWG) void quantize_kernel(RouteRows r, const T *__restrict__ x, int64_t ldx, int8_t *__restrict__ q,
+                                                       int64_t ldq, uint32_t padded, float *__restrict__ scale)
+{
+    __shared__ uint32_t s_max[kWG / kWave];
+    for (uint32_t t = blockIdx.x; t < r.tokens; t += gridDim.x) {
+        constexpr int E = Unit<T>::kElems;
+        const T *row = x + (int64_t)t * ldx;
+        uint32_t top = 0;
+        for (uint32_t col = threadIdx.x * E; col < r.cols; col += kWG * E) {
+            const Unit<T> u = load_some(row + col, (int)min((uint32_t)E, r.cols - col));
+#pragma unroll
+            for (int j = 0; j < E; ++j) top = max(top, __float_as_uint((float)u.v[j]) & 0x7fffffffu);
+        }
+        top = lanes_fold(top, [](uint32_t a, uint32_t b) { return max(a, b); });
+        if ((threadIdx.x & 63) == 0) s_max[threadIdx.x / 64] = top;
+        __syncthreads();
+        top = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+        const float s = __uint_as_float(top) / 127.0f;
+        for (uint32_t col = threadIdx.x * E; col < padded; col += kWG * E) {
+            const int have = col < r.cols ? (int)min((uint32_t)E, r.cols - col) : 0, n = (int)min((uint32_t)E, padded - col);
+            const Unit<T> u = load_some(row + col, have);
+            int8_t b[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) b[j] = j < have ? (int8_t)(int)quantised((float)u.v[j], s) : (int8_t)0;
+            for (uint32_t k = 0; k < r.choices; ++k) {
+                const int32_t slot = ROUTED ? r.choice_slot[t * r.choices + k] : (int32_t)t;
+                int8_t *to = q + (int64_t)(slot < 0 ? -1 - slot : slot) * ldq + col;
+                for (int j = 0; j < n; ++j) to[j] = slot < 0 ? (int8_t)0 : b[j];
+            }
+        }
+        for (uint32_t k = threadIdx.x; k < r.choices; k += kWG) {
+            const int32_t slot = ROUTED ? r.choice_slot[t * r.choices + k] : (int32_t)t;
+            scale[slot < 0 ? -1 - slot : slot] = slot < 0 ? 0.0f : s;
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ launches
+
+template <class F>
+static void by_type(int type, F f)
+{
+    if (type == SEER_F32) f((float *)nullptr);
+    else if (type == SEER_BF16) f((bf16_t *)nullptr);
+    else f((f16_t *)nullptr);
+}
+
+// A workgroup per 4 KB of a row and token; more of either is looped over.
+static dim3 grid_of(const RouteRows &r, uint32_t elems)
+{
+    return dim3(std::min(1024u, (r.cols + kWG * elems - 1) / (kWG * elems)), std::min(r.tokens, 65535u));
+}
+
+void launch_route_gather(const RouteRows &rows, const float *weight, const seer_dense &x, const seer_dense &out, hipStream_t st)
+{
+    by_type(x.type, [&](auto *of) {
+        using T = std::remove_pointer_t<decltype(of)>;
+        const dim3 grid = grid_of(rows, Unit<T>::kElems), wg(kWG);
+        const T *xp = static_cast<const T *>(x.data);
+        T *op = static_cast<T *>(out.data);
+        if (weight) hipLaunchKernelGGL((gather_kernel<T, true>), grid, wg, 0, st, rows, weight, xp, x.ld, op, out.ld);
+        else hipLaunchKernelGGL((gather_kernel<T, false>), grid, wg, 0, st, rows, weight, xp, x.ld, op, out.ld);
+    });
+}
+
+void launch_route_combine(const RouteRows &rows, const float *weight, const seer_dense &z, const seer_dense &y, hipStream_t st)
+{
+    by_type(z.type, [&](auto *of) {
+        using T = std::remove_pointer_t<decltype(of)>;
+        const dim3 grid = grid_of(rows, Unit<T>::kElems), wg(kWG);
+        const T *zp = static_cast<const T *>(z.data);
+        T *yp = static_cast<T *>(y.data);
+        if (weight) hipLaunchKernelGGL((combine_kernel<T, true>), grid, wg, 0, st, rows, weight, zp, z.ld, yp, y.ld);
+        else hipLaunchKernelGGL((combine_kernel<T, false>), grid, wg, 0, st, rows, weight, zp, z.ld, yp, y.ld);
+    });
+}
+
+void launch_route_grad(const RouteRows &rows, const float *weight, const seer_dense &dy, const seer_dense *z,
+                       const seer_dense *dz, float *dweight, hipStream_t st)
+{
+    by_type(dy.type, [&](auto *of) {
+        using T = std::remove_pointer_t<decltype(of)>;
+        hipLaunchKernelGGL((route_grad_kernel<T>), dim3(std::min(rows.tokens, kMaxGrid)), dim3(kWG), 0, st, rows, weight,
+                           static_cast<const T *>(dy.data), dy.ld, z ? static_cast<const T *>(z->data) : (const T *)nullptr, z ? z->ld : 0,
+                           dz ? static_cast<T *>(dz->data) : (T *)nullptr, dz ? dz->ld : 0, dweight);
+    });
+}
+
+void launch_quantize(const RouteRows &rows, const seer_dense &x, const seer_dense &q, float *scale, hipStream_t st)
+{
+    const uint32_t padded = (uint32_t)std::min<int64_t>(q.ld, (x.cols + 15) & ~(int64_t)15);
+    by_type(x.type, [&](auto *of) {
+        using T = std::remove_pointer_t<decltype(of)>;
+        const dim3 grid(std::min(rows.tokens, kMaxGrid)), wg(kWG);
+        const T *xp = static_cast<const T *>(x.data);
+        int8_t *qp = static_cast<int8_t *>(q.data);
+        if (rows.choice_slot) hipLaunchKernelGGL((quantize_kernel<T, true>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
+        else hipLaunchKernelGGL((quantize_kernel<T, false>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
+    });
+}
+
+} // namespace seer

@@ -30,11 +30,21 @@ static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
 namespace {
 
+std::atomic<int> g_last_hip_error{0};
+
+} // namespace
+
+int seer::hip_fail(hipError_t e)
+{
+    g_last_hip_error.store((int)e);
+    return SEER_EHIP;
+}
+
+namespace {
+
 constexpr int kMaxDevices = 64;
 std::mutex g_scratch_mutex;
 void *g_scratch_ptr[kMaxDevices] = {};     // device address of `scratch` on each device, once looked up
-
-std::atomic<int> g_last_hip_error{0};
 
 // Tuning hooks (negative = choose automatically).
 std::atomic<int> g_tune_wm_lanes{-1};
@@ -87,12 +97,6 @@ std::condition_variable g_mailbox_freed;
 char *g_mailbox_host = nullptr, *g_mailbox_dev = nullptr;
 uint64_t g_mailbox_free = ~0ull;        // bit k: slot k is free
 uint64_t g_mailbox_seq = 0;
-
-int hip_fail(hipError_t e)
-{
-    g_last_hip_error.store((int)e);
-    return SEER_EHIP;
-}
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
