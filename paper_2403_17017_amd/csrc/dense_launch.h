@@ -36,6 +36,7 @@ struct I8Args {
     uint32_t rows, channels, columns, groups;
     int32_t type;
 };
+bool i8_product_fits(const I8Args &a);
 size_t i8_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t columns, uint32_t groups);
 void launch_i8_product(const I8Args &a, void *workspace, hipStream_t st);
 

@@ -10,9 +10,9 @@ namespace seer {
 
 typedef int v4i32 __attribute__((ext_vector_type(4)));
 
-// The rows of tile `tile` of `tokens` rows: those of group g from `begin` to `end`.  Group number `groups` stands for
-// the rows behind the last one.  All lanes of a wave take part.
-struct TileRows { uint32_t group, begin, end; };
+// A tile: the rows of group `group` from `begin` to `end`, and which of the `across` tiles beside one another.  Group number
+// `groups` stands for the rows behind the last one.
+struct Tile { uint32_t group, begin, end, column; };
 
 __device__ __forceinline__ uint32_t group_begin(const I8Args &a, uint32_t g)
 {
@@ -22,43 +22,78 @@ __device__ __forceinline__ uint32_t group_begin(const I8Args &a, uint32_t g)
     return p < 0 ? 0 : min((uint32_t)p, a.rows);
 }
 
-__device__ __forceinline__ bool find_tile(const I8Args &a, uint32_t tile, uint32_t tokens, TileRows *t)
+// What lane l knows of group at + l: its rows, the tiles that they take, and those of the groups from `at` up to and with it.
+struct GroupTiles { uint32_t from, to, tiles, sum; };
+
+__device__ __forceinline__ GroupTiles group_tiles(const I8Args &a, uint32_t at, uint32_t tokens)
+{
+    const uint32_t lane = threadIdx.x & 63, g = min(at + lane, a.groups + 1);
+    GroupTiles t;
+    t.from = group_begin(a, g);
+    t.to = group_begin(a, g + 1);
+    t.tiles = t.to > t.from ? (t.to - t.from + tokens - 1) / tokens : 0;
+    t.sum = t.tiles;
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t other = __shfl_up(t.sum, d, 64);
+        if ((int)lane >= d) t.sum += other;
+    }
+    return t;
+}
+
+// Tiles lie in the order of the groups; in a group, kPanel rows of tiles make a panel that is gone through column by
+// column, so that workgroups that run at the same time on an XCD share rows of both matrices in its L2.
+constexpr uint32_t kPanel = 4;
+
+__device__ __forceinline__ Tile tile_in_group(uint32_t group, uint32_t from, uint32_t to, uint32_t local, uint32_t tokens, uint32_t across)
+{
+    const uint32_t down = (to - from + tokens - 1) / tokens, panel = local / (kPanel * across), rest = local % (kPanel * across);
+    const uint32_t height = min(kPanel, down - panel * kPanel), row = panel * kPanel + rest % height;
+    Tile t;
+    t.group = group;
+    t.begin = from + row * tokens;
+    t.end = min(to, t.begin + tokens);
+    t.column = rest / height;
+    return t;
+}
+
+// The tile of workgroup `block` among the tiles there are: as many for each XCD.  False: there is none.  All lanes of a wave
+// take part; the result is uniform.
+__device__ __forceinline__ bool find_tile(const I8Args &a, uint32_t block, uint32_t tokens, uint32_t across, Tile *t)
 {
     if (!a.group_ptr) {
-        t->group = 0;
-        t->begin = tile * tokens;
-        t->end = min(a.rows, t->begin + tokens);
-        return t->begin < a.rows;
+        const uint32_t all = (a.rows + tokens - 1) / tokens * across, w = tile_of_block(block, all, 1);
+        if (w >= all) return false;
+        *t = tile_in_group(0, 0, a.rows, w, tokens, across);
+        return true;
     }
-    const uint32_t lane = threadIdx.x & 63;
+    GroupTiles g;
+    uint32_t all = 0;
+    for (uint32_t at = 0; at <= a.groups; at += 64) {
+        g = group_tiles(a, at, tokens);
+        all += (uint32_t)__builtin_amdgcn_readlane((int)g.sum, 63);
+    }
+    const uint32_t w = tile_of_block(block, all * across, 1);
+    if (w >= all * across) return false;
     uint32_t before = 0;
     for (uint32_t at = 0; at <= a.groups; at += 64) {
-        const uint32_t g = at + lane;
-        const uint32_t from = group_begin(a, min(g, a.groups + 1)), to = group_begin(a, min(g + 1, a.groups + 1));
-        const uint32_t tiles = to > from ? (to - from + tokens - 1) / tokens : 0;
-        uint32_t sum = tiles;
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t other = __shfl_up(sum, d, 64);
-            if ((int)lane >= d) sum += other;
-        }
-        const uint64_t past = __ballot(before + sum > tile);
+        if (a.groups >= 64) g = group_tiles(a, at, tokens);        // (else it is there)
+        const uint64_t past = __ballot((before + g.sum) * across > w);
         if (past) {
             const int l = __ffsll((unsigned long long)past) - 1;
-            const uint32_t first = before + (uint32_t)__builtin_amdgcn_readlane((int)(sum - tiles), l);
-            t->group = at + (uint32_t)l;
-            t->begin = (uint32_t)__builtin_amdgcn_readlane((int)from, l) + (tile - first) * tokens;
-            t->end = min((uint32_t)__builtin_amdgcn_readlane((int)to, l), t->begin + tokens);
+            const uint32_t first = before + (uint32_t)__builtin_amdgcn_readlane((int)(g.sum - g.tiles), l);
+            *t = tile_in_group(at + (uint32_t)l, (uint32_t)__builtin_amdgcn_readlane((int)g.from, l),
+                               (uint32_t)__builtin_amdgcn_readlane((int)g.to, l), w - first * across, tokens, across);
             return true;
         }
-        before += (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
+        before += (uint32_t)__builtin_amdgcn_readlane((int)g.sum, 63);
     }
     return false;
 }
 
-// Tiles of `tokens` rows that any division of the rows into groups needs.
-static uint32_t most_tiles(const I8Args &a, uint32_t tokens)
+// Rows of tiles of `tokens` rows that any division of the rows into groups needs.
+static uint64_t most_tiles(const I8Args &a, uint32_t tokens)
 {
-    return a.group_ptr ? a.rows / tokens + std::min(a.groups + 1, a.rows) : (a.rows + tokens - 1) / tokens;
+    return a.group_ptr ? (uint64_t)a.rows / tokens + std::min(a.groups + 1, a.rows) : ((uint64_t)a.rows + tokens - 1) / tokens;
 }
 
 __device__ __forceinline__ void store_1(const I8Args &a, uint32_t row, uint32_t channel, float v)
@@ -87,15 +122,14 @@ __device__ __forceinline__ v4i32 load_16(const int8_t *p, int n)
     return v;
 }
 
-__global__ __launch_bounds__(256) void i8_any_kernel(I8Args a, uint32_t tiles)
+__global__ __launch_bounds__(256) void i8_any_kernel(I8Args a, uint32_t blocks)
 {
     __shared__ __attribute__((aligned(16))) int8_t s_a[kAnyTokens * kAnyPitch], s_b[kAnyChannels * kAnyPitch];
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    const uint32_t across = (a.channels + kAnyChannels - 1) / kAnyChannels;
-    for (uint64_t w = blockIdx.x; w < (uint64_t)across * tiles; w += gridDim.x) {
-    TileRows t;
-    if (!find_tile(a, (uint32_t)(w / across), kAnyTokens, &t)) return;
-    const uint32_t n0 = (uint32_t)(w % across) * kAnyChannels;
+    for (uint32_t w = blockIdx.x; w < blocks; w += gridDim.x) {
+    Tile t;
+    if (!find_tile(a, w, kAnyTokens, (a.channels + kAnyChannels - 1) / kAnyChannels, &t)) continue;
+    const uint32_t n0 = t.column * kAnyChannels;
     v4i32 acc[2][2] = {};
     if (t.group < a.groups) {
         const int8_t *b = a.b + (int64_t)t.group * a.channels * a.ldb;
@@ -155,45 +189,44 @@ __device__ __forceinline__ void store_4(T *row, uint32_t n, uint32_t channels, c
 
 // ------------------------------------------------------------------ tiles
 //
-// kTileChannels channels x TOKENS tokens per workgroup of eight waves, 128 columns at a time, straight from memory into one of
-// two LDS buffers while the other is multiplied.  A row's eight pieces of 16 bytes lie in the order of their number
-// xor the row's last three bits, so that the eight lanes that read at a time use all banks.
-constexpr uint32_t kTileChannels = 256, kTileCols = 128, kTileThreads = 512;
+// 256 channels x TOKENS tokens per workgroup of eight waves.  64 columns at a time come straight from memory into one of
+// four LDS buffers, three steps before they are multiplied: a step's multiplications (512 matrix instructions of a workgroup,
+// 2 x 16 cycles x 32 on each SIMD) take less time than memory does to answer.  A row's four pieces of 16 bytes lie
+// in the order of their number xor (row / 2 + row / 8) % 4, so that lanes that read together use all banks.
+constexpr uint32_t kTileChannels = 256, kTileCols = 64, kTileThreads = 512;
 
 typedef __attribute__((address_space(3))) int8_t lds_byte;
 
-// TOKENS x CHANNELS: WC x WT waves of CI * 16 channels x TJ * 16 tokens.
+// WC x 8 / WC waves, each of CI * 16 channels x TJ * 16 tokens.
 template <int WC, int CI, int TJ>
 struct TileShape {
     static constexpr int kWT = 8 / WC;
     static constexpr uint32_t kTokens = kWT * TJ * 16;
+    static constexpr uint32_t kLoadsA = kTokens >= 128 ? kTokens / 128 : 1, kLoadsB = kTileChannels / 128;  // of a lane, each step
+    static constexpr uint32_t kBytes = (kTokens + kTileChannels) * kTileCols;
     static_assert(WC * CI * 16 == (int)kTileChannels, "waves cover the channels");
 };
 
-// ROWS rows of kTileCols columns to LDS: at[i] is where the calling lane's piece of rows i * 64 + wave * 8 ... lies, `col` is uniform.
-template <uint32_t ROWS>
-__device__ __forceinline__ void fetch_tile(__amdgpu_buffer_rsrc_t rows, const uint32_t (&at)[ROWS / 64], uint32_t back, uint32_t col,
-                                           uint32_t wave, int8_t *lds)
+// Waits until all but the last `LOADS` of the wave's loads have arrived and its LDS reads are through, then for the other waves.
+template <uint32_t LOADS>
+__device__ __forceinline__ void step_barrier()
 {
-#pragma unroll
-    for (uint32_t i = 0; i < ROWS / 64; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rows, (lds_byte *)(lds + (i * 8 + wave) * 1024), 16, (int)(at[i] - back), (int)col, 0, 0);
+    if constexpr (LOADS == 8) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if constexpr (LOADS == 6) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 template <class T, int WC, int CI, int TJ>
-__global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a, uint32_t tiles)
+__global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
 {
     using Shape = TileShape<WC, CI, TJ>;
-    constexpr uint32_t TOKENS = Shape::kTokens;
-    __shared__ __attribute__((aligned(1024))) int8_t s_a0[TOKENS * kTileCols], s_b0[kTileChannels * kTileCols];
-    __shared__ __attribute__((aligned(1024))) int8_t s_a1[TOKENS * kTileCols], s_b1[kTileChannels * kTileCols];
+    constexpr uint32_t TOKENS = Shape::kTokens, LA = Shape::kLoadsA, LB = Shape::kLoadsB;
+    __shared__ __attribute__((aligned(1024))) int8_t s_0[Shape::kBytes], s_1[Shape::kBytes], s_2[Shape::kBytes], s_3[Shape::kBytes];
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), lane = threadIdx.x & 63;
     const uint32_t across = (a.channels + kTileChannels - 1) / kTileChannels;
-    const uint32_t w = tile_of_block(blockIdx.x, across * tiles, 1);
-    if (w >= across * tiles) return;
-    TileRows t;
-    if (!find_tile(a, w / across, TOKENS, &t)) return;
-    const uint32_t n0 = (w % across) * kTileChannels;
+    Tile t;
+    if (!find_tile(a, blockIdx.x, TOKENS, across, &t)) return;
+    const uint32_t n0 = t.column * kTileChannels;
     const uint32_t wc = wave % WC, wt = wave / WC;
     T *out = static_cast<T *>(a.out);
     v4i32 acc[CI][TJ];
@@ -209,83 +242,103 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a, uint
                                                           (int)((rows - 1) * lda + a.columns), 0x00020000);
         const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(a.b + ((int64_t)t.group * a.channels + n0) * a.ldb), 0,
                                                           (int)((chans - 1) * ldb + a.columns), 0x00020000);
-        // a wave's load brings eight rows, eight pieces each; rows that are not there are taken as the last one
-        const uint32_t piece = ((lane & 7) ^ (lane >> 3)) * 16;
-        uint32_t at_a[TOKENS / 64], at_b[kTileChannels / 64];
+        // a wave's load brings sixteen rows, four pieces each; rows that are not there are taken as the last one
+        const auto order = [](uint32_t row) { return (row / 2 + row / 8) & 3; };
+        const uint32_t piece = ((lane & 3) ^ order(lane / 4)) * 16;
+        uint32_t at_a[LA], at_b[LB];
 #pragma unroll
-        for (uint32_t i = 0; i < TOKENS / 64; ++i) at_a[i] = min((i * 8 + wave) * 8 + lane / 8, rows - 1) * lda + piece;
+        for (uint32_t i = 0; i < LA; ++i) at_a[i] = min(((i * 8 + wave) * 16) % TOKENS + lane / 4, rows - 1) * lda + piece;
 #pragma unroll
-        for (uint32_t i = 0; i < kTileChannels / 64; ++i) at_b[i] = min((i * 8 + wave) * 8 + lane / 8, chans - 1) * ldb + piece;
-        const auto fetch = [&](uint32_t k0, int8_t *la, int8_t *lb) {
-            // pieces behind the last column are not loaded: the first one of the 128 columns is
-            const uint32_t back = k0 + piece < a.columns ? 0 : piece;
-            fetch_tile<TOKENS>(ra, at_a, back, k0, wave, la);
-            fetch_tile<kTileChannels>(rb, at_b, back, k0, wave, lb);
+        for (uint32_t i = 0; i < LB; ++i) at_b[i] = min((i * 8 + wave) * 16 + lane / 4, chans - 1) * ldb + piece;
+        const uint32_t steps = (a.columns + kTileCols - 1) / kTileCols;
+        const auto fetch = [&](uint32_t step, int8_t *lds) {
+            // steps behind the last one load the last one again, into a buffer that is not read; pieces behind the last column
+            // are not loaded: the step's first one is
+            const uint32_t k0 = min(step, steps - 1) * kTileCols, back = k0 + piece < a.columns ? 0 : piece;
+#pragma unroll
+            for (uint32_t i = 0; i < LA; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte *)(lds + ((i * 8 + wave) * 1024) % (TOKENS * kTileCols)), 16, (int)(at_a[i] - back), (int)k0, 0, 0);
+#pragma unroll
+            for (uint32_t i = 0; i < LB; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte *)(lds + TOKENS * kTileCols + (i * 8 + wave) * 1024), 16, (int)(at_b[i] - back), (int)k0, 0, 0);
         };
-        const uint32_t from = (lane & 15) * kTileCols + (((lane >> 4) ^ (lane & 7)) * 16);
-        const uint32_t from_b = wc * CI * 16 * kTileCols + from, from_a = wt * TJ * 16 * kTileCols + from;
-        const auto multiply = [&](const int8_t *la, const int8_t *lb) {
+        const uint32_t from = (lane & 15) * kTileCols + (((lane >> 4) ^ order(lane & 15)) * 16);
+        const uint32_t from_a = wt * TJ * 16 * kTileCols + from, from_b = (TOKENS + wc * CI * 16) * kTileCols + from;
+        const bool busy = wt * TJ * 16 < rows;          // (waves without tokens only fetch)
+        const auto multiply = [&](const int8_t *lds) {
+            if (!busy) return;
+            v4i32 fb[CI], fa[TJ];
 #pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) {
-                const int8_t *pa = la + (from_a ^ (h * 64)), *pb = lb + (from_b ^ (h * 64));
-                v4i32 fb[CI], fa[TJ];
+            for (int j = 0; j < TJ; ++j) fa[j] = *reinterpret_cast<const v4i32 *>(lds + from_a + j * 16 * kTileCols);
 #pragma unroll
-                for (int j = 0; j < TJ; ++j) fa[j] = *reinterpret_cast<const v4i32 *>(pa + j * 16 * kTileCols);
+            for (int i = 0; i < CI; ++i) fb[i] = *reinterpret_cast<const v4i32 *>(lds + from_b + i * 16 * kTileCols);
 #pragma unroll
-                for (int i = 0; i < CI; ++i) fb[i] = *reinterpret_cast<const v4i32 *>(pb + i * 16 * kTileCols);
+            for (int i = 0; i < CI; ++i)
 #pragma unroll
-                for (int i = 0; i < CI; ++i)
-#pragma unroll
-                    for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[i], fa[j], acc[i][j], 0, 0, 0);
-            }
+                for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[i], fa[j], acc[i][j], 0, 0, 0);
         };
+        const auto step = [&](uint32_t s, int8_t *lds, int8_t *next) {
+            step_barrier<2 * (LA + LB)>();          // this step's columns are there, and the buffer before it is no longer read
+            fetch(s + 3, next);
+            multiply(lds);
+        };
+        fetch(0, s_0);
+        fetch(1, s_1);
+        fetch(2, s_2);
         // zeros for the tokens' pieces behind the last column
-        const auto clear_end = [&](uint32_t k0, int8_t *la) {
-            for (uint32_t i = threadIdx.x; i < TOKENS * 8; i += kTileThreads)
-                if (k0 + ((i ^ (i >> 3)) & 7) * 16 >= a.columns) *reinterpret_cast<v4i32 *>(la + i * 16) = v4i32{0, 0, 0, 0};
-            __syncthreads();
+        const auto clear_end = [&](int8_t *lds) {
+            const uint32_t k0 = (steps - 1) * kTileCols;
+            step_barrier<0>();
+            for (uint32_t i = threadIdx.x; i < TOKENS * 4; i += kTileThreads)
+                if (k0 + ((i & 3) ^ order((i / 4) & 15)) * 16 >= a.columns) *reinterpret_cast<v4i32 *>(lds + i * 16) = v4i32{0, 0, 0, 0};
         };
-        fetch(0, s_a0, s_b0);
-        uint32_t k0 = 0;
-        for (; k0 + 2 * kTileCols <= a.columns; k0 += 2 * kTileCols) {
-            __syncthreads();                         // the first buffer is there, the second no longer read
-            fetch(k0 + kTileCols, s_a1, s_b1);
-            multiply(s_a0, s_b0);
-            __syncthreads();
-            if (k0 + 2 * kTileCols < a.columns) fetch(k0 + 2 * kTileCols, s_a0, s_b0);
-            multiply(s_a1, s_b1);
+        const uint32_t whole = a.columns / kTileCols;
+        uint32_t s = 0;
+        for (; s + 4 <= whole; s += 4) {
+            step(s, s_0, s_3);
+            step(s + 1, s_1, s_0);
+            step(s + 2, s_2, s_1);
+            step(s + 3, s_3, s_2);
         }
-        if (k0 < a.columns) {                        // up to 255 columns are left, the first 128 of them on their way
-            const bool more = k0 + kTileCols < a.columns;
-            __syncthreads();
-            if (more) fetch(k0 + kTileCols, s_a1, s_b1);
-            else clear_end(k0, s_a0);
-            multiply(s_a0, s_b0);
-            if (more) {
-                __syncthreads();
-                clear_end(k0 + kTileCols, s_a1);
-                multiply(s_a1, s_b1);
+        if (s < steps) {                            // up to four steps are left, the last of them perhaps not whole
+            if (s == whole) clear_end(s_0);
+            step(s, s_0, s_3);
+            if (s + 1 < steps) {
+                if (s + 1 == whole) clear_end(s_1);
+                step(s + 1, s_1, s_0);
+            }
+            if (s + 2 < steps) {
+                if (s + 2 == whole) clear_end(s_2);
+                step(s + 2, s_2, s_1);
+            }
+            if (s + 3 < steps) {
+                if (s + 3 == whole) clear_end(s_3);
+                step(s + 3, s_3, s_2);
             }
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // nothing is on its way to LDS when the workgroup ends
     }
+    // every scale is fetched before the first store: a wait for a load is one for all stores before it, too
     const bool zero = t.group >= a.groups;
     const float *sb = a.b_scale + (int64_t)(zero ? 0 : t.group) * a.channels;
+    const uint32_t n1 = n0 + wc * CI * 16 + (lane >> 4) * 4, row1 = t.begin + wt * TJ * 16 + (lane & 15);
+    float of_row[TJ], of_channel[CI][4];
 #pragma unroll
-    for (int i = 0; i < CI; ++i) {
-        const uint32_t n = n0 + (wc * CI + i) * 16 + (lane >> 4) * 4;
-        if (n >= a.channels) continue;
-        float scale[4];
+    for (int j = 0; j < TJ; ++j) of_row[j] = a.a_scale[min(row1 + j * 16, t.end - 1)];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) scale[v] = sb[min(n + v, a.channels - 1)];
+    for (int i = 0; i < CI; ++i)
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) {
-            const uint32_t row = t.begin + (wt * TJ + j) * 16 + (lane & 15);
-            if (row >= t.end) continue;
-            const float sa = a.a_scale[row];
+        for (int v = 0; v < 4; ++v) of_channel[i][v] = sb[min(n1 + i * 16 + v, a.channels - 1)];
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) {
+        if (row1 + j * 16 >= t.end) continue;
+        T *row = out + (int64_t)(row1 + j * 16) * a.ldo;
+#pragma unroll
+        for (int i = 0; i < CI; ++i) {
             float v[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = zero ? 0.0f : (float)acc[i][j][u] * (sa * scale[u]);
-            store_4(out + (int64_t)row * a.ldo, n, a.channels, v);
+            for (int u = 0; u < 4; ++u) v[u] = zero ? 0.0f : (float)acc[i][j][u] * (of_row[j] * of_channel[i][u]);
+            if (n1 + i * 16 < a.channels) store_4(row, n1 + i * 16, a.channels, v);
         }
     }
 }
@@ -375,12 +428,22 @@ static bool in_pieces(const I8Args &a)
            whole((uintptr_t)a.ldb) && a.columns % 16 == 0 && a.columns > 0;
 }
 
-template <class T, int WC, int CI, int TJ>
-static void launch_tiles(const I8Args &a, hipStream_t st)
+// Workgroups for the tiles that there may be.
+static uint64_t most_blocks(const I8Args &a, uint32_t tokens, uint32_t channels)
 {
-    constexpr uint32_t tokens = TileShape<WC, CI, TJ>::kTokens;
-    const uint32_t across = (a.channels + kTileChannels - 1) / kTileChannels, tiles = most_tiles(a, tokens);
-    hipLaunchKernelGGL((i8_tile_kernel<T, WC, CI, TJ>), dim3(8 * tiles_per_xcd(across * tiles)), dim3(kTileThreads), 0, st, a, tiles);
+    return (most_tiles(a, tokens) * ((a.channels + channels - 1) / channels) + kXCD - 1) / kXCD * kXCD;
+}
+
+// The arithmetic on tiles is 32-bit.
+bool i8_product_fits(const I8Args &a) { return most_blocks(a, kAnyTokens, kAnyChannels) < (1u << 30); }
+
+template <class T, int WC, int CI, int TJ>
+static bool launch_tiles(const I8Args &a, hipStream_t st)
+{
+    const uint64_t blocks = most_blocks(a, TileShape<WC, CI, TJ>::kTokens, kTileChannels);
+    if (blocks * kTileThreads >= 1ull << 32) return false;          // (a launch has fewer lanes)
+    hipLaunchKernelGGL((i8_tile_kernel<T, WC, CI, TJ>), dim3((uint32_t)blocks), dim3(kTileThreads), 0, st, a);
+    return true;
 }
 
 template <class T>
@@ -393,13 +456,10 @@ static bool launch_pieces(const I8Args &a, hipStream_t st)
         hipLaunchKernelGGL((i8_few_kernel<T>), dim3((a.channels + 15) / 16, a.groups + (a.group_ptr ? 1 : 0)), dim3(kFewWaves * 64), 0, st, a, share);
         return true;
     }
-    // (offsets into a tile are 32-bit, and so is the number of workgroups' lanes)
-    const uint64_t across = (a.channels + kTileChannels - 1) / kTileChannels;
-    if (a.lda >= (1 << 23) || a.ldb >= (1 << 23) || across * most_tiles(a, 64) >= (1u << 22)) return false;
-    if (mean > 160) launch_tiles<T, 2, 8, 4>(a, st);
-    else if (mean > 80) launch_tiles<T, 2, 8, 2>(a, st);
-    else launch_tiles<T, 4, 4, 2>(a, st);
-    return true;
+    if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return false;     // offsets into a tile are 32-bit
+    if (mean > 160) return launch_tiles<T, 2, 8, 4>(a, st);
+    if (mean > 80) return launch_tiles<T, 2, 8, 2>(a, st);
+    return launch_tiles<T, 4, 4, 2>(a, st);
 }
 
 void launch_i8_product(const I8Args &a, void *, hipStream_t st)
@@ -407,9 +467,8 @@ void launch_i8_product(const I8Args &a, void *, hipStream_t st)
     if (in_pieces(a)) {
         if (a.type == SEER_F32 ? launch_pieces<float>(a, st) : a.type == SEER_BF16 ? launch_pieces<bf16_t>(a, st) : launch_pieces<f16_t>(a, st)) return;
     }
-    const uint32_t across = (a.channels + kAnyChannels - 1) / kAnyChannels, tiles = most_tiles(a, kAnyTokens);
-    const uint32_t grid = (uint32_t)std::min<uint64_t>((uint64_t)across * tiles, 1u << 22);
-    hipLaunchKernelGGL(i8_any_kernel, dim3(grid), dim3(256), 0, st, a, tiles);
+    const uint32_t blocks = (uint32_t)most_blocks(a, kAnyTokens, kAnyChannels);
+    hipLaunchKernelGGL(i8_any_kernel, dim3(std::min(blocks, 1u << 22)), dim3(256), 0, st, a, blocks);
 }
 
 } // namespace seer

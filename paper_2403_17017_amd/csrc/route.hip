@@ -319,51 +319,155 @@ __global__ __launch_bounds__(kWG) void route_grad_kernel(RouteRows r, const floa
     }
 }
 
-// A row's largest magnitude comes from the bits: they order as the magnitudes do, and a NaN's are above
-// infinity's, so a NaN anywhere is found.
+// q = x / scale to the nearest integer, the division rounded to fp32 first; |x| <= 127 scale.
 __device__ __forceinline__ float quantised(float x, float scale)
 {
     const float v = rintf(x / scale);
     return scale > 0 ? fminf(fmaxf(v, -127.0f), 127.0f) : 0.0f;
 }
 
-// One workgroup per row of x; routed: its copies go to the slots of its choices.
-template <class T, bool ROUTED>
+// One wave or workgroup per row of x (WAVES); routed: its copies go to the slots of its choices.  A lane takes 16 elements at a
+// time, whose 16 bytes of q go out in one store; the first HELD of them stay in registers between the two passes
+// over the row (the others are read again).
+typedef uint32_t q_vec __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t q_whole __attribute__((ext_vector_type(4)));
+
+// The scale of a row, and what its elements are multiplied by instead of being divided by it: off by at most 1.5 units in the
+// last place, 2.3e-5 for quotients of up to 127, so that the nearest integer is the same unless the product is
+// that close to the middle between two (kNearHalf leaves twice the room); then, and for scales that have no
+// reciprocal (subnormal ones, 0, infinity, NaN: by = 0), the division itself is done.
+struct RowScale { float scale, by; };
+constexpr float kNearHalf = 0.49995f;
+__device__ __forceinline__ RowScale row_scale(uint32_t top)
+{
+    RowScale s;
+    s.scale = __uint_as_float(top) / 127.0f;
+    s.by = s.scale >= 0x1p-100f && s.scale <= 0x1p120f ? 1.0f / s.scale : 0.0f;
+    return s;
+}
+
+template <class T>
+struct Sixteen {
+    static constexpr int kElems = Unit<T>::kElems, kUnits = 16 / kElems;
+    Unit<T> u[kUnits];
+    __device__ __forceinline__ void load(const T *p, int n)         // n: elements that there are, more than 16 or none at all, too
+    {
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const int have = n - i * kElems;
+            u[i] = have > 0 ? load_some(p + i * kElems, have) : zero_unit<T>();
+        }
+    }
+    __device__ __forceinline__ float at(int j) const { return (float)u[j / kElems].v[j % kElems]; }
+    // The largest magnitude as the bits of a float: they order as the magnitudes do, and a NaN's are above infinity's, so a
+    // NaN anywhere is found.  16-bit types are compared two at a time before they are converted.
+    __device__ __forceinline__ uint32_t largest() const
+    {
+        if constexpr (sizeof(T) == 2) {
+            typedef unsigned short two __attribute__((ext_vector_type(2)));
+            typedef uint32_t words __attribute__((ext_vector_type(4)));
+            two top = {0, 0};
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) {
+                const words w = __builtin_bit_cast(words, u[i].v) & 0x7fff7fffu;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(two, (uint32_t)w[j]));
+            }
+            const unsigned short bits = top.x > top.y ? top.x : top.y;
+            return __float_as_uint((float)__builtin_bit_cast(T, bits));
+        } else {
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(at(j)) & 0x7fffffffu);
+            return top;
+        }
+    }
+    __device__ __forceinline__ q_whole quantise(const RowScale &s) const
+    {
+        constexpr float kMagic = 0x1.8p23f;      // v + kMagic is rounded to an integer, whose last byte is that of the sum
+        uint32_t b[16];
+        float worst = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float v = at(j) * s.by, up = v + kMagic;
+            worst = fmaxf(worst, fabsf(v - (up - kMagic)));
+            b[j] = __float_as_uint(up);
+        }
+        if (!(worst < kNearHalf) || s.by == 0) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) b[j] = (uint32_t)(int)quantised(at(j), s.scale);
+        }
+        q_whole q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t low = __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400), high = __builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x0c0c0400);
+            q[i] = low | high << 16;
+        }
+        return q;
+    }
+};
+
+template <class T, bool ROUTED, int WAVES, int HELD>
 __global__ __launch_bounds__(kWG) void quantize_kernel(RouteRows r, const T *__restrict__ x, int64_t ldx, int8_t *__restrict__ q,
                                                        int64_t ldq, uint32_t padded, float *__restrict__ scale)
 {
-    __shared__ uint32_t s_max[kWG / kWave];
-    for (uint32_t t = blockIdx.x; t < r.tokens; t += gridDim.x) {
-        constexpr int E = Unit<T>::kElems;
+    __shared__ uint32_t s_max[2][kWG / kWave];
+    constexpr uint32_t LANES = WAVES * kWave, ROWS = kWG / LANES;
+    const uint32_t lane = threadIdx.x % LANES;
+    uint32_t turn = 0;
+    for (uint32_t t = blockIdx.x * ROWS + threadIdx.x / LANES; t < r.tokens; t += gridDim.x * ROWS) {
         const T *row = x + (int64_t)t * ldx;
+        Sixteen<T> held[HELD];
         uint32_t top = 0;
-        for (uint32_t col = threadIdx.x * E; col < r.cols; col += kWG * E) {
-            const Unit<T> u = load_some(row + col, (int)min((uint32_t)E, r.cols - col));
 #pragma unroll
-            for (int j = 0; j < E; ++j) top = max(top, __float_as_uint((float)u.v[j]) & 0x7fffffffu);
+        for (int h = 0; h < HELD; ++h) {
+            const uint32_t col = (h * LANES + lane) * 16;
+            held[h].load(row + col, col < r.cols ? (int)(r.cols - col) : 0);
+        }
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+            if (h == 0 || (h * LANES + lane) * 16 < r.cols) top = max(top, held[h].largest());
+        for (uint32_t col = (HELD * LANES + lane) * 16; col < r.cols; col += LANES * 16) {
+            Sixteen<T> v;
+            v.load(row + col, (int)(r.cols - col));
+            top = max(top, v.largest());
         }
         top = lanes_fold(top, [](uint32_t a, uint32_t b) { return max(a, b); });
-        if ((threadIdx.x & 63) == 0) s_max[threadIdx.x / 64] = top;
-        __syncthreads();
-        top = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
-        const float s = __uint_as_float(top) / 127.0f;
-        for (uint32_t col = threadIdx.x * E; col < padded; col += kWG * E) {
-            const int have = col < r.cols ? (int)min((uint32_t)E, r.cols - col) : 0, n = (int)min((uint32_t)E, padded - col);
-            const Unit<T> u = load_some(row + col, have);
-            int8_t b[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) b[j] = j < have ? (int8_t)(int)quantised((float)u.v[j], s) : (int8_t)0;
+        if constexpr (WAVES > 1) {                     // (two sets: one barrier a row is enough)
+            if ((threadIdx.x & 63) == 0) s_max[turn][threadIdx.x / 64] = top;
+            __syncthreads();
+            top = max(max(s_max[turn][0], s_max[turn][1]), max(s_max[turn][2], s_max[turn][3]));
+            turn ^= 1;
+        }
+        const RowScale s = row_scale(top);
+        const auto store = [&](uint32_t col, const Sixteen<T> &v) {
+            const q_whole b = v.quantise(s);            // (the zeros behind the row's end give 0)
             for (uint32_t k = 0; k < r.choices; ++k) {
                 const int32_t slot = ROUTED ? r.choice_slot[t * r.choices + k] : (int32_t)t;
                 int8_t *to = q + (int64_t)(slot < 0 ? -1 - slot : slot) * ldq + col;
-                for (int j = 0; j < n; ++j) to[j] = slot < 0 ? (int8_t)0 : b[j];
+                q_whole out = b;
+                if (slot < 0) out = (q_whole)0u;
+                if (col + 16 <= padded) {
+                    *reinterpret_cast<q_vec *>(to) = out;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (col + j < padded) to[j] = (int8_t)(out[j / 4] >> (j % 4 * 8));
+                }
             }
+        };
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+            if ((h * LANES + lane) * 16 < padded) store((h * LANES + lane) * 16, held[h]);
+        for (uint32_t col = (HELD * LANES + lane) * 16; col < padded; col += LANES * 16) {
+            Sixteen<T> v;
+            v.load(row + col, (int)(r.cols - col));
+            store(col, v);
         }
-        for (uint32_t k = threadIdx.x; k < r.choices; k += kWG) {
+        for (uint32_t k = lane; k < r.choices; k += LANES) {
             const int32_t slot = ROUTED ? r.choice_slot[t * r.choices + k] : (int32_t)t;
-            scale[slot < 0 ? -1 - slot : slot] = slot < 0 ? 0.0f : s;
+            scale[slot < 0 ? -1 - slot : slot] = slot < 0 ? 0.0f : s.scale;
         }
-        __syncthreads();
     }
 }
 
@@ -418,16 +522,24 @@ void launch_route_grad(const RouteRows &rows, const float *weight, const seer_de
     });
 }
 
+template <class T, int WAVES, int HELD>
+static void launch_quantize_of(const RouteRows &rows, const seer_dense &x, const seer_dense &q, float *scale, hipStream_t st)
+{
+    const uint32_t padded = (uint32_t)std::min<int64_t>(q.ld, (x.cols + 15) & ~(int64_t)15), per = kWG / kWave / WAVES;
+    const dim3 grid(std::min((rows.tokens + per - 1) / per, kMaxGrid)), wg(kWG);
+    const T *xp = static_cast<const T *>(x.data);
+    int8_t *qp = static_cast<int8_t *>(q.data);
+    if (rows.choice_slot) hipLaunchKernelGGL((quantize_kernel<T, true, WAVES, HELD>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
+    else hipLaunchKernelGGL((quantize_kernel<T, false, WAVES, HELD>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
+}
+
 void launch_quantize(const RouteRows &rows, const seer_dense &x, const seer_dense &q, float *scale, hipStream_t st)
 {
-    const uint32_t padded = (uint32_t)std::min<int64_t>(q.ld, (x.cols + 15) & ~(int64_t)15);
     by_type(x.type, [&](auto *of) {
         using T = std::remove_pointer_t<decltype(of)>;
-        const dim3 grid(std::min(rows.tokens, kMaxGrid)), wg(kWG);
-        const T *xp = static_cast<const T *>(x.data);
-        int8_t *qp = static_cast<int8_t *>(q.data);
-        if (rows.choice_slot) hipLaunchKernelGGL((quantize_kernel<T, true>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
-        else hipLaunchKernelGGL((quantize_kernel<T, false>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
+        if (rows.cols <= 1024) launch_quantize_of<T, 1, 1>(rows, x, q, scale, st);
+        else if (rows.cols <= 4096) launch_quantize_of<T, 4, 1>(rows, x, q, scale, st);
+        else launch_quantize_of<T, 4, 2>(rows, x, q, scale, st);
     });
 }
 

@@ -213,3 +213,21 @@ def test_refusals():
     assert e.value.status == -6
     with pytest.raises(S.SeerError):
         S.seer_i8_quantize(torch.zeros(4, 8, device="cuda:0"), q=a)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_quantize_at_and_beside_the_middle(kind):
+    """Quotients at n + 1/2 and a few units in the last place to either side: the division decides."""
+    base = np.array([127.0, 3.3, 1e-3, 0.7, 2.0 ** -99, 2.0 ** -101, 1.7e38, 1.0 / 3]) if kind != "f16" else np.array([127.0, 3.3, 0.11, 0.7, 60000.0])
+    rows = []
+    for top in base:
+        top = np.float64(np.float32(top))
+        scale = np.float32(top) / np.float32(127)
+        half = np.arange(-126.5, 127, 1.0).astype(np.float64) * np.float64(scale)
+        near = np.concatenate([half * (1 + k * 2.0 ** -23) for k in range(-3, 4)])
+        rows.append(np.concatenate([[top], near]))
+    x = rounded(np.array(rows), kind)
+    q, s = S.seer_i8_quantize(x)
+    want_q, want_s = O.quantize(host(x))
+    assert np.array_equal(host(s).astype(np.float32), want_s)
+    assert np.array_equal(host(q), want_q)
