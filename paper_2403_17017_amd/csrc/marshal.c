@@ -159,6 +159,271 @@ static PyObject *m_bind(PyObject *self, PyObject *args)
     Py_RETURN_NONE;
 }
 
+/* ---- the routed layer (routed.py): tensors are described from their own attributes */
+
+static int (*f_route)(const void *, int32_t, const seer_routing *, void *, size_t, void *);
+static int (*f_gather)(const seer_routing *, const seer_dense *, const float *, const seer_dense *, void *);
+static int (*f_combine)(const seer_routing *, const seer_dense *, const float *, const seer_dense *, void *);
+static int (*f_grad)(const seer_routing *, const seer_dense *, const seer_dense *, const float *, const seer_dense *, float *, void *);
+static int (*f_quantize)(const seer_dense *, const seer_dense *, float *, void *);
+static int (*f_gather_i8)(const seer_routing *, const seer_dense *, const seer_dense *, float *, void *);
+static int (*f_product)(const seer_dense *, const float *, const seer_dense *, const float *, const int32_t *, int32_t,
+                        const seer_dense *, void *, size_t, void *);
+static int (*f_norm)(const seer_grad *, int32_t, float *, void *, size_t, void *);
+static int (*f_clip)(const seer_grad *, int32_t, float, float *, void *, size_t, void *);
+
+static PyObject *s_shape, *s_stride, *s_dtype, *s_is_cuda, *s_is_contiguous, *s_tokens, *s_choices, *s_experts, *s_expert_ptr,
+    *s_slot_choice, *s_choice_slot;
+static PyObject *types[6];                   /* torch's dtypes in the order of seer_type */
+
+static int refuse(PyObject *error, const char *what, const char *is)
+{
+    PyErr_Format(error, "%s %s", what, is);
+    return -1;
+}
+
+/* Truth of an attribute (call: of what it returns). */
+static int truth(PyObject *t, PyObject *name, int call)
+{
+    PyObject *v = call ? PyObject_CallMethodNoArgs(t, name) : PyObject_GetAttr(t, name);
+    if (!v) return -1;
+    const int is = PyObject_IsTrue(v);
+    Py_DECREF(v);
+    return is;
+}
+
+static int type_of(PyObject *t, const char *what)
+{
+    PyObject *d = PyObject_GetAttr(t, s_dtype);
+    if (!d) return -1;
+    for (int i = 0; i < 6; ++i)
+        if (d == types[i]) {
+            Py_DECREF(d);
+            return i;
+        }
+    PyErr_Format(PyExc_TypeError, "%s is %S", what, d);
+    Py_DECREF(d);
+    return -1;
+}
+
+/* The entries of a tuple of at most 3 integers; how many, or -1. */
+static int numbers(PyObject *tuple, int64_t out[3])
+{
+    if (!tuple) return -1;
+    int n = -1;
+    if (PyTuple_Check(tuple) && PyTuple_GET_SIZE(tuple) <= 3) {
+        n = (int)PyTuple_GET_SIZE(tuple);
+        for (int i = 0; i < n; ++i) out[i] = (int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(tuple, i));
+        if (PyErr_Occurred()) n = -1;
+    } else n = 4;
+    Py_DECREF(tuple);
+    return n;
+}
+
+static int on_gpu(PyObject *t, const char *what)
+{
+    const int is = truth(t, s_is_cuda, 0);
+    if (is < 0) return -1;
+    return is ? 0 : refuse(PyExc_ValueError, what, "is not on a GPU");
+}
+
+/* A 2-D tensor (deep: or a 3-D one, matrices one behind the other, *groups of them) as rows; ld as the library counts it. */
+static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer_dense *d)
+{
+    int64_t n[3], by[3];
+    const int dims = numbers(PyObject_GetAttr(t, s_shape), n);
+    if (dims < 0) return -1;
+    if (dims != 2 && !(deep && dims == 3)) return refuse(PyExc_ValueError, what, deep ? "is to be [groups, channels, columns]" : "is to be a matrix with contiguous rows");
+    if (numbers(PyObject_CallMethodNoArgs(t, s_stride), by) < 0) return -1;
+    if (dims == 2) {
+        n[2] = n[1], by[2] = by[1], n[1] = n[0], by[1] = by[0];
+        n[0] = 1, by[0] = 0;
+    }
+    if (n[2] > 1 && by[2] != 1 && n[0] > 0 && n[1] > 0) return refuse(PyExc_ValueError, what, "is to be a matrix with contiguous rows");
+    if (n[0] > 1 && n[1] > 1 && by[0] != n[1] * by[1]) return refuse(PyExc_ValueError, what, "is to have its matrices one behind the other");
+    if (on_gpu(t, what)) return -1;
+    uint64_t at;
+    if ((d->type = type_of(t, what)) < 0 || address_of(t, &at)) return -1;
+    d->data = (void *)(uintptr_t)at;
+    d->rows = n[0] * n[1];
+    d->cols = n[2];
+    d->ld = n[1] > 1 ? by[1] : n[0] > 1 ? by[0] : by[1] > n[2] ? by[1] : n[2];
+    if (groups) *groups = (int32_t)n[0];
+    return 0;
+}
+
+/* A contiguous tensor of n elements of a type; None: null. */
+static int vector(PyObject *t, const char *what, int type, int64_t n, uint64_t *at)
+{
+    *at = 0;
+    if (t == Py_None) return 0;
+    uint64_t count;
+    PyObject *d = PyObject_GetAttr(t, s_dtype);
+    if (!d) return -1;
+    const int same = d == types[type];
+    Py_DECREF(d);
+    const int whole = truth(t, s_is_contiguous, 1), there = truth(t, s_is_cuda, 0);
+    if (whole < 0 || there < 0 || taken(PyObject_CallMethodNoArgs(t, s_numel), as_size, &count)) return -1;
+    if (!same || !whole || !there || (int64_t)count != n) {
+        PyErr_Format(PyExc_ValueError, "%s is to be a contiguous %S tensor of %lld elements on the GPU", what, types[type], (long long)n);
+        return -1;
+    }
+    return address_of(t, at);
+}
+
+/* all: with the order of the slots; else only choice_slot, which is all that rows go by. */
+static int routing_of(PyObject *r, int all, seer_routing *c)
+{
+    uint64_t tokens, choices, experts, ptr = 0, order = 0, slots;
+    if (size_attr(r, s_tokens, &tokens) || size_attr(r, s_choices, &choices) || size_attr(r, s_experts, &experts) ||
+        address_attr(r, s_choice_slot, &slots) ||
+        (all && (address_attr(r, s_expert_ptr, &ptr) || address_attr(r, s_slot_choice, &order))))
+        return -1;
+    c->tokens = (int32_t)tokens;
+    c->choices = (int32_t)choices;
+    c->experts = (int32_t)experts;
+    c->expert_ptr = P(int32_t *, ptr);
+    c->slot_choice = P(int32_t *, order);
+    c->choice_slot = P(int32_t *, slots);
+    return 0;
+}
+
+static int space(PyObject *workspace, uint64_t *at, uint64_t *bytes)
+{
+    *at = *bytes = 0;
+    if (workspace == Py_None) return 0;
+    return address_of(workspace, at) || taken(PyObject_CallMethodNoArgs(workspace, s_numel), as_size, bytes) ? -1 : 0;
+}
+
+static int given(Py_ssize_t n, Py_ssize_t want)
+{
+    if (n == want) return 0;
+    PyErr_Format(PyExc_TypeError, "expected %zd arguments", want);
+    return -1;
+}
+
+#define ASYNC(call)                                                                                                                \
+    int rc;                                                                                                                        \
+    Py_BEGIN_ALLOW_THREADS                                                                                                         \
+    rc = call;                                                                                                                     \
+    Py_END_ALLOW_THREADS                                                                                                           \
+    return PyLong_FromLong(rc)
+
+static PyObject *m_route(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_routing r;
+    uint64_t at, ws, bytes, stream;
+    if (given(n, 4) || routing_of(a[1], 1, &r)) return NULL;
+    const int type = type_of(a[0], "expert");
+    if (type < 0 || vector(a[0], "expert", type, (int64_t)r.tokens * r.choices, &at) || space(a[2], &ws, &bytes) || as_size(a[3], &stream))
+        return NULL;
+    ASYNC(f_route(P(const void *, at), type, &r, P(void *, ws), (size_t)bytes, P(void *, stream)));
+}
+
+/* (routing, matrix by token, matrix by slot, weight, stream), whichever way the rows go */
+static int rows_parse(PyObject *const *a, Py_ssize_t n, const char *first, const char *second, seer_routing *r, seer_dense *x,
+                      seer_dense *y, uint64_t *weight, uint64_t *stream)
+{
+    return given(n, 5) || routing_of(a[0], 0, r) || matrix(a[1], first, 0, NULL, x) || matrix(a[2], second, 0, NULL, y) ||
+           vector(a[3], "weight", SEER_F32, (int64_t)r->tokens * r->choices, weight) || as_size(a[4], stream);
+}
+
+static PyObject *m_gather(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_routing r;
+    seer_dense x, out;
+    uint64_t weight, stream;
+    if (rows_parse(a, n, "x", "out", &r, &x, &out, &weight, &stream)) return NULL;
+    ASYNC(f_gather(&r, &x, P(const float *, weight), &out, P(void *, stream)));
+}
+
+static PyObject *m_combine(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_routing r;
+    seer_dense z, y;
+    uint64_t weight, stream;
+    if (rows_parse(a, n, "z", "y", &r, &z, &y, &weight, &stream)) return NULL;
+    ASYNC(f_combine(&r, &z, P(const float *, weight), &y, P(void *, stream)));
+}
+
+/* (routing, dy, z or None, weight or None, dz or None, dweight or None, stream) */
+static PyObject *m_grad(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_routing r;
+    seer_dense dy, z, dz;
+    uint64_t weight, dweight, stream;
+    if (given(n, 7) || routing_of(a[0], 0, &r) || matrix(a[1], "dy", 0, NULL, &dy) || (a[2] != Py_None && matrix(a[2], "z", 0, NULL, &z)) ||
+        vector(a[3], "weight", SEER_F32, (int64_t)r.tokens * r.choices, &weight) || (a[4] != Py_None && matrix(a[4], "dz", 0, NULL, &dz)) ||
+        vector(a[5], "dweight", SEER_F32, (int64_t)r.tokens * r.choices, &dweight) || as_size(a[6], &stream))
+        return NULL;
+    ASYNC(f_grad(&r, &dy, a[2] != Py_None ? &z : NULL, P(const float *, weight), a[4] != Py_None ? &dz : NULL, P(float *, dweight),
+                 P(void *, stream)));
+}
+
+/* (routing or None, x, q, scale, stream) */
+static PyObject *m_quantize(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_routing r;
+    seer_dense x, q;
+    uint64_t scale, stream;
+    const int routed = n == 5 && a[0] != Py_None;
+    if (given(n, 5) || (routed && routing_of(a[0], 0, &r)) || matrix(a[1], "x", 0, NULL, &x) || matrix(a[2], "q", 0, NULL, &q) ||
+        vector(a[3], "scale", SEER_F32, routed ? (int64_t)r.tokens * r.choices : x.rows, &scale) || as_size(a[4], &stream))
+        return NULL;
+    ASYNC(routed ? f_gather_i8(&r, &x, &q, P(float *, scale), P(void *, stream)) : f_quantize(&x, &q, P(float *, scale), P(void *, stream)));
+}
+
+/* (a, a_scale, b, b_scale, group_ptr or None, out, workspace or None, stream) */
+static PyObject *m_product(PyObject *self, PyObject *const *v, Py_ssize_t n)
+{
+    seer_dense a, b, out;
+    int32_t groups;
+    uint64_t sa, sb, ptr, ws, bytes, stream;
+    if (given(n, 8) || matrix(v[0], "a", 0, NULL, &a) || vector(v[1], "a_scale", SEER_F32, a.rows, &sa) || matrix(v[2], "b", 1, &groups, &b) ||
+        vector(v[3], "b_scale", SEER_F32, b.rows, &sb) || vector(v[4], "group_ptr", SEER_I32, (int64_t)groups + 1, &ptr) ||
+        matrix(v[5], "out", 0, NULL, &out) || space(v[6], &ws, &bytes) || as_size(v[7], &stream))
+        return NULL;
+    ASYNC(f_product(&a, P(const float *, sa), &b, P(const float *, sb), P(const int32_t *, ptr), groups, &out, P(void *, ws), (size_t)bytes,
+                    P(void *, stream)));
+}
+
+/* (address of the seer_grad array, count, max_norm or None, norm, workspace, stream) */
+static PyObject *m_clip(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    uint64_t list, count, norm, ws, bytes, stream;
+    if (given(n, 6) || as_size(a[0], &list) || as_size(a[1], &count) || vector(a[3], "norm", SEER_F32, 1, &norm) || space(a[4], &ws, &bytes) ||
+        as_size(a[5], &stream))
+        return NULL;
+    const int clip = a[2] != Py_None;
+    const double most = clip ? PyFloat_AsDouble(a[2]) : 0;
+    if (PyErr_Occurred()) return NULL;
+    ASYNC(clip ? f_clip(P(const seer_grad *, list), (int32_t)count, (float)most, P(float *, norm), P(void *, ws), (size_t)bytes, P(void *, stream))
+               : f_norm(P(const seer_grad *, list), (int32_t)count, P(float *, norm), P(void *, ws), (size_t)bytes, P(void *, stream)));
+}
+
+static PyObject *m_bind_routed(PyObject *self, PyObject *args)
+{
+    unsigned long long f[9];
+    PyObject *t[6];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKOOOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, t, t + 1, t + 2, t + 3, t + 4, t + 5))
+        return NULL;
+    f_route = P(int (*)(const void *, int32_t, const seer_routing *, void *, size_t, void *), f[0]);
+    f_gather = P(int (*)(const seer_routing *, const seer_dense *, const float *, const seer_dense *, void *), f[1]);
+    f_combine = P(int (*)(const seer_routing *, const seer_dense *, const float *, const seer_dense *, void *), f[2]);
+    f_grad = P(int (*)(const seer_routing *, const seer_dense *, const seer_dense *, const float *, const seer_dense *, float *, void *), f[3]);
+    f_quantize = P(int (*)(const seer_dense *, const seer_dense *, float *, void *), f[4]);
+    f_gather_i8 = P(int (*)(const seer_routing *, const seer_dense *, const seer_dense *, float *, void *), f[5]);
+    f_product = P(int (*)(const seer_dense *, const float *, const seer_dense *, const float *, const int32_t *, int32_t, const seer_dense *,
+                          void *, size_t, void *), f[6]);
+    f_norm = P(int (*)(const seer_grad *, int32_t, float *, void *, size_t, void *), f[7]);
+    f_clip = P(int (*)(const seer_grad *, int32_t, float, float *, void *, size_t, void *), f[8]);
+    for (int i = 0; i < 6; ++i) {
+        Py_INCREF(t[i]);
+        Py_XSETREF(types[i], t[i]);
+    }
+    Py_RETURN_NONE;
+}
+
 static PyMethodDef methods[] = {
     {"bind", m_bind, METH_VARARGS, "bind(spmv, spmv_auto, spmv_model, spmv_prepared): addresses of the library's functions"},
     {"spmv", (PyCFunction)(void (*)(void))m_spmv, METH_FASTCALL, "spmv(kernel_id, A, x, y, workspace, stream) -> status"},
@@ -167,6 +432,15 @@ static PyMethodDef methods[] = {
      "spmv_model(model address, A, x, y, workspace, stream) -> (status, path, kernel id)"},
     {"spmv_prepared", (PyCFunction)(void (*)(void))m_prepared, METH_FASTCALL,
      "spmv_prepared(plan address, A, x, y, workspace, stream) -> status"},
+    {"bind_routed", m_bind_routed, METH_VARARGS, "bind_routed(addresses of the routed layer's functions, torch's dtypes)"},
+    {"route", (PyCFunction)(void (*)(void))m_route, METH_FASTCALL, "route(expert, routing, workspace, stream) -> status"},
+    {"gather", (PyCFunction)(void (*)(void))m_gather, METH_FASTCALL, "gather(routing, x, out, weight, stream) -> status"},
+    {"combine", (PyCFunction)(void (*)(void))m_combine, METH_FASTCALL, "combine(routing, z, y, weight, stream) -> status"},
+    {"grad", (PyCFunction)(void (*)(void))m_grad, METH_FASTCALL, "grad(routing, dy, z, weight, dz, dweight, stream) -> status"},
+    {"quantize", (PyCFunction)(void (*)(void))m_quantize, METH_FASTCALL, "quantize(routing, x, q, scale, stream) -> status"},
+    {"product", (PyCFunction)(void (*)(void))m_product, METH_FASTCALL,
+     "product(a, a_scale, b, b_scale, group_ptr, out, workspace, stream) -> status"},
+    {"clip", (PyCFunction)(void (*)(void))m_clip, METH_FASTCALL, "clip(list address, count, max_norm, norm, workspace, stream) -> status"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the asynchronous calls", -1,
@@ -182,6 +456,12 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_values = PyUnicode_InternFromString("values");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_numel = PyUnicode_InternFromString("numel");
+    PyObject **const names[] = {&s_shape, &s_stride, &s_dtype, &s_is_cuda, &s_is_contiguous, &s_tokens, &s_choices, &s_experts, &s_expert_ptr,
+                                &s_slot_choice, &s_choice_slot};
+    const char *const spelt[] = {"shape", "stride", "dtype", "is_cuda", "is_contiguous", "tokens", "choices", "experts", "expert_ptr",
+                                 "slot_choice", "choice_slot"};
+    for (size_t i = 0; i < sizeof spelt / sizeof *spelt; ++i)
+        if (!(*names[i] = PyUnicode_InternFromString(spelt[i]))) return NULL;
     if (!s_rows || !s_cols || !s_nnz || !s_row_ptr || !s_col_idx || !s_values || !s_data_ptr || !s_numel) return NULL;
     return PyModule_Create(&module);
 }

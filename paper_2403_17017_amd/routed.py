@@ -29,15 +29,23 @@ class seer_grad(C.Structure):
     _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("type", C.c_int32)]
 
 
-_types = None
+_types = None       # torch's dtypes, the number of each as the library has it
+_torch = None
 
 
-def _type_ids():
-    global _types
+def _ready():
+    """The library and the native marshalling of its calls, loaded; torch is imported here."""
+    global _types, _torch
     if _types is None:
+        B.lib()
         import torch
-        _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3, torch.int32: 4, torch.int64: 5}
-    return _types
+        ids = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int8: 3, torch.int32: 4, torch.int64: 5}
+        L, m = B.lib(), B._marshal
+        m.bind_routed(*(C.cast(f, C.c_void_p).value for f in (
+            L.seer_route, L.seer_route_gather, L.seer_route_combine, L.seer_route_grad, L.seer_i8_quantize, L.seer_route_gather_i8,
+            L.seer_i8_product, L.seer_grad_norm, L.seer_grad_clip)), *ids)
+        _types, _torch = ids, torch
+    return B._marshal
 
 
 def bind(L):
@@ -63,39 +71,18 @@ def bind(L):
 
 def _new(shape, dtype, like, stream):
     """Memory for an output or a workspace that `stream` is going to write."""
-    import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     if not hasattr(stream, "cuda_stream"):
         raise ValueError("pass every output and workspace when stream is a raw handle: the allocator does not know it")
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=like.device)
+    with _torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _dense(t, what):
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1 and t.shape[0] > 0):
+def _matrix_shape(t, what):
+    if t.dim() != 2:
         raise ValueError(f"{what} is to be a matrix with contiguous rows")
-    if not t.is_cuda:
-        raise ValueError(f"{what} is not on a GPU")
-    type_id = _type_ids().get(t.dtype)
-    if type_id is None:
-        raise TypeError(f"{what} is {t.dtype}")
-    rows, cols = t.shape
-    return seer_dense(t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else max(cols, t.stride(0)), type_id)
-
-
-def _vector(t, what, dtype, n):
-    """The address of a contiguous tensor of n elements (None: null)."""
-    if t is None:
-        return None
-    if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda or t.numel() != n:
-        raise ValueError(f"{what} is to be a contiguous {dtype} tensor of {n} elements on the GPU")
-    return t.data_ptr()
-
-
-def _check(rc, what):
-    if rc:
-        raise SeerError(rc, what)
+    return t.shape
 
 
 class Routing:
@@ -105,24 +92,29 @@ class Routing:
     __slots__ = ("experts", "tokens", "choices", "expert_ptr", "slot_choice", "choice_slot")
 
     def __init__(self, experts: int, expert_ptr, slot_choice, choice_slot):
-        import torch
+        _ready()
         self.experts = int(experts)
         self.tokens, self.choices = choice_slot.shape
         self.expert_ptr, self.slot_choice, self.choice_slot = expert_ptr, slot_choice, choice_slot
-        _vector(expert_ptr, "expert_ptr", torch.int32, self.experts + 1)
-        _vector(slot_choice, "slot_choice", torch.int32, self.tokens * self.choices)
-        _vector(choice_slot, "choice_slot", torch.int32, self.tokens * self.choices)
+        for t, n in ((expert_ptr, self.experts + 1), (slot_choice, self.tokens * self.choices), (choice_slot, self.tokens * self.choices)):
+            if t.dtype != _torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() != n:
+                raise ValueError("a routing has contiguous int32 tensors of experts + 1, tokens * choices and as many elements on the GPU")
 
     @classmethod
     def empty(cls, tokens: int, choices: int, experts: int, device="cuda:0") -> "Routing":
         """Memory for seer_route to fill."""
-        import torch
-        n = lambda *shape: torch.empty(shape, dtype=torch.int32, device=device)
+        _ready()
+        n = lambda *shape: _torch.empty(shape, dtype=_torch.int32, device=device)
         return cls(experts, n(experts + 1), n(tokens * choices), n(tokens, choices))
 
-    def c_struct(self) -> seer_routing:
-        return seer_routing(self.tokens, self.choices, self.experts, self.expert_ptr.data_ptr(), self.slot_choice.data_ptr(),
-                            self.choice_slot.data_ptr())
+    @classmethod
+    def _new(cls, tokens, choices, experts, like, stream):
+        """The same in one piece, for seer_route."""
+        self, count = cls.__new__(cls), tokens * choices
+        self.experts, self.tokens, self.choices = experts, tokens, choices
+        self.expert_ptr, self.slot_choice, slots = _new((experts + 1 + 2 * count,), _torch.int32, like, stream).split((experts + 1, count, count))
+        self.choice_slot = slots.view(tokens, choices)
+        return self
 
 
 def route_workspace_bytes(tokens: int, choices: int, experts: int) -> int:
@@ -132,91 +124,91 @@ def route_workspace_bytes(tokens: int, choices: int, experts: int) -> int:
 def seer_route(expert, experts: int, routing: Routing = None, workspace=None, stream=None) -> Routing:
     """The choices expert [tokens, choices] (int32 or int64; anything outside [0, experts) is no expert's) sorted by
     expert; asynchronous on the stream."""
-    import torch
-    L = B.lib()
-    if expert.dim() != 2 or not expert.is_contiguous() or not expert.is_cuda or expert.dtype not in (torch.int32, torch.int64):
+    m = _ready()
+    if expert.dim() != 2 or not expert.is_cuda or expert.dtype not in (_torch.int32, _torch.int64):
         raise ValueError("expert is to be a contiguous int32 or int64 matrix [tokens, choices] on the GPU")
     tokens, choices = expert.shape
     if routing is None:
-        n = max(int(experts), 0)
-        routing = Routing(n, _new((n + 1,), torch.int32, expert, stream), _new((tokens * choices,), torch.int32, expert, stream),
-                          _new((tokens, choices), torch.int32, expert, stream))
+        routing = Routing._new(tokens, choices, max(int(experts), 0), expert, stream)
     elif (routing.tokens, routing.choices, routing.experts) != (tokens, choices, experts):
         raise ValueError("routing has other sizes")
-    need = L.seer_route_workspace_bytes(tokens, choices, experts)
-    if need and workspace is None:
-        workspace = _new((need,), torch.uint8, expert, stream)
-    _check(L.seer_route(expert.data_ptr(), _type_ids()[expert.dtype], C.byref(routing.c_struct()),
-                        workspace.data_ptr() if workspace is not None else None,
-                        workspace.numel() if workspace is not None else 0, _stream_handle(stream)), "seer_route")
+    if workspace is None:
+        need = B._lib.seer_route_workspace_bytes(tokens, choices, routing.experts)
+        if need:
+            workspace = _new((need,), _torch.uint8, expert, stream)
+    rc = m.route(expert, routing, workspace, _stream_handle(stream))
+    if rc:
+        raise SeerError(rc, "seer_route")
     return routing
-
-
-def _weight(weight, r):
-    import torch
-    return _vector(weight, "weight", torch.float32, r.tokens * r.choices)
 
 
 def seer_route_gather(r: Routing, x, out=None, weight=None, stream=None):
     """x [tokens, n] brought into the experts' order, out [tokens * choices, n], rows times weight if given."""
+    m = _ready()
     if out is None:
-        out = _new((r.tokens * r.choices, x.shape[1]), x.dtype, x, stream)
-    _check(B.lib().seer_route_gather(C.byref(r.c_struct()), C.byref(_dense(x, "x")), _weight(weight, r), C.byref(_dense(out, "out")),
-                                     _stream_handle(stream)), "seer_route_gather")
+        out = _new((r.tokens * r.choices, _matrix_shape(x, "x")[1]), x.dtype, x, stream)
+    rc = m.gather(r, x, out, weight, _stream_handle(stream))
+    if rc:
+        raise SeerError(rc, "seer_route_gather")
     return out
 
 
 def seer_route_combine(r: Routing, z, y=None, weight=None, stream=None):
     """The experts' rows z [tokens * choices, n] added up by token, times weight if given: y [tokens, n]."""
+    m = _ready()
     if y is None:
-        y = _new((r.tokens, z.shape[1]), z.dtype, z, stream)
-    _check(B.lib().seer_route_combine(C.byref(r.c_struct()), C.byref(_dense(z, "z")), _weight(weight, r), C.byref(_dense(y, "y")),
-                                      _stream_handle(stream)), "seer_route_combine")
+        y = _new((r.tokens, _matrix_shape(z, "z")[1]), z.dtype, z, stream)
+    rc = m.combine(r, z, y, weight, _stream_handle(stream))
+    if rc:
+        raise SeerError(rc, "seer_route_combine")
     return y
 
 
 def seer_route_grad(r: Routing, dy, z, weight=None, dz=None, dweight=None, stream=None, need_dz=True, need_dweight=True):
     """(dz, dweight): the gradients of seer_route_combine in z and weight for that of its output, dy."""
-    import torch
+    m = _ready()
     if dz is None and need_dz:
-        dz = _new((r.tokens * r.choices, dy.shape[1]), dy.dtype, dy, stream)
+        dz = _new((r.tokens * r.choices, _matrix_shape(dy, "dy")[1]), dy.dtype, dy, stream)
     if dweight is None and need_dweight:
-        dweight = _new((r.tokens, r.choices), torch.float32, dy, stream)
-    _check(B.lib().seer_route_grad(C.byref(r.c_struct()), C.byref(_dense(dy, "dy")), C.byref(_dense(z, "z")) if z is not None else None,
-                                   _weight(weight, r), C.byref(_dense(dz, "dz")) if dz is not None else None,
-                                   _vector(dweight, "dweight", torch.float32, r.tokens * r.choices), _stream_handle(stream)),
-           "seer_route_grad")
+        dweight = _new((r.tokens, r.choices), _torch.float32, dy, stream)
+    rc = m.grad(r, dy, z, weight, dz, dweight, _stream_handle(stream))
+    if rc:
+        raise SeerError(rc, "seer_route_grad")
     return dz, dweight
 
 
 def _new_i8(rows, cols, like, stream):
     """int8 rows at distances of a multiple of 16, which is what products read fastest."""
-    import torch
-    return _new((rows, (cols + 15) // 16 * 16), torch.int8, like, stream)[:, :cols]
+    if cols % 16 == 0:
+        return _new((rows, cols), _torch.int8, like, stream)
+    return _new((rows, (cols + 15) // 16 * 16), _torch.int8, like, stream)[:, :cols]
 
 
 def seer_i8_quantize(x, q=None, scale=None, stream=None):
     """(q, scale): the rows of x in 8-bit integers with a scale each."""
-    import torch
+    m = _ready()
+    rows, cols = _matrix_shape(x, "x")
     if q is None:
-        q = _new_i8(x.shape[0], x.shape[1], x, stream)
+        q = _new_i8(rows, cols, x, stream)
     if scale is None:
-        scale = _new((x.shape[0],), torch.float32, x, stream)
-    _check(B.lib().seer_i8_quantize(C.byref(_dense(x, "x")), C.byref(_dense(q, "q")),
-                                    _vector(scale, "scale", torch.float32, x.shape[0]), _stream_handle(stream)), "seer_i8_quantize")
+        scale = _new((rows,), _torch.float32, x, stream)
+    rc = m.quantize(None, x, q, scale, _stream_handle(stream))
+    if rc:
+        raise SeerError(rc, "seer_i8_quantize")
     return q, scale
 
 
 def seer_route_gather_i8(r: Routing, x, q=None, scale=None, stream=None):
     """(q, scale): x [tokens, n] in 8-bit integers, brought into the experts' order."""
-    import torch
+    m = _ready()
     rows = r.tokens * r.choices
     if q is None:
-        q = _new_i8(rows, x.shape[1], x, stream)
+        q = _new_i8(rows, _matrix_shape(x, "x")[1], x, stream)
     if scale is None:
-        scale = _new((rows,), torch.float32, x, stream)
-    _check(B.lib().seer_route_gather_i8(C.byref(r.c_struct()), C.byref(_dense(x, "x")), C.byref(_dense(q, "q")),
-                                        _vector(scale, "scale", torch.float32, rows), _stream_handle(stream)), "seer_route_gather_i8")
+        scale = _new((rows,), _torch.float32, x, stream)
+    rc = m.quantize(r, x, q, scale, _stream_handle(stream))
+    if rc:
+        raise SeerError(rc, "seer_route_gather_i8")
     return q, scale
 
 
@@ -228,31 +220,27 @@ def seer_i8_product(a, a_scale, b, b_scale, out=None, group_ptr=None, dtype=None
     """out[i, n] = a_scale[i] * b_scale[g, n] * sum_k a[i, k] * b[g, n, k] for the rows i of group g (group_ptr, int32
     [groups + 1]; None: one group).  a int8 [rows, k], b int8 [groups, channels, k] or, for one group, [channels, k];
     out of type dtype (bfloat16 if neither is given)."""
-    import torch
-    L = B.lib()
-    if b.dim() == 2:
-        b = b.unsqueeze(0)
-    if b.dim() != 3:
+    m = _ready()
+    if a_scale is None or b_scale is None:
+        raise ValueError("a_scale and b_scale are wanted")
+    shape = b.shape
+    if len(shape) not in (2, 3):
         raise ValueError("b is to be [groups, channels, columns]")
-    groups, channels, columns = b.shape
-    if groups > 1 and channels > 1 and b.stride(0) != channels * b.stride(1):
-        raise ValueError("the matrices of b are to lie one behind the other")
+    groups, channels, columns = shape if len(shape) == 3 else (1, *shape)
+    rows = _matrix_shape(a, "a")[0]
+    if b.dtype != _torch.int8:
+        raise ValueError("b is to be an int8 tensor")
     if out is None:
-        out = _new((a.shape[0], channels), dtype or torch.bfloat16, a, stream)
+        out = _new((rows, channels), dtype or _torch.bfloat16, a, stream)
     elif dtype is not None and out.dtype != dtype:
         raise TypeError(f"out is {out.dtype}, not {dtype}")
-    need = L.seer_i8_product_workspace_bytes(a.shape[0], channels, columns, groups)
-    if need and workspace is None:
-        workspace = _new((need,), torch.uint8, a, stream)
-    if not b.is_cuda or b.dtype != torch.int8 or (columns > 1 and b.stride(2) != 1):
-        raise ValueError("b is to be an int8 tensor on the GPU with contiguous rows")
-    ld = b.stride(1) if channels > 1 else b.stride(0) if groups > 1 else columns
-    _check(L.seer_i8_product(C.byref(_dense(a, "a")), _vector(a_scale, "a_scale", torch.float32, a.shape[0]),
-                             C.byref(seer_dense(b.data_ptr(), groups * channels, columns, ld, 3)),
-                             _vector(b_scale, "b_scale", torch.float32, groups * channels),
-                             _vector(group_ptr, "group_ptr", torch.int32, groups + 1), groups, C.byref(_dense(out, "out")),
-                             workspace.data_ptr() if workspace is not None else None,
-                             workspace.numel() if workspace is not None else 0, _stream_handle(stream)), "seer_i8_product")
+    if workspace is None:
+        need = B._lib.seer_i8_product_workspace_bytes(rows, channels, columns, groups)
+        if need:
+            workspace = _new((need,), _torch.uint8, a, stream)
+    rc = m.product(a, a_scale, b, b_scale, group_ptr, out, workspace, _stream_handle(stream))
+    if rc:
+        raise SeerError(rc, "seer_i8_product")
     return out
 
 
@@ -265,7 +253,8 @@ class GradTensors:
     (else it is clipped in place).  Keeps the tensors; made once for gradients that stay where they are."""
 
     def __init__(self, grads, outs=None):
-        ids = _type_ids()
+        _ready()
+        ids = _types
         self.grads, self.outs = list(grads), list(outs) if outs is not None else None
         to = self.outs if self.outs is not None else self.grads
         if len(to) != len(self.grads):
@@ -282,33 +271,28 @@ class GradTensors:
             self.c[i] = seer_grad(g.data_ptr(), o.data_ptr(), g.numel(), ids[g.dtype])
 
 
-def _grad_call(tensors, norm, workspace, stream):
-    import torch
+def _grad_call(what, tensors, max_norm, norm, workspace, stream):
+    m = _ready()
     if not isinstance(tensors, GradTensors):
         tensors = GradTensors(tensors)
     if norm is None:
         if not tensors.count:
             raise ValueError("pass norm= where there are no tensors: nothing says which GPU it is to lie on")
-        norm = _new((), torch.float32, tensors.grads[0], stream)
+        norm = _new((), _torch.float32, tensors.grads[0], stream)
     if workspace is None:
-        workspace = _new((grad_workspace_bytes(),), torch.uint8, norm, stream)
-    return tensors, norm, workspace
+        workspace = _new((grad_workspace_bytes(),), _torch.uint8, norm, stream)
+    rc = m.clip(C.addressof(tensors.c), tensors.count, max_norm, norm, workspace, _stream_handle(stream))
+    if rc:
+        raise SeerError(rc, what)
+    return norm
 
 
 def seer_grad_norm(tensors, norm=None, workspace=None, stream=None):
     """The norm over all gradients (a GradTensors, or a list of tensors), as a tensor of one fp32 element."""
-    import torch
-    tensors, norm, workspace = _grad_call(tensors, norm, workspace, stream)
-    _check(B.lib().seer_grad_norm(tensors.c, tensors.count, _vector(norm, "norm", torch.float32, 1), workspace.data_ptr(),
-                                  workspace.numel(), _stream_handle(stream)), "seer_grad_norm")
-    return norm
+    return _grad_call("seer_grad_norm", tensors, None, norm, workspace, stream)
 
 
 def seer_grad_clip(tensors, max_norm: float, norm=None, workspace=None, stream=None):
     """Clips the gradients by their norm, which is returned: each becomes itself times max_norm / (norm + 1e-6) where that
     is less than 1, in place or in the GradTensors' outputs."""
-    import torch
-    tensors, norm, workspace = _grad_call(tensors, norm, workspace, stream)
-    _check(B.lib().seer_grad_clip(tensors.c, tensors.count, float(max_norm), _vector(norm, "norm", torch.float32, 1),
-                                  workspace.data_ptr(), workspace.numel(), _stream_handle(stream)), "seer_grad_clip")
-    return norm
+    return _grad_call("seer_grad_clip", tensors, float(max_norm), norm, workspace, stream)
