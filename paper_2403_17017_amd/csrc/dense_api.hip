@@ -250,8 +250,7 @@ int seer_grad_clip(const seer_grad *tensors, int32_t count, float max_norm, floa
     if (rc != SEER_OK) return rc;
     if (!(max_norm >= 0.0f)) return SEER_EINVAL;
     if (!workspace || !aligned16(workspace) || workspace_bytes < grad_workspace_bytes()) return SEER_EWORKSPACE;
-    launch_grad_norm(tensors, count, norm, workspace, on(stream));
-    launch_grad_clip(tensors, count, max_norm, norm, on(stream));
+    launch_grad_clip(tensors, count, max_norm, norm, workspace, on(stream));
     return done();
 }
 

@@ -43,6 +43,6 @@ void launch_i8_product(const I8Args &a, void *workspace, hipStream_t st);
 constexpr uint32_t kGradParts = 2048;       // partial sums of squares
 inline size_t grad_workspace_bytes() { return kGradParts * sizeof(double); }
 void launch_grad_norm(const seer_grad *tensors, int32_t count, float *norm, void *workspace, hipStream_t st);
-void launch_grad_clip(const seer_grad *tensors, int32_t count, float max_norm, const float *norm, hipStream_t st);
+void launch_grad_clip(const seer_grad *tensors, int32_t count, float max_norm, float *norm, void *workspace, hipStream_t st);
 
 } // namespace seer

@@ -1,163 +1,223 @@
 // The norm over many gradient tensors, and the gradients clipped by it.  A list of tensors is a matrix of ragged
 // rows; the work is cut into chunks of equal size whatever tensor they belong to.  Where the tensors lie travels in
-// the kernel arguments, as many as fit at a time.
+// the kernel arguments, as many as fit 4 KB at a time.  Bound by bytes: every gradient is read for the norm and, since that has to be
+// known first, once more; the second pass goes backwards, so that it begins with what the first has left in the last-level cache.
 #include "dense.hiph"
 #include "dense_launch.h"
 
 namespace seer {
 
-constexpr uint32_t kGradUnits = 16;                 // units of 16 bytes per lane and chunk
-constexpr int kGradList = 128;
-constexpr uint32_t kGradChunk = kWG * kGradUnits;   // units per chunk
+constexpr uint32_t kGradUnits = 4;                  // units of 16 bytes per lane and chunk
+constexpr uint32_t kGradChunk = kWG * kGradUnits;   // units per chunk (16 KB; 8 and 32 KB: 2 % slower, 2 and 8 KB: 10 %)
+constexpr int kSquareList = 288, kScaleList = 180;
 
+// Tensors of one type: `end` chunks up to and with each, `rest` elements in the last chunk of each less one.
+template <int N>
 struct GradList {
-    const void *grad[kGradList];
-    int64_t n[kGradList];
-    uint32_t end[kGradList];                        // chunks up to and with this tensor's
+    const void *grad[N];
+    uint32_t end[N];
+    uint16_t rest[N];
     uint32_t count;
-    int add;                                        // sums are added to what an earlier launch left
 };
-struct ClipList {
-    GradList g;
-    void *out[kGradList];
+template <int N>
+struct OutList {
+    void *out[N];
+};
+static_assert(sizeof(GradList<kSquareList>) + 24 <= 4096 && sizeof(GradList<kScaleList>) + sizeof(OutList<kScaleList>) + 32 <= 4096,
+              "the lists fit the kernel arguments");
+
+// A chunk: `have` elements from element `begin` on of tensor i.
+struct Chunk {
+    uint32_t i, have;
+    int64_t begin;
 };
 
-// The tensor that chunk c belongs to (uniform).
-__device__ __forceinline__ uint32_t tensor_of(const GradList &l, uint32_t c)
+// Chunk c of the list, of E elements a unit; `back`: a tensor's chunks are counted from its end.  The lanes of a wave look for the
+// tensor together; the result is uniform.
+template <int E, int N>
+__device__ __forceinline__ Chunk chunk_of(const GradList<N> &l, uint32_t c, bool back)
 {
-    uint32_t lo = 0, hi = l.count - 1;
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (l.end[mid] > c) hi = mid;
-        else lo = mid + 1;
+    uint32_t i = 0;
+    for (uint32_t at = 0; at < l.count; at += kWave) {
+        const uint32_t mine = at + (threadIdx.x & 63);
+        const uint64_t past = __ballot(mine < l.count && l.end[min(mine, (uint32_t)N - 1)] <= c);
+        i += (uint32_t)__popcll(past);
+        if (past != ~0ull) break;
     }
-    return lo;
+    const uint32_t first = i ? l.end[i - 1] : 0, last = l.end[i] - 1 - first;
+    const uint32_t k = back ? last - (c - first) : c - first;
+    return Chunk{i, k == last ? (uint32_t)l.rest[i] + 1 : kGradChunk * E, (int64_t)k * (kGradChunk * E)};
+}
+
+// Sum over a workgroup in a fixed order, in every lane.
+__device__ __forceinline__ double workgroup_sum(double v, double *s_sum)
+{
+    v = lanes_fold(v, [](double a, double b) { return a + b; });
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x / 64] = v;
+    __syncthreads();
+    return (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
 }
 
 // Sums of squares in fp64: no gradient is too large or too small to be squared, and a billion terms lose nothing.
+// part[b] is added to where an earlier launch has left something there (b < left).
 template <class T>
-__global__ __launch_bounds__(kWG) void grad_square_kernel(GradList l, double *__restrict__ part)
+__global__ __launch_bounds__(kWG) void grad_square_kernel(GradList<kSquareList> l, double *__restrict__ part, uint32_t left)
 {
     constexpr int E = Unit<T>::kElems;
     __shared__ double s_sum[kWG / kWave];
-    double sum = 0;
+    double sum[2] = {0, 0};
+    const auto add = [&](const Unit<T> &u) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const double v = (double)(float)u.v[j];
+            sum[j & 1] = fma(v, v, sum[j & 1]);
+        }
+    };
     for (uint32_t c = blockIdx.x; c < l.end[l.count - 1]; c += gridDim.x) {
-        const uint32_t i = tensor_of(l, c);
-        const T *g = static_cast<const T *>(l.grad[i]);
-        const int64_t n = l.n[i], begin = (int64_t)(c - (i ? l.end[i - 1] : 0)) * kGradChunk * E;
+        const Chunk k = chunk_of<E>(l, c, false);
+        const T *g = static_cast<const T *>(l.grad[k.i]) + k.begin + threadIdx.x * E;
+        if (k.have == kGradChunk * E) {
+            Unit<T> u[kGradUnits];
 #pragma unroll
-        for (uint32_t k = 0; k < kGradUnits; ++k) {
-            const int64_t at = begin + (int64_t)(k * kWG + threadIdx.x) * E;
-            if (at >= n) break;
-            const Unit<T> u = load_some(g + at, (int)min((int64_t)E, n - at));
+            for (uint32_t h = 0; h < kGradUnits; ++h) u[h] = load_unit(g + h * kWG * E);
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const double v = (double)(float)u.v[j];
-                sum = fma(v, v, sum);
+            for (uint32_t h = 0; h < kGradUnits; ++h) add(u[h]);
+        } else {
+            for (uint32_t at = threadIdx.x * E; at < k.have; at += kWG * E, g += kWG * E)
+                add(load_some(g, (int)min((uint32_t)E, k.have - at)));
+        }
+    }
+    const double all = workgroup_sum(sum[0] + sum[1], s_sum);
+    if (threadIdx.x == 0) part[blockIdx.x] = blockIdx.x < left ? part[blockIdx.x] + all : all;
+}
+
+__device__ __forceinline__ float norm_of(const double *part, uint32_t parts, double *s_sum)
+{
+    double v[kGradParts / kWG], sum = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kGradParts / kWG; ++i) v[i] = i * kWG + threadIdx.x < parts ? part[i * kWG + threadIdx.x] : 0.0;
+#pragma unroll
+    for (uint32_t i = 0; i < kGradParts / kWG; ++i) sum += v[i];
+    return (float)sqrt(workgroup_sum(sum, s_sum));
+}
+
+__global__ __launch_bounds__(kWG) void grad_norm_kernel(const double *__restrict__ part, uint32_t parts, float *__restrict__ norm)
+{
+    __shared__ double s_sum[kWG / kWave];
+    const float n = norm_of(part, parts, s_sum);
+    if (threadIdx.x == 0) norm[0] = n;
+}
+
+// Every workgroup folds the partial sums for itself (16 KB at most, from L2): quicker than a launch of one workgroup between
+// the two passes.
+template <class T>
+__global__ __launch_bounds__(kWG) void grad_scale_kernel(GradList<kScaleList> l, OutList<kScaleList> o, const double *__restrict__ part,
+                                                         uint32_t parts, float max_norm, float *__restrict__ norm)
+{
+    constexpr int E = Unit<T>::kElems;
+    __shared__ double s_sum[kWG / kWave];
+    const float n = norm_of(part, parts, s_sum);
+    if (blockIdx.x == 0 && threadIdx.x == 0) norm[0] = n;
+    float by = max_norm / (n + 1e-6f);
+    if (by >= 1.0f) by = 1.0f;
+    const auto scaled = [by](Unit<T> u) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) u.v[j] = (T)(by * (float)u.v[j]);
+        return u;
+    };
+    for (uint32_t c = blockIdx.x; c < l.end[l.count - 1]; c += gridDim.x) {
+        const Chunk k = chunk_of<E>(l, c, true);
+        if (by == 1.0f && l.grad[k.i] == o.out[k.i]) continue;          // nothing changes
+        const T *g = static_cast<const T *>(l.grad[k.i]) + k.begin + threadIdx.x * E;
+        T *out = static_cast<T *>(o.out[k.i]) + k.begin + threadIdx.x * E;
+        if (k.have == kGradChunk * E) {
+            Unit<T> u[kGradUnits];
+#pragma unroll
+            for (uint32_t h = 0; h < kGradUnits; ++h) u[h] = stream_unit(g + h * kWG * E);
+#pragma unroll
+            for (uint32_t h = 0; h < kGradUnits; ++h) stream_unit(out + h * kWG * E, scaled(u[h]));
+        } else {
+            for (uint32_t at = threadIdx.x * E; at < k.have; at += kWG * E, g += kWG * E, out += kWG * E) {
+                const int have = (int)min((uint32_t)E, k.have - at);
+                store_some(out, scaled(load_some(g, have)), have);
             }
         }
     }
-    sum = lanes_fold(sum, [](double a, double b) { return a + b; });
-    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x / 64] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
-        part[blockIdx.x] = l.add ? part[blockIdx.x] + sum : sum;
-    }
 }
 
-__global__ __launch_bounds__(kWG) void grad_fold_kernel(const double *__restrict__ part, uint32_t n, float *__restrict__ norm)
-{
-    __shared__ double s_sum[kWG / kWave];
-    double sum = 0;
-    for (uint32_t i = threadIdx.x; i < n; i += kWG) sum += part[i];
-    sum = lanes_fold(sum, [](double a, double b) { return a + b; });
-    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x / 64] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) norm[0] = (float)sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
-}
-
-template <class T>
-__global__ __launch_bounds__(kWG) void grad_scale_kernel(ClipList l, const float *__restrict__ norm, float max_norm)
-{
-    constexpr int E = Unit<T>::kElems;
-    float by = max_norm / (norm[0] + 1e-6f);
-    if (by >= 1.0f) by = 1.0f;
-    for (uint32_t c = blockIdx.x; c < l.g.end[l.g.count - 1]; c += gridDim.x) {
-        const uint32_t i = tensor_of(l.g, c);
-        const T *g = static_cast<const T *>(l.g.grad[i]);
-        T *out = static_cast<T *>(l.out[i]);
-        if (by == 1.0f && g == out) continue;           // nothing changes
-        const int64_t n = l.g.n[i], begin = (int64_t)(c - (i ? l.g.end[i - 1] : 0)) * kGradChunk * E;
-#pragma unroll
-        for (uint32_t k = 0; k < kGradUnits; ++k) {
-            const int64_t at = begin + (int64_t)(k * kWG + threadIdx.x) * E;
-            if (at >= n) break;
-            const int have = (int)min((int64_t)E, n - at);
-            Unit<T> u = load_some(g + at, have);
-#pragma unroll
-            for (int j = 0; j < E; ++j) u.v[j] = (T)(by * (float)u.v[j]);
-            store_some(out + at, u, have);
-        }
-    }
-}
-
-// The tensors of one type from number `from` on that fit one launch; `from` is where the next list begins.
-template <class T>
-static bool next_list(const seer_grad *tensors, int32_t count, int type, int32_t *from, GradList *l, void **out)
+// The tensors of one type from number *from on (step 1: upwards, -1: downwards) that fit one launch; *from is where the next
+// list begins.
+template <class T, int N>
+static bool next_list(const seer_grad *tensors, int32_t count, int type, int32_t *from, int32_t step, GradList<N> *l, OutList<N> *o)
 {
     constexpr uint64_t per = (uint64_t)kGradChunk * Unit<T>::kElems;
+    static_assert(per <= 65536, "the rest of a chunk has 16 bits");
     l->count = 0;
     uint64_t chunks = 0;
-    for (; *from < count && l->count < kGradList; ++*from) {
+    for (; *from >= 0 && *from < count && l->count < (uint32_t)N; *from += step) {
         const seer_grad &t = tensors[*from];
         if (t.type != type || t.n == 0) continue;
         const uint64_t more = ((uint64_t)t.n + per - 1) / per;
         if (l->count && chunks + more > 0x7fffffffu) break;
         l->grad[l->count] = t.grad;
-        l->n[l->count] = t.n;
-        if (out) out[l->count] = t.out;
+        l->rest[l->count] = (uint16_t)(((uint64_t)t.n - 1) % per);
+        if (o) o->out[l->count] = t.out;
         chunks += more;
         l->end[l->count++] = (uint32_t)chunks;
     }
     return l->count != 0;
 }
 
-template <class F>
-static void each_type(F f)
+template <int N>
+static uint32_t grid_of(const GradList<N> &l) { return std::min(l.end[l.count - 1], kGradParts); }
+
+template <class T>
+static void launch_squares(const seer_grad *tensors, int32_t count, int type, double *part, uint32_t *parts, hipStream_t st)
 {
-    f((float *)nullptr, SEER_F32);
-    f((bf16_t *)nullptr, SEER_BF16);
-    f((f16_t *)nullptr, SEER_F16);
+    GradList<kSquareList> l;
+    for (int32_t from = 0; next_list<T>(tensors, count, type, &from, 1, &l, (OutList<kSquareList> *)nullptr);) {
+        const uint32_t grid = grid_of(l);
+        hipLaunchKernelGGL((grad_square_kernel<T>), dim3(grid), dim3(kWG), 0, st, l, part, *parts);
+        *parts = std::max(*parts, grid);
+    }
+}
+
+template <class T>
+static bool launch_scales(const seer_grad *tensors, int32_t count, int type, const double *part, uint32_t parts, float max_norm, float *norm,
+                          hipStream_t st)
+{
+    GradList<kScaleList> l;
+    OutList<kScaleList> o;
+    bool any = false;
+    for (int32_t from = count - 1; next_list<T>(tensors, count, type, &from, -1, &l, &o); any = true)
+        hipLaunchKernelGGL((grad_scale_kernel<T>), dim3(grid_of(l)), dim3(kWG), 0, st, l, o, part, parts, max_norm, norm);
+    return any;
+}
+
+static uint32_t launch_all_squares(const seer_grad *tensors, int32_t count, double *part, hipStream_t st)
+{
+    uint32_t parts = 0;
+    launch_squares<float>(tensors, count, SEER_F32, part, &parts, st);
+    launch_squares<f16_t>(tensors, count, SEER_F16, part, &parts, st);
+    launch_squares<bf16_t>(tensors, count, SEER_BF16, part, &parts, st);
+    return parts;
 }
 
 void launch_grad_norm(const seer_grad *tensors, int32_t count, float *norm, void *workspace, hipStream_t st)
 {
     double *part = static_cast<double *>(workspace);
-    uint32_t parts = 0;
-    bool first = true;
-    // the partials of the launch with the most workgroups; the first launch writes all of them
-    each_type([&](auto *of, int type) {
-        using T = std::remove_pointer_t<decltype(of)>;
-        GradList l;
-        for (int32_t from = 0; next_list<T>(tensors, count, type, &from, &l, nullptr);) {
-            l.add = !first;
-            parts = kGradParts;
-            hipLaunchKernelGGL((grad_square_kernel<T>), dim3(kGradParts), dim3(kWG), 0, st, l, part);
-            first = false;
-        }
-    });
-    hipLaunchKernelGGL(grad_fold_kernel, dim3(1), dim3(kWG), 0, st, part, parts, norm);
+    const uint32_t parts = launch_all_squares(tensors, count, part, st);
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kWG), 0, st, part, parts, norm);
 }
 
-void launch_grad_clip(const seer_grad *tensors, int32_t count, float max_norm, const float *norm, hipStream_t st)
+void launch_grad_clip(const seer_grad *tensors, int32_t count, float max_norm, float *norm, void *workspace, hipStream_t st)
 {
-    each_type([&](auto *of, int type) {
-        using T = std::remove_pointer_t<decltype(of)>;
-        ClipList l;
-        for (int32_t from = 0; next_list<T>(tensors, count, type, &from, &l.g, l.out);)
-            hipLaunchKernelGGL((grad_scale_kernel<T>), dim3(std::min(l.g.end[l.g.count - 1], 4096u)), dim3(kWG), 0, st, l, norm, max_norm);
-    });
+    double *part = static_cast<double *>(workspace);
+    const uint32_t parts = launch_all_squares(tensors, count, part, st);
+    const bool b = launch_scales<bf16_t>(tensors, count, SEER_BF16, part, parts, max_norm, norm, st);
+    const bool h = launch_scales<f16_t>(tensors, count, SEER_F16, part, parts, max_norm, norm, st);
+    const bool f = launch_scales<float>(tensors, count, SEER_F32, part, parts, max_norm, norm, st);
+    if (!b && !h && !f) hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(kWG), 0, st, part, parts, norm);
 }
 
 } // namespace seer

@@ -98,19 +98,20 @@ __device__ void scan_lds(uint32_t *v, uint32_t n, uint32_t *s_wave)
 struct SortArgs {
     const void *expert;
     uint32_t count, experts, per_wave, groups;
+    uint32_t runs;          // waves that count (the others only add up)
     int key_bits;
     int32_t *expert_ptr, *slot_choice, *choice_slot;
     uint32_t *counts;       // [groups][buckets], in the workspace; null with one workgroup
 };
 
 // pass 0: everything in one workgroup; 1: counts of each workgroup's share; 2: the slots.
-// LDS: cnt [waves][buckets], base [buckets + 1].
+// LDS: cnt [waves][buckets], base [buckets + 1], in pass 2 before [buckets], too.
 template <class I, int PASS>
 __global__ __launch_bounds__(kSortWaves * 64) void route_kernel(SortArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
     __shared__ uint32_t s_wave[kSortWaves];
-    const uint32_t waves = blockDim.x / 64, wave = threadIdx.x / 64, buckets = a.experts + 1;
+    const uint32_t waves = a.runs, wave = threadIdx.x / 64, buckets = a.experts + 1;
     uint32_t *cnt = lds, *base = lds + waves * buckets;
     const I *expert = static_cast<const I *>(a.expert);
     const uint32_t begin = blockIdx.x * waves * a.per_wave, end = min(a.count, begin + waves * a.per_wave);
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void route_kernel(SortArgs a)
         for (uint32_t i = threadIdx.x; i < waves * buckets; i += blockDim.x) cnt[i] = 0;
         __syncthreads();
         const uint32_t from = min(end, begin + wave * a.per_wave);
-        count_run(expert, from, min(end, from + a.per_wave), a.experts, a.key_bits, cnt + wave * buckets, a.choice_slot);
+        if (wave < waves) count_run(expert, from, min(end, from + a.per_wave), a.experts, a.key_bits, cnt + wave * buckets, a.choice_slot);
         __syncthreads();
         // each wave's counters become the entries of the key in earlier waves, base the workgroup's
         for (uint32_t k = threadIdx.x; k < buckets; k += blockDim.x) {
@@ -135,17 +136,19 @@ __global__ __launch_bounds__(kSortWaves * 64) void route_kernel(SortArgs a)
         __syncthreads();
         scan_lds(base, buckets, s_wave);
     } else {
-        // the counters of the waves again, without ranks, and the counts of all workgroups
-        for (uint32_t i = threadIdx.x; i < waves * buckets; i += blockDim.x) cnt[i] = 0;
-        for (uint32_t k = threadIdx.x; k < buckets; k += blockDim.x) {
-            uint32_t sum = 0;
-            for (uint32_t g = 0; g < a.groups; ++g) sum += a.counts[(size_t)g * buckets + k];
-            base[k] = sum;
-        }
+        // the counters of the waves again, without ranks, beside the counts of all workgroups and of those before this one
+        uint32_t *before = base + buckets + 1;
+        for (uint32_t i = threadIdx.x; i < (waves + 2) * buckets + 1; i += blockDim.x) lds[i] = 0;
         __syncthreads();
         const uint32_t from = min(end, begin + wave * a.per_wave), to = min(end, from + a.per_wave);
-        for (uint32_t c = from + (threadIdx.x & 63); c < to; c += 64)
+        for (uint32_t c = from + (threadIdx.x & 63); wave < waves && c < to; c += 64)
             atomicAdd(&cnt[wave * buckets + key_of(expert, c, a.experts)], 1u);
+        for (uint32_t i = threadIdx.x, all = a.groups * buckets; i < all; i += blockDim.x) {
+            const uint32_t n = a.counts[i], g = i / buckets, k = i - g * buckets;
+            atomicAdd(&base[k], n);
+            if (g < blockIdx.x) atomicAdd(&before[k], n);
+        }
+        __syncthreads();
         scan_lds(base, buckets, s_wave);
         if (blockIdx.x == 0)
             for (uint32_t k = threadIdx.x; k <= a.experts; k += blockDim.x) a.expert_ptr[k] = (int32_t)base[k];
@@ -157,28 +160,26 @@ __global__ __launch_bounds__(kSortWaves * 64) void route_kernel(SortArgs a)
                 cnt[w * buckets + k] = sum;
                 sum += n;
             }
-            for (uint32_t g = 0; g < blockIdx.x; ++g) base[k] += a.counts[(size_t)g * buckets + k];
+            base[k] += before[k];
         }
         __syncthreads();
     }
     if constexpr (PASS == 0)
         for (uint32_t k = threadIdx.x; k <= a.experts; k += blockDim.x) a.expert_ptr[k] = (int32_t)base[k];
-    place_choices(expert, begin, end, a.per_wave, a.experts, cnt, base, a.slot_choice, a.choice_slot);
+    if (wave < waves) place_choices(expert, begin, end, a.per_wave, a.experts, cnt, base, a.slot_choice, a.choice_slot);
 }
 
-// Waves whose counters fit the LDS beside the bases.
-static uint32_t sort_waves(uint32_t experts)
-{
-    return experts <= 1024 ? kSortWaves : experts <= 2048 ? kSortWaves / 2 : kSortWaves / 4;
-}
+// Waves whose counters fit the LDS beside the workgroup's (16: up to 147 KB; 6: up to 131 KB).
+static uint32_t sort_waves(uint32_t experts) { return experts <= 2048 ? kSortWaves : 6; }
 
-// Choices that one workgroup sorts on its own, and those of each workgroup where there are more.
-constexpr uint32_t kSortAlone = 4096, kSortShare = 4096;
-
+// What one workgroup sorts on its own, and what each takes where there are more: the second launch of those reads the
+// counts of all workgroups in each, so that shares grow with the number of experts.  Measured, us, one workgroup and
+// two launches: 160 experts, 2048 choices 6.5 and 7.9, 4096 9.7 and 8.1; 4096 experts, 4096 choices 35 and 45.  98 304
+// choices in shares of 1024, 2048 and 4096: 160 experts 12.9, 12.2, 14.5, 1024 experts 39, 27, 24.5.
 static uint32_t sort_groups(uint32_t count, uint32_t experts, uint32_t *per_wave)
 {
-    const uint32_t waves = sort_waves(experts);
-    uint32_t groups = count <= kSortAlone ? 1 : std::min((count + kSortShare - 1) / kSortShare, kSortMaxGroups);
+    const uint32_t waves = sort_waves(experts), most = std::max(1024u, 4 * experts);
+    const uint32_t groups = count <= std::max(2048u, 2 * experts) ? 1 : std::min((count + most - 1) / most, kSortMaxGroups);
     const uint32_t share = (count + groups - 1) / groups;
     *per_wave = std::max(64u, ((share + waves - 1) / waves + 63) & ~63u);
     return (count + waves * *per_wave - 1) / (waves * *per_wave);
@@ -194,7 +195,7 @@ size_t route_workspace_bytes(uint32_t count, uint32_t experts)
 template <class I>
 static void launch_route_of(SortArgs a, uint32_t waves, hipStream_t st)
 {
-    const size_t lds = ((size_t)waves * (a.experts + 1) + a.experts + 2) * 4;
+    const size_t lds = ((size_t)(a.runs + 2) * (a.experts + 1) + 1) * 4;
     if (a.groups <= 1) {
         hipLaunchKernelGGL((route_kernel<I, 0>), dim3(1), dim3(waves * 64), lds, st, a);
         return;
@@ -211,6 +212,7 @@ void launch_route(const void *expert, bool wide, uint32_t count, uint32_t expert
     a.count = count;
     a.experts = experts;
     a.groups = sort_groups(count, experts, &a.per_wave);
+    a.runs = std::min(sort_waves(experts), std::max(1u, (count + a.per_wave - 1) / a.per_wave));
     for (a.key_bits = 1; (experts >> a.key_bits) != 0; ++a.key_bits) {}
     a.expert_ptr = expert_ptr;
     a.slot_choice = slot_choice;
@@ -264,7 +266,7 @@ __global__ __launch_bounds__(kWG) void combine_kernel(RouteRows r, const float *
             const uint32_t c = t * r.choices + k;
             const int32_t slot = r.choice_slot[c];
             if (slot < 0) continue;
-            const Unit<T> u = load_some(z + (int64_t)slot * ldz + col, n);
+            const Unit<T> u = stream_some(z + (int64_t)slot * ldz + col, n);
             const float s = WEIGHTED ? weight[c] : 1.0f;
 #pragma unroll
             for (int j = 0; j < E; ++j) acc[j] += s * (float)u.v[j];
@@ -272,7 +274,7 @@ __global__ __launch_bounds__(kWG) void combine_kernel(RouteRows r, const float *
         Unit<T> v;
 #pragma unroll
         for (int j = 0; j < E; ++j) v.v[j] = (T)acc[j];
-        store_some(y + (int64_t)t * ldy + col, v, n);
+        stream_some(y + (int64_t)t * ldy + col, v, n);
     }
 }
 
@@ -295,7 +297,7 @@ __global__ __launch_bounds__(kWG) void route_grad_kernel(RouteRows r, const floa
                 const int n = (int)min((uint32_t)E, r.cols - col);
                 const Unit<T> g = load_some(dy + (int64_t)t * lddy + col, n);
                 if (dweight && slot >= 0) {
-                    const Unit<T> u = load_some(z + p * ldz + col, n);
+                    const Unit<T> u = stream_some(z + p * ldz + col, n);
 #pragma unroll
                     for (int j = 0; j < E; ++j) dot += (float)g.v[j] * (float)u.v[j];
                 }
@@ -305,7 +307,7 @@ __global__ __launch_bounds__(kWG) void route_grad_kernel(RouteRows r, const floa
 #pragma unroll
                         for (int j = 0; j < E; ++j) v.v[j] = (T)(s * (float)g.v[j]);
                     }
-                    store_some(dz + p * lddz + col, v, n);
+                    stream_some(dz + p * lddz + col, v, n);
                 }
             }
             if (dweight) {
