@@ -316,7 +316,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
                 step(s + 3, s_3, s_2);
             }
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // nothing is on its way to LDS when the workgroup ends
     }
     // every scale is fetched before the first store: a wait for a load is one for all stores before it, too
     const bool zero = t.group >= a.groups;
@@ -329,17 +328,39 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
     for (int i = 0; i < CI; ++i)
 #pragma unroll
         for (int v = 0; v < 4; ++v) of_channel[i][v] = sb[min(n1 + i * 16 + v, a.channels - 1)];
+    // A lane's results are four channels each of TJ * CI tokens.  They change places in LDS, in a region of the wave's own, so
+    // that stores are of 16 bytes and lines are written whole (8-byte stores, 16 rows at a time: 4096 x 4096 x 256
+    // EPILOGUE_FIGURES).  A row's pieces lie in the order of their number xor the row.
+    constexpr int CIP = CI * (int)sizeof(T) > 16 ? 16 / (int)sizeof(T) : CI;      // channels go by up to 256 bytes of a row
+    constexpr uint32_t PIECES = CIP * sizeof(T), ROW = PIECES * 16, E = Unit<T>::kElems;
+    static_assert(8 * TJ * 16 * ROW <= 4 * Shape::kBytes && 2 * TJ * 16 * ROW <= Shape::kBytes && CI % CIP == 0, "two waves to a buffer");
+    step_barrier<0>();                              // nothing is on its way to LDS, and nobody reads the last columns any more
+    int8_t *mine = (wave < 2 ? s_0 : wave < 4 ? s_1 : wave < 6 ? s_2 : s_3) + (wave & 1) * (TJ * 16 * ROW);
 #pragma unroll
-    for (int j = 0; j < TJ; ++j) {
-        if (row1 + j * 16 >= t.end) continue;
-        T *row = out + (int64_t)(row1 + j * 16) * a.ldo;
+    for (int first = 0; first < CI; first += CIP) {
 #pragma unroll
-        for (int i = 0; i < CI; ++i) {
-            float v[4];
+        for (int j = 0; j < TJ; ++j)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = zero ? 0.0f : (float)acc[i][j][u] * (of_row[j] * of_channel[i][u]);
-            if (n1 + i * 16 < a.channels) store_4(row, n1 + i * 16, a.channels, v);
+            for (int i = 0; i < CIP; ++i) {
+                typedef T four __attribute__((ext_vector_type(4)));
+                four v;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = zero ? (T)0.0f : (T)((float)acc[first + i][j][u] * (of_row[j] * of_channel[first + i][u]));
+                const uint32_t row = j * 16 + (lane & 15), at = (i * 16 + (lane >> 4) * 4) * (uint32_t)sizeof(T);
+                *reinterpret_cast<four *>(mine + row * ROW + ((at / 16) ^ (row % PIECES)) * 16 + at % 16) = v;
+            }
+        __builtin_amdgcn_wave_barrier();            // (a wave's LDS accesses are served in order)
+#pragma unroll
+        for (uint32_t part = 0; part < TJ * 16 * PIECES / 64; ++part) {
+            const uint32_t row = part * (64 / PIECES) + lane / PIECES, piece16 = lane % PIECES;
+            const uint32_t to = t.begin + wt * TJ * 16 + row, n = n0 + (wc * CI + first) * 16 + piece16 * E;
+            if (to < t.end && n < a.channels) {
+                Unit<T> u;
+                u.v = *reinterpret_cast<const typename Unit<T>::whole *>(mine + row * ROW + (piece16 ^ (row % PIECES)) * 16);
+                store_some(out + (int64_t)to * a.ldo + n, u, (int)min(E, a.channels - n));
+            }
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -374,7 +395,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void i8_few_kernel(I8Args a, uint32
         for (; k + kFewUnroll * 64 <= k_end; k += kFewUnroll * 64) {
             v4i32 fb[kFewUnroll], fa[kFewUnroll];
 #pragma unroll
-            for (uint32_t u = 0; u < kFewUnroll; ++u) fb[u] = __builtin_nontemporal_load(reinterpret_cast<const v4i32 *>(pb + k + u * 64));
+            for (uint32_t u = 0; u < kFewUnroll; ++u) fb[u] = *reinterpret_cast<const v4i32 *>(pb + k + u * 64);
 #pragma unroll
             for (uint32_t u = 0; u < kFewUnroll; ++u) fa[u] = *reinterpret_cast<const v4i32 *>(pa0 + k + u * 64);
 #pragma unroll

@@ -540,7 +540,7 @@ void launch_quantize(const RouteRows &rows, const seer_dense &x, const seer_dens
     by_type(x.type, [&](auto *of) {
         using T = std::remove_pointer_t<decltype(of)>;
         if (rows.cols <= 1024) launch_quantize_of<T, 1, 1>(rows, x, q, scale, st);
-        else if (rows.cols <= 4096) launch_quantize_of<T, 4, 1>(rows, x, q, scale, st);
+        else if (rows.cols <= 5120) launch_quantize_of<T, 4, 1>(rows, x, q, scale, st);
         else launch_quantize_of<T, 4, 2>(rows, x, q, scale, st);
     });
 }
