@@ -213,6 +213,8 @@ __device__ __forceinline__ void step_barrier()
 {
     if constexpr (LOADS == 8) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     else if constexpr (LOADS == 6) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if constexpr (LOADS == 12) asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    else if constexpr (LOADS == 9) asm volatile("s_waitcnt vmcnt(9) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
@@ -265,57 +267,72 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
         const uint32_t from = (lane & 15) * kTileCols + (((lane >> 4) ^ order(lane & 15)) * 16);
         const uint32_t from_a = wt * TJ * 16 * kTileCols + from, from_b = (TOKENS + wc * CI * 16) * kTileCols + from;
         const bool busy = wt * TJ * 16 < rows;          // (waves without tokens only fetch)
-        const auto multiply = [&](const int8_t *lds) {
-            if (!busy) return;
-            v4i32 fb[CI], fa[TJ];
+        struct Frags { v4i32 b[CI], a[TJ]; };
+        const auto read = [&](const int8_t *lds, Frags &f) {
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) fa[j] = *reinterpret_cast<const v4i32 *>(lds + from_a + j * 16 * kTileCols);
+            for (int j = 0; j < TJ; ++j) f.a[j] = *reinterpret_cast<const v4i32 *>(lds + from_a + j * 16 * kTileCols);
 #pragma unroll
-            for (int i = 0; i < CI; ++i) fb[i] = *reinterpret_cast<const v4i32 *>(lds + from_b + i * 16 * kTileCols);
+            for (int i = 0; i < CI; ++i) f.b[i] = *reinterpret_cast<const v4i32 *>(lds + from_b + i * 16 * kTileCols);
+        };
+        const auto multiply = [&](const Frags &f) {
 #pragma unroll
             for (int i = 0; i < CI; ++i)
 #pragma unroll
-                for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[i], fa[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[i], f.a[j], acc[i][j], 0, 0, 0);
         };
-        const auto step = [&](uint32_t s, int8_t *lds, int8_t *next) {
-            step_barrier<2 * (LA + LB)>();          // this step's columns are there, and the buffer before it is no longer read
-            fetch(s + 3, next);
-            multiply(lds);
+        // Step s multiplies what step s - 1 has read, reads the columns of step s + 1 and sends for those of step s + 4, into the buffer
+        // whose columns are in registers.
+        Frags even, odd;
+        const auto step = [&](uint32_t s, int8_t *own, const int8_t *next, Frags &now, Frags &then) {
+            step_barrier<2 * (LA + LB)>();          // the next columns are there, and nobody reads the own ones any more
+            fetch(s + 4, own);
+            if (!busy) return;
+            read(next, then);
+            multiply(now);
+#pragma unroll
+            for (int i = 0; i < CI + TJ; ++i) {     // a read behind every few multiplications: the first ones wait for nothing
+                __builtin_amdgcn_sched_group_barrier(0x008, CI * TJ / (CI + TJ), 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+        };
+        // zeros for the tokens' pieces behind the last column
+        const uint32_t whole = a.columns / kTileCols;
+        const auto clear_end = [&](int8_t *lds) {
+            step_barrier<0>();
+            for (uint32_t i = threadIdx.x; i < TOKENS * 4; i += kTileThreads)
+                if (whole * kTileCols + ((i & 3) ^ order((i / 4) & 15)) * 16 >= a.columns) *reinterpret_cast<v4i32 *>(lds + i * 16) = v4i32{0, 0, 0, 0};
+            step_barrier<0>();
         };
         fetch(0, s_0);
         fetch(1, s_1);
         fetch(2, s_2);
-        // zeros for the tokens' pieces behind the last column
-        const auto clear_end = [&](int8_t *lds) {
-            const uint32_t k0 = (steps - 1) * kTileCols;
-            step_barrier<0>();
-            for (uint32_t i = threadIdx.x; i < TOKENS * 4; i += kTileThreads)
-                if (k0 + ((i & 3) ^ order((i / 4) & 15)) * 16 >= a.columns) *reinterpret_cast<v4i32 *>(lds + i * 16) = v4i32{0, 0, 0, 0};
-        };
-        const uint32_t whole = a.columns / kTileCols;
+        fetch(3, s_3);
+        step_barrier<3 * (LA + LB)>();
+        if (whole == 0) clear_end(s_0);
+        read(s_0, even);
         uint32_t s = 0;
-        for (; s + 4 <= whole; s += 4) {
-            step(s, s_0, s_3);
-            step(s + 1, s_1, s_0);
-            step(s + 2, s_2, s_1);
-            step(s + 3, s_3, s_2);
+        for (; s + 4 < whole; s += 4) {
+            step(s, s_0, s_1, even, odd);
+            step(s + 1, s_1, s_2, odd, even);
+            step(s + 2, s_2, s_3, even, odd);
+            step(s + 3, s_3, s_0, odd, even);
         }
-        if (s < steps) {                            // up to four steps are left, the last of them perhaps not whole
-            if (s == whole) clear_end(s_0);
-            step(s, s_0, s_3);
+        // up to five steps are left, the last of them perhaps not whole
+        const auto last = [&](uint32_t s, int8_t *own, int8_t *next, Frags &now, Frags &then) {
+            if (s >= steps) return;
+            step_barrier<2 * (LA + LB)>();
+            fetch(s + 4, own);
             if (s + 1 < steps) {
-                if (s + 1 == whole) clear_end(s_1);
-                step(s + 1, s_1, s_0);
+                if (s + 1 == whole) clear_end(next);
+                read(next, then);
             }
-            if (s + 2 < steps) {
-                if (s + 2 == whole) clear_end(s_2);
-                step(s + 2, s_2, s_1);
-            }
-            if (s + 3 < steps) {
-                if (s + 3 == whole) clear_end(s_3);
-                step(s + 3, s_3, s_2);
-            }
-        }
+            if (busy) multiply(now);
+        };
+        last(s, s_0, s_1, even, odd);
+        last(s + 1, s_1, s_2, odd, even);
+        last(s + 2, s_2, s_3, even, odd);
+        last(s + 3, s_3, s_0, odd, even);
+        last(s + 4, s_0, s_1, even, odd);
     }
     // every scale is fetched before the first store: a wait for a load is one for all stores before it, too
     const bool zero = t.group >= a.groups;
@@ -329,8 +346,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
 #pragma unroll
         for (int v = 0; v < 4; ++v) of_channel[i][v] = sb[min(n1 + i * 16 + v, a.channels - 1)];
     // A lane's results are four channels each of TJ * CI tokens.  They change places in LDS, in a region of the wave's own, so
-    // that stores are of 16 bytes and lines are written whole (8-byte stores, 16 rows at a time: 4096 x 4096 x 256
-    // EPILOGUE_FIGURES).  A row's pieces lie in the order of their number xor the row.
+    // that stores are of 16 bytes and lines are written whole (4096 x 4096 x 256, where the stores are most of the
+    // time: 15.4 us, and 18.3 with 8-byte stores, 16 rows at a time).  A row's pieces lie in the order of their number xor the row.
     constexpr int CIP = CI * (int)sizeof(T) > 16 ? 16 / (int)sizeof(T) : CI;      // channels go by up to 256 bytes of a row
     constexpr uint32_t PIECES = CIP * sizeof(T), ROW = PIECES * 16, E = Unit<T>::kElems;
     static_assert(8 * TJ * 16 * ROW <= 4 * Shape::kBytes && 2 * TJ * 16 * ROW <= Shape::kBytes && CI % CIP == 0, "two waves to a buffer");
