@@ -383,74 +383,108 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
 
 // ------------------------------------------------------------------ few rows to a group
 //
-// 16 channels of one group per workgroup, whose waves each take a share of the columns; weights come straight from memory, once per 32
-// rows, and the waves' sums meet in LDS.  Bound by the bytes of b.
-constexpr uint32_t kFewWaves = 4, kFewUnroll = 8;
+// CI * 16 channels of one group per workgroup, whose waves each take a share of the columns; both operands come straight from memory, the
+// weights once per 64 rows, and the waves' sums meet in LDS.  Bound by the bytes of b.
+constexpr uint32_t kFewRows = 64;
 
-template <class T>
-__global__ __launch_bounds__(kFewWaves * 64) void i8_few_kernel(I8Args a, uint32_t share)
+// 16 TJ rows from `at` on: the calling wave's columns [k_begin, k_end), U pieces of each row at a time.
+template <int CI, int TJ, int U>
+__device__ __forceinline__ void few_sums(const int8_t *const (&pb)[CI], const int8_t *const (&pa)[TJ], uint32_t k_begin, uint32_t k_end, uint32_t q,
+                                         v4i32 (&acc)[CI][TJ])
 {
-    __shared__ __attribute__((aligned(16))) v4i32 s_acc[2][kFewWaves][64];
+#pragma unroll
+    for (int i = 0; i < CI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) acc[i][j] = v4i32{0, 0, 0, 0};
+    uint32_t k = k_begin;
+    for (; k + U * 64 <= k_end; k += U * 64) {
+        v4i32 fb[U][CI], fa[U][TJ];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < CI; ++i) fb[u][i] = *reinterpret_cast<const v4i32 *>(pb[i] + k + u * 64);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) fa[u][j] = *reinterpret_cast<const v4i32 *>(pa[j] + k + u * 64);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < CI; ++i)
+#pragma unroll
+                for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u][i], fa[u][j], acc[i][j], 0, 0, 0);
+    }
+    for (; k < k_end; k += 64) {
+        const bool in = k + q < k_end;
+        v4i32 fb[CI], fa[TJ];
+#pragma unroll
+        for (int i = 0; i < CI; ++i) fb[i] = in ? *reinterpret_cast<const v4i32 *>(pb[i] + k) : v4i32{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) fa[j] = in ? *reinterpret_cast<const v4i32 *>(pa[j] + k) : v4i32{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < CI; ++i)
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[i], fa[j], acc[i][j], 0, 0, 0);
+    }
+}
+
+template <class T, int CI, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8Args a, uint32_t share)
+{
+    __shared__ __attribute__((aligned(16))) v4i32 s_acc[2][WAVES][CI][64];
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), lane = threadIdx.x & 63;
-    const uint32_t n0 = blockIdx.x * 16, g = blockIdx.y;
+    const uint32_t n0 = blockIdx.x * (CI * 16), g = blockIdx.y;
     const uint32_t begin = group_begin(a, g), end = group_begin(a, g + 1);
     T *out = static_cast<T *>(a.out);
     if (g == a.groups) {                            // the rows behind the groups
-        for (uint32_t row = begin + threadIdx.x / 16; row < end; row += kFewWaves * 4)
-            if (n0 + (threadIdx.x & 15) < a.channels) out[(int64_t)row * a.ldo + n0 + (threadIdx.x & 15)] = (T)0.0f;
+        constexpr uint32_t kChannels = CI * 16;
+        const uint32_t n = n0 + threadIdx.x % kChannels;
+        for (uint32_t row = begin + threadIdx.x / kChannels; row < end; row += WAVES * 64 / kChannels)
+            if (n < a.channels) out[(int64_t)row * a.ldo + n] = (T)0.0f;
         return;
     }
     const uint32_t k_begin = min(a.columns, wave * share), k_end = min(a.columns, k_begin + share);
     const uint32_t q = (lane >> 4) * 16;
-    const int8_t *pb = a.b + ((int64_t)g * a.channels + min(n0 + (lane & 15), a.channels - 1)) * a.ldb + q;
-    for (uint32_t at = begin; at < end; at += 32) {
-        const bool two = end - at > 16;
-        const int8_t *pa0 = a.a + (int64_t)min(at + (lane & 15), end - 1) * a.lda + q;
-        const int8_t *pa1 = a.a + (int64_t)min(at + 16 + (lane & 15), end - 1) * a.lda + q;
-        v4i32 acc0 = {0, 0, 0, 0}, acc1 = {0, 0, 0, 0};
-        uint32_t k = k_begin;
-        for (; k + kFewUnroll * 64 <= k_end; k += kFewUnroll * 64) {
-            v4i32 fb[kFewUnroll], fa[kFewUnroll];
+    const int8_t *pb[CI];
 #pragma unroll
-            for (uint32_t u = 0; u < kFewUnroll; ++u) fb[u] = *reinterpret_cast<const v4i32 *>(pb + k + u * 64);
+    for (int i = 0; i < CI; ++i) pb[i] = a.b + ((int64_t)g * a.channels + min(n0 + i * 16 + (lane & 15), a.channels - 1)) * a.ldb + q;
+    const float *sb = a.b_scale + (int64_t)g * a.channels;
+
+    const auto rows = [&](uint32_t at, auto count, auto pieces) {
+        constexpr int TJ = decltype(count)::value;
+        const int8_t *pa[TJ];
 #pragma unroll
-            for (uint32_t u = 0; u < kFewUnroll; ++u) fa[u] = *reinterpret_cast<const v4i32 *>(pa0 + k + u * 64);
+        for (int j = 0; j < TJ; ++j) pa[j] = a.a + (int64_t)min(at + j * 16 + (lane & 15), end - 1) * a.lda + q;
+        v4i32 acc[CI][TJ];
+        few_sums<CI, TJ, decltype(pieces)::value>(pb, pa, k_begin, k_end, q, acc);
+        // 16 rows at a time the waves' sums meet; wave i adds up and stores channels i * 16 ...
 #pragma unroll
-            for (uint32_t u = 0; u < kFewUnroll; ++u) acc0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u], fa[u], acc0, 0, 0, 0);
-            if (two) {
+        for (int j = 0; j < TJ; ++j) {
 #pragma unroll
-                for (uint32_t u = 0; u < kFewUnroll; ++u) fa[u] = *reinterpret_cast<const v4i32 *>(pa1 + k + u * 64);
+            for (int i = 0; i < CI; ++i) s_acc[j & 1][wave][i][lane] = acc[i][j];
+            __syncthreads();
+            if (wave < CI) {
+                v4i32 sum = s_acc[j & 1][0][wave][lane];
 #pragma unroll
-                for (uint32_t u = 0; u < kFewUnroll; ++u) acc1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[u], fa[u], acc1, 0, 0, 0);
-            }
-        }
-        for (; k < k_end; k += 64) {
-            v4i32 fb = {0, 0, 0, 0}, f0 = fb, f1 = fb;
-            if (k + q < k_end) {
-                fb = *reinterpret_cast<const v4i32 *>(pb + k);
-                f0 = *reinterpret_cast<const v4i32 *>(pa0 + k);
-                f1 = *reinterpret_cast<const v4i32 *>(pa1 + k);
-            }
-            acc0 = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb, f0, acc0, 0, 0, 0);
-            acc1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb, f1, acc1, 0, 0, 0);
-        }
-        s_acc[0][wave][lane] = acc0;
-        s_acc[1][wave][lane] = acc1;
-        __syncthreads();
-        if (wave < 2 && (wave == 0 || two)) {
-            v4i32 sum = s_acc[wave][0][lane];
-            for (uint32_t o = 1; o < kFewWaves; ++o) sum += s_acc[wave][o][lane];
-            const uint32_t row = at + wave * 16 + (lane & 15), n = n0 + (lane >> 4) * 4;
-            if (row < end && n < a.channels) {
-                const float *sb = a.b_scale + (int64_t)g * a.channels;
-                const float sa = a.a_scale[row];
-                float v[4];
+                for (int o = 1; o < WAVES; ++o) sum += s_acc[j & 1][o][wave][lane];
+                const uint32_t row = at + j * 16 + (lane & 15), n = n0 + wave * 16 + (lane >> 4) * 4;
+                if (row < end && n < a.channels) {
+                    const float sa = a.a_scale[row];
+                    float v[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = (float)sum[u] * (sa * sb[min(n + u, a.channels - 1)]);
-                store_4(out + (int64_t)row * a.ldo, n, a.channels, v);
+                    for (int u = 0; u < 4; ++u) v[u] = (float)sum[u] * (sa * sb[min(n + u, a.channels - 1)]);
+                    store_4(out + (int64_t)row * a.ldo, n, a.channels, v);
+                }
             }
         }
         __syncthreads();
+    };
+    using std::integral_constant;
+    for (uint32_t at = begin; at < end; at += kFewRows) {
+        const uint32_t left = end - at;
+        if (left <= 16) rows(at, integral_constant<int, 1>{}, integral_constant<int, 8>{});
+        else if (left <= 32) rows(at, integral_constant<int, 2>{}, integral_constant<int, 4>{});
+        else rows(at, integral_constant<int, 4>{}, integral_constant<int, 4>{});
     }
 }
 
@@ -484,19 +518,40 @@ static bool launch_tiles(const I8Args &a, hipStream_t st)
     return true;
 }
 
+template <class T, int CI, int WAVES>
+static bool launch_few(const I8Args &a, hipStream_t st)
+{
+    const uint32_t groups = a.groups + (a.group_ptr ? 1 : 0), share = ((a.columns + WAVES - 1) / WAVES + 63) & ~63u;
+    if (groups > 65535) return false;
+    hipLaunchKernelGGL((i8_few_kernel<T, CI, WAVES>), dim3((a.channels + CI * 16 - 1) / (CI * 16), groups), dim3(WAVES * 64), 0, st, a, share);
+    return true;
+}
+
+// Which kernel, by the mean rows of a group and by how many tiles there are.  Measured, us (groups x channels x columns, rows to
+// a group 1 / sqrt(rank)): few rows, tiles of 64, of 128 and of 256 tokens
+//   32 x 4096 x 4096, mean   8: 105 128 134 138     16: 128 132 138 143     32: 161 155 140 144     64: 233 144 172 151
+//                           96: 326 168 162 193    128: 415 188 164 195    192: 592 242 222 197    512: 1474 536 399 354
+//   64 x 1024 x 2048, mean   8: 26 24 26 28         16: 30 34 27 29         64: 61 35 41 48        256: 215 69 66 62
+//    1 x 8192 x 8192, rows   1: 13 38 39 51         64: 26 48 48 52         96: 42 46 51 54        128: 48 48 55 56
+//                          256: 94 46 55 83        512: 186 55 58 85
+//    1 x 2048 x 2048, rows   1: 4.7 10 12 18        64: 9.0 12.5 13 18     128: 16 12.6 18 19
+// so that few rows are for products that would leave CUs without a tile, or up to 12 rows, and larger tiles are for as many
+// of them as there are CUs or nearly.  Few rows: 16 channels to a workgroup where 32 are fewer than half of the
+// CUs (2048 x 2048, one row: 3.8 and 4.7); eight waves to share the columns where each has 512 or more and there is
+// more than one row (8192 x 8192, 64 rows: 25.6 and 27.8; one row: 14.0 and 13.1; 2048 columns, 64 groups of 8: 29 and 26).
 template <class T>
 static bool launch_pieces(const I8Args &a, hipStream_t st)
 {
     const uint32_t mean = a.rows / a.groups;
-    if (mean <= 32) {
-        if (a.groups >= 65535) return false;
-        const uint32_t share = ((a.columns + kFewWaves - 1) / kFewWaves + 63) & ~63u;
-        hipLaunchKernelGGL((i8_few_kernel<T>), dim3((a.channels + 15) / 16, a.groups + (a.group_ptr ? 1 : 0)), dim3(kFewWaves * 64), 0, st, a, share);
-        return true;
+    const uint64_t tiles_64 = most_blocks(a, 64, kTileChannels);
+    if (mean <= (tiles_64 >= 256 ? 12 : tiles_64 >= 128 ? 32 : 96)) {
+        if ((uint64_t)((a.channels + 31) / 32) * a.groups < 128) return launch_few<T, 1, 4>(a, st);
+        return mean > 1 && a.columns >= 4096 ? launch_few<T, 2, 8>(a, st) : launch_few<T, 2, 4>(a, st);
     }
     if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return false;     // offsets into a tile are 32-bit
-    if (mean > 160) return launch_tiles<T, 2, 8, 4>(a, st);
-    if (mean > 80) return launch_tiles<T, 2, 8, 2>(a, st);
+    constexpr uint64_t kEnough = 192;
+    if (mean > 160 && most_blocks(a, 256, kTileChannels) >= kEnough) return launch_tiles<T, 2, 8, 4>(a, st);
+    if ((mean > 80 || (mean <= 32 && tiles_64 >= 256)) && most_blocks(a, 128, kTileChannels) >= kEnough) return launch_tiles<T, 2, 8, 2>(a, st);
     return launch_tiles<T, 4, 4, 2>(a, st);
 }
 

@@ -231,3 +231,19 @@ def test_quantize_at_and_beside_the_middle(kind):
     want_q, want_s = O.quantize(host(x))
     assert np.array_equal(host(s).astype(np.float32), want_s)
     assert np.array_equal(host(q), want_q)
+
+
+MANY = [  # rows, groups, channels, columns: what the choice of a kernel goes by
+    (1, 1, 4200, 4096), (3, 1, 40, 4160), (20, 1, 4112, 4160), (70, 1, 1000, 1024), (150, 1, 700, 1040), (90, 2, 300, 4224), (130, 40, 200, 192), (600, 40, 2100, 64),
+    (1300, 40, 2050, 80), (3000, 40, 2050, 64), (4100, 40, 2050, 128), (7700, 40, 2050, 64), (400, 1, 8500, 64), (2600, 1, 5200, 64), (900, 20, 300, 4096),
+]
+
+
+@pytest.mark.parametrize("shape", MANY, ids=str)
+def test_every_kernel(shape):
+    announce(f"i8 {shape}")
+    rows, groups, N, K = shape
+    rng = np.random.default_rng(rows)
+    cuts = np.sort(rng.integers(0, rows + 1, groups - 1)) if groups > 1 else None
+    ptr = None if groups == 1 else [0, *cuts.tolist(), rows]
+    check_product(i8(rng, rows, K), i8(rng, groups, N, K), ptr, "bf16", rng)
