@@ -22,21 +22,15 @@ __device__ __forceinline__ uint32_t group_begin(const I8Args &a, uint32_t g)
     return p < 0 ? 0 : min((uint32_t)p, a.rows);
 }
 
-// What lane l knows of group at + l: its rows, the tiles that they take, and those of the groups from `at` up to and with it.
-struct GroupTiles { uint32_t from, to, tiles, sum; };
+// What a lane knows of group g: its rows, and the tiles that they take.
+struct GroupTiles { uint32_t from, to, tiles; };
 
-__device__ __forceinline__ GroupTiles group_tiles(const I8Args &a, uint32_t at, uint32_t tokens)
+__device__ __forceinline__ GroupTiles group_tiles(const I8Args &a, uint32_t g, uint32_t tokens)
 {
-    const uint32_t lane = threadIdx.x & 63, g = min(at + lane, a.groups + 1);
     GroupTiles t;
-    t.from = group_begin(a, g);
-    t.to = group_begin(a, g + 1);
+    t.from = group_begin(a, min(g, a.groups + 1));
+    t.to = group_begin(a, min(g + 1, a.groups + 1));
     t.tiles = t.to > t.from ? (t.to - t.from + tokens - 1) / tokens : 0;
-    t.sum = t.tiles;
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t other = __shfl_up(t.sum, d, 64);
-        if ((int)lane >= d) t.sum += other;
-    }
     return t;
 }
 
@@ -56,9 +50,12 @@ __device__ __forceinline__ Tile tile_in_group(uint32_t group, uint32_t from, uin
     return t;
 }
 
-// The tile of workgroup `block` among the tiles there are: as many for each XCD.  False: there is none.  All lanes of a wave
-// take part; the result is uniform.
-__device__ __forceinline__ bool find_tile(const I8Args &a, uint32_t block, uint32_t tokens, uint32_t across, Tile *t)
+// The tile of workgroup `block` among the tiles there are: as many for each XCD.  False: there is none.  All WAVES waves of the
+// workgroup take part, a group to a lane; the result is uniform.  s: LDS of the workgroup, free again after the next barrier.
+struct TileSearch { uint32_t sum[16], found[4]; };
+
+template <uint32_t WAVES>
+__device__ __forceinline__ bool find_tile(const I8Args &a, uint32_t block, uint32_t tokens, uint32_t across, TileSearch *s, Tile *t)
 {
     if (!a.group_ptr) {
         const uint32_t all = (a.rows + tokens - 1) / tokens * across, w = tile_of_block(block, all, 1);
@@ -66,28 +63,53 @@ __device__ __forceinline__ bool find_tile(const I8Args &a, uint32_t block, uint3
         *t = tile_in_group(0, 0, a.rows, w, tokens, across);
         return true;
     }
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    // tiles of the groups from `at` up to the lane's and with it; `all`: of all WAVES * 64 groups
+    const auto prefix = [&](uint32_t tiles, uint32_t *all) {
+        uint32_t sum = tiles;
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t other = __shfl_up(sum, d, 64);
+            if ((int)lane >= d) sum += other;
+        }
+        __syncthreads();
+        if (lane == 63) s->sum[wave] = sum;
+        __syncthreads();
+        *all = 0;
+#pragma unroll
+        for (uint32_t w = 0; w < WAVES; ++w) {
+            if (w < wave) sum += s->sum[w];
+            *all += s->sum[w];
+        }
+        return sum;
+    };
+    constexpr uint32_t kAtOnce = WAVES * 64;
+    uint32_t all = 0, before = 0, sum = 0, here = 0;
     GroupTiles g;
-    uint32_t all = 0;
-    for (uint32_t at = 0; at <= a.groups; at += 64) {
-        g = group_tiles(a, at, tokens);
-        all += (uint32_t)__builtin_amdgcn_readlane((int)g.sum, 63);
+    for (uint32_t at = 0; at <= a.groups; at += kAtOnce) {
+        g = group_tiles(a, at + threadIdx.x, tokens);
+        sum = prefix(g.tiles, &here);
+        all += here;
     }
     const uint32_t w = tile_of_block(block, all * across, 1);
     if (w >= all * across) return false;
-    uint32_t before = 0;
-    for (uint32_t at = 0; at <= a.groups; at += 64) {
-        if (a.groups >= 64) g = group_tiles(a, at, tokens);        // (else it is there)
-        const uint64_t past = __ballot((before + g.sum) * across > w);
-        if (past) {
-            const int l = __ffsll((unsigned long long)past) - 1;
-            const uint32_t first = before + (uint32_t)__builtin_amdgcn_readlane((int)(g.sum - g.tiles), l);
-            *t = tile_in_group(at + (uint32_t)l, (uint32_t)__builtin_amdgcn_readlane((int)g.from, l),
-                               (uint32_t)__builtin_amdgcn_readlane((int)g.to, l), w - first * across, tokens, across);
-            return true;
+    for (uint32_t at = 0; at <= a.groups; at += kAtOnce) {
+        if (a.groups >= kAtOnce) {                  // (else they are known)
+            g = group_tiles(a, at + threadIdx.x, tokens);
+            sum = prefix(g.tiles, &here);
         }
-        before += (uint32_t)__builtin_amdgcn_readlane((int)g.sum, 63);
+        const uint32_t last = (before + sum) * across, first = last - g.tiles * across;
+        if (first <= w && w < last) {               // one lane of the workgroup
+            s->found[0] = at + threadIdx.x;
+            s->found[1] = g.from;
+            s->found[2] = g.to;
+            s->found[3] = w - first;
+        }
+        before += here;
     }
-    return false;
+    __syncthreads();
+    const auto uniform = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+    *t = tile_in_group(uniform(s->found[0]), uniform(s->found[1]), uniform(s->found[2]), uniform(s->found[3]), tokens, across);
+    return true;
 }
 
 // Rows of tiles of `tokens` rows that any division of the rows into groups needs.
@@ -125,10 +147,11 @@ __device__ __forceinline__ v4i32 load_16(const int8_t *p, int n)
 __global__ __launch_bounds__(256) void i8_any_kernel(I8Args a, uint32_t blocks)
 {
     __shared__ __attribute__((aligned(16))) int8_t s_a[kAnyTokens * kAnyPitch], s_b[kAnyChannels * kAnyPitch];
+    __shared__ TileSearch s_search;
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
     for (uint32_t w = blockIdx.x; w < blocks; w += gridDim.x) {
     Tile t;
-    if (!find_tile(a, w, kAnyTokens, (a.channels + kAnyChannels - 1) / kAnyChannels, &t)) continue;
+    if (!find_tile<4>(a, w, kAnyTokens, (a.channels + kAnyChannels - 1) / kAnyChannels, &s_search, &t)) continue;
     const uint32_t n0 = t.column * kAnyChannels;
     v4i32 acc[2][2] = {};
     if (t.group < a.groups) {
@@ -227,7 +250,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), lane = threadIdx.x & 63;
     const uint32_t across = (a.channels + kTileChannels - 1) / kTileChannels;
     Tile t;
-    if (!find_tile(a, blockIdx.x, TOKENS, across, &t)) return;
+    if (!find_tile<8>(a, blockIdx.x, TOKENS, across, reinterpret_cast<TileSearch *>(s_0), &t)) return;
+    __syncthreads();                                // (s_0 is filled from now on)
     const uint32_t n0 = t.column * kTileChannels;
     const uint32_t wc = wave % WC, wt = wave / WC;
     T *out = static_cast<T *>(a.out);
@@ -507,7 +531,7 @@ static uint64_t most_blocks(const I8Args &a, uint32_t tokens, uint32_t channels)
 }
 
 // The arithmetic on tiles is 32-bit.
-bool i8_product_fits(const I8Args &a) { return most_blocks(a, kAnyTokens, kAnyChannels) < (1u << 30); }
+bool i8_product_fits(const I8Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, kAnyTokens, kAnyChannels) < (1u << 30); }
 
 template <class T, int WC, int CI, int TJ>
 static bool launch_tiles(const I8Args &a, hipStream_t st)
@@ -518,11 +542,11 @@ static bool launch_tiles(const I8Args &a, hipStream_t st)
     return true;
 }
 
+static_assert(SEER_MAX_EXPERTS < 65535, "groups are a dimension of the grid of the kernel for few rows");
 template <class T, int CI, int WAVES>
 static bool launch_few(const I8Args &a, hipStream_t st)
 {
     const uint32_t groups = a.groups + (a.group_ptr ? 1 : 0), share = ((a.columns + WAVES - 1) / WAVES + 63) & ~63u;
-    if (groups > 65535) return false;
     hipLaunchKernelGGL((i8_few_kernel<T, CI, WAVES>), dim3((a.channels + CI * 16 - 1) / (CI * 16), groups), dim3(WAVES * 64), 0, st, a, share);
     return true;
 }

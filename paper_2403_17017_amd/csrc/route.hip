@@ -328,9 +328,8 @@ __device__ __forceinline__ float quantised(float x, float scale)
     return scale > 0 ? fminf(fmaxf(v, -127.0f), 127.0f) : 0.0f;
 }
 
-// One wave or workgroup per row of x (WAVES); routed: its copies go to the slots of its choices.  A lane takes 16 elements at a
-// time, whose 16 bytes of q go out in one store; the first HELD of them stay in registers between the two passes
-// over the row (the others are read again).
+// Quantisation, of a row of x at a time; routed: its copies go to the slots of its choices.  A lane takes 16 elements at a
+// time, whose 16 bytes of q go out in one store.
 typedef uint32_t q_vec __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint32_t q_whole __attribute__((ext_vector_type(4)));
 
@@ -352,12 +351,21 @@ template <class T>
 struct Sixteen {
     static constexpr int kElems = Unit<T>::kElems, kUnits = 16 / kElems;
     Unit<T> u[kUnits];
-    __device__ __forceinline__ void load(const T *p, int n)         // n: elements that there are, more than 16 or none at all, too
+    __device__ __forceinline__ void load16(const T *p)
     {
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int have = n - i * kElems;
-            u[i] = have > 0 ? load_some(p + i * kElems, have) : zero_unit<T>();
+        for (int i = 0; i < kUnits; ++i) u[i] = load_unit(p + i * kElems);
+    }
+    __device__ __forceinline__ void load(const T *p, int n)         // n: elements that there are, more than 16 or none at all, too
+    {
+        if (n >= 16) {
+            load16(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) {
+                const int have = n - i * kElems;
+                u[i] = have > 0 ? load_some(p + i * kElems, have) : zero_unit<T>();
+            }
         }
     }
     __device__ __forceinline__ float at(int j) const { return (float)u[j / kElems].v[j % kElems]; }
@@ -397,7 +405,10 @@ struct Sixteen {
         }
         if (!(worst < kNearHalf) || s.by == 0) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) b[j] = (uint32_t)(int)quantised(at(j), s.scale);
+            for (int j = 0; j < 16; ++j) {
+                b[j] = (uint32_t)(int)quantised(at(j), s.scale);
+                asm volatile("" : "+v"(b[j]));       // (not to be done by everybody and thrown away, nor all 16 at a time)
+            }
         }
         q_whole q;
 #pragma unroll
@@ -409,46 +420,87 @@ struct Sixteen {
     }
 };
 
-template <class T, bool ROUTED, int WAVES, int HELD>
-__global__ __launch_bounds__(kWG) void quantize_kernel(RouteRows r, const T *__restrict__ x, int64_t ldx, int8_t *__restrict__ q,
-                                                       int64_t ldq, uint32_t padded, float *__restrict__ scale)
+// The largest of `top` over the WAVES waves of a row; s_max: two sets, taken in turn, so that one barrier a row is enough.
+template <int WAVES>
+__device__ __forceinline__ uint32_t row_largest(uint32_t top, uint32_t (*s_max)[WAVES], uint32_t *turn)
 {
-    __shared__ uint32_t s_max[2][kWG / kWave];
-    constexpr uint32_t LANES = WAVES * kWave, ROWS = kWG / LANES;
-    const uint32_t lane = threadIdx.x % LANES;
+    top = lanes_fold(top, [](uint32_t a, uint32_t b) { return max(a, b); });
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) s_max[*turn][threadIdx.x / 64] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = max(top, s_max[*turn][w]);
+        *turn ^= 1;
+    }
+    return top;
+}
+
+// Rows of whole sixteens, HELD of them to a lane of the WAVES waves of a row at most: each row stays in registers.  Bound by how many rows are
+// under way, hence few registers: 3001 rows of 4112 in 10 us (3.6 TB/s), in a kernel that also knew the ends of other rows
+// (106 registers) 24 us; 8192 rows of 4096 to four experts each 35 us (5.8 TB/s) and 49.
+template <class T, bool ROUTED, int WAVES, int HELD>
+__global__ __launch_bounds__(WAVES < 4 ? kWG : WAVES * kWave) void quantize_whole_kernel(RouteRows r, const T *__restrict__ x, int64_t ldx, int8_t *__restrict__ q,
+                                                                                        int64_t ldq, float *__restrict__ scale)
+{
+    __shared__ uint32_t s_max[2][WAVES];
+    constexpr uint32_t LANES = WAVES * kWave, ROWS = LANES < kWG ? kWG / LANES : 1;
+    const uint32_t lane = threadIdx.x % LANES, sub = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / LANES));
     uint32_t turn = 0;
-    for (uint32_t t = blockIdx.x * ROWS + threadIdx.x / LANES; t < r.tokens; t += gridDim.x * ROWS) {
+    for (uint32_t t = blockIdx.x * ROWS + sub; t < r.tokens; t += gridDim.x * ROWS) {
         const T *row = x + (int64_t)t * ldx;
         Sixteen<T> held[HELD];
         uint32_t top = 0;
 #pragma unroll
         for (int h = 0; h < HELD; ++h) {
             const uint32_t col = (h * LANES + lane) * 16;
-            held[h].load(row + col, col < r.cols ? (int)(r.cols - col) : 0);
+            if (col < r.cols) held[h].load16(row + col);
         }
 #pragma unroll
         for (int h = 0; h < HELD; ++h)
-            if (h == 0 || (h * LANES + lane) * 16 < r.cols) top = max(top, held[h].largest());
-        for (uint32_t col = (HELD * LANES + lane) * 16; col < r.cols; col += LANES * 16) {
+            if ((h * LANES + lane) * 16 < r.cols) top = max(top, held[h].largest());
+        const RowScale s = row_scale(row_largest<WAVES>(top, s_max, &turn));
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            const uint32_t col = (h * LANES + lane) * 16;
+            if (col >= r.cols) continue;
+            const q_whole b = held[h].quantise(s);
+            for (uint32_t k = 0; k < r.choices; ++k) {
+                const int32_t slot = ROUTED ? r.choice_slot[t * r.choices + k] : (int32_t)t;
+                *reinterpret_cast<q_vec *>(q + (int64_t)(slot < 0 ? -1 - slot : slot) * ldq + col) = slot < 0 ? (q_whole)0u : b;
+            }
+        }
+        for (uint32_t k = lane; k < r.choices; k += LANES) {
+            const int32_t slot = ROUTED ? r.choice_slot[t * r.choices + k] : (int32_t)t;
+            scale[slot < 0 ? -1 - slot : slot] = slot < 0 ? 0.0f : s.scale;
+        }
+    }
+}
+
+// Any other row, one workgroup to each, read twice.
+template <class T, bool ROUTED>
+__global__ __launch_bounds__(kWG) void quantize_kernel(RouteRows r, const T *__restrict__ x, int64_t ldx, int8_t *__restrict__ q,
+                                                       int64_t ldq, uint32_t padded, float *__restrict__ scale)
+{
+    constexpr int WAVES = kWG / kWave;
+    __shared__ uint32_t s_max[2][WAVES];
+    uint32_t turn = 0;
+    for (uint32_t t = blockIdx.x; t < r.tokens; t += gridDim.x) {
+        const T *row = x + (int64_t)t * ldx;
+        uint32_t top = 0;
+        for (uint32_t col = threadIdx.x * 16; col < r.cols; col += kWG * 16) {
             Sixteen<T> v;
             v.load(row + col, (int)(r.cols - col));
             top = max(top, v.largest());
         }
-        top = lanes_fold(top, [](uint32_t a, uint32_t b) { return max(a, b); });
-        if constexpr (WAVES > 1) {                     // (two sets: one barrier a row is enough)
-            if ((threadIdx.x & 63) == 0) s_max[turn][threadIdx.x / 64] = top;
-            __syncthreads();
-            top = max(max(s_max[turn][0], s_max[turn][1]), max(s_max[turn][2], s_max[turn][3]));
-            turn ^= 1;
-        }
-        const RowScale s = row_scale(top);
-        const auto store = [&](uint32_t col, const Sixteen<T> &v) {
+        const RowScale s = row_scale(row_largest<WAVES>(top, s_max, &turn));
+        for (uint32_t col = threadIdx.x * 16; col < padded; col += kWG * 16) {
+            Sixteen<T> v;
+            v.load(row + col, (int)(r.cols - col));
             const q_whole b = v.quantise(s);            // (the zeros behind the row's end give 0)
             for (uint32_t k = 0; k < r.choices; ++k) {
                 const int32_t slot = ROUTED ? r.choice_slot[t * r.choices + k] : (int32_t)t;
                 int8_t *to = q + (int64_t)(slot < 0 ? -1 - slot : slot) * ldq + col;
-                q_whole out = b;
-                if (slot < 0) out = (q_whole)0u;
+                const q_whole out = slot < 0 ? (q_whole)0u : b;
                 if (col + 16 <= padded) {
                     *reinterpret_cast<q_vec *>(to) = out;
                 } else {
@@ -457,16 +509,8 @@ __global__ __launch_bounds__(kWG) void quantize_kernel(RouteRows r, const T *__r
                         if (col + j < padded) to[j] = (int8_t)(out[j / 4] >> (j % 4 * 8));
                 }
             }
-        };
-#pragma unroll
-        for (int h = 0; h < HELD; ++h)
-            if ((h * LANES + lane) * 16 < padded) store((h * LANES + lane) * 16, held[h]);
-        for (uint32_t col = (HELD * LANES + lane) * 16; col < padded; col += LANES * 16) {
-            Sixteen<T> v;
-            v.load(row + col, (int)(r.cols - col));
-            store(col, v);
         }
-        for (uint32_t k = lane; k < r.choices; k += LANES) {
+        for (uint32_t k = threadIdx.x; k < r.choices; k += kWG) {
             const int32_t slot = ROUTED ? r.choice_slot[t * r.choices + k] : (int32_t)t;
             scale[slot < 0 ? -1 - slot : slot] = slot < 0 ? 0.0f : s.scale;
         }
@@ -525,23 +569,33 @@ void launch_route_grad(const RouteRows &rows, const float *weight, const seer_de
 }
 
 template <class T, int WAVES, int HELD>
-static void launch_quantize_of(const RouteRows &rows, const seer_dense &x, const seer_dense &q, float *scale, hipStream_t st)
+static void launch_quantize_whole(const RouteRows &rows, const seer_dense &x, const seer_dense &q, float *scale, hipStream_t st)
 {
-    const uint32_t padded = (uint32_t)std::min<int64_t>(q.ld, (x.cols + 15) & ~(int64_t)15), per = kWG / kWave / WAVES;
-    const dim3 grid(std::min((rows.tokens + per - 1) / per, kMaxGrid)), wg(kWG);
+    const uint32_t per = WAVES < 4 ? 4 / WAVES : 1;
+    const dim3 grid(std::min((rows.tokens + per - 1) / per, kMaxGrid)), wg(WAVES < 4 ? kWG : WAVES * kWave);
     const T *xp = static_cast<const T *>(x.data);
     int8_t *qp = static_cast<int8_t *>(q.data);
-    if (rows.choice_slot) hipLaunchKernelGGL((quantize_kernel<T, true, WAVES, HELD>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
-    else hipLaunchKernelGGL((quantize_kernel<T, false, WAVES, HELD>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
+    if (rows.choice_slot) hipLaunchKernelGGL((quantize_whole_kernel<T, true, WAVES, HELD>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, scale);
+    else hipLaunchKernelGGL((quantize_whole_kernel<T, false, WAVES, HELD>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, scale);
 }
 
 void launch_quantize(const RouteRows &rows, const seer_dense &x, const seer_dense &q, float *scale, hipStream_t st)
 {
     by_type(x.type, [&](auto *of) {
         using T = std::remove_pointer_t<decltype(of)>;
-        if (rows.cols <= 1024) launch_quantize_of<T, 1, 1>(rows, x, q, scale, st);
-        else if (rows.cols <= 5120) launch_quantize_of<T, 4, 1>(rows, x, q, scale, st);
-        else launch_quantize_of<T, 4, 2>(rows, x, q, scale, st);
+        if (rows.cols % 16 == 0 && rows.cols <= 16384) {
+            if (rows.cols <= 1024) launch_quantize_whole<T, 1, 1>(rows, x, q, scale, st);
+            else if (rows.cols <= 4096) launch_quantize_whole<T, 4, 1>(rows, x, q, scale, st);
+            else if (rows.cols <= 8192) launch_quantize_whole<T, 4, 2>(rows, x, q, scale, st);
+            else launch_quantize_whole<T, 8, 2>(rows, x, q, scale, st);
+            return;
+        }
+        const uint32_t padded = (uint32_t)std::min<int64_t>(q.ld, (x.cols + 15) & ~(int64_t)15);
+        const dim3 grid(std::min(rows.tokens, kMaxGrid)), wg(kWG);
+        const T *xp = static_cast<const T *>(x.data);
+        int8_t *qp = static_cast<int8_t *>(q.data);
+        if (rows.choice_slot) hipLaunchKernelGGL((quantize_kernel<T, true>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
+        else hipLaunchKernelGGL((quantize_kernel<T, false>), grid, wg, 0, st, rows, xp, x.ld, qp, q.ld, padded, scale);
     });
 }
 

@@ -13,6 +13,7 @@ from . import binding as B
 from .binding import SeerError, _stream_handle
 
 MAX_EXPERTS = 4096
+EINVAL, EWORKSPACE, ELIMIT = -1, -4, -6
 I8_MAX_K = 131071
 
 
@@ -128,15 +129,17 @@ def seer_route(expert, experts: int, routing: Routing = None, workspace=None, st
     if expert.dim() != 2 or not expert.is_cuda or expert.dtype not in (_torch.int32, _torch.int64):
         raise ValueError("expert is to be a contiguous int32 or int64 matrix [tokens, choices] on the GPU")
     tokens, choices = expert.shape
+    if not 0 < experts <= MAX_EXPERTS:
+        raise SeerError(ELIMIT if experts > 0 else EINVAL, "seer_route")
     if routing is None:
-        routing = Routing._new(tokens, choices, max(int(experts), 0), expert, stream)
+        routing = Routing._new(tokens, choices, int(experts), expert, stream)
     elif (routing.tokens, routing.choices, routing.experts) != (tokens, choices, experts):
         raise ValueError("routing has other sizes")
-    if workspace is None:
-        need = B._lib.seer_route_workspace_bytes(tokens, choices, routing.experts)
-        if need:
-            workspace = _new((need,), _torch.uint8, expert, stream)
-    rc = m.route(expert, routing, workspace, _stream_handle(stream))
+    h = _stream_handle(stream)
+    rc = m.route(expert, routing, workspace, h)
+    if rc == EWORKSPACE and workspace is None:           # (small ones need none, and asking costs as much as the call)
+        workspace = _new((route_workspace_bytes(tokens, choices, experts),), _torch.uint8, expert, stream)
+        rc = m.route(expert, routing, workspace, h)
     if rc:
         raise SeerError(rc, "seer_route")
     return routing
@@ -234,11 +237,11 @@ def seer_i8_product(a, a_scale, b, b_scale, out=None, group_ptr=None, dtype=None
         out = _new((rows, channels), dtype or _torch.bfloat16, a, stream)
     elif dtype is not None and out.dtype != dtype:
         raise TypeError(f"out is {out.dtype}, not {dtype}")
-    if workspace is None:
-        need = B._lib.seer_i8_product_workspace_bytes(rows, channels, columns, groups)
-        if need:
-            workspace = _new((need,), _torch.uint8, a, stream)
-    rc = m.product(a, a_scale, b, b_scale, group_ptr, out, workspace, _stream_handle(stream))
+    h = _stream_handle(stream)
+    rc = m.product(a, a_scale, b, b_scale, group_ptr, out, workspace, h)
+    if rc == EWORKSPACE and workspace is None:
+        workspace = _new((i8_product_workspace_bytes(rows, channels, columns, groups),), _torch.uint8, a, stream)
+        rc = m.product(a, a_scale, b, b_scale, group_ptr, out, workspace, h)
     if rc:
         raise SeerError(rc, "seer_i8_product")
     return out

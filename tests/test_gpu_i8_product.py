@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
-@pytest.mark.parametrize("shape", [(1, 1), (1, 8192), (3, 15), (5, 16), (4, 17), (33, 1000), (2, 9001), (0, 8), (64, 4096), (3, 0)], ids=str)
+@pytest.mark.parametrize("shape", [(1, 1), (1, 8192), (3, 15), (5, 16), (4, 17), (33, 1000), (2, 9001), (0, 8), (64, 4096), (3, 0), (9, 1024), (7, 1040), (5, 4112), (3, 8208), (2, 16384), (2, 16400)], ids=str)
 def test_quantize(shape, kind):
     announce(f"quantize {shape} {kind}")
     rng = np.random.default_rng(shape[1])
@@ -247,3 +247,14 @@ def test_every_kernel(shape):
     cuts = np.sort(rng.integers(0, rows + 1, groups - 1)) if groups > 1 else None
     ptr = None if groups == 1 else [0, *cuts.tolist(), rows]
     check_product(i8(rng, rows, K), i8(rng, groups, N, K), ptr, "bf16", rng)
+
+
+@pytest.mark.parametrize("groups", [63, 64, 255, 256, 511, 512, 513, 1100, 4096])
+@pytest.mark.parametrize("columns", [64, 70])
+def test_many_groups(groups, columns):
+    """As many groups as lanes look for a tile, and one more or less; sizes that give tiles and few rows."""
+    announce(f"i8 {groups} groups of {columns}")
+    rng = np.random.default_rng(groups)
+    for rows, N in ((groups // 3, 16), (40 * groups, 24)):
+        lengths = rng.multinomial(rows, rng.dirichlet(np.full(groups, 0.3)))
+        check_product(i8(rng, rows, columns), i8(rng, groups, N, columns), np.concatenate([[0], np.cumsum(lengths)]).tolist(), "f16", rng)
