@@ -216,41 +216,51 @@ __device__ __forceinline__ void store_4(T *row, uint32_t n, uint32_t channels, c
 // four LDS buffers, three steps before they are multiplied: a step's multiplications (512 matrix instructions of a workgroup,
 // 2 x 16 cycles x 32 on each SIMD) take less time than memory does to answer.  A row's four pieces of 16 bytes lie
 // in the order of their number xor (row / 2 + row / 8) % 4, so that lanes that read together use all banks.
-constexpr uint32_t kTileChannels = 256, kTileCols = 64, kTileThreads = 512;
+constexpr uint32_t kTileChannels = 256, kTileCols = 64;
 
 typedef __attribute__((address_space(3))) int8_t lds_byte;
 
-// WC x 8 / WC waves, each of CI * 16 channels x TJ * 16 tokens.
-template <int WC, int CI, int TJ>
+// WC x WAVES / WC waves, each of CI * 16 channels x TJ * 16 tokens.
+template <int WAVES, int WC, int CI, int TJ>
 struct TileShape {
-    static constexpr int kWT = 8 / WC;
-    static constexpr uint32_t kTokens = kWT * TJ * 16;
-    static constexpr uint32_t kLoadsA = kTokens >= 128 ? kTokens / 128 : 1, kLoadsB = kTileChannels / 128;  // of a lane, each step
+    static constexpr int kWT = WAVES / WC;
+    static constexpr uint32_t kThreads = WAVES * 64, kTokens = kWT * TJ * 16;
+    // loads of a lane, each step: a wave's load brings 16 rows
+    static constexpr uint32_t kLoadsA = kTokens >= WAVES * 16 ? kTokens / (WAVES * 16) : 1, kLoadsB = kTileChannels / (WAVES * 16);
     static constexpr uint32_t kBytes = (kTokens + kTileChannels) * kTileCols;
     static_assert(WC * CI * 16 == (int)kTileChannels, "waves cover the channels");
 };
+
+// The columns of one product shared out: workgroups of share `s` multiply columns s * share ... and leave sums of 32-bit integers,
+// [shares][rows][pitch], which i8_join_kernel adds up and scales.
+struct SharedColumns { int32_t *sums; uint32_t blocks, share, pitch; };
 
 // Waits until all but the last `LOADS` of the wave's loads have arrived and its LDS reads are through, then for the other waves.
 template <uint32_t LOADS>
 __device__ __forceinline__ void step_barrier()
 {
-    if constexpr (LOADS == 8) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    else if constexpr (LOADS == 6) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    else if constexpr (LOADS == 12) asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    else if constexpr (LOADS == 9) asm volatile("s_waitcnt vmcnt(9) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
 }
 
-template <class T, int WC, int CI, int TJ>
-__global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
+template <class T, int WAVES, int WC, int CI, int TJ>
+__global__ __launch_bounds__(WAVES * 64, 2) void i8_tile_kernel(I8Args a, SharedColumns shared)
 {
-    using Shape = TileShape<WC, CI, TJ>;
+    // (T = int32_t: sums of one share of the columns, as they are)
+    constexpr bool kShared = std::is_same<T, int32_t>::value;
+    using Shape = TileShape<WAVES, WC, CI, TJ>;
     constexpr uint32_t TOKENS = Shape::kTokens, LA = Shape::kLoadsA, LB = Shape::kLoadsB;
     __shared__ __attribute__((aligned(1024))) int8_t s_0[Shape::kBytes], s_1[Shape::kBytes], s_2[Shape::kBytes], s_3[Shape::kBytes];
+    int8_t *const buffer[4] = {s_0, s_1, s_2, s_3};
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), lane = threadIdx.x & 63;
     const uint32_t across = (a.channels + kTileChannels - 1) / kTileChannels;
     Tile t;
-    if (!find_tile<8>(a, blockIdx.x, TOKENS, across, reinterpret_cast<TileSearch *>(s_0), &t)) return;
+    const uint32_t part = kShared ? blockIdx.x / shared.blocks : 0;
+    if constexpr (kShared) {
+        a.a += part * shared.share;
+        a.b += part * shared.share;
+        a.columns = min(shared.share, a.columns - part * shared.share);
+    }
+    if (!find_tile<WAVES>(a, kShared ? blockIdx.x % shared.blocks : blockIdx.x, TOKENS, across, reinterpret_cast<TileSearch *>(s_0), &t)) return;
     __syncthreads();                                // (s_0 is filled from now on)
     const uint32_t n0 = t.column * kTileChannels;
     const uint32_t wc = wave % WC, wt = wave / WC;
@@ -273,9 +283,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
         const uint32_t piece = ((lane & 3) ^ order(lane / 4)) * 16;
         uint32_t at_a[LA], at_b[LB];
 #pragma unroll
-        for (uint32_t i = 0; i < LA; ++i) at_a[i] = min(((i * 8 + wave) * 16) % TOKENS + lane / 4, rows - 1) * lda + piece;
+        for (uint32_t i = 0; i < LA; ++i) at_a[i] = min(((i * WAVES + wave) * 16) % TOKENS + lane / 4, rows - 1) * lda + piece;
 #pragma unroll
-        for (uint32_t i = 0; i < LB; ++i) at_b[i] = min((i * 8 + wave) * 16 + lane / 4, chans - 1) * ldb + piece;
+        for (uint32_t i = 0; i < LB; ++i) at_b[i] = min((i * WAVES + wave) * 16 + lane / 4, chans - 1) * ldb + piece;
         const uint32_t steps = (a.columns + kTileCols - 1) / kTileCols;
         const auto fetch = [&](uint32_t step, int8_t *lds) {
             // steps behind the last one load the last one again, into a buffer that is not read; pieces behind the last column
@@ -283,10 +293,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
             const uint32_t k0 = min(step, steps - 1) * kTileCols, back = k0 + piece < a.columns ? 0 : piece;
 #pragma unroll
             for (uint32_t i = 0; i < LA; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte *)(lds + ((i * 8 + wave) * 1024) % (TOKENS * kTileCols)), 16, (int)(at_a[i] - back), (int)k0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte *)(lds + ((i * WAVES + wave) * 1024) % (TOKENS * kTileCols)), 16, (int)(at_a[i] - back), (int)k0, 0, 0);
 #pragma unroll
             for (uint32_t i = 0; i < LB; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte *)(lds + TOKENS * kTileCols + (i * 8 + wave) * 1024), 16, (int)(at_b[i] - back), (int)k0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte *)(lds + TOKENS * kTileCols + (i * WAVES + wave) * 1024), 16, (int)(at_b[i] - back), (int)k0, 0, 0);
         };
         const uint32_t from = (lane & 15) * kTileCols + (((lane >> 4) ^ order(lane & 15)) * 16);
         const uint32_t from_a = wt * TJ * 16 * kTileCols + from, from_b = (TOKENS + wc * CI * 16) * kTileCols + from;
@@ -304,10 +314,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
 #pragma unroll
                 for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[i], f.a[j], acc[i][j], 0, 0, 0);
         };
-        // Step s multiplies what step s - 1 has read, reads the columns of step s + 1 and sends for those of step s + 4, into the buffer
-        // whose columns are in registers.
-        Frags even, odd;
-        const auto step = [&](uint32_t s, int8_t *own, const int8_t *next, Frags &now, Frags &then) {
+        // Step s multiplies what step s - 1 has read, reads the columns of step s + 1 and sends for those of step s + 4, into the
+        // buffer whose columns are in registers.
+        Frags frags[2];
+        const auto step = [&](uint32_t s, int8_t *own, const int8_t *next, const Frags &now, Frags &then) {
             step_barrier<2 * (LA + LB)>();          // the next columns are there, and nobody reads the own ones any more
             fetch(s + 4, own);
             if (!busy) return;
@@ -323,41 +333,44 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
         const uint32_t whole = a.columns / kTileCols;
         const auto clear_end = [&](int8_t *lds) {
             step_barrier<0>();
-            for (uint32_t i = threadIdx.x; i < TOKENS * 4; i += kTileThreads)
+            for (uint32_t i = threadIdx.x; i < TOKENS * 4; i += Shape::kThreads)
                 if (whole * kTileCols + ((i & 3) ^ order((i / 4) & 15)) * 16 >= a.columns) *reinterpret_cast<v4i32 *>(lds + i * 16) = v4i32{0, 0, 0, 0};
             step_barrier<0>();
         };
-        fetch(0, s_0);
-        fetch(1, s_1);
-        fetch(2, s_2);
-        fetch(3, s_3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) fetch(i, buffer[i]);
         step_barrier<3 * (LA + LB)>();
         if (whole == 0) clear_end(s_0);
-        read(s_0, even);
+        read(s_0, frags[0]);
         uint32_t s = 0;
-        for (; s + 4 < whole; s += 4) {
-            step(s, s_0, s_1, even, odd);
-            step(s + 1, s_1, s_2, odd, even);
-            step(s + 2, s_2, s_3, even, odd);
-            step(s + 3, s_3, s_0, odd, even);
-        }
+        for (; s + 4 < whole; s += 4)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) step(s + i, buffer[i], buffer[(i + 1) % 4], frags[i % 2], frags[(i + 1) % 2]);
         // up to five steps are left, the last of them perhaps not whole
-        const auto last = [&](uint32_t s, int8_t *own, int8_t *next, Frags &now, Frags &then) {
-            if (s >= steps) return;
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            if (s + i >= steps) break;
             step_barrier<2 * (LA + LB)>();
-            fetch(s + 4, own);
-            if (s + 1 < steps) {
-                if (s + 1 == whole) clear_end(next);
-                read(next, then);
+            fetch(s + i + 4, buffer[i % 4]);
+            if (s + i + 1 < steps) {
+                if (s + i + 1 == whole) clear_end(buffer[(i + 1) % 4]);
+                read(buffer[(i + 1) % 4], frags[(i + 1) % 2]);
             }
-            if (busy) multiply(now);
-        };
-        last(s, s_0, s_1, even, odd);
-        last(s + 1, s_1, s_2, odd, even);
-        last(s + 2, s_2, s_3, even, odd);
-        last(s + 3, s_3, s_0, odd, even);
-        last(s + 4, s_0, s_1, even, odd);
+            if (busy) multiply(frags[i % 2]);
+        }
     }
+    if constexpr (kShared) {
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+#pragma unroll
+            for (int i = 0; i < CI; ++i) {
+                const uint32_t row = t.begin + (wt * TJ + j) * 16 + (lane & 15), n = n0 + (wc * CI + i) * 16 + (lane >> 4) * 4;
+                if (row < t.end && n < shared.pitch)
+                    *reinterpret_cast<v4i32 *>(shared.sums + ((size_t)part * a.rows + row) * shared.pitch + n) = acc[i][j];
+            }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // nothing is on its way to LDS when the workgroup ends
+        return;
+    } else {
     // every scale is fetched before the first store: a wait for a load is one for all stores before it, too
     const bool zero = t.group >= a.groups;
     const float *sb = a.b_scale + (int64_t)(zero ? 0 : t.group) * a.channels;
@@ -374,9 +387,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
     // time: 15.4 us, and 18.3 with 8-byte stores, 16 rows at a time).  A row's pieces lie in the order of their number xor the row.
     constexpr int CIP = CI * (int)sizeof(T) > 16 ? 16 / (int)sizeof(T) : CI;      // channels go by up to 256 bytes of a row
     constexpr uint32_t PIECES = CIP * sizeof(T), ROW = PIECES * 16, E = Unit<T>::kElems;
-    static_assert(8 * TJ * 16 * ROW <= 4 * Shape::kBytes && 2 * TJ * 16 * ROW <= Shape::kBytes && CI % CIP == 0, "two waves to a buffer");
+    constexpr uint32_t kPer = WAVES / 4;            // waves to a buffer
+    static_assert(WAVES % 4 == 0 && kPer * TJ * 16 * ROW <= Shape::kBytes && CI % CIP == 0, "the waves' regions fit");
     step_barrier<0>();                              // nothing is on its way to LDS, and nobody reads the last columns any more
-    int8_t *mine = (wave < 2 ? s_0 : wave < 4 ? s_1 : wave < 6 ? s_2 : s_3) + (wave & 1) * (TJ * 16 * ROW);
+    const uint32_t turn = wave / kPer;
+    int8_t *mine = (turn == 0 ? s_0 : turn == 1 ? s_1 : turn == 2 ? s_2 : s_3) + (wave % kPer) * (TJ * 16 * ROW);
 #pragma unroll
     for (int first = 0; first < CI; first += CIP) {
 #pragma unroll
@@ -402,6 +417,25 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(I8Args a)
             }
         }
         __builtin_amdgcn_wave_barrier();
+    }
+    }
+}
+
+// The sums of all shares, scaled: four channels to a lane.
+template <class T>
+__global__ __launch_bounds__(kWG) void i8_join_kernel(I8Args a, SharedColumns shared, uint32_t shares)
+{
+    const uint32_t quads = shared.pitch / 4;
+    for (uint64_t w = (uint64_t)blockIdx.x * kWG + threadIdx.x; w < (uint64_t)a.rows * quads; w += (uint64_t)gridDim.x * kWG) {
+        const uint32_t row = (uint32_t)(w / quads), n = (uint32_t)(w % quads) * 4;
+        v4i32 sum = {0, 0, 0, 0};
+        for (uint32_t s = 0; s < shares; ++s)
+            sum += *reinterpret_cast<const v4i32 *>(shared.sums + ((size_t)s * a.rows + row) * shared.pitch + n);
+        const float sa = a.a_scale[row];
+        float v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = (float)sum[u] * (sa * a.b_scale[min(n + u, a.channels - 1)]);
+        store_4(static_cast<T *>(a.out) + (int64_t)row * a.ldo, n, a.channels, v);
     }
 }
 
@@ -514,8 +548,6 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8Args a, uint32_t s
 
 // ------------------------------------------------------------------ launches
 
-size_t i8_workspace_bytes(uint32_t, uint32_t, uint32_t, uint32_t) { return 0; }
-
 // Whole pieces of 16 bytes at multiples of 16: what the kernels for tiles and for few rows load.
 static bool in_pieces(const I8Args &a)
 {
@@ -533,12 +565,13 @@ static uint64_t most_blocks(const I8Args &a, uint32_t tokens, uint32_t channels)
 // The arithmetic on tiles is 32-bit.
 bool i8_product_fits(const I8Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, kAnyTokens, kAnyChannels) < (1u << 30); }
 
-template <class T, int WC, int CI, int TJ>
+template <class T, int WAVES, int WC, int CI, int TJ>
 static bool launch_tiles(const I8Args &a, hipStream_t st)
 {
-    const uint64_t blocks = most_blocks(a, TileShape<WC, CI, TJ>::kTokens, kTileChannels);
-    if (blocks * kTileThreads >= 1ull << 32) return false;          // (a launch has fewer lanes)
-    hipLaunchKernelGGL((i8_tile_kernel<T, WC, CI, TJ>), dim3((uint32_t)blocks), dim3(kTileThreads), 0, st, a);
+    using Shape = TileShape<WAVES, WC, CI, TJ>;
+    const uint64_t blocks = most_blocks(a, Shape::kTokens, kTileChannels);
+    if (blocks * Shape::kThreads >= 1ull << 32) return false;       // (a launch has fewer lanes)
+    hipLaunchKernelGGL((i8_tile_kernel<T, WAVES, WC, CI, TJ>), dim3((uint32_t)blocks), dim3(Shape::kThreads), 0, st, a, SharedColumns{});
     return true;
 }
 
@@ -563,27 +596,92 @@ static bool launch_few(const I8Args &a, hipStream_t st)
 // of them as there are CUs or nearly.  Few rows: 16 channels to a workgroup where 32 are fewer than half of the
 // CUs (2048 x 2048, one row: 3.8 and 4.7); eight waves to share the columns where each has 512 or more and there is
 // more than one row (8192 x 8192, 64 rows: 25.6 and 27.8; one row: 14.0 and 13.1; 2048 columns, 64 groups of 8: 29 and 26).
+constexpr uint32_t kCUs = 256;
+
+static bool few_rows(const I8Args &a)
+{
+    const uint64_t tiles = most_blocks(a, 64, kTileChannels);
+    return a.rows / a.groups <= (tiles >= 256 ? 12u : tiles >= 128 ? 32u : 64u);
+}
+
+// One product whose tiles of 64 tokens leave CUs idle has its columns shared out, as many shares as its time is expected to be least
+// for: 0.33 us for every step of 64 columns, 1 us for every 3 MB of sums written and read, 8 us for the second launch.  Measured, us, one
+// and several shares (channels x columns, rows 128, 256, 512, 1024):
+//   512 x 8192:  34 34 34 36 and 15 18 20 25      2048 x 8192: 34 35 45 46 and 21 25 31 44
+//   8192 x 8192: 46 46 55 74 and 32 45 54 73      2048 x 2048: 12.5 12.7 13 14 and 13 16 25 27 (hence one)
+static uint32_t column_shares(const I8Args &a)
+{
+    if (a.group_ptr || few_rows(a) || a.columns == 0) return 1;
+    const uint64_t tiles = most_blocks(a, 64, kTileChannels);
+    if (tiles > kCUs * 2 / 3) return 1;
+    const double steps = (double)a.columns / kTileCols, sums = 8.0 * a.rows * a.channels;
+    const uint32_t most = (uint32_t)std::min<uint64_t>({kCUs * 3 / 2 / tiles, (uint64_t)steps / 6, 16});
+    uint32_t best = 1;
+    double least = 0.33 * steps;
+    for (uint32_t n = 2; n <= most; ++n) {
+        const double t = 0.33 * steps / n + n * sums / 3e6 + 8;
+        if (t < least) {
+            least = t;
+            best = n;
+        }
+    }
+    return best;
+}
+static SharedColumns shared_columns(const I8Args &a, uint32_t shares, void *workspace)
+{
+    const uint32_t steps = (a.columns + kTileCols - 1) / kTileCols;
+    return SharedColumns{static_cast<int32_t *>(workspace), (uint32_t)most_blocks(a, 64, kTileChannels), (steps + shares - 1) / shares * kTileCols,
+                         (a.channels + 3) & ~3u};
+}
+
+size_t i8_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t columns, uint32_t groups)
+{
+    I8Args a{};
+    a.rows = rows;
+    a.channels = channels;
+    a.columns = columns;
+    a.groups = groups;
+    if (rows == 0 || channels == 0 || groups != 1 || columns % 16 != 0) return 0;
+    const uint32_t shares = column_shares(a);
+    return shares > 1 ? (size_t)shares * rows * ((channels + 3) & ~3u) * 4 : 0;
+}
+
 template <class T>
-static bool launch_pieces(const I8Args &a, hipStream_t st)
+static bool launch_shared(const I8Args &a, void *workspace, hipStream_t st)
+{
+    uint32_t shares = column_shares(a);
+    if (shares <= 1) return false;
+    const SharedColumns c = shared_columns(a, shares, workspace);
+    shares = (a.columns + c.share - 1) / c.share;
+    hipLaunchKernelGGL((i8_tile_kernel<int32_t, 4, 4, 4, 4>), dim3(c.blocks * shares), dim3(256), 0, st, a, c);
+    const uint64_t lanes = (uint64_t)a.rows * (c.pitch / 4);
+    hipLaunchKernelGGL((i8_join_kernel<T>), dim3((uint32_t)std::min<uint64_t>((lanes + kWG - 1) / kWG, 8 * kCUs)), dim3(kWG), 0, st, a, c, shares);
+    return true;
+}
+
+template <class T>
+static bool launch_pieces(const I8Args &a, void *workspace, hipStream_t st)
 {
     const uint32_t mean = a.rows / a.groups;
     const uint64_t tiles_64 = most_blocks(a, 64, kTileChannels);
-    if (mean <= (tiles_64 >= 256 ? 12 : tiles_64 >= 128 ? 32 : 96)) {
+    if (few_rows(a)) {
         if ((uint64_t)((a.channels + 31) / 32) * a.groups < 128) return launch_few<T, 1, 4>(a, st);
         return mean > 1 && a.columns >= 4096 ? launch_few<T, 2, 8>(a, st) : launch_few<T, 2, 4>(a, st);
     }
     if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return false;     // offsets into a tile are 32-bit
+    if (workspace && launch_shared<T>(a, workspace, st)) return true;
     constexpr uint64_t kEnough = 192;
-    if (mean > 160 && most_blocks(a, 256, kTileChannels) >= kEnough) return launch_tiles<T, 2, 8, 4>(a, st);
-    if ((mean > 80 || (mean <= 32 && tiles_64 >= 256)) && most_blocks(a, 128, kTileChannels) >= kEnough) return launch_tiles<T, 2, 8, 2>(a, st);
-    return launch_tiles<T, 4, 4, 2>(a, st);
+    if (mean > 160 && most_blocks(a, 256, kTileChannels) >= kEnough) return launch_tiles<T, 8, 2, 8, 4>(a, st);
+    if ((mean > 80 || (mean <= 32 && tiles_64 >= 256)) && most_blocks(a, 128, kTileChannels) >= kEnough) return launch_tiles<T, 8, 2, 8, 2>(a, st);
+    return launch_tiles<T, 4, 4, 4, 4>(a, st);
 }
 
-void launch_i8_product(const I8Args &a, void *, hipStream_t st)
+void launch_i8_product(const I8Args &a, void *workspace, hipStream_t st)
 {
-    if (in_pieces(a)) {
-        if (a.type == SEER_F32 ? launch_pieces<float>(a, st) : a.type == SEER_BF16 ? launch_pieces<bf16_t>(a, st) : launch_pieces<f16_t>(a, st)) return;
-    }
+    if (in_pieces(a) && (a.type == SEER_F32    ? launch_pieces<float>(a, workspace, st)
+                         : a.type == SEER_BF16 ? launch_pieces<bf16_t>(a, workspace, st)
+                                               : launch_pieces<f16_t>(a, workspace, st)))
+        return;
     const uint32_t blocks = (uint32_t)most_blocks(a, kAnyTokens, kAnyChannels);
     hipLaunchKernelGGL(i8_any_kernel, dim3(std::min(blocks, 1u << 22)), dim3(256), 0, st, a, blocks);
 }

@@ -148,7 +148,7 @@ def test_strides_and_alignment(shape, where):
 
 def test_the_largest_sums_are_exact():
     K = 131071
-    for M, N in ((1, 16), (70, 64)):
+    for M, N in ((1, 16), (70, 64), (97, 300)):
         a = torch.full((M, K), -128, dtype=torch.int8, device="cuda:0")
         b = torch.full((1, N, K), -128, dtype=torch.int8, device="cuda:0")
         b[0, 1] = 127
@@ -258,3 +258,34 @@ def test_many_groups(groups, columns):
     for rows, N in ((groups // 3, 16), (40 * groups, 24)):
         lengths = rng.multinomial(rows, rng.dirichlet(np.full(groups, 0.3)))
         check_product(i8(rng, rows, columns), i8(rng, groups, N, columns), np.concatenate([[0], np.cumsum(lengths)]).tolist(), "f16", rng)
+
+
+SHARED = [  # rows, channels, columns: one product whose columns are shared out between workgroups
+    (97, 16, 3088), (100, 300, 4112), (129, 257, 8192), (500, 130, 4112), (1000, 500, 6160), (300, 1001, 5136), (3000, 129, 8208),
+]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("shape", SHARED, ids=str)
+def test_shared_columns(shape, kind):
+    announce(f"i8 shared {shape} {kind}")
+    M, N, K = shape
+    assert S.i8_product_workspace_bytes(M, N, K) > 0
+    rng = np.random.default_rng(M + K)
+    check_product(i8(rng, M, K), i8(rng, 1, N, K), None, kind, rng)
+
+
+def test_shared_columns_with_a_workspace_of_the_callers():
+    rng = np.random.default_rng(8)
+    M, N, K = 300, 200, 4096
+    a, b = i8(rng, M, K), i8(rng, 1, N, K)
+    sa, sb = torch.rand(M, device="cuda:0"), torch.rand(1, N, device="cuda:0")
+    need = S.i8_product_workspace_bytes(M, N, K)
+    want = S.seer_i8_product(a, sa, b, sb)
+    ws = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda:0")
+    assert torch.equal(S.seer_i8_product(a, sa, b, sb, workspace=ws[:need]), want)
+    assert bool((ws[need:] == 255).all())
+    with pytest.raises(S.SeerError):
+        S.seer_i8_product(a, sa, b, sb, workspace=ws[: need - 1])
+    ptr = torch.tensor([0, M], dtype=torch.int32, device="cuda:0")
+    assert torch.equal(S.seer_i8_product(a, sa, b, sb, group_ptr=ptr), want)
