@@ -593,7 +593,8 @@ static bool launch_few(const I8Args &a, hipStream_t st)
 //                          256: 94 46 55 83        512: 186 55 58 85
 //    1 x 2048 x 2048, rows   1: 4.7 10 12 18        64: 9.0 12.5 13 18     128: 16 12.6 18 19
 // so that few rows are for products that would leave CUs without a tile, or up to 12 rows, and larger tiles are for as many
-// of them as there are CUs or nearly.  Few rows: 16 channels to a workgroup where 32 are fewer than half of the
+// of them as there are CUs or nearly.  Every workgroup of few rows reads all of a, at some 26 GB/s a CU: from 33 rows on, long columns are
+// faster in tiles, if few enough to be shared out (below; 512 x 8192, 64 rows: 21.6 and 15.3).  Few rows: 16 channels to a workgroup where 32 are fewer than half of the
 // CUs (2048 x 2048, one row: 3.8 and 4.7); eight waves to share the columns where each has 512 or more and there is
 // more than one row (8192 x 8192, 64 rows: 25.6 and 27.8; one row: 14.0 and 13.1; 2048 columns, 64 groups of 8: 29 and 26).
 constexpr uint32_t kCUs = 256;
@@ -601,7 +602,8 @@ constexpr uint32_t kCUs = 256;
 static bool few_rows(const I8Args &a)
 {
     const uint64_t tiles = most_blocks(a, 64, kTileChannels);
-    return a.rows / a.groups <= (tiles >= 256 ? 12u : tiles >= 128 ? 32u : 64u);
+    const uint32_t most = tiles >= 256 ? 12 : tiles >= 128 ? 32 : a.columns > 4096 && tiles <= 64 && !a.group_ptr ? 32 : 64;
+    return a.rows / a.groups <= most;
 }
 
 // One product whose tiles of 64 tokens leave CUs idle has its columns shared out, as many shares as its time is expected to be least
