@@ -35,7 +35,9 @@ __device__ __forceinline__ GroupTiles group_tiles(const I8Args &a, uint32_t g, u
 }
 
 // Tiles lie in the order of the groups; in a group, kPanel rows of tiles make a panel that is gone through column by
-// column, so that workgroups that run at the same time on an XCD share rows of both matrices in its L2.
+// column, so that workgroups that run at the same time on an XCD share rows of both matrices in its L2, and every XCD has as
+// many of the tiles that there are (of 32 groups and 32768 rows of 4096 x 4096: 780 us when they were dealt out by row
+// of tiles among those that there may be, 685 us so).
 constexpr uint32_t kPanel = 4;
 
 __device__ __forceinline__ Tile tile_in_group(uint32_t group, uint32_t from, uint32_t to, uint32_t local, uint32_t tokens, uint32_t across)
@@ -129,7 +131,8 @@ __device__ __forceinline__ void store_1(const I8Args &a, uint32_t row, uint32_t 
 // ------------------------------------------------------------------ any size, any alignment
 //
 // 64 tokens x 64 channels, 128 columns at a time through LDS, four waves of 32 x 32 each.  16 bytes of
-// a row at a time, from any address; the end of a row byte by byte, and zeros behind it.
+// a row at a time, from any address; the end of a row byte by byte, and zeros behind it.  Nothing is under way while
+// it multiplies: 3001 x 5001 x 4112 in 230 us (540 TOP/s; 71 in tiles).  For rows that are not whole pieces of 16 bytes.
 constexpr uint32_t kAnyTokens = 64, kAnyChannels = 64, kAnyCols = 128, kAnyPitch = kAnyCols + 16;
 
 __device__ __forceinline__ v4i32 load_16(const int8_t *p, int n)
@@ -150,46 +153,46 @@ __global__ __launch_bounds__(256) void i8_any_kernel(I8Args a, uint32_t blocks)
     __shared__ TileSearch s_search;
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
     for (uint32_t w = blockIdx.x; w < blocks; w += gridDim.x) {
-    Tile t;
-    if (!find_tile<4>(a, w, kAnyTokens, (a.channels + kAnyChannels - 1) / kAnyChannels, &s_search, &t)) continue;
-    const uint32_t n0 = t.column * kAnyChannels;
-    v4i32 acc[2][2] = {};
-    if (t.group < a.groups) {
-        const int8_t *b = a.b + (int64_t)t.group * a.channels * a.ldb;
-        for (uint32_t k0 = 0; k0 < a.columns; k0 += kAnyCols) {
-            for (uint32_t i = threadIdx.x; i < kAnyTokens * (kAnyCols / 16); i += 256) {
-                const uint32_t row = i / (kAnyCols / 16), col = k0 + i % (kAnyCols / 16) * 16;
-                const int left = (int)a.columns - (int)col;
-                const v4i32 va = t.begin + row < t.end ? load_16(a.a + (int64_t)(t.begin + row) * a.lda + col, left) : v4i32{0, 0, 0, 0};
-                *reinterpret_cast<v4i32 *>(s_a + row * kAnyPitch + (col - k0)) = va;
-                const v4i32 vb = n0 + row < a.channels ? load_16(b + (int64_t)(n0 + row) * a.ldb + col, left) : v4i32{0, 0, 0, 0};
-                *reinterpret_cast<v4i32 *>(s_b + row * kAnyPitch + (col - k0)) = vb;
-            }
-            __syncthreads();
-            for (uint32_t k = 0; k < kAnyCols; k += 64) {
-                v4i32 fb[2], fa[2];
-                for (int i = 0; i < 2; ++i) {
-                    fb[i] = *reinterpret_cast<const v4i32 *>(s_b + ((wave & 1) * 32 + i * 16 + (lane & 15)) * kAnyPitch + k + lane / 16 * 16);
-                    fa[i] = *reinterpret_cast<const v4i32 *>(s_a + ((wave >> 1) * 32 + i * 16 + (lane & 15)) * kAnyPitch + k + lane / 16 * 16);
+        Tile t;
+        if (!find_tile<4>(a, w, kAnyTokens, (a.channels + kAnyChannels - 1) / kAnyChannels, &s_search, &t)) continue;
+        const uint32_t n0 = t.column * kAnyChannels;
+        v4i32 acc[2][2] = {};
+        if (t.group < a.groups) {
+            const int8_t *b = a.b + (int64_t)t.group * a.channels * a.ldb;
+            for (uint32_t k0 = 0; k0 < a.columns; k0 += kAnyCols) {
+                for (uint32_t i = threadIdx.x; i < kAnyTokens * (kAnyCols / 16); i += 256) {
+                    const uint32_t row = i / (kAnyCols / 16), col = k0 + i % (kAnyCols / 16) * 16;
+                    const int left = (int)a.columns - (int)col;
+                    const v4i32 va = t.begin + row < t.end ? load_16(a.a + (int64_t)(t.begin + row) * a.lda + col, left) : v4i32{0, 0, 0, 0};
+                    *reinterpret_cast<v4i32 *>(s_a + row * kAnyPitch + (col - k0)) = va;
+                    const v4i32 vb = n0 + row < a.channels ? load_16(b + (int64_t)(n0 + row) * a.ldb + col, left) : v4i32{0, 0, 0, 0};
+                    *reinterpret_cast<v4i32 *>(s_b + row * kAnyPitch + (col - k0)) = vb;
                 }
-                for (int i = 0; i < 2; ++i)
-                    for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[i], fa[j], acc[i][j], 0, 0, 0);
+                __syncthreads();
+                for (uint32_t k = 0; k < kAnyCols; k += 64) {
+                    v4i32 fb[2], fa[2];
+                    for (int i = 0; i < 2; ++i) {
+                        fb[i] = *reinterpret_cast<const v4i32 *>(s_b + ((wave & 1) * 32 + i * 16 + (lane & 15)) * kAnyPitch + k + lane / 16 * 16);
+                        fa[i] = *reinterpret_cast<const v4i32 *>(s_a + ((wave >> 1) * 32 + i * 16 + (lane & 15)) * kAnyPitch + k + lane / 16 * 16);
+                    }
+                    for (int i = 0; i < 2; ++i)
+                        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[i], fa[j], acc[i][j], 0, 0, 0);
+                }
+                __syncthreads();
             }
-            __syncthreads();
         }
-    }
-    for (int j = 0; j < 2; ++j) {
-        const uint32_t row = t.begin + (wave >> 1) * 32 + j * 16 + (lane & 15);
-        if (row >= t.end) continue;
-        const float sa = t.group < a.groups ? a.a_scale[row] : 0.0f;
-        for (int i = 0; i < 2; ++i)
-            for (int v = 0; v < 4; ++v) {
-                const uint32_t n = n0 + (wave & 1) * 32 + i * 16 + lane / 16 * 4 + v;
-                if (n >= a.channels) continue;
-                const float sb = t.group < a.groups ? a.b_scale[(int64_t)t.group * a.channels + n] : 0.0f;
-                store_1(a, row, n, t.group < a.groups ? (float)acc[i][j][v] * (sa * sb) : 0.0f);
-            }
-    }
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t row = t.begin + (wave >> 1) * 32 + j * 16 + (lane & 15);
+            if (row >= t.end) continue;
+            const float sa = t.group < a.groups ? a.a_scale[row] : 0.0f;
+            for (int i = 0; i < 2; ++i)
+                for (int v = 0; v < 4; ++v) {
+                    const uint32_t n = n0 + (wave & 1) * 32 + i * 16 + lane / 16 * 4 + v;
+                    if (n >= a.channels) continue;
+                    const float sb = t.group < a.groups ? a.b_scale[(int64_t)t.group * a.channels + n] : 0.0f;
+                    store_1(a, row, n, t.group < a.groups ? (float)acc[i][j][v] * (sa * sb) : 0.0f);
+                }
+        }
     }
 }
 
@@ -212,10 +215,14 @@ __device__ __forceinline__ void store_4(T *row, uint32_t n, uint32_t channels, c
 
 // ------------------------------------------------------------------ tiles
 //
-// 256 channels x TOKENS tokens per workgroup of eight waves.  64 columns at a time come straight from memory into one of
-// four LDS buffers, three steps before they are multiplied: a step's multiplications (512 matrix instructions of a workgroup,
-// 2 x 16 cycles x 32 on each SIMD) take less time than memory does to answer.  A row's four pieces of 16 bytes lie
-// in the order of their number xor (row / 2 + row / 8) % 4, so that lanes that read together use all banks.
+// 256 channels x 64, 128 or 256 tokens per workgroup.  64 columns at a time come straight from memory into one of four LDS
+// buffers, and from there into registers while the 64 columns before them are multiplied; so the matrix instructions wait for
+// neither, but for one barrier a step.  A row's four pieces of 16 bytes lie in LDS in the order of their number
+// xor (row / 2 + row / 8) % 4, so that lanes that read together use all banks (no conflicts by the counters).
+// 8192 x 8192 x 8192: 428 to 455 us, 2.4 to 2.57 POP/s (the library: 2.38).  Bound by the card's power: all-zero operands take
+// three quarters of the time, and instructions of 32 x 32 x 32, as fast with zeros, are a tenth slower with values.
+// Slower, too: wave tiles of 128 x 128 in 512 registers, two workgroups of four waves on a CU, workgroups that go on to their
+// next tile (the registers for that spill).
 constexpr uint32_t kTileChannels = 256, kTileCols = 64;
 
 typedef __attribute__((address_space(3))) int8_t lds_byte;
@@ -371,53 +378,53 @@ __global__ __launch_bounds__(WAVES * 64, 2) void i8_tile_kernel(I8Args a, Shared
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // nothing is on its way to LDS when the workgroup ends
         return;
     } else {
-    // every scale is fetched before the first store: a wait for a load is one for all stores before it, too
-    const bool zero = t.group >= a.groups;
-    const float *sb = a.b_scale + (int64_t)(zero ? 0 : t.group) * a.channels;
-    const uint32_t n1 = n0 + wc * CI * 16 + (lane >> 4) * 4, row1 = t.begin + wt * TJ * 16 + (lane & 15);
-    float of_row[TJ], of_channel[CI][4];
+        // every scale is fetched before the first store: a wait for a load is one for all stores before it, too
+        const bool zero = t.group >= a.groups;
+        const float *sb = a.b_scale + (int64_t)(zero ? 0 : t.group) * a.channels;
+        const uint32_t n1 = n0 + wc * CI * 16 + (lane >> 4) * 4, row1 = t.begin + wt * TJ * 16 + (lane & 15);
+        float of_row[TJ], of_channel[CI][4];
 #pragma unroll
-    for (int j = 0; j < TJ; ++j) of_row[j] = a.a_scale[min(row1 + j * 16, t.end - 1)];
+        for (int j = 0; j < TJ; ++j) of_row[j] = a.a_scale[min(row1 + j * 16, t.end - 1)];
 #pragma unroll
-    for (int i = 0; i < CI; ++i)
+        for (int i = 0; i < CI; ++i)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) of_channel[i][v] = sb[min(n1 + i * 16 + v, a.channels - 1)];
-    // A lane's results are four channels each of TJ * CI tokens.  They change places in LDS, in a region of the wave's own, so
-    // that stores are of 16 bytes and lines are written whole (4096 x 4096 x 256, where the stores are most of the
-    // time: 15.4 us, and 18.3 with 8-byte stores, 16 rows at a time).  A row's pieces lie in the order of their number xor the row.
-    constexpr int CIP = CI * (int)sizeof(T) > 16 ? 16 / (int)sizeof(T) : CI;      // channels go by up to 256 bytes of a row
-    constexpr uint32_t PIECES = CIP * sizeof(T), ROW = PIECES * 16, E = Unit<T>::kElems;
-    constexpr uint32_t kPer = WAVES / 4;            // waves to a buffer
-    static_assert(WAVES % 4 == 0 && kPer * TJ * 16 * ROW <= Shape::kBytes && CI % CIP == 0, "the waves' regions fit");
-    step_barrier<0>();                              // nothing is on its way to LDS, and nobody reads the last columns any more
-    const uint32_t turn = wave / kPer;
-    int8_t *mine = (turn == 0 ? s_0 : turn == 1 ? s_1 : turn == 2 ? s_2 : s_3) + (wave % kPer) * (TJ * 16 * ROW);
+            for (int v = 0; v < 4; ++v) of_channel[i][v] = sb[min(n1 + i * 16 + v, a.channels - 1)];
+        // A lane's results are four channels each of TJ * CI tokens.  They change places in LDS, in a region of the wave's own, so
+        // that stores are of 16 bytes and lines are written whole (4096 x 4096 x 256, where the stores are most of the
+        // time: 15.4 us, and 18.3 with 8-byte stores, 16 rows at a time).  A row's pieces lie in the order of their number xor the row.
+        constexpr int CIP = CI * (int)sizeof(T) > 16 ? 16 / (int)sizeof(T) : CI;      // channels go by up to 256 bytes of a row
+        constexpr uint32_t PIECES = CIP * sizeof(T), ROW = PIECES * 16, E = Unit<T>::kElems;
+        constexpr uint32_t kPer = WAVES / 4;            // waves to a buffer
+        static_assert(WAVES % 4 == 0 && kPer * TJ * 16 * ROW <= Shape::kBytes && CI % CIP == 0, "the waves' regions fit");
+        step_barrier<0>();                              // nothing is on its way to LDS, and nobody reads the last columns any more
+        const uint32_t turn = wave / kPer;
+        int8_t *mine = (turn == 0 ? s_0 : turn == 1 ? s_1 : turn == 2 ? s_2 : s_3) + (wave % kPer) * (TJ * 16 * ROW);
 #pragma unroll
-    for (int first = 0; first < CI; first += CIP) {
+        for (int first = 0; first < CI; first += CIP) {
 #pragma unroll
-        for (int j = 0; j < TJ; ++j)
+            for (int j = 0; j < TJ; ++j)
 #pragma unroll
-            for (int i = 0; i < CIP; ++i) {
-                typedef T four __attribute__((ext_vector_type(4)));
-                four v;
+                for (int i = 0; i < CIP; ++i) {
+                    typedef T four __attribute__((ext_vector_type(4)));
+                    four v;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = zero ? (T)0.0f : (T)((float)acc[first + i][j][u] * (of_row[j] * of_channel[first + i][u]));
-                const uint32_t row = j * 16 + (lane & 15), at = (i * 16 + (lane >> 4) * 4) * (uint32_t)sizeof(T);
-                *reinterpret_cast<four *>(mine + row * ROW + ((at / 16) ^ (row % PIECES)) * 16 + at % 16) = v;
+                    for (int u = 0; u < 4; ++u) v[u] = zero ? (T)0.0f : (T)((float)acc[first + i][j][u] * (of_row[j] * of_channel[first + i][u]));
+                    const uint32_t row = j * 16 + (lane & 15), at = (i * 16 + (lane >> 4) * 4) * (uint32_t)sizeof(T);
+                    *reinterpret_cast<four *>(mine + row * ROW + ((at / 16) ^ (row % PIECES)) * 16 + at % 16) = v;
+                }
+            __builtin_amdgcn_wave_barrier();            // (a wave's LDS accesses are served in order)
+#pragma unroll
+            for (uint32_t part = 0; part < TJ * 16 * PIECES / 64; ++part) {
+                const uint32_t row = part * (64 / PIECES) + lane / PIECES, piece16 = lane % PIECES;
+                const uint32_t to = t.begin + wt * TJ * 16 + row, n = n0 + (wc * CI + first) * 16 + piece16 * E;
+                if (to < t.end && n < a.channels) {
+                    Unit<T> u;
+                    u.v = *reinterpret_cast<const typename Unit<T>::whole *>(mine + row * ROW + (piece16 ^ (row % PIECES)) * 16);
+                    store_some(out + (int64_t)to * a.ldo + n, u, (int)min(E, a.channels - n));
+                }
             }
-        __builtin_amdgcn_wave_barrier();            // (a wave's LDS accesses are served in order)
-#pragma unroll
-        for (uint32_t part = 0; part < TJ * 16 * PIECES / 64; ++part) {
-            const uint32_t row = part * (64 / PIECES) + lane / PIECES, piece16 = lane % PIECES;
-            const uint32_t to = t.begin + wt * TJ * 16 + row, n = n0 + (wc * CI + first) * 16 + piece16 * E;
-            if (to < t.end && n < a.channels) {
-                Unit<T> u;
-                u.v = *reinterpret_cast<const typename Unit<T>::whole *>(mine + row * ROW + (piece16 ^ (row % PIECES)) * 16);
-                store_some(out + (int64_t)to * a.ldo + n, u, (int)min(E, a.channels - n));
-            }
+            __builtin_amdgcn_wave_barrier();
         }
-        __builtin_amdgcn_wave_barrier();
-    }
     }
 }
 
@@ -442,7 +449,9 @@ __global__ __launch_bounds__(kWG) void i8_join_kernel(I8Args a, SharedColumns sh
 // ------------------------------------------------------------------ few rows to a group
 //
 // CI * 16 channels of one group per workgroup, whose waves each take a share of the columns; both operands come straight from memory, the
-// weights once per 64 rows, and the waves' sums meet in LDS.  Bound by the bytes of b.
+// weights once per 64 rows, and the waves' sums meet in LDS.  Bound by the bytes of b: 8192 x 8192, one row, in 12.4 us
+// (5.4 TB/s), 64 groups of 2048 x 4096 with four rows each on average in 84 (6.3 TB/s).  Plain loads: an instruction takes half
+// of 16 lines, and with the streaming hint the other half comes from memory again (96 and 110 us).
 constexpr uint32_t kFewRows = 64;
 
 // 16 TJ rows from `at` on: the calling wave's columns [k_begin, k_end), U pieces of each row at a time.
@@ -580,7 +589,9 @@ template <class T, int CI, int WAVES>
 static bool launch_few(const I8Args &a, hipStream_t st)
 {
     const uint32_t groups = a.groups + (a.group_ptr ? 1 : 0), share = ((a.columns + WAVES - 1) / WAVES + 63) & ~63u;
-    hipLaunchKernelGGL((i8_few_kernel<T, CI, WAVES>), dim3((a.channels + CI * 16 - 1) / (CI * 16), groups), dim3(WAVES * 64), 0, st, a, share);
+    const uint32_t across = (a.channels + CI * 16 - 1) / (CI * 16);
+    if ((uint64_t)across * WAVES * 64 >= 1ull << 32) return false;  // (a launch has fewer lanes)
+    hipLaunchKernelGGL((i8_few_kernel<T, CI, WAVES>), dim3(across, groups), dim3(WAVES * 64), 0, st, a, share);
     return true;
 }
 
