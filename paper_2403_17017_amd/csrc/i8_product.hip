@@ -603,8 +603,8 @@ static bool launch_few(const I8Args &a, hipStream_t st)
 //    1 x 8192 x 8192, rows   1: 13 38 39 51         64: 26 48 48 52         96: 42 46 51 54        128: 48 48 55 56
 //                          256: 94 46 55 83        512: 186 55 58 85
 //    1 x 2048 x 2048, rows   1: 4.7 10 12 18        64: 9.0 12.5 13 18     128: 16 12.6 18 19
-// so that few rows are for products that would leave CUs without a tile, or up to 12 rows, and larger tiles are for as many
-// of them as there are CUs or nearly.  Every workgroup of few rows reads all of a, at some 26 GB/s a CU: from 33 rows on, long columns are
+// so that few rows are for products that would leave CUs without a tile, or up to 12 rows, and with several groups larger tiles are for
+// as many of them as there are CUs or nearly; for one, see tile_cost.  Every workgroup of few rows reads all of a, at some 26 GB/s a CU: from 33 rows on, long columns are
 // faster in tiles, if few enough to be shared out (below; 512 x 8192, 64 rows: 21.6 and 15.3).  Few rows: 16 channels to a workgroup where 32 are fewer than half of the
 // CUs (2048 x 2048, one row: 3.8 and 4.7); eight waves to share the columns where each has 512 or more and there is
 // more than one row (8192 x 8192, 64 rows: 25.6 and 27.8; one row: 14.0 and 13.1; 2048 columns, 64 groups of 8: 29 and 26).
@@ -617,28 +617,45 @@ static bool few_rows(const I8Args &a)
     return a.rows / a.groups <= most;
 }
 
-// One product whose tiles of 64 tokens leave CUs idle has its columns shared out, as many shares as its time is expected to be least
-// for: 0.33 us for every step of 64 columns, 1 us for every 3 MB of sums written and read, 8 us for the second launch.  Measured, us, one
-// and several shares (channels x columns, rows 128, 256, 512, 1024):
+// For one product, what its time would be, in us: rounds of as many tiles as there are CUs, a step of 64 columns costing more
+// when more of them are at work.  Measured (8192 channels, 16 | 64 steps): tiles of 64 tokens 128: 9.9 | 26, 256: 12 | 31, 384: 19 | 49,
+// 1024: 35 | 105; of 128 tokens 64: 13 | 33, 192: 16 | 36, 256: 17 | 42, 384: 28 | 70, 1024: 61 | 158; of 256 tokens
+// 32: 19 | 48, 128: 21 | 50, 192: 23 | 57, 256: 26 | 64, 416: 44 | 115, 1024: 93 | 247.
+struct TileCost { uint32_t tokens; double least, more, above /* share of the CUs */, round; };
+constexpr TileCost kCost64 = {64, 0.345, 0.02, 0, 3}, kCost128 = {128, 0.41, 0.09, 0, 7.5}, kCost256 = {256, 0.6, 0.2, 0.5, 10};
+
+static double tile_cost(const I8Args &a, const TileCost &c, uint32_t shares)
+{
+    const uint64_t tiles = ((uint64_t)a.rows + c.tokens - 1) / c.tokens * ((a.channels + kTileChannels - 1) / kTileChannels) * shares;
+    const double steps = ((double)a.columns / kTileCols) / shares;
+    const auto round = [&](double full) {
+        return steps * (c.least + c.more * std::max(0.0, (full - c.above) / (1 - c.above))) + c.round;
+    };
+    const uint64_t rest = tiles % kCUs;
+    return (double)(tiles / kCUs) * round(1) + (rest ? round((double)rest / kCUs) : 0);
+}
+
+// Tiles of 64 tokens that leave CUs idle have the columns shared out, at 1 us for every 3 MB of sums written and read and 8 us for the
+// second launch.  Measured, us, one and several shares (channels x columns, rows 128, 256, 512, 1024):
 //   512 x 8192:  34 34 34 36 and 15 18 20 25      2048 x 8192: 34 35 45 46 and 21 25 31 44
 //   8192 x 8192: 46 46 55 74 and 32 45 54 73      2048 x 2048: 12.5 12.7 13 14 and 13 16 25 27 (hence one)
-static uint32_t column_shares(const I8Args &a)
+static uint32_t column_shares(const I8Args &a, double *least)
 {
+    *least = tile_cost(a, kCost64, 1);
     if (a.group_ptr || few_rows(a) || a.columns == 0) return 1;
     const uint64_t tiles = most_blocks(a, 64, kTileChannels);
     if (tiles > kCUs * 2 / 3) return 1;
-    const double steps = (double)a.columns / kTileCols, sums = 8.0 * a.rows * a.channels;
-    const uint32_t most = (uint32_t)std::min<uint64_t>({kCUs * 3 / 2 / tiles, (uint64_t)steps / 6, 16});
+    const double sums = 8.0 * a.rows * a.channels;
+    const uint32_t most = (uint32_t)std::min<uint64_t>({kCUs * 3 / 2 / tiles, (uint64_t)a.columns / kTileCols / 6, 16});
     uint32_t best = 1;
-    double least = 0.33 * steps;
     for (uint32_t n = 2; n <= most; ++n) {
-        const double t = 0.33 * steps / n + n * sums / 3e6 + 8;
-        if (t < least) {
-            least = t;
+        const double t = tile_cost(a, kCost64, n) + n * sums / 3e6 + 8;
+        if (t < *least) {
+            *least = t;
             best = n;
         }
     }
-    return best;
+    return std::min(tile_cost(a, kCost128, 1), tile_cost(a, kCost256, 1)) < *least ? 1 : best;
 }
 static SharedColumns shared_columns(const I8Args &a, uint32_t shares, void *workspace)
 {
@@ -655,14 +672,16 @@ size_t i8_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t columns, ui
     a.columns = columns;
     a.groups = groups;
     if (rows == 0 || channels == 0 || groups != 1 || columns % 16 != 0) return 0;
-    const uint32_t shares = column_shares(a);
+    double least;
+    const uint32_t shares = column_shares(a, &least);
     return shares > 1 ? (size_t)shares * rows * ((channels + 3) & ~3u) * 4 : 0;
 }
 
 template <class T>
 static bool launch_shared(const I8Args &a, void *workspace, hipStream_t st)
 {
-    uint32_t shares = column_shares(a);
+    double least;
+    uint32_t shares = column_shares(a, &least);
     if (shares <= 1) return false;
     const SharedColumns c = shared_columns(a, shares, workspace);
     shares = (a.columns + c.share - 1) / c.share;
@@ -683,6 +702,11 @@ static bool launch_pieces(const I8Args &a, void *workspace, hipStream_t st)
     }
     if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return false;     // offsets into a tile are 32-bit
     if (workspace && launch_shared<T>(a, workspace, st)) return true;
+    if (!a.group_ptr) {
+        const double t64 = tile_cost(a, kCost64, 1), t128 = tile_cost(a, kCost128, 1), t256 = tile_cost(a, kCost256, 1);
+        if (t256 <= std::min(t64, t128)) return launch_tiles<T, 8, 2, 8, 4>(a, st);
+        return t128 <= t64 ? launch_tiles<T, 8, 2, 8, 2>(a, st) : launch_tiles<T, 4, 4, 4, 4>(a, st);
+    }
     constexpr uint64_t kEnough = 192;
     if (mean > 160 && most_blocks(a, 256, kTileChannels) >= kEnough) return launch_tiles<T, 8, 2, 8, 4>(a, st);
     if ((mean > 80 || (mean <= 32 && tiles_64 >= 256)) && most_blocks(a, 128, kTileChannels) >= kEnough) return launch_tiles<T, 8, 2, 8, 2>(a, st);

@@ -109,13 +109,15 @@ class Routing:
         return cls(experts, n(experts + 1), n(tokens * choices), n(tokens, choices))
 
     @classmethod
-    def _new(cls, tokens, choices, experts, like, stream):
-        """The same in one piece, for seer_route."""
+    def _new(cls, tokens, choices, experts, like, stream, workspace_bytes):
+        """(a routing, a workspace for seer_route or None), in one piece of memory."""
         self, count = cls.__new__(cls), tokens * choices
         self.experts, self.tokens, self.choices = experts, tokens, choices
-        self.expert_ptr, self.slot_choice, slots = _new((experts + 1 + 2 * count,), _torch.int32, like, stream).split((experts + 1, count, count))
+        words = workspace_bytes // 4
+        workspace, self.expert_ptr, self.slot_choice, slots = _new((words + experts + 1 + 2 * count,), _torch.int32, like, stream).split(
+            (words, experts + 1, count, count))
         self.choice_slot = slots.view(tokens, choices)
-        return self
+        return self, workspace.view(_torch.uint8) if words else None
 
 
 def route_workspace_bytes(tokens: int, choices: int, experts: int) -> int:
@@ -132,12 +134,15 @@ def seer_route(expert, experts: int, routing: Routing = None, workspace=None, st
     if not 0 < experts <= MAX_EXPERTS:
         raise SeerError(ELIMIT if experts > 0 else EINVAL, "seer_route")
     if routing is None:
-        routing = Routing._new(tokens, choices, int(experts), expert, stream)
+        # (asking costs as much as the call, and up to 2048 choices need none)
+        need = route_workspace_bytes(tokens, choices, experts) if workspace is None and tokens * choices > 2048 else 0
+        routing, room = Routing._new(tokens, choices, int(experts), expert, stream, need)
+        workspace = room if workspace is None else workspace
     elif (routing.tokens, routing.choices, routing.experts) != (tokens, choices, experts):
         raise ValueError("routing has other sizes")
     h = _stream_handle(stream)
     rc = m.route(expert, routing, workspace, h)
-    if rc == EWORKSPACE and workspace is None:           # (small ones need none, and asking costs as much as the call)
+    if rc == EWORKSPACE and workspace is None:
         workspace = _new((route_workspace_bytes(tokens, choices, experts),), _torch.uint8, expert, stream)
         rc = m.route(expert, routing, workspace, h)
     if rc:
