@@ -22,6 +22,19 @@ __device__ __forceinline__ uint32_t group_begin(const I8Args &a, uint32_t g)
     return p < 0 ? 0 : min((uint32_t)p, a.rows);
 }
 
+// The last group that begins at or before a row; `groups`: none's.
+__device__ __forceinline__ uint32_t group_of(const I8Args &a, uint32_t row)
+{
+    uint32_t low = 0, high = a.groups + 1;
+    if (!a.group_ptr) return 0;
+    while (low + 1 < high) {
+        const uint32_t mid = (low + high) / 2;
+        if (group_begin(a, mid) <= row) low = mid;
+        else high = mid;
+    }
+    return low;
+}
+
 // What a lane knows of group g: its rows, and the tiles that they take.
 struct GroupTiles { uint32_t from, to, tiles; };
 
@@ -238,7 +251,7 @@ struct TileShape {
     static_assert(WC * CI * 16 == (int)kTileChannels, "waves cover the channels");
 };
 
-// The columns of one product shared out: workgroups of share `s` multiply columns s * share ... and leave sums of 32-bit integers,
+// The columns shared out: workgroups of share `s` multiply columns s * share ... and leave sums of 32-bit integers,
 // [shares][rows][pitch], which i8_join_kernel adds up and scales.
 struct SharedColumns { int32_t *sums; uint32_t blocks, share, pitch; };
 
@@ -438,10 +451,11 @@ __global__ __launch_bounds__(kWG) void i8_join_kernel(I8Args a, SharedColumns sh
         v4i32 sum = {0, 0, 0, 0};
         for (uint32_t s = 0; s < shares; ++s)
             sum += *reinterpret_cast<const v4i32 *>(shared.sums + ((size_t)s * a.rows + row) * shared.pitch + n);
-        const float sa = a.a_scale[row];
+        const uint32_t g = group_of(a, row);
+        const float sa = a.a_scale[row], *sb = a.b_scale + (int64_t)min(g, a.groups - 1) * a.channels;
         float v[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v[u] = (float)sum[u] * (sa * a.b_scale[min(n + u, a.channels - 1)]);
+        for (int u = 0; u < 4; ++u) v[u] = g < a.groups ? (float)sum[u] * (sa * sb[min(n + u, a.channels - 1)]) : 0.0f;
         store_4(static_cast<T *>(a.out) + (int64_t)row * a.ldo, n, a.channels, v);
     }
 }
@@ -604,16 +618,18 @@ static bool launch_few(const I8Args &a, hipStream_t st)
 //                          256: 94 46 55 83        512: 186 55 58 85
 //    1 x 2048 x 2048, rows   1: 4.7 10 12 18        64: 9.0 12.5 13 18     128: 16 12.6 18 19
 // so that few rows are for products that would leave CUs without a tile, or up to 12 rows, and with several groups larger tiles are for
-// as many of them as there are CUs or nearly; for one, see tile_cost.  Every workgroup of few rows reads all of a, at some 26 GB/s a CU: from 33 rows on, long columns are
-// faster in tiles, if few enough to be shared out (below; 512 x 8192, 64 rows: 21.6 and 15.3).  Few rows: 16 channels to a workgroup where 32 are fewer than half of the
-// CUs (2048 x 2048, one row: 3.8 and 4.7); eight waves to share the columns where each has 512 or more and there is
+// as many of them as there are CUs or nearly; for one, see tile_cost.  Every workgroup of few rows reads all of its group's rows, at some
+// 26 GB/s a CU: long columns are sooner faster in tiles, if few enough to be shared out (below; 1 x 512 x 8192, 64 rows: 21.6 and 15.3;
+// 32 x 256 x 8192, mean 24 | 48: 41 | 69 and 24 | 26), and so are the longest of several groups (32 x 256 x 4096, mean 33 | 48: 24 | 35
+// and 23 | 20; 16 x 512 x 1024, mean 33: 8.9 and 9.7).  Few rows: 16 channels to a workgroup where 32 are fewer than half of the CUs (2048 x 2048, one row: 3.8 and 4.7); eight waves to share the columns where each has 512 or more and there is
 // more than one row (8192 x 8192, 64 rows: 25.6 and 27.8; one row: 14.0 and 13.1; 2048 columns, 64 groups of 8: 29 and 26).
 constexpr uint32_t kCUs = 256;
 
 static bool few_rows(const I8Args &a)
 {
     const uint64_t tiles = most_blocks(a, 64, kTileChannels);
-    const uint32_t most = tiles >= 256 ? 12 : tiles >= 128 ? 32 : a.columns > 4096 && tiles <= 64 && !a.group_ptr ? 32 : 64;
+    const bool several = a.group_ptr != nullptr, long_columns = a.columns > 4096 && tiles <= 64;
+    const uint32_t most = tiles >= 256 ? 12 : tiles >= 128 ? 32 : several ? (long_columns ? 16 : a.columns >= 2048 ? 32 : 64) : long_columns ? 32 : 64;
     return a.rows / a.groups <= most;
 }
 
@@ -626,7 +642,7 @@ constexpr TileCost kCost64 = {64, 0.345, 0.02, 0, 3}, kCost128 = {128, 0.41, 0.0
 
 static double tile_cost(const I8Args &a, const TileCost &c, uint32_t shares)
 {
-    const uint64_t tiles = ((uint64_t)a.rows + c.tokens - 1) / c.tokens * ((a.channels + kTileChannels - 1) / kTileChannels) * shares;
+    const uint64_t tiles = most_tiles(a, c.tokens) * ((a.channels + kTileChannels - 1) / kTileChannels) * shares;
     const double steps = ((double)a.columns / kTileCols) / shares;
     const auto round = [&](double full) {
         return steps * (c.least + c.more * std::max(0.0, (full - c.above) / (1 - c.above))) + c.round;
@@ -639,10 +655,11 @@ static double tile_cost(const I8Args &a, const TileCost &c, uint32_t shares)
 // second launch.  Measured, us, one and several shares (channels x columns, rows 128, 256, 512, 1024):
 //   512 x 8192:  34 34 34 36 and 15 18 20 25      2048 x 8192: 34 35 45 46 and 21 25 31 44
 //   8192 x 8192: 46 46 55 74 and 32 45 54 73      2048 x 2048: 12.5 12.7 13 14 and 13 16 25 27 (hence one)
+// and of groups (mean 66, 100, 160, 256): 10 x 256 x 6656: 37 39 41 41 and 17 19 21 30, 32 x 256 x 4096: 26 28 29 30 and 20 22 28 30.
 static uint32_t column_shares(const I8Args &a, double *least)
 {
     *least = tile_cost(a, kCost64, 1);
-    if (a.group_ptr || few_rows(a) || a.columns == 0) return 1;
+    if (few_rows(a) || a.columns == 0) return 1;
     const uint64_t tiles = most_blocks(a, 64, kTileChannels);
     if (tiles > kCUs * 2 / 3) return 1;
     const double sums = 8.0 * a.rows * a.channels;
@@ -655,8 +672,9 @@ static uint32_t column_shares(const I8Args &a, double *least)
             best = n;
         }
     }
-    return std::min(tile_cost(a, kCost128, 1), tile_cost(a, kCost256, 1)) < *least ? 1 : best;
+    return !a.group_ptr && std::min(tile_cost(a, kCost128, 1), tile_cost(a, kCost256, 1)) < *least ? 1 : best;
 }
+
 static SharedColumns shared_columns(const I8Args &a, uint32_t shares, void *workspace)
 {
     const uint32_t steps = (a.columns + kTileCols - 1) / kTileCols;
@@ -671,9 +689,12 @@ size_t i8_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t columns, ui
     a.channels = channels;
     a.columns = columns;
     a.groups = groups;
-    if (rows == 0 || channels == 0 || groups != 1 || columns % 16 != 0) return 0;
+    if (rows == 0 || channels == 0 || columns % 16 != 0) return 0;
+    static const int32_t some = 0;                  // one group may come with its group_ptr or without
     double least;
-    const uint32_t shares = column_shares(a, &least);
+    uint32_t shares = groups == 1 ? column_shares(a, &least) : 1;
+    a.group_ptr = &some;
+    shares = std::max(shares, column_shares(a, &least));
     return shares > 1 ? (size_t)shares * rows * ((channels + 3) & ~3u) * 4 : 0;
 }
 

@@ -230,81 +230,96 @@ void launch_route(const void *expert, bool wide, uint32_t count, uint32_t expert
 
 constexpr uint32_t kMaxGrid = 1u << 20;     // workgroups; more work is looped over
 
+// LANES lanes to a row, kWG / LANES rows to a workgroup.  The token of a lane; uniform in a wave where it can be.
+template <int LANES>
+__device__ __forceinline__ uint32_t token_of(uint32_t block)
+{
+    const uint32_t t = block * (kWG / LANES) + threadIdx.x / LANES;
+    return LANES >= kWave ? (uint32_t)__builtin_amdgcn_readfirstlane((int)t) : t;
+}
+
 // 16 411 tokens of 4096 bf16 to six experts each: 170 us, 5.5 TB/s; by slot, with the stores in order and every row read six times
 // from the last-level cache, 230; with streaming stores 181; with two or four units a lane 178 and 174.
-template <class T, bool WEIGHTED>
+template <class T, int LANES>
 __global__ __launch_bounds__(kWG) void gather_kernel(RouteRows r, const float *__restrict__ weight, const T *__restrict__ x,
                                                      int64_t ldx, T *__restrict__ out, int64_t ldo)
 {
     constexpr int E = Unit<T>::kElems;
-    for (uint32_t t = blockIdx.y; t < r.tokens; t += gridDim.y)
-    for (uint32_t col = (blockIdx.x * kWG + threadIdx.x) * E; col < r.cols; col += gridDim.x * kWG * E) {
-        const int n = (int)min((uint32_t)E, r.cols - col);
-        const Unit<T> u = load_some(x + (int64_t)t * ldx + col, n);
-        for (uint32_t k = 0; k < r.choices; ++k) {
-            const uint32_t c = t * r.choices + k;
-            const int32_t slot = r.choice_slot[c];
-            Unit<T> v = u;
-            if constexpr (WEIGHTED) {
-                const float s = weight[c];
+    for (uint32_t b = blockIdx.y; b * (kWG / LANES) < r.tokens; b += gridDim.y) {
+        const uint32_t t = token_of<LANES>(b);
+        if (t >= r.tokens) continue;
+        for (uint32_t col = (blockIdx.x * LANES + threadIdx.x % LANES) * E; col < r.cols; col += gridDim.x * LANES * E) {
+            const int n = (int)min((uint32_t)E, r.cols - col);
+            const Unit<T> u = load_some(x + (int64_t)t * ldx + col, n);
+            for (uint32_t k = 0; k < r.choices; ++k) {
+                const uint32_t c = t * r.choices + k;
+                const int32_t slot = r.choice_slot[c];
+                Unit<T> v = u;
+                if (weight) {
+                    const float s = weight[c];
 #pragma unroll
-                for (int j = 0; j < E; ++j) v.v[j] = (T)(s * (float)u.v[j]);
+                    for (int j = 0; j < E; ++j) v.v[j] = (T)(s * (float)u.v[j]);
+                }
+                if (slot < 0) v = zero_unit<T>();
+                store_some(out + (int64_t)(slot < 0 ? -1 - slot : slot) * ldo + col, v, n);
             }
-            if (slot < 0) v = zero_unit<T>();
-            store_some(out + (int64_t)(slot < 0 ? -1 - slot : slot) * ldo + col, v, n);
         }
     }
 }
 
 // 32 768 tokens of 4096 bf16 from four experts each: 225 us, 6.0 TB/s; 253 without the streaming hint on rows that are used once.
-template <class T, bool WEIGHTED, bool STREAM>
+template <class T, bool STREAM, int LANES>
 __global__ __launch_bounds__(kWG) void combine_kernel(RouteRows r, const float *__restrict__ weight, const T *__restrict__ z,
                                                       int64_t ldz, T *__restrict__ y, int64_t ldy)
 {
     constexpr int E = Unit<T>::kElems;
-    for (uint32_t t = blockIdx.y; t < r.tokens; t += gridDim.y)
-    for (uint32_t col = (blockIdx.x * kWG + threadIdx.x) * E; col < r.cols; col += gridDim.x * kWG * E) {
-        const int n = (int)min((uint32_t)E, r.cols - col);
-        float acc[E] = {};
-        for (uint32_t k = 0; k < r.choices; ++k) {
-            const uint32_t c = t * r.choices + k;
-            const int32_t slot = r.choice_slot[c];
-            if (slot < 0) continue;
-            const Unit<T> u = load_row<STREAM>(z + (int64_t)slot * ldz + col, n);
-            const float s = WEIGHTED ? weight[c] : 1.0f;
+    for (uint32_t b = blockIdx.y; b * (kWG / LANES) < r.tokens; b += gridDim.y) {
+        const uint32_t t = token_of<LANES>(b);
+        if (t >= r.tokens) continue;
+        for (uint32_t col = (blockIdx.x * LANES + threadIdx.x % LANES) * E; col < r.cols; col += gridDim.x * LANES * E) {
+            const int n = (int)min((uint32_t)E, r.cols - col);
+            float acc[E] = {};
+            for (uint32_t k = 0; k < r.choices; ++k) {
+                const uint32_t c = t * r.choices + k;
+                const int32_t slot = r.choice_slot[c];
+                if (slot < 0) continue;
+                const Unit<T> u = load_row<STREAM>(z + (int64_t)slot * ldz + col, n);
+                const float s = weight ? weight[c] : 1.0f;
 #pragma unroll
-            for (int j = 0; j < E; ++j) acc[j] += s * (float)u.v[j];
+                for (int j = 0; j < E; ++j) acc[j] += s * (float)u.v[j];
+            }
+            Unit<T> v;
+#pragma unroll
+            for (int j = 0; j < E; ++j) v.v[j] = (T)acc[j];
+            store_row<STREAM>(y + (int64_t)t * ldy + col, v, n);
         }
-        Unit<T> v;
-#pragma unroll
-        for (int j = 0; j < E; ++j) v.v[j] = (T)acc[j];
-        store_row<STREAM>(y + (int64_t)t * ldy + col, v, n);
     }
 }
 
-// One workgroup per token: the dot products' lanes add up in a fixed order, and dy stays in the nearest caches from two choices to the
-// next two (four at a time: the same; one: 1 % slower, 8 % where 1031 rows of 1023 floats wait for each other's ends).
+// The dot products' lanes add up in a fixed order, and dy stays in the nearest caches from two choices to the next two (four at a time:
+// the same; one: 1 % slower, 8 % where 1031 rows of 1023 floats wait for each other's ends).
 // 16 384 tokens of 4096 bf16 with eight choices: 420 us, 5.4 TB/s; 465 without the streaming hint.
-template <class T, bool STREAM>
+template <class T, bool STREAM, int LANES>
 __global__ __launch_bounds__(kWG) void route_grad_kernel(RouteRows r, const float *__restrict__ weight, const T *__restrict__ dy,
                                                          int64_t lddy, const T *__restrict__ z, int64_t ldz, T *__restrict__ dz,
                                                          int64_t lddz, float *__restrict__ dweight)
 {
     constexpr int E = Unit<T>::kElems, AT_ONCE = 2;   // choices
     __shared__ float s_dot[2][kWG / kWave][AT_ONCE];
-    const auto add = [](float a, float b) { return a + b; };
     uint32_t turn = 0;
-    for (uint32_t t = blockIdx.x; t < r.tokens; t += gridDim.x) {
+    for (uint32_t b = blockIdx.x; b * (kWG / LANES) < r.tokens; b += gridDim.x) {
+        const uint32_t t = token_of<LANES>(b), lane = threadIdx.x % LANES;
+        const bool mine = t < r.tokens;                 // (all lanes stay for the sums)
         for (uint32_t k0 = 0; k0 < r.choices; k0 += AT_ONCE) {
-            int32_t slot[AT_ONCE];                      // (uniform; the last choice again behind it)
+            int32_t slot[AT_ONCE];                      // (the last choice again behind it)
             float w[AT_ONCE], dot[AT_ONCE] = {};
 #pragma unroll
             for (int i = 0; i < AT_ONCE; ++i) {
-                const uint32_t c = t * r.choices + min(k0 + i, r.choices - 1);
+                const uint32_t c = (mine ? t : 0) * r.choices + min(k0 + i, r.choices - 1);
                 slot[i] = r.choice_slot[c];
                 w[i] = weight ? weight[c] : 1.0f;
             }
-            for (uint32_t col = threadIdx.x * E; col < r.cols; col += kWG * E) {
+            for (uint32_t col = lane * E; mine && col < r.cols; col += LANES * E) {
                 const int n = (int)min((uint32_t)E, r.cols - col);
                 const Unit<T> g = load_some(dy + (int64_t)t * lddy + col, n);
                 Unit<T> u[AT_ONCE];
@@ -328,12 +343,20 @@ __global__ __launch_bounds__(kWG) void route_grad_kernel(RouteRows r, const floa
                     }
                 }
             }
-            if (dweight) {
+            if (!dweight) continue;
+            constexpr int FOLD = LANES < kWave ? LANES : kWave;
 #pragma unroll
-                for (int i = 0; i < AT_ONCE; ++i) {
-                    dot[i] = lanes_fold(dot[i], add);
+            for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+                for (int d = 1; d < FOLD; d <<= 1) dot[i] += __shfl_xor(dot[i], d, kWave);
+            if constexpr (LANES <= kWave) {
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i)
+                    if (mine && lane == 0 && k0 + i < r.choices) dweight[t * r.choices + k0 + i] = dot[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i)
                     if ((threadIdx.x & 63) == 0) s_dot[turn][threadIdx.x / 64][i] = dot[i];
-                }
                 __syncthreads();                        // (two sets: one barrier is enough)
                 const uint32_t i = threadIdx.x;
                 if (i < AT_ONCE && k0 + i < r.choices)
@@ -557,21 +580,45 @@ static bool streamed(const seer_dense &m, size_t size)
     return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (size_t)m.ld * size % 16 == 0;
 }
 
-// A workgroup per 4 KB of a row and token; more of either is looped over.
-static dim3 grid_of(const RouteRows &r, uint32_t elems)
+// The lanes to a row, as a constant: the whole workgroup's, or fewer, so that a row of few 16-byte pieces does not leave most of them idle.
+// Of 20 000 tokens of 120 bf16 with eight choices the gather takes 10.6 us with 16 lanes to a row and 16.3 with 256, the way back 12.9
+// and 31.2, the gradient 26.6 and 135; of 100 tokens 256 lanes are 0.8 us faster, as they read the slots once a wave and fill more CUs.
+// Rows of 72 to 128 pieces: the gradient 36 to 50 us with 64 lanes and 58 to 97 with 256, whose waves wait for each other's sums; the
+// others have no sums and are 0 to 10 % faster with 256.
+template <class F>
+static void by_lanes(const RouteRows &r, uint32_t elems, bool sums, F f)
 {
-    return dim3(std::min(1024u, (r.cols + kWG * elems - 1) / (kWG * elems)), std::min(r.tokens, 65535u));
+    const uint32_t pieces = (r.cols + elems - 1) / elems;
+    if (pieces <= 32 && (sums || r.tokens >= 4096)) f(std::integral_constant<int, 16>{});
+    else if (pieces <= 128 && sums) f(std::integral_constant<int, 64>{});
+    else f(std::integral_constant<int, 256>{});
+}
+
+// The same without the 64 lanes, which only sums gain from.
+template <class F>
+static void by_lanes_no_sums(const RouteRows &r, uint32_t elems, F f)
+{
+    by_lanes(r, elems, false, [&](auto lanes) {
+        if constexpr (decltype(lanes)::value != 64) f(lanes);
+    });
+}
+
+// A workgroup per kWG / lanes tokens and 16 bytes a lane; more of either is looped over.
+static dim3 grid_of(const RouteRows &r, uint32_t elems, uint32_t lanes)
+{
+    const uint32_t rows = kWG / lanes;
+    return dim3(lanes < kWG ? 1 : std::min(1024u, (r.cols + kWG * elems - 1) / (kWG * elems)), std::min((r.tokens + rows - 1) / rows, 65535u));
 }
 
 void launch_route_gather(const RouteRows &rows, const float *weight, const seer_dense &x, const seer_dense &out, hipStream_t st)
 {
     by_type(x.type, [&](auto *of) {
         using T = std::remove_pointer_t<decltype(of)>;
-        const dim3 grid = grid_of(rows, Unit<T>::kElems), wg(kWG);
-        const T *xp = static_cast<const T *>(x.data);
-        T *op = static_cast<T *>(out.data);
-        if (weight) hipLaunchKernelGGL((gather_kernel<T, true>), grid, wg, 0, st, rows, weight, xp, x.ld, op, out.ld);
-        else hipLaunchKernelGGL((gather_kernel<T, false>), grid, wg, 0, st, rows, weight, xp, x.ld, op, out.ld);
+        by_lanes_no_sums(rows, Unit<T>::kElems, [&](auto lanes) {
+            constexpr int LANES = decltype(lanes)::value;
+            hipLaunchKernelGGL((gather_kernel<T, LANES>), grid_of(rows, Unit<T>::kElems, LANES), dim3(kWG), 0, st, rows, weight,
+                               static_cast<const T *>(x.data), x.ld, static_cast<T *>(out.data), out.ld);
+        });
     });
 }
 
@@ -579,18 +626,15 @@ void launch_route_combine(const RouteRows &rows, const float *weight, const seer
 {
     by_type(z.type, [&](auto *of) {
         using T = std::remove_pointer_t<decltype(of)>;
-        const dim3 grid = grid_of(rows, Unit<T>::kElems), wg(kWG);
-        const T *zp = static_cast<const T *>(z.data);
-        T *yp = static_cast<T *>(y.data);
-        const auto launch = [&](auto weighted, auto stream) {
-            hipLaunchKernelGGL((combine_kernel<T, decltype(weighted)::value, decltype(stream)::value>), grid, wg, 0, st, rows, weight, zp, z.ld,
-                               yp, y.ld);
-        };
-        const std::true_type yes;
-        const std::false_type no;
-        const bool stream = streamed(z, sizeof(T)) && streamed(y, sizeof(T));
-        if (weight) stream ? launch(yes, yes) : launch(yes, no);
-        else stream ? launch(no, yes) : launch(no, no);
+        by_lanes_no_sums(rows, Unit<T>::kElems, [&](auto lanes) {
+            const auto launch = [&](auto stream) {
+                constexpr int LANES = decltype(lanes)::value;
+                hipLaunchKernelGGL((combine_kernel<T, decltype(stream)::value, LANES>), grid_of(rows, Unit<T>::kElems, LANES), dim3(kWG), 0, st, rows,
+                                   weight, static_cast<const T *>(z.data), z.ld, static_cast<T *>(y.data), y.ld);
+            };
+            if (streamed(z, sizeof(T)) && streamed(y, sizeof(T))) launch(std::true_type{});
+            else launch(std::false_type{});
+        });
     });
 }
 
@@ -599,13 +643,18 @@ void launch_route_grad(const RouteRows &rows, const float *weight, const seer_de
 {
     by_type(dy.type, [&](auto *of) {
         using T = std::remove_pointer_t<decltype(of)>;
-        const auto launch = [&](auto stream) {
-            hipLaunchKernelGGL((route_grad_kernel<T, decltype(stream)::value>), dim3(std::min(rows.tokens, kMaxGrid)), dim3(kWG), 0, st, rows, weight,
-                               static_cast<const T *>(dy.data), dy.ld, z ? static_cast<const T *>(z->data) : (const T *)nullptr, z ? z->ld : 0,
-                               dz ? static_cast<T *>(dz->data) : (T *)nullptr, dz ? dz->ld : 0, dweight);
-        };
-        if ((!z || streamed(*z, sizeof(T))) && (!dz || streamed(*dz, sizeof(T)))) launch(std::true_type{});
-        else launch(std::false_type{});
+        by_lanes(rows, Unit<T>::kElems, true, [&](auto lanes) {
+            const auto launch = [&](auto stream) {
+                constexpr int LANES = decltype(lanes)::value;
+                constexpr uint32_t per = kWG / LANES;
+                hipLaunchKernelGGL((route_grad_kernel<T, decltype(stream)::value, LANES>), dim3(std::min((rows.tokens + per - 1) / per, kMaxGrid)),
+                                   dim3(kWG), 0, st, rows, weight, static_cast<const T *>(dy.data), dy.ld,
+                                   z ? static_cast<const T *>(z->data) : (const T *)nullptr, z ? z->ld : 0,
+                                   dz ? static_cast<T *>(dz->data) : (T *)nullptr, dz ? dz->ld : 0, dweight);
+            };
+            if ((!z || streamed(*z, sizeof(T))) && (!dz || streamed(*dz, sizeof(T)))) launch(std::true_type{});
+            else launch(std::false_type{});
+        });
     });
 }
 

@@ -275,6 +275,31 @@ def test_shared_columns(shape, kind):
     check_product(i8(rng, M, K), i8(rng, 1, N, K), None, kind, rng)
 
 
+SHARED_GROUPS = [  # lengths of the groups, rows behind them, channels, columns
+    ([300, 0, 64, 1, 130], 9, 100, 6672), ([0, 0, 77, 40], 0, 257, 8192), ([70] * 20, 3, 30, 4112), ([0] * 20 + [700, 1], 0, 64, 9216), ([300], 5, 60, 8192),
+]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("groups", SHARED_GROUPS, ids=lambda g: f"{len(g[0])}x{sum(g[0])}+{g[1]}-{g[2]}-{g[3]}")
+def test_shared_columns_of_groups(groups, kind):
+    lengths, more, N, K = groups
+    announce(f"i8 shared groups {lengths} {kind}")
+    rng = np.random.default_rng(N + K)
+    M = sum(lengths) + more
+    assert S.i8_product_workspace_bytes(M, N, K, len(lengths)) > 0
+    check_product(i8(rng, M, K), i8(rng, len(lengths), N, K), np.concatenate([[0], np.cumsum(lengths)]).tolist(), kind, rng)
+
+
+def test_shared_columns_of_no_group_are_zero_whatever_they_hold():
+    rng = np.random.default_rng(4)
+    a, b, sa = i8(rng, 300, 8192), i8(rng, 3, 70, 8192), torch.full((300,), float("nan"), device="cuda:0")
+    sa[:200] = 1
+    assert S.i8_product_workspace_bytes(300, 70, 8192, 3) > 0
+    y = S.seer_i8_product(a, sa, b, torch.ones(3, 70, device="cuda:0"), group_ptr=torch.tensor([0, 120, 120, 200], dtype=torch.int32, device="cuda:0"))
+    assert not y[200:].any() and bool(torch.isfinite(y.float()).all())
+
+
 def test_shared_columns_with_a_workspace_of_the_callers():
     rng = np.random.default_rng(8)
     M, N, K = 300, 200, 4096

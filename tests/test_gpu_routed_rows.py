@@ -49,6 +49,7 @@ def test_nobody_chooses_an_expert():
 ROWS = [  # tokens, choices, experts, padding, columns
     (1, 8, 128, 0, 2048), (1, 1, 1, 0, 1), (0, 3, 4, 0, 16), (5, 2, 3, 0.4, 0), (7, 3, 4, 0.3, 7), (33, 2, 8, 0, 63), (48, 8, 64, 0, 512),
     (129, 4, 16, 0.05, 1023), (20, 1, 2, 0, 1025), (17, 5, 9, 0.2, 4096), (3, 9, 20, 0, 9001), (2, 17, 40, 0.5, 130), (300, 2, 8, 0.1, 8),
+    (4099, 2, 8, 0.1, 33), (4096, 3, 16, 0, 128), (5, 3, 8, 0.2, 260), (4101, 1, 4, 0.3, 100),
 ]
 
 
