@@ -387,6 +387,56 @@ static PyObject *m_product(PyObject *self, PyObject *const *v, Py_ssize_t n)
                     P(void *, stream)));
 }
 
+/* One tensor of a list of gradients. */
+static int gradient(PyObject *t, uint64_t *at, uint64_t *n, int *type)
+{
+    const int there = truth(t, s_is_cuda, 0), whole = there < 0 ? -1 : truth(t, s_is_contiguous, 1);
+    if (whole < 0) return -1;
+    if (!there || !whole) return refuse(PyExc_ValueError, "gradients and outputs", "are to be contiguous and on the GPU");
+    if ((*type = type_of(t, "a gradient")) < 0) return -1;
+    return address_of(t, at) || taken(PyObject_CallMethodNoArgs(t, s_numel), as_size, n) ? -1 : 0;
+}
+
+/* (list of gradients, list of outputs or None, address of the seer_grad array to fill, its length) */
+static PyObject *m_grads(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    uint64_t list, count;
+    if (given(n, 4) || as_size(a[2], &list) || as_size(a[3], &count)) return NULL;
+    const int apart = a[1] != Py_None;
+    if (!PyList_Check(a[0]) || (apart && !PyList_Check(a[1]))) {
+        PyErr_SetString(PyExc_TypeError, "lists are wanted");
+        return NULL;
+    }
+    seer_grad *const out = P(seer_grad *, list);
+    for (uint64_t i = 0; i < count; ++i) {
+        if ((uint64_t)PyList_GET_SIZE(a[0]) != count || (apart && (uint64_t)PyList_GET_SIZE(a[1]) != count)) {
+            PyErr_SetString(PyExc_ValueError, "as many outputs as gradients are wanted");
+            return NULL;
+        }
+        uint64_t at, to, elems, room;
+        int type, as;
+        PyObject *g = PyList_GET_ITEM(a[0], (Py_ssize_t)i), *o = apart ? PyList_GET_ITEM(a[1], (Py_ssize_t)i) : g;
+        Py_INCREF(g);
+        Py_INCREF(o);
+        int rc = gradient(g, &at, &elems, &type);
+        if (!rc && apart) rc = gradient(o, &to, &room, &as);
+        else to = at, room = elems, as = type;
+        if (!rc && (as != type || room != elems)) rc = refuse(PyExc_ValueError, "an output", "is to have its gradient's type and size");
+        if (!rc && type > SEER_F16) {
+            PyErr_Format(PyExc_TypeError, "a gradient is %S", types[type]);
+            rc = -1;
+        }
+        Py_DECREF(g);
+        Py_DECREF(o);
+        if (rc) return NULL;
+        out[i].grad = P(const void *, at);
+        out[i].out = P(void *, to);
+        out[i].n = (int64_t)elems;
+        out[i].type = type;
+    }
+    Py_RETURN_NONE;
+}
+
 /* (address of the seer_grad array, count, max_norm or None, norm, workspace, stream) */
 static PyObject *m_clip(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
@@ -440,6 +490,7 @@ static PyMethodDef methods[] = {
     {"quantize", (PyCFunction)(void (*)(void))m_quantize, METH_FASTCALL, "quantize(routing, x, q, scale, stream) -> status"},
     {"product", (PyCFunction)(void (*)(void))m_product, METH_FASTCALL,
      "product(a, a_scale, b, b_scale, group_ptr, out, workspace, stream) -> status"},
+    {"grads", (PyCFunction)(void (*)(void))m_grads, METH_FASTCALL, "grads(gradients, outputs or None, list address, count)"},
     {"clip", (PyCFunction)(void (*)(void))m_clip, METH_FASTCALL, "clip(list address, count, max_norm, norm, workspace, stream) -> status"},
     {NULL, NULL, 0, NULL}};
 

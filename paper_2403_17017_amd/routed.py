@@ -261,22 +261,13 @@ class GradTensors:
     (else it is clipped in place).  Keeps the tensors; made once for gradients that stay where they are."""
 
     def __init__(self, grads, outs=None):
-        _ready()
-        ids = _types
+        m = _ready()
         self.grads, self.outs = list(grads), list(outs) if outs is not None else None
-        to = self.outs if self.outs is not None else self.grads
-        if len(to) != len(self.grads):
-            raise ValueError("as many outputs as gradients are wanted")
         self.count = len(self.grads)
+        if self.outs is not None and len(self.outs) != self.count:
+            raise ValueError("as many outputs as gradients are wanted")
         self.c = (seer_grad * max(self.count, 1))()
-        for i, (g, o) in enumerate(zip(self.grads, to)):
-            if not g.is_cuda or not o.is_cuda or not g.is_contiguous() or not o.is_contiguous():
-                raise ValueError("gradients and outputs are to be contiguous and on the GPU")
-            if g.dtype != o.dtype or g.numel() != o.numel():
-                raise ValueError("an output is to have its gradient's type and size")
-            if ids.get(g.dtype, 9) > 2:
-                raise TypeError(f"a gradient is {g.dtype}")
-            self.c[i] = seer_grad(g.data_ptr(), o.data_ptr(), g.numel(), ids[g.dtype])
+        m.grads(self.grads, self.outs, C.addressof(self.c), self.count)
 
 
 def _grad_call(what, tensors, max_norm, norm, workspace, stream):
