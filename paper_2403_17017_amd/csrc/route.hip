@@ -267,8 +267,9 @@ __global__ __launch_bounds__(kWG) void gather_kernel(RouteRows r, const float *_
     }
 }
 
-// 32 768 tokens of 4096 bf16 from four experts each: 225 us, 6.0 TB/s; 253 without the streaming hint on rows that are used once.
-template <class T, bool STREAM, int LANES>
+// AT_ONCE choices are fetched together.
+// 32 768 tokens of 4096 bf16 from four experts each: 224 us, 6.0 TB/s; 253 without the streaming hint on rows that are used once.
+template <class T, bool STREAM, int LANES, int AT_ONCE>
 __global__ __launch_bounds__(kWG) void combine_kernel(RouteRows r, const float *__restrict__ weight, const T *__restrict__ z,
                                                       int64_t ldz, T *__restrict__ y, int64_t ldy)
 {
@@ -279,14 +280,25 @@ __global__ __launch_bounds__(kWG) void combine_kernel(RouteRows r, const float *
         for (uint32_t col = (blockIdx.x * LANES + threadIdx.x % LANES) * E; col < r.cols; col += gridDim.x * LANES * E) {
             const int n = (int)min((uint32_t)E, r.cols - col);
             float acc[E] = {};
-            for (uint32_t k = 0; k < r.choices; ++k) {
-                const uint32_t c = t * r.choices + k;
-                const int32_t slot = r.choice_slot[c];
-                if (slot < 0) continue;
-                const Unit<T> u = load_row<STREAM>(z + (int64_t)slot * ldz + col, n);
-                const float s = weight ? weight[c] : 1.0f;
+            for (uint32_t k0 = 0; k0 < r.choices; k0 += AT_ONCE) {
+                int32_t slot[AT_ONCE];
+                float s[AT_ONCE];
+                Unit<T> u[AT_ONCE];
 #pragma unroll
-                for (int j = 0; j < E; ++j) acc[j] += s * (float)u.v[j];
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    const uint32_t c = t * r.choices + min(k0 + i, r.choices - 1);
+                    slot[i] = r.choice_slot[c];
+                    s[i] = weight ? weight[c] : 1.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i)
+                    if (slot[i] >= 0 && k0 + i < r.choices) u[i] = load_row<STREAM>(z + (int64_t)slot[i] * ldz + col, n);
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i)
+                    if (slot[i] >= 0 && k0 + i < r.choices) {
+#pragma unroll
+                        for (int j = 0; j < E; ++j) acc[j] += s[i] * (float)u[i].v[j];
+                    }
             }
             Unit<T> v;
 #pragma unroll
@@ -622,18 +634,27 @@ void launch_route_gather(const RouteRows &rows, const float *weight, const seer_
     });
 }
 
+// Four choices at once for short rows (20 000 tokens of 120 bf16, eight choices: 9.3 us; one: 12.9), two for others (9295 x 5 x 576 bf16
+// 15.0 and 16.2, 4000 x 4 x 1040 9.1 and 10.1), one where the rows do not fit the last-level cache, whose pages are then read in longer
+// runs (32 768 x 4 x 4096: 224 us; two 227, four 228).
 void launch_route_combine(const RouteRows &rows, const float *weight, const seer_dense &z, const seer_dense &y, hipStream_t st)
 {
     by_type(z.type, [&](auto *of) {
         using T = std::remove_pointer_t<decltype(of)>;
         by_lanes_no_sums(rows, Unit<T>::kElems, [&](auto lanes) {
-            const auto launch = [&](auto stream) {
+            const auto launch = [&](auto stream, auto at_once) {
                 constexpr int LANES = decltype(lanes)::value;
-                hipLaunchKernelGGL((combine_kernel<T, decltype(stream)::value, LANES>), grid_of(rows, Unit<T>::kElems, LANES), dim3(kWG), 0, st, rows,
-                                   weight, static_cast<const T *>(z.data), z.ld, static_cast<T *>(y.data), y.ld);
+                hipLaunchKernelGGL((combine_kernel<T, decltype(stream)::value, LANES, decltype(at_once)::value>),
+                                   grid_of(rows, Unit<T>::kElems, LANES), dim3(kWG), 0, st, rows, weight, static_cast<const T *>(z.data), z.ld,
+                                   static_cast<T *>(y.data), y.ld);
             };
-            if (streamed(z, sizeof(T)) && streamed(y, sizeof(T))) launch(std::true_type{});
-            else launch(std::false_type{});
+            const auto launch_at = [&](auto at_once) {
+                if (streamed(z, sizeof(T)) && streamed(y, sizeof(T))) launch(std::true_type{}, at_once);
+                else launch(std::false_type{}, at_once);
+            };
+            if constexpr (decltype(lanes)::value < kWave) launch_at(std::integral_constant<int, 4>{});
+            else if ((uint64_t)z.rows * z.cols * sizeof(T) > 256u << 20) launch_at(std::integral_constant<int, 1>{});
+            else launch_at(std::integral_constant<int, 2>{});
         });
     });
 }
