@@ -578,7 +578,7 @@ int seer_route_grad(const seer_routing *r, const seer_dense *dy, const seer_dens
  * q[i][j] = x[i][j] / scale[i] (an fp32 division) to the nearest integer, ties to even, in -127 .. 127; 0 where scale is 0.
  * A row with an infinity or a NaN has it as its scale, whose products then are not finite, either; its
  * q are 0 (infinity) or unspecified.  q (SEER_I8) has x's rows and columns; where its rows are further apart, the columns up to the
- * next multiple of 16 (not beyond ld) are set to 0.  scale: DEVICE fp32 [rows]. */
+ * next multiple of 16 (not beyond ld) are set to 0, so memory reaches that far behind the last row, too.  scale: DEVICE fp32 [rows]. */
 int seer_i8_quantize(const seer_dense *x, const seer_dense *q, float *scale, void *stream);
 
 /* seer_route_gather without weights into 8-bit integers: q and scale have tokens * choices rows; rows of slots

@@ -1,7 +1,7 @@
 """MI355X-native hot path of the Seer SpMV case study: six CSR SpMV schedules, one over the ELL and one over the COO
 format (three of the eight with a preprocessing pass), the row-length feature reduction and the decision-tree
-kernel selector, all inside libseer.so (hand-written HIP for gfx950) behind a C ABI;
-this package is the thin Python binding over it."""
+kernel selector, and the operators of a routed (mixture of experts) layer, whose choices are such a matrix: all inside
+libseer.so (hand-written HIP for gfx950) behind a C ABI; this package is the thin Python binding over it."""
 from .binding import (  # noqa: F401
     COO_WM, CSR_A, CSR_BM, CSR_S, CSR_MP, CSR_TM, CSR_WM, CSR_WO, ELL_TM, ONE_CALL_KERNELS, F_ITERATIONS, FEATURE_NAMES, NUM_DIRECT_KERNELS, NUM_FEATURES,
     NUM_KERNELS, DeviceCSR, Model, Plan, SeerError, Tree,

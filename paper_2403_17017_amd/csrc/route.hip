@@ -593,7 +593,7 @@ static bool streamed(const seer_dense &m, size_t size)
 }
 
 // The lanes to a row, as a constant: the whole workgroup's, or fewer, so that a row of few 16-byte pieces does not leave most of them idle.
-// Of 20 000 tokens of 120 bf16 with eight choices the gather takes 10.6 us with 16 lanes to a row and 16.3 with 256, the way back 12.9
+// Of 20 000 tokens of 120 bf16 with eight choices the gather takes 10.6 us with 16 lanes to a row and 16.3 with 256, the way back 9.3
 // and 31.2, the gradient 26.6 and 135; of 100 tokens 256 lanes are 0.8 us faster, as they read the slots once a wave and fill more CUs.
 // Rows of 72 to 128 pieces: the gradient 36 to 50 us with 64 lanes and 58 to 97 with 256, whose waves wait for each other's sums; the
 // others have no sums and are 0 to 10 % faster with 256.

@@ -192,12 +192,21 @@ def _new_i8(rows, cols, like, stream):
     return _new((rows, (cols + 15) // 16 * 16), _torch.int8, like, stream)[:, :cols]
 
 
+def _room_for_pieces(q, cols):
+    """The columns up to the next multiple of 16 are written where rows are further apart: in the last row, too."""
+    rows, ld = q.shape[0], q.stride(0) if q.dim() == 2 else 0
+    if rows and ld > cols and q.storage_offset() + (rows - 1) * ld + min(ld, (cols + 15) // 16 * 16) > q.untyped_storage().nbytes():
+        raise ValueError("the memory of q ends within the last row's columns up to the next multiple of 16")
+
+
 def seer_i8_quantize(x, q=None, scale=None, stream=None):
     """(q, scale): the rows of x in 8-bit integers with a scale each."""
     m = _ready()
     rows, cols = _matrix_shape(x, "x")
     if q is None:
         q = _new_i8(rows, cols, x, stream)
+    elif cols % 16:
+        _room_for_pieces(q, cols)
     if scale is None:
         scale = _new((rows,), _torch.float32, x, stream)
     rc = m.quantize(None, x, q, scale, _stream_handle(stream))
@@ -210,8 +219,11 @@ def seer_route_gather_i8(r: Routing, x, q=None, scale=None, stream=None):
     """(q, scale): x [tokens, n] in 8-bit integers, brought into the experts' order."""
     m = _ready()
     rows = r.tokens * r.choices
+    cols = _matrix_shape(x, "x")[1]
     if q is None:
-        q = _new_i8(rows, _matrix_shape(x, "x")[1], x, stream)
+        q = _new_i8(rows, cols, x, stream)
+    elif cols % 16:
+        _room_for_pieces(q, cols)
     if scale is None:
         scale = _new((rows,), _torch.float32, x, stream)
     rc = m.quantize(r, x, q, scale, _stream_handle(stream))

@@ -215,6 +215,20 @@ def test_refusals():
         S.seer_i8_quantize(torch.zeros(4, 8, device="cuda:0"), q=a)
 
 
+def test_memory_that_ends_before_the_last_rows_zeros_is_refused():
+    x = torch.randn(3, 20, device="cuda:0")
+    whole = torch.full((2 * 40 + 32,), 55, dtype=torch.int8, device="cuda:0")
+    S.seer_i8_quantize(x, q=whole.as_strided((3, 20), (40, 1)))
+    assert not whole.as_strided((3, 12), (40, 1), 20).any() and bool((whole.as_strided((2, 8), (40, 1), 32) == 55).all())
+    short = torch.zeros(2 * 40 + 31, dtype=torch.int8, device="cuda:0").as_strided((3, 20), (40, 1))
+    with pytest.raises(ValueError):
+        S.seer_i8_quantize(x, q=short)
+    r = S.seer_route(torch.zeros(3, 1, dtype=torch.int64, device="cuda:0"), 1)
+    with pytest.raises(ValueError):
+        S.seer_route_gather_i8(r, x, q=short)
+    S.seer_i8_quantize(x, q=torch.zeros(2 * 25 + 25, dtype=torch.int8, device="cuda:0").as_strided((3, 20), (25, 1)))   # up to ld
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 def test_quantize_at_and_beside_the_middle(kind):
     """Quotients at n + 1/2 and a few units in the last place to either side: the division decides."""
