@@ -92,57 +92,81 @@ __global__ __launch_bounds__(kWG) void grad_square_kernel(GradList<kSquareList> 
     if (threadIdx.x == 0) part[blockIdx.x] = blockIdx.x < left ? part[blockIdx.x] + all : all;
 }
 
-__device__ __forceinline__ float norm_of(const double *part, uint32_t parts, double *s_sum)
-{
-    double v[kGradParts / kWG], sum = 0;
+// The partial sums, as each lane of a workgroup adds them up; fetched before, folded when the rest of a kernel's loads are on their way.
+struct Partial {
+    double v[kGradParts / kWG];
+    __device__ __forceinline__ void fetch(const double *part, uint32_t parts)
+    {
 #pragma unroll
-    for (uint32_t i = 0; i < kGradParts / kWG; ++i) v[i] = i * kWG + threadIdx.x < parts ? part[i * kWG + threadIdx.x] : 0.0;
+        for (uint32_t i = 0; i < kGradParts / kWG; ++i) v[i] = i * kWG + threadIdx.x < parts ? part[i * kWG + threadIdx.x] : 0.0;
+    }
+    __device__ __forceinline__ float norm(double *s_sum) const
+    {
+        double sum = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < kGradParts / kWG; ++i) sum += v[i];
-    return (float)sqrt(workgroup_sum(sum, s_sum));
-}
+        for (uint32_t i = 0; i < kGradParts / kWG; ++i) sum += v[i];
+        return (float)sqrt(workgroup_sum(sum, s_sum));
+    }
+};
 
 __global__ __launch_bounds__(kWG) void grad_norm_kernel(const double *__restrict__ part, uint32_t parts, float *__restrict__ norm)
 {
     __shared__ double s_sum[kWG / kWave];
-    const float n = norm_of(part, parts, s_sum);
+    Partial p;
+    p.fetch(part, parts);
+    const float n = p.norm(s_sum);
     if (threadIdx.x == 0) norm[0] = n;
 }
 
 // Every workgroup folds the partial sums for itself (16 KB at most, from L2): quicker than a launch of one workgroup between
-// the two passes.
+// the two passes.  Its first chunk is fetched meanwhile
+// (61 tensors of 24 MB, both passes: 18.0 us, 19.3 without).
 template <class T>
 __global__ __launch_bounds__(kWG) void grad_scale_kernel(GradList<kScaleList> l, OutList<kScaleList> o, const double *__restrict__ part,
                                                          uint32_t parts, float max_norm, float *__restrict__ norm)
 {
     constexpr int E = Unit<T>::kElems;
+    constexpr uint32_t kWhole = kGradChunk * E;
     __shared__ double s_sum[kWG / kWave];
-    const float n = norm_of(part, parts, s_sum);
+    const uint32_t chunks = l.end[l.count - 1];
+    Unit<T> u[kGradUnits];
+    const auto fetch = [&](const Chunk &k) {
+        const T *g = static_cast<const T *>(l.grad[k.i]) + k.begin + threadIdx.x * E;
+        if (k.have == kWhole) {
+#pragma unroll
+            for (uint32_t h = 0; h < kGradUnits; ++h) u[h] = stream_unit(g + h * kWG * E);
+        }
+    };
+    Partial p;
+    p.fetch(part, parts);
+    Chunk k = chunk_of<E>(l, blockIdx.x, true);         // (there are no more workgroups than chunks)
+    fetch(k);
+    const float n = p.norm(s_sum);
     if (blockIdx.x == 0 && threadIdx.x == 0) norm[0] = n;
     float by = max_norm / (n + 1e-6f);
     if (by >= 1.0f) by = 1.0f;
-    const auto scaled = [by](Unit<T> u) {
+    const auto scaled = [by](Unit<T> v) {
 #pragma unroll
-        for (int j = 0; j < E; ++j) u.v[j] = (T)(by * (float)u.v[j]);
-        return u;
+        for (int j = 0; j < E; ++j) v.v[j] = (T)(by * (float)v.v[j]);
+        return v;
     };
-    for (uint32_t c = blockIdx.x; c < l.end[l.count - 1]; c += gridDim.x) {
-        const Chunk k = chunk_of<E>(l, c, true);
-        if (by == 1.0f && l.grad[k.i] == o.out[k.i]) continue;          // nothing changes
-        const T *g = static_cast<const T *>(l.grad[k.i]) + k.begin + threadIdx.x * E;
+    for (uint32_t c = blockIdx.x;;) {
         T *out = static_cast<T *>(o.out[k.i]) + k.begin + threadIdx.x * E;
-        if (k.have == kGradChunk * E) {
-            Unit<T> u[kGradUnits];
-#pragma unroll
-            for (uint32_t h = 0; h < kGradUnits; ++h) u[h] = stream_unit(g + h * kWG * E);
+        if (by == 1.0f && l.grad[k.i] == o.out[k.i]) {
+            // nothing changes
+        } else if (k.have == kWhole) {
 #pragma unroll
             for (uint32_t h = 0; h < kGradUnits; ++h) stream_unit(out + h * kWG * E, scaled(u[h]));
         } else {
+            const T *g = static_cast<const T *>(l.grad[k.i]) + k.begin + threadIdx.x * E;
             for (uint32_t at = threadIdx.x * E; at < k.have; at += kWG * E, g += kWG * E, out += kWG * E) {
                 const int have = (int)min((uint32_t)E, k.have - at);
                 store_some(out, scaled(load_some(g, have)), have);
             }
         }
+        if ((c += gridDim.x) >= chunks) return;
+        k = chunk_of<E>(l, c, true);
+        if (by != 1.0f || l.grad[k.i] != o.out[k.i]) fetch(k);
     }
 }
 
