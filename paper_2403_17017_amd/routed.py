@@ -113,11 +113,15 @@ class Routing:
         """(a routing, a workspace for seer_route or None), in one piece of memory."""
         self, count = cls.__new__(cls), tokens * choices
         self.experts, self.tokens, self.choices = experts, tokens, choices
-        words = workspace_bytes // 4
-        workspace, self.expert_ptr, self.slot_choice, slots = _new((words + experts + 1 + 2 * count,), _torch.int32, like, stream).split(
-            (words, experts + 1, count, count))
+        words, sizes = workspace_bytes // 4, (experts + 1, count, count)
+        memory, workspace = _new((words + experts + 1 + 2 * count,), _torch.int32, like, stream), None
+        if words:
+            workspace, self.expert_ptr, self.slot_choice, slots = memory.split_with_sizes((words, *sizes))
+            workspace = workspace.view(_torch.uint8)
+        else:
+            self.expert_ptr, self.slot_choice, slots = memory.split_with_sizes(sizes)
         self.choice_slot = slots.view(tokens, choices)
-        return self, workspace.view(_torch.uint8) if words else None
+        return self, workspace
 
 
 def route_workspace_bytes(tokens: int, choices: int, experts: int) -> int:
