@@ -145,7 +145,7 @@ __device__ __forceinline__ void store_1(const I8Args &a, uint32_t row, uint32_t 
 //
 // 64 tokens x 64 channels, 128 columns at a time through LDS, four waves of 32 x 32 each.  16 bytes of
 // a row at a time, from any address; the end of a row byte by byte, and zeros behind it.  Nothing is under way while
-// it multiplies: 3001 x 5001 x 4112 in 230 us (540 TOP/s; 71 in tiles).  For rows that are not whole pieces of 16 bytes.
+// it multiplies: 3001 x 5001 x 4112 in 230 us (540 TOP/s; 71 in tiles).  For rows that do not lie at multiples of 16 bytes.
 constexpr uint32_t kAnyTokens = 64, kAnyChannels = 64, kAnyCols = 128, kAnyPitch = kAnyCols + 16;
 
 __device__ __forceinline__ v4i32 load_16(const int8_t *p, int n)
@@ -157,6 +157,17 @@ __device__ __forceinline__ v4i32 load_16(const int8_t *p, int n)
     v4i32 v = {0, 0, 0, 0};
     for (int j = 0; j < 16; ++j)
         if (j < n) v[j / 4] |= (int)(uint8_t)p[j] << (j % 4 * 8);
+    return v;
+}
+
+// The first n bytes, and zeros behind them.
+__device__ __forceinline__ v4i32 first_bytes(v4i32 v, int n)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int keep = min(max(n - 4 * j, 0), 4);
+        v[j] = keep ? v[j] & (int)(~0u >> (32 - 8 * keep)) : 0;
+    }
     return v;
 }
 
@@ -294,10 +305,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void i8_tile_kernel(I8Args a, Shared
     if (t.group < a.groups) {
         const uint32_t rows = t.end - t.begin, chans = min(kTileChannels, a.channels - n0);
         const uint32_t lda = (uint32_t)a.lda, ldb = (uint32_t)a.ldb;
+        const uint32_t readable = (a.columns + 15) & ~15u;      // (rows lie at multiples of 16: the last piece is theirs to its end)
         const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(a.a + (int64_t)t.begin * a.lda), 0,
-                                                          (int)((rows - 1) * lda + a.columns), 0x00020000);
+                                                          (int)((rows - 1) * lda + readable), 0x00020000);
         const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(a.b + ((int64_t)t.group * a.channels + n0) * a.ldb), 0,
-                                                          (int)((chans - 1) * ldb + a.columns), 0x00020000);
+                                                          (int)((chans - 1) * ldb + readable), 0x00020000);
         // a wave's load brings sixteen rows, four pieces each; rows that are not there are taken as the last one
         const auto order = [](uint32_t row) { return (row / 2 + row / 8) & 3; };
         const uint32_t piece = ((lane & 3) ^ order(lane / 4)) * 16;
@@ -349,12 +361,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void i8_tile_kernel(I8Args a, Shared
                 __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
         };
-        // zeros for the tokens' pieces behind the last column
+        // zeros for the tokens' columns behind the last one
         const uint32_t whole = a.columns / kTileCols;
         const auto clear_end = [&](int8_t *lds) {
             step_barrier<0>();
-            for (uint32_t i = threadIdx.x; i < TOKENS * 4; i += Shape::kThreads)
-                if (whole * kTileCols + ((i & 3) ^ order((i / 4) & 15)) * 16 >= a.columns) *reinterpret_cast<v4i32 *>(lds + i * 16) = v4i32{0, 0, 0, 0};
+            for (uint32_t i = threadIdx.x; i < TOKENS * 4; i += Shape::kThreads) {
+                v4i32 *const at = reinterpret_cast<v4i32 *>(lds + i * 16);
+                const int n = (int)a.columns - (int)(whole * kTileCols + ((i & 3) ^ order((i / 4) & 15)) * 16);
+                if (n < 16) *at = first_bytes(*at, n);
+            }
             step_barrier<0>();
         };
 #pragma unroll
@@ -497,11 +512,12 @@ __device__ __forceinline__ void few_sums(const int8_t *const (&pb)[CI], const in
     }
     for (; k < k_end; k += 64) {
         const bool in = k + q < k_end;
+        const int have = (int)k_end - (int)(k + q);     // columns of the piece (b's others meet zeros)
         v4i32 fb[CI], fa[TJ];
 #pragma unroll
         for (int i = 0; i < CI; ++i) fb[i] = in ? *reinterpret_cast<const v4i32 *>(pb[i] + k) : v4i32{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) fa[j] = in ? *reinterpret_cast<const v4i32 *>(pa[j] + k) : v4i32{0, 0, 0, 0};
+        for (int j = 0; j < TJ; ++j) fa[j] = in ? first_bytes(*reinterpret_cast<const v4i32 *>(pa[j] + k), have) : v4i32{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < CI; ++i)
 #pragma unroll
@@ -571,12 +587,14 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8Args a, uint32_t s
 
 // ------------------------------------------------------------------ launches
 
-// Whole pieces of 16 bytes at multiples of 16: what the kernels for tiles and for few rows load.
+// Rows at multiples of 16 bytes: what the kernels for tiles and for few rows load in pieces of 16.  The last piece of a row may
+// end before its 16 bytes do; it is loaded whole all the same (an aligned piece of which a byte is there is in memory), and what
+// lies behind the last column of a is taken as zero.
 static bool in_pieces(const I8Args &a)
 {
     const auto whole = [](uintptr_t v) { return v % 16 == 0; };
     return whole(reinterpret_cast<uintptr_t>(a.a)) && whole(reinterpret_cast<uintptr_t>(a.b)) && whole((uintptr_t)a.lda) &&
-           whole((uintptr_t)a.ldb) && a.columns % 16 == 0 && a.columns > 0;
+           whole((uintptr_t)a.ldb) && a.columns > 0;
 }
 
 // Workgroups for the tiles that there may be.
@@ -689,7 +707,7 @@ size_t i8_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t columns, ui
     a.channels = channels;
     a.columns = columns;
     a.groups = groups;
-    if (rows == 0 || channels == 0 || columns % 16 != 0) return 0;
+    if (rows == 0 || channels == 0) return 0;
     static const int32_t some = 0;                  // one group may come with its group_ptr or without
     double least;
     uint32_t shares = groups == 1 ? column_shares(a, &least) : 1;

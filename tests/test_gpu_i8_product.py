@@ -274,6 +274,25 @@ def test_many_groups(groups, columns):
         check_product(i8(rng, rows, columns), i8(rng, groups, N, columns), np.concatenate([[0], np.cumsum(lengths)]).tolist(), "f16", rng)
 
 
+PARTLY = [  # rows, channels, columns, how far the rows lie apart: rows at multiples of 16 that end within 16 bytes
+    (1, 17, 1, 16), (3, 40, 15, 16), (5, 64, 17, 32), (1, 300, 4111, 4112), (40, 130, 1001, 1008), (70, 300, 63, 64), (130, 257, 65, 80),
+    (500, 513, 259, 272), (700, 1025, 1023, 1040), (1000, 2049, 130, 144), (300, 200, 8191, 8192), (97, 16, 3089, 3104),
+]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("shape", PARTLY, ids=str)
+def test_rows_that_end_within_a_piece(shape, kind):
+    """What lies between the rows' ends and the next multiple of 16 is anything, and has no part in the sums."""
+    announce(f"i8 partly {shape} {kind}")
+    M, N, K, ld = shape
+    rng = np.random.default_rng(M + K)
+    check_product(spread(i8(rng, M, K), ld, 99), spread(i8(rng, N, K), ld, -77)[None], None, kind, rng)
+    lengths = rng.multinomial(M, [0.5, 0.1, 0.4])
+    b = spread(i8(rng, 3 * N, K), ld, 55).unflatten(0, (3, N))
+    check_product(spread(i8(rng, M, K), ld, 99), b, np.concatenate([[0], np.cumsum(lengths)]).tolist(), kind, rng)
+
+
 SHARED = [  # rows, channels, columns: one product whose columns are shared out between workgroups
     (97, 16, 3088), (100, 300, 4112), (129, 257, 8192), (500, 130, 4112), (1000, 500, 6160), (300, 1001, 5136), (3000, 129, 8208),
 ]
