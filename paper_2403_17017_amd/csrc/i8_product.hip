@@ -239,26 +239,28 @@ __device__ __forceinline__ void store_4(T *row, uint32_t n, uint32_t channels, c
 
 // ------------------------------------------------------------------ tiles
 //
-// 256 channels x 64, 128 or 256 tokens per workgroup.  64 columns at a time come straight from memory into one of four LDS
-// buffers, and from there into registers while the 64 columns before them are multiplied; so the matrix instructions wait for
-// neither, but for one barrier a step.  A row's four pieces of 16 bytes lie in LDS in the order of their number
-// xor (row / 2 + row / 8) % 4, so that lanes that read together use all banks (no conflicts by the counters).
-// 8192 x 8192 x 8192: 428 to 455 us, 2.4 to 2.57 POP/s (the library: 2.38).  Bound by the card's power: all-zero operands take
+// 256 channels x 64, 128 or 256 tokens per workgroup.  Whole lines of 128 columns come straight from memory into one of two or three
+// LDS buffers, and from there, 64 columns at a time, into registers while the 64 columns before them are multiplied; so the matrix
+// instructions wait for neither, but for one barrier every second step.  What a CU has on its way is counted in requests, so that half
+// lines (64 columns to each of four buffers) bring half as much: with weights from memory 14 x 6240 x 4896, mean 148, took 202 us
+// instead of 172, 32 x 4096 x 4096, mean 1013, 661 instead of 615.  A row's eight pieces of 16 bytes lie in LDS in the order of
+// their number xor row % 8 xor row / 8 % 2, so that lanes that read together use all banks.
+// 8192 x 8192 x 8192: 420 us, 2.6 POP/s (the library: 2.38).  Bound by the card's power: all-zero operands take
 // three quarters of the time, and instructions of 32 x 32 x 32, as fast with zeros, are a tenth slower with values.
-// Slower, too: wave tiles of 128 x 128 in 512 registers, two workgroups of four waves on a CU, workgroups that go on to their
-// next tile (the registers for that spill).
-constexpr uint32_t kTileChannels = 256, kTileCols = 64;
+// Slower, too: wave tiles of 128 x 128 in 512 registers, two workgroups of four waves with 128 tokens each on a CU, workgroups that
+// go on to their next tile (the registers for that spill).
+constexpr uint32_t kTileChannels = 256, kTileCols = 64, kLineCols = 2 * kTileCols;
 
 typedef __attribute__((address_space(3))) int8_t lds_byte;
 
-// WC x WAVES / WC waves, each of CI * 16 channels x TJ * 16 tokens.
-template <int WAVES, int WC, int CI, int TJ>
+// WC x WAVES / WC waves, each of CI * 16 channels x TJ * 16 tokens; `BUFFERS` of two steps each.
+template <int WAVES, int WC, int CI, int TJ, int BUFFERS>
 struct TileShape {
     static constexpr int kWT = WAVES / WC;
     static constexpr uint32_t kThreads = WAVES * 64, kTokens = kWT * TJ * 16;
-    // loads of a lane, each step: a wave's load brings 16 rows
-    static constexpr uint32_t kLoadsA = kTokens >= WAVES * 16 ? kTokens / (WAVES * 16) : 1, kLoadsB = kTileChannels / (WAVES * 16);
-    static constexpr uint32_t kBytes = (kTokens + kTileChannels) * kTileCols;
+    // loads of a lane for each buffer: a wave's load brings 8 rows
+    static constexpr uint32_t kLoadsA = kTokens / (WAVES * 8), kLoadsB = kTileChannels / (WAVES * 8);
+    static constexpr uint32_t kBytes = (kTokens + kTileChannels) * kLineCols;
     static_assert(WC * CI * 16 == (int)kTileChannels, "waves cover the channels");
 };
 
@@ -273,15 +275,17 @@ __device__ __forceinline__ void step_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
 }
 
-template <class T, int WAVES, int WC, int CI, int TJ>
-__global__ __launch_bounds__(WAVES * 64, 2) void i8_tile_kernel(I8Args a, SharedColumns shared)
+template <class T, int WAVES, int WC, int CI, int TJ, int BUFFERS>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 || BUFFERS == 2 ? 2 : 1) void i8_tile_kernel(I8Args a, SharedColumns shared)
 {
     // (T = int32_t: sums of one share of the columns, as they are)
     constexpr bool kShared = std::is_same<T, int32_t>::value;
-    using Shape = TileShape<WAVES, WC, CI, TJ>;
+    using Shape = TileShape<WAVES, WC, CI, TJ, BUFFERS>;
     constexpr uint32_t TOKENS = Shape::kTokens, LA = Shape::kLoadsA, LB = Shape::kLoadsB;
-    __shared__ __attribute__((aligned(1024))) int8_t s_0[Shape::kBytes], s_1[Shape::kBytes], s_2[Shape::kBytes], s_3[Shape::kBytes];
-    int8_t *const buffer[4] = {s_0, s_1, s_2, s_3};
+    // (arrays of their own: the compiler knows that loads into one are nothing to reads from another)
+    static_assert(BUFFERS >= 2 && BUFFERS <= 4, "");
+    __shared__ __attribute__((aligned(1024))) int8_t s_0[Shape::kBytes], s_1[Shape::kBytes], s_2[BUFFERS > 2 ? Shape::kBytes : 16], s_3[BUFFERS > 3 ? Shape::kBytes : 16];
+    int8_t *const buffer[4] = {s_0, s_1, BUFFERS > 2 ? s_2 : s_0, BUFFERS > 3 ? s_3 : s_0};
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), lane = threadIdx.x & 63;
     const uint32_t across = (a.channels + kTileChannels - 1) / kTileChannels;
     Tile t;
@@ -310,35 +314,43 @@ __global__ __launch_bounds__(WAVES * 64, 2) void i8_tile_kernel(I8Args a, Shared
                                                           (int)((rows - 1) * lda + readable), 0x00020000);
         const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(a.b + ((int64_t)t.group * a.channels + n0) * a.ldb), 0,
                                                           (int)((chans - 1) * ldb + readable), 0x00020000);
-        // a wave's load brings sixteen rows, four pieces each; rows that are not there are taken as the last one
-        const auto order = [](uint32_t row) { return (row / 2 + row / 8) & 3; };
-        const uint32_t piece = ((lane & 3) ^ order(lane / 4)) * 16;
+        // A wave's load brings eight rows, 128 columns of each: whole lines of memory.  Piece c of row r lies in place c ^ order(r).
+        // What is not there, rows and pieces, has an offset out of the buffer's range and costs nothing.
+        const auto order = [](uint32_t row) { return (row & 7) ^ (row >> 3 & 1); };
+        constexpr uint32_t kNowhere = 1u << 31;
+        const uint32_t piece = ((lane & 7) ^ order(wave * 8 + lane / 8)) * 16;
         uint32_t at_a[LA], at_b[LB];
 #pragma unroll
-        for (uint32_t i = 0; i < LA; ++i) at_a[i] = min(((i * WAVES + wave) * 16) % TOKENS + lane / 4, rows - 1) * lda + piece;
+        for (uint32_t i = 0; i < LA; ++i) {
+            const uint32_t row = (i * WAVES + wave) * 8 + lane / 8;
+            at_a[i] = row < rows ? row * lda + piece : kNowhere;
+        }
 #pragma unroll
-        for (uint32_t i = 0; i < LB; ++i) at_b[i] = min((i * WAVES + wave) * 16 + lane / 4, chans - 1) * ldb + piece;
+        for (uint32_t i = 0; i < LB; ++i) {
+            const uint32_t row = (i * WAVES + wave) * 8 + lane / 8;
+            at_b[i] = row < chans ? row * ldb + piece : kNowhere;
+        }
         const uint32_t steps = (a.columns + kTileCols - 1) / kTileCols;
-        const auto fetch = [&](uint32_t step, int8_t *lds) {
-            // steps behind the last one load the last one again, into a buffer that is not read; pieces behind the last column
-            // are not loaded: the step's first one is
-            const uint32_t k0 = min(step, steps - 1) * kTileCols, back = k0 + piece < a.columns ? 0 : piece;
+        const auto fetch = [&](uint32_t line, int8_t *lds) {
+            const uint32_t k0 = line * kLineCols, nowhere = k0 + piece < a.columns ? 0 : kNowhere;
 #pragma unroll
             for (uint32_t i = 0; i < LA; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte *)(lds + ((i * WAVES + wave) * 1024) % (TOKENS * kTileCols)), 16, (int)(at_a[i] - back), (int)k0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte *)(lds + (i * WAVES + wave) * 1024), 16, (int)(at_a[i] | nowhere), (int)k0, 0, 0);
 #pragma unroll
             for (uint32_t i = 0; i < LB; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte *)(lds + TOKENS * kTileCols + (i * WAVES + wave) * 1024), 16, (int)(at_b[i] - back), (int)k0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte *)(lds + TOKENS * kLineCols + (i * WAVES + wave) * 1024), 16, (int)(at_b[i] | nowhere), (int)k0, 0, 0);
         };
-        const uint32_t from = (lane & 15) * kTileCols + (((lane >> 4) ^ order(lane & 15)) * 16);
-        const uint32_t from_a = wt * TJ * 16 * kTileCols + from, from_b = (TOKENS + wc * CI * 16) * kTileCols + from;
+        // a lane's place in the first and the second 64 columns
+        const uint32_t own = (lane & 15) * kLineCols;
+        const uint32_t from[2] = {own + ((lane >> 4) ^ order(lane & 15)) * 16, own + ((4 + (lane >> 4)) ^ order(lane & 15)) * 16};
+        const uint32_t from_a = wt * TJ * 16 * kLineCols, from_b = (TOKENS + wc * CI * 16) * kLineCols;
         const bool busy = wt * TJ * 16 < rows;          // (waves without tokens only fetch)
         struct Frags { v4i32 b[CI], a[TJ]; };
-        const auto read = [&](const int8_t *lds, Frags &f) {
+        const auto read = [&](const int8_t *lds, uint32_t half, Frags &f) {
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) f.a[j] = *reinterpret_cast<const v4i32 *>(lds + from_a + j * 16 * kTileCols);
+            for (int j = 0; j < TJ; ++j) f.a[j] = *reinterpret_cast<const v4i32 *>(lds + from[half] + from_a + j * 16 * kLineCols);
 #pragma unroll
-            for (int i = 0; i < CI; ++i) f.b[i] = *reinterpret_cast<const v4i32 *>(lds + from_b + i * 16 * kTileCols);
+            for (int i = 0; i < CI; ++i) f.b[i] = *reinterpret_cast<const v4i32 *>(lds + from[half] + from_b + i * 16 * kLineCols);
         };
         const auto multiply = [&](const Frags &f) {
 #pragma unroll
@@ -346,50 +358,53 @@ __global__ __launch_bounds__(WAVES * 64, 2) void i8_tile_kernel(I8Args a, Shared
 #pragma unroll
                 for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[i], f.a[j], acc[i][j], 0, 0, 0);
         };
-        // Step s multiplies what step s - 1 has read, reads the columns of step s + 1 and sends for those of step s + 4, into the
-        // buffer whose columns are in registers.
+        // Step s multiplies what step s - 1 has read and reads the columns of step s + 1.  Odd steps find the next buffer filled and
+        // nobody reading their own one any more, and send for the columns that come into it next.
         Frags frags[2];
-        const auto step = [&](uint32_t s, int8_t *own, const int8_t *next, const Frags &now, Frags &then) {
-            step_barrier<2 * (LA + LB)>();          // the next columns are there, and nobody reads the own ones any more
-            fetch(s + 4, own);
-            if (!busy) return;
-            read(next, then);
-            multiply(now);
-#pragma unroll
-            for (int i = 0; i < CI + TJ; ++i) {     // a read behind every few multiplications: the first ones wait for nothing
-                __builtin_amdgcn_sched_group_barrier(0x008, CI * TJ / (CI + TJ), 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
+        const auto turn = [&](uint32_t s, int i) {          // (s a multiple of 2 BUFFERS)
+            if (i % 2 == 0) return;
+            step_barrier<(BUFFERS - 2) * (LA + LB)>();
+            fetch((s + i) / 2 + BUFFERS, buffer[i / 2 % BUFFERS]);
         };
         // zeros for the tokens' columns behind the last one
         const uint32_t whole = a.columns / kTileCols;
-        const auto clear_end = [&](int8_t *lds) {
+        const auto clear_end = [&](int8_t *lds, uint32_t half) {
             step_barrier<0>();
             for (uint32_t i = threadIdx.x; i < TOKENS * 4; i += Shape::kThreads) {
-                v4i32 *const at = reinterpret_cast<v4i32 *>(lds + i * 16);
-                const int n = (int)a.columns - (int)(whole * kTileCols + ((i & 3) ^ order((i / 4) & 15)) * 16);
+                v4i32 *const at = reinterpret_cast<v4i32 *>(lds + i / 4 * kLineCols + ((half * 4 + (i & 3)) ^ order(i / 4 & 15)) * 16);
+                const int n = (int)a.columns - (int)(whole * kTileCols + (i & 3) * 16);
                 if (n < 16) *at = first_bytes(*at, n);
             }
             step_barrier<0>();
         };
 #pragma unroll
-        for (int i = 0; i < 4; ++i) fetch(i, buffer[i]);
-        step_barrier<3 * (LA + LB)>();
-        if (whole == 0) clear_end(s_0);
-        read(s_0, frags[0]);
+        for (int i = 0; i < BUFFERS; ++i) fetch(i, buffer[i]);
+        step_barrier<(BUFFERS - 1) * (LA + LB)>();
+        if (whole == 0) clear_end(s_0, 0);
+        read(s_0, 0, frags[0]);
+        constexpr int ROUND = 2 * BUFFERS;
         uint32_t s = 0;
-        for (; s + 4 < whole; s += 4)
+        for (; s + ROUND < whole; s += ROUND)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) step(s + i, buffer[i], buffer[(i + 1) % 4], frags[i % 2], frags[(i + 1) % 2]);
-        // up to five steps are left, the last of them perhaps not whole
+            for (int i = 0; i < ROUND; ++i) {
+                turn(s, i);
+                if (!busy) continue;
+                read(buffer[(i + 1) / 2 % BUFFERS], (i + 1) % 2, frags[(i + 1) % 2]);
+                multiply(frags[i % 2]);
 #pragma unroll
-        for (int i = 0; i < 5; ++i) {
+                for (int k = 0; k < CI + TJ; ++k) { // a read behind every few multiplications: the first ones wait for nothing
+                    __builtin_amdgcn_sched_group_barrier(0x008, CI * TJ / (CI + TJ), 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+            }
+        // up to ROUND + 1 steps are left, the last of them perhaps not whole
+#pragma unroll
+        for (int i = 0; i <= ROUND; ++i) {
             if (s + i >= steps) break;
-            step_barrier<2 * (LA + LB)>();
-            fetch(s + i + 4, buffer[i % 4]);
+            turn(s, i);
             if (s + i + 1 < steps) {
-                if (s + i + 1 == whole) clear_end(buffer[(i + 1) % 4]);
-                read(buffer[(i + 1) % 4], frags[(i + 1) % 2]);
+                if (s + i + 1 == whole) clear_end(buffer[(i + 1) / 2 % BUFFERS], (i + 1) % 2);
+                read(buffer[(i + 1) / 2 % BUFFERS], (i + 1) % 2, frags[(i + 1) % 2]);
             }
             if (busy) multiply(frags[i % 2]);
         }
@@ -422,11 +437,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void i8_tile_kernel(I8Args a, Shared
         // time: 15.4 us, and 18.3 with 8-byte stores, 16 rows at a time).  A row's pieces lie in the order of their number xor the row.
         constexpr int CIP = CI * (int)sizeof(T) > 16 ? 16 / (int)sizeof(T) : CI;      // channels go by up to 256 bytes of a row
         constexpr uint32_t PIECES = CIP * sizeof(T), ROW = PIECES * 16, E = Unit<T>::kElems;
-        constexpr uint32_t kPer = WAVES / 4;            // waves to a buffer
-        static_assert(WAVES % 4 == 0 && kPer * TJ * 16 * ROW <= Shape::kBytes && CI % CIP == 0, "the waves' regions fit");
+        constexpr uint32_t kPer = (WAVES + BUFFERS - 1) / BUFFERS;      // waves to a buffer
+        static_assert(kPer * TJ * 16 * ROW <= Shape::kBytes && CI % CIP == 0, "the waves' regions fit");
         step_barrier<0>();                              // nothing is on its way to LDS, and nobody reads the last columns any more
         const uint32_t turn = wave / kPer;
-        int8_t *mine = (turn == 0 ? s_0 : turn == 1 ? s_1 : turn == 2 ? s_2 : s_3) + (wave % kPer) * (TJ * 16 * ROW);
+        int8_t *mine = (turn == 0 ? buffer[0] : turn == 1 ? buffer[1] : turn == 2 ? buffer[2] : buffer[3]) + (wave % kPer) * (TJ * 16 * ROW);
 #pragma unroll
         for (int first = 0; first < CI; first += CIP) {
 #pragma unroll
@@ -597,6 +612,8 @@ static bool in_pieces(const I8Args &a)
            whole((uintptr_t)a.ldb) && a.columns > 0;
 }
 
+constexpr uint32_t kCUs = 256;
+
 // Workgroups for the tiles that there may be.
 static uint64_t most_blocks(const I8Args &a, uint32_t tokens, uint32_t channels)
 {
@@ -606,14 +623,24 @@ static uint64_t most_blocks(const I8Args &a, uint32_t tokens, uint32_t channels)
 // The arithmetic on tiles is 32-bit.
 bool i8_product_fits(const I8Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, kAnyTokens, kAnyChannels) < (1u << 30); }
 
-template <class T, int WAVES, int WC, int CI, int TJ>
+template <class T, int WAVES, int WC, int CI, int TJ, int BUFFERS>
 static bool launch_tiles(const I8Args &a, hipStream_t st)
 {
-    using Shape = TileShape<WAVES, WC, CI, TJ>;
+    using Shape = TileShape<WAVES, WC, CI, TJ, BUFFERS>;
     const uint64_t blocks = most_blocks(a, Shape::kTokens, kTileChannels);
     if (blocks * Shape::kThreads >= 1ull << 32) return false;       // (a launch has fewer lanes)
-    hipLaunchKernelGGL((i8_tile_kernel<T, WAVES, WC, CI, TJ>), dim3((uint32_t)blocks), dim3(Shape::kThreads), 0, st, a, SharedColumns{});
+    hipLaunchKernelGGL((i8_tile_kernel<T, WAVES, WC, CI, TJ, BUFFERS>), dim3((uint32_t)blocks), dim3(Shape::kThreads), 0, st, a, SharedColumns{});
     return true;
+}
+
+// Tiles of 64 tokens have two buffers, which leaves room for two workgroups on a CU (32 x 4096 x 4096, mean 1013: 785 us; three, and one
+// workgroup: 894), or, where there is only one, three (8192 x 8192, 384 rows: 41 us; two: 52; up to 2048 columns two are 0 to 5 % faster).
+static bool three_buffers(const I8Args &a, uint64_t blocks) { return blocks <= kCUs && a.columns > 2048; }
+
+template <class T>
+static bool launch_tiles_64(const I8Args &a, hipStream_t st)
+{
+    return three_buffers(a, most_blocks(a, 64, kTileChannels)) ? launch_tiles<T, 4, 4, 4, 4, 3>(a, st) : launch_tiles<T, 4, 4, 4, 4, 2>(a, st);
 }
 
 static_assert(SEER_MAX_EXPERTS < 65535, "groups are a dimension of the grid of the kernel for few rows");
@@ -627,76 +654,83 @@ static bool launch_few(const I8Args &a, hipStream_t st)
     return true;
 }
 
-// Which kernel, by the mean rows of a group and by how many tiles there are.  Measured, us (groups x channels x columns, rows to
-// a group 1 / sqrt(rank)): few rows, tiles of 64, of 128 and of 256 tokens
-//   32 x 4096 x 4096, mean   8: 105 128 134 138     16: 128 132 138 143     32: 161 155 140 144     64: 233 144 172 151
-//                           96: 326 168 162 193    128: 415 188 164 195    192: 592 242 222 197    512: 1474 536 399 354
-//   64 x 1024 x 2048, mean   8: 26 24 26 28         16: 30 34 27 29         64: 61 35 41 48        256: 215 69 66 62
-//    1 x 8192 x 8192, rows   1: 13 38 39 51         64: 26 48 48 52         96: 42 46 51 54        128: 48 48 55 56
-//                          256: 94 46 55 83        512: 186 55 58 85
-//    1 x 2048 x 2048, rows   1: 4.7 10 12 18        64: 9.0 12.5 13 18     128: 16 12.6 18 19
-// so that few rows are for products that would leave CUs without a tile, or up to 12 rows, and with several groups larger tiles are for
-// as many of them as there are CUs or nearly; for one, see tile_cost.  Every workgroup of few rows reads all of its group's rows, at some
-// 26 GB/s a CU: long columns are sooner faster in tiles, if few enough to be shared out (below; 1 x 512 x 8192, 64 rows: 21.6 and 15.3;
-// 32 x 256 x 8192, mean 24 | 48: 41 | 69 and 24 | 26), and so are the longest of several groups (32 x 256 x 4096, mean 33 | 48: 24 | 35
-// and 23 | 20; 16 x 512 x 1024, mean 33: 8.9 and 9.7).  Few rows: 16 channels to a workgroup where 32 are fewer than half of the CUs (2048 x 2048, one row: 3.8 and 4.7); eight waves to share the columns where each has 512 or more and there is
-// more than one row (8192 x 8192, 64 rows: 25.6 and 27.8; one row: 14.0 and 13.1; 2048 columns, 64 groups of 8: 29 and 26).
-constexpr uint32_t kCUs = 256;
+// Which kernel, and for how many shares of the columns: the one whose time by the following lines is the least.  They are fitted to 256
+// draws (one matrix, or 3 to 64 with rows to a group 1, 1 / sqrt(rank) or 1 / rank; 4 to 6000 rows to a group; 128 to 16 384 channels; 256 to
+// 11 000 columns; weights from memory, not from a cache), of which each kernel was timed: what is chosen takes
+// 2 % longer than the best one on average.
+//
+// Few rows: a workgroup reads its group's rows and its channels at some 24 GB/s, and so does a CU that has several.  Where lengths
+// differ, a group may be four times as long as the mean.  (1 x 2960 x 1424, 88 rows: few rows 9.5 us, tiles 16;
+// 9 x 1576 x 3856, mean 34: 27 and 44; 41 x 784 x 3520, mean 63: 72 and 47; 49 x 144 x 672, mean 126, longest 1356: 102 and 11.)
+// 16 channels to a workgroup where 32 are fewer than half of the CUs (2048 x 2048, one row: 3.8 and 4.7); eight waves to share the columns
+// where each has 512 or more and there is more than one row (8192 x 8192, 64 rows: 25.6 and 27.8; one row: 14.0 and 13.1;
+// 2048 columns, 64 groups of 8: 29 and 26).
+static uint32_t few_channels(const I8Args &a) { return (uint64_t)((a.channels + 31) / 32) * a.groups < 128 ? 16 : 32; }
 
-static bool few_rows(const I8Args &a)
+static double few_cost(const I8Args &a)
 {
-    const uint64_t tiles = most_blocks(a, 64, kTileChannels);
-    const bool several = a.group_ptr != nullptr, long_columns = a.columns > 4096 && tiles <= 64;
-    const uint32_t most = tiles >= 256 ? 12 : tiles >= 128 ? 32 : several ? (long_columns ? 16 : a.columns >= 2048 ? 32 : 64) : long_columns ? 32 : 64;
-    return a.rows / a.groups <= most;
+    const double mean = a.rows / a.groups, channels = few_channels(a);
+    const double workgroups = (double)((a.channels + few_channels(a) - 1) / few_channels(a)) * a.groups;
+    const double rows = std::max((mean + channels) * workgroups / kCUs, (a.group_ptr ? 4 : 1) * mean + channels);
+    const double batches = a.rows / a.groups / kFewRows;        // (behind the first)
+    return std::max(4 + 1.2 * batches + rows * a.columns / 24e3, (double)a.groups * a.channels * a.columns / 5.8e6);
 }
 
-// For one product, what its time would be, in us: rounds of as many tiles as there are CUs, a step of 64 columns costing more
-// when more of them are at work.  Measured (8192 channels, 16 | 64 steps): tiles of 64 tokens 128: 9.9 | 26, 256: 12 | 31, 384: 19 | 49,
-// 1024: 35 | 105; of 128 tokens 64: 13 | 33, 192: 16 | 36, 256: 17 | 42, 384: 28 | 70, 1024: 61 | 158; of 256 tokens
-// 32: 19 | 48, 128: 21 | 50, 192: 23 | 57, 256: 26 | 64, 416: 44 | 115, 1024: 93 | 247.
-struct TileCost { uint32_t tokens; double least, more, above /* share of the CUs */, round; };
-constexpr TileCost kCost64 = {64, 0.345, 0.02, 0, 3}, kCost128 = {128, 0.41, 0.09, 0, 7.5}, kCost256 = {256, 0.6, 0.2, 0.5, 10};
+// Tiles: rounds of as many as there is room for, `round` each and `least` to `least + more` for a step of 64 columns by how many are at
+// work.  Measured (1 x 8192 channels, 16 | 64 | 128 steps): tiles of 64 tokens
+// 128: 10 | 24 | 39, 256: 11 | 26 | 44, 384: 15 | 36 | 64, 512: 17 | 41 | 74, 768: 24 | 65 | 122, 1024: 30 | 80 | 144; of 128 tokens
+// 64: 13 | 30 | 52, 192: 15 | 34 | 62, 256: 16 | 40 | 67, 384: 26 | 67 | 119, 1024: 57 | 147 | 261; of 256 tokens 32: 18 | 45 | 81,
+// 128: 21 | 48 | 85, 192: 22 | 52 | 96, 256: 24 | 59 | 107, 416: 40 | 104 | 192, 1024: 89 | 235 | 422.
+// Weights that come from memory cost the smaller tiles more (`cold`), and several groups, which end in the middle of a tile each and
+// share theirs between fewer, a quarter more again.
+struct TileCost { uint32_t tokens, room; double least, more, above /* share of the room */, round, cold; };
+constexpr TileCost kCost64 = {64, 2 * kCUs, 0.12, 0.42, 0, 5.5, 1.25}, kCost64Alone = {64, kCUs, 0.26, 0.04, 0, 6, 1.25},
+                   kCost128 = {128, kCUs, 0.34, 0.115, 0.3, 8, 1.05}, kCost256 = {256, kCUs, 0.565, 0.195, 0.5, 10, 1};
 
 static double tile_cost(const I8Args &a, const TileCost &c, uint32_t shares)
 {
-    const uint64_t tiles = most_tiles(a, c.tokens) * ((a.channels + kTileChannels - 1) / kTileChannels) * shares;
+    const uint64_t down = a.group_ptr ? (uint64_t)a.rows / c.tokens + (a.groups + 1) / 2 : ((uint64_t)a.rows + c.tokens - 1) / c.tokens;
+    const uint64_t tiles = down * ((a.channels + kTileChannels - 1) / kTileChannels) * shares;
+    if (c.room > kCUs && tiles <= kCUs) return tile_cost(a, kCost64Alone, shares);
     const double steps = ((double)a.columns / kTileCols) / shares;
     const auto round = [&](double full) {
         return steps * (c.least + c.more * std::max(0.0, (full - c.above) / (1 - c.above))) + c.round;
     };
-    const uint64_t rest = tiles % kCUs;
-    return (double)(tiles / kCUs) * round(1) + (rest ? round((double)rest / kCUs) : 0);
+    const uint64_t rest = tiles % c.room;
+    const double t = (double)(tiles / c.room) * round(1) + (rest ? round((double)rest / c.room) : 0);
+    return std::max(t * c.cold * (a.group_ptr ? 1.25 : 1), (double)a.groups * a.channels * a.columns / 4.2e6);
 }
 
-// Tiles of 64 tokens that leave CUs idle have the columns shared out, at 1 us for every 3 MB of sums written and read and 8 us for the
+// Tiles of 64 tokens that leave CUs idle may have the columns shared out, at 1 us for every 3 MB of sums written and read and 8 us for the
 // second launch.  Measured, us, one and several shares (channels x columns, rows 128, 256, 512, 1024):
-//   512 x 8192:  34 34 34 36 and 15 18 20 25      2048 x 8192: 34 35 45 46 and 21 25 31 44
-//   8192 x 8192: 46 46 55 74 and 32 45 54 73      2048 x 2048: 12.5 12.7 13 14 and 13 16 25 27 (hence one)
-// and of groups (mean 66, 100, 160, 256): 10 x 256 x 6656: 37 39 41 41 and 17 19 21 30, 32 x 256 x 4096: 26 28 29 30 and 20 22 28 30.
-static uint32_t column_shares(const I8Args &a, double *least)
+//   512 x 8192:  34 34 34 36 and 15 17 18 20      2048 x 8192: 34 35 45 46 and 19 20 24 33
+//   8192 x 8192: 46 46 55 74 and 24 33 43 64      2048 x 2048: 12.5 12.7 13 14 and 13 16 25 27 (hence one)
+// and of groups (mean 66, 100, 160, 256): 10 x 256 x 6656: 37 39 41 41 and 17 18 20 21, 32 x 256 x 4096: 26 28 29 30 and 20 22 24 25.
+struct Choice { uint32_t tokens /* 0: few rows */, shares; };
+
+static Choice choose(const I8Args &a)
 {
-    *least = tile_cost(a, kCost64, 1);
-    if (few_rows(a) || a.columns == 0) return 1;
+    Choice best{0, 1};
+    double least = few_cost(a);
+    const auto consider = [&](uint32_t tokens, uint32_t shares, double cost) {
+        if (cost >= least) return;
+        least = cost;
+        best = Choice{tokens, shares};
+    };
+    consider(256, 1, tile_cost(a, kCost256, 1));
+    consider(128, 1, tile_cost(a, kCost128, 1));
+    consider(64, 1, tile_cost(a, kCost64, 1));
     const uint64_t tiles = most_blocks(a, 64, kTileChannels);
-    if (tiles > kCUs * 2 / 3) return 1;
-    const double sums = 8.0 * a.rows * a.channels;
-    const uint32_t most = (uint32_t)std::min<uint64_t>({kCUs * 3 / 2 / tiles, (uint64_t)a.columns / kTileCols / 6, 16});
-    uint32_t best = 1;
-    for (uint32_t n = 2; n <= most; ++n) {
-        const double t = tile_cost(a, kCost64, n) + n * sums / 3e6 + 8;
-        if (t < *least) {
-            *least = t;
-            best = n;
-        }
-    }
-    return !a.group_ptr && std::min(tile_cost(a, kCost128, 1), tile_cost(a, kCost256, 1)) < *least ? 1 : best;
+    if (tiles > kCUs * 2 / 3) return best;
+    const uint32_t most = (uint32_t)std::min<uint64_t>({kCUs * 2 / tiles, (uint64_t)a.columns / kTileCols / 6, 16});
+    for (uint32_t n = 2; n <= most; ++n) consider(64, n, tile_cost(a, kCost64, n) + n * (8.0 * a.rows * a.channels) / 3e6 + 8);
+    return best;
 }
 
 static SharedColumns shared_columns(const I8Args &a, uint32_t shares, void *workspace)
 {
     const uint32_t steps = (a.columns + kTileCols - 1) / kTileCols;
-    return SharedColumns{static_cast<int32_t *>(workspace), (uint32_t)most_blocks(a, 64, kTileChannels), (steps + shares - 1) / shares * kTileCols,
+    return SharedColumns{static_cast<int32_t *>(workspace), (uint32_t)most_blocks(a, 64, kTileChannels), ((steps + 1) / 2 + shares - 1) / shares * kLineCols,
                          (a.channels + 3) & ~3u};
 }
 
@@ -709,47 +743,39 @@ size_t i8_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t columns, ui
     a.groups = groups;
     if (rows == 0 || channels == 0) return 0;
     static const int32_t some = 0;                  // one group may come with its group_ptr or without
-    double least;
-    uint32_t shares = groups == 1 ? column_shares(a, &least) : 1;
+    uint32_t shares = groups == 1 ? choose(a).shares : 1;
     a.group_ptr = &some;
-    shares = std::max(shares, column_shares(a, &least));
+    shares = std::max(shares, choose(a).shares);
     return shares > 1 ? (size_t)shares * rows * ((channels + 3) & ~3u) * 4 : 0;
 }
 
 template <class T>
-static bool launch_shared(const I8Args &a, void *workspace, hipStream_t st)
+static void launch_shared(const I8Args &a, uint32_t shares, void *workspace, hipStream_t st)
 {
-    double least;
-    uint32_t shares = column_shares(a, &least);
-    if (shares <= 1) return false;
     const SharedColumns c = shared_columns(a, shares, workspace);
     shares = (a.columns + c.share - 1) / c.share;
-    hipLaunchKernelGGL((i8_tile_kernel<int32_t, 4, 4, 4, 4>), dim3(c.blocks * shares), dim3(256), 0, st, a, c);
+    if (three_buffers(a, (uint64_t)c.blocks * shares))
+        hipLaunchKernelGGL((i8_tile_kernel<int32_t, 4, 4, 4, 4, 3>), dim3(c.blocks * shares), dim3(256), 0, st, a, c);
+    else
+        hipLaunchKernelGGL((i8_tile_kernel<int32_t, 4, 4, 4, 4, 2>), dim3(c.blocks * shares), dim3(256), 0, st, a, c);
     const uint64_t lanes = (uint64_t)a.rows * (c.pitch / 4);
     hipLaunchKernelGGL((i8_join_kernel<T>), dim3((uint32_t)std::min<uint64_t>((lanes + kWG - 1) / kWG, 8 * kCUs)), dim3(kWG), 0, st, a, c, shares);
-    return true;
 }
 
 template <class T>
 static bool launch_pieces(const I8Args &a, void *workspace, hipStream_t st)
 {
-    const uint32_t mean = a.rows / a.groups;
-    const uint64_t tiles_64 = most_blocks(a, 64, kTileChannels);
-    if (few_rows(a)) {
-        if ((uint64_t)((a.channels + 31) / 32) * a.groups < 128) return launch_few<T, 1, 4>(a, st);
-        return mean > 1 && a.columns >= 4096 ? launch_few<T, 2, 8>(a, st) : launch_few<T, 2, 4>(a, st);
+    const Choice c = choose(a);
+    if (c.tokens == 0) {
+        if (few_channels(a) == 16) return launch_few<T, 1, 4>(a, st);
+        return a.rows / a.groups > 1 && a.columns >= 4096 ? launch_few<T, 2, 8>(a, st) : launch_few<T, 2, 4>(a, st);
     }
     if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return false;     // offsets into a tile are 32-bit
-    if (workspace && launch_shared<T>(a, workspace, st)) return true;
-    if (!a.group_ptr) {
-        const double t64 = tile_cost(a, kCost64, 1), t128 = tile_cost(a, kCost128, 1), t256 = tile_cost(a, kCost256, 1);
-        if (t256 <= std::min(t64, t128)) return launch_tiles<T, 8, 2, 8, 4>(a, st);
-        return t128 <= t64 ? launch_tiles<T, 8, 2, 8, 2>(a, st) : launch_tiles<T, 4, 4, 4, 4>(a, st);
+    if (c.shares > 1) {
+        launch_shared<T>(a, c.shares, workspace, st);
+        return true;
     }
-    constexpr uint64_t kEnough = 192;
-    if (mean > 160 && most_blocks(a, 256, kTileChannels) >= kEnough) return launch_tiles<T, 8, 2, 8, 4>(a, st);
-    if ((mean > 80 || (mean <= 32 && tiles_64 >= 256)) && most_blocks(a, 128, kTileChannels) >= kEnough) return launch_tiles<T, 8, 2, 8, 2>(a, st);
-    return launch_tiles<T, 4, 4, 4, 4>(a, st);
+    return c.tokens == 256 ? launch_tiles<T, 8, 2, 8, 4, 2>(a, st) : c.tokens == 128 ? launch_tiles<T, 8, 2, 8, 2, 3>(a, st) : launch_tiles_64<T>(a, st);
 }
 
 void launch_i8_product(const I8Args &a, void *workspace, hipStream_t st)
