@@ -274,6 +274,21 @@ def test_many_groups(groups, columns):
         check_product(i8(rng, rows, columns), i8(rng, groups, N, columns), np.concatenate([[0], np.cumsum(lengths)]).tolist(), "f16", rng)
 
 
+@pytest.mark.parametrize("steps", range(15))
+@pytest.mark.parametrize("size", [(300, 500), (424, 13960), (3000, 4100)], ids=str)
+def test_any_number_of_steps(size, steps):
+    """Columns around every multiple of 64 that a round of the tiles' buffers may end at."""
+    M, N = size
+    rng = np.random.default_rng(steps)
+    for K in (64 * steps + 16, 64 * steps + 48, 64 * steps + 64):
+        announce(f"i8 steps {size} {K}")
+        a, b = rng.integers(-127, 128, (M, K)).astype(np.int8), rng.integers(-127, 128, (N, K)).astype(np.int8)
+        ones = torch.ones(max(M, N), device="cuda:0")
+        got = S.seer_i8_product(torch.from_numpy(a).cuda(), ones[:M], torch.from_numpy(b).cuda()[None], ones[None, :N], dtype=torch.float32)
+        want = a.astype(np.float32) @ b.astype(np.float32).T         # exact: below 2^24
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
 PARTLY = [  # rows, channels, columns, how far the rows lie apart: rows at multiples of 16 that end within 16 bytes
     (1, 17, 1, 16), (3, 40, 15, 16), (5, 64, 17, 32), (1, 300, 4111, 4112), (40, 130, 1001, 1008), (70, 300, 63, 64), (130, 257, 65, 80),
     (500, 513, 259, 272), (700, 1025, 1023, 1040), (1000, 2049, 130, 144), (300, 200, 8191, 8192), (97, 16, 3089, 3104),
