@@ -133,93 +133,6 @@ static uint64_t most_tiles(const I8Args &a, uint32_t tokens)
     return a.group_ptr ? (uint64_t)a.rows / tokens + std::min(a.groups + 1, a.rows) : ((uint64_t)a.rows + tokens - 1) / tokens;
 }
 
-__device__ __forceinline__ void store_1(const I8Args &a, uint32_t row, uint32_t channel, float v)
-{
-    const int64_t at = (int64_t)row * a.ldo + channel;
-    if (a.type == SEER_F32) static_cast<float *>(a.out)[at] = v;
-    else if (a.type == SEER_BF16) static_cast<bf16_t *>(a.out)[at] = (bf16_t)v;
-    else static_cast<f16_t *>(a.out)[at] = (f16_t)v;
-}
-
-// ------------------------------------------------------------------ any size, any alignment
-//
-// 64 tokens x 64 channels, 128 columns at a time through LDS, four waves of 32 x 32 each.  16 bytes of
-// a row at a time, from any address; the end of a row byte by byte, and zeros behind it.  Nothing is under way while
-// it multiplies: 3001 x 5001 x 4112 in 230 us (540 TOP/s; 71 in tiles).  For rows that do not lie at multiples of 16 bytes.
-constexpr uint32_t kAnyTokens = 64, kAnyChannels = 64, kAnyCols = 128, kAnyPitch = kAnyCols + 16;
-
-__device__ __forceinline__ v4i32 load_16(const int8_t *p, int n)
-{
-    if (n >= 16) {
-        typedef int v4i_a1 __attribute__((ext_vector_type(4), aligned(1)));
-        return *reinterpret_cast<const v4i_a1 *>(p);
-    }
-    v4i32 v = {0, 0, 0, 0};
-    for (int j = 0; j < 16; ++j)
-        if (j < n) v[j / 4] |= (int)(uint8_t)p[j] << (j % 4 * 8);
-    return v;
-}
-
-// The first n bytes, and zeros behind them.
-__device__ __forceinline__ v4i32 first_bytes(v4i32 v, int n)
-{
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int keep = min(max(n - 4 * j, 0), 4);
-        v[j] = keep ? v[j] & (int)(~0u >> (32 - 8 * keep)) : 0;
-    }
-    return v;
-}
-
-__global__ __launch_bounds__(256) void i8_any_kernel(I8Args a, uint32_t blocks)
-{
-    __shared__ __attribute__((aligned(16))) int8_t s_a[kAnyTokens * kAnyPitch], s_b[kAnyChannels * kAnyPitch];
-    __shared__ TileSearch s_search;
-    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    for (uint32_t w = blockIdx.x; w < blocks; w += gridDim.x) {
-        Tile t;
-        if (!find_tile<4>(a, w, kAnyTokens, (a.channels + kAnyChannels - 1) / kAnyChannels, &s_search, &t)) continue;
-        const uint32_t n0 = t.column * kAnyChannels;
-        v4i32 acc[2][2] = {};
-        if (t.group < a.groups) {
-            const int8_t *b = a.b + (int64_t)t.group * a.channels * a.ldb;
-            for (uint32_t k0 = 0; k0 < a.columns; k0 += kAnyCols) {
-                for (uint32_t i = threadIdx.x; i < kAnyTokens * (kAnyCols / 16); i += 256) {
-                    const uint32_t row = i / (kAnyCols / 16), col = k0 + i % (kAnyCols / 16) * 16;
-                    const int left = (int)a.columns - (int)col;
-                    const v4i32 va = t.begin + row < t.end ? load_16(a.a + (int64_t)(t.begin + row) * a.lda + col, left) : v4i32{0, 0, 0, 0};
-                    *reinterpret_cast<v4i32 *>(s_a + row * kAnyPitch + (col - k0)) = va;
-                    const v4i32 vb = n0 + row < a.channels ? load_16(b + (int64_t)(n0 + row) * a.ldb + col, left) : v4i32{0, 0, 0, 0};
-                    *reinterpret_cast<v4i32 *>(s_b + row * kAnyPitch + (col - k0)) = vb;
-                }
-                __syncthreads();
-                for (uint32_t k = 0; k < kAnyCols; k += 64) {
-                    v4i32 fb[2], fa[2];
-                    for (int i = 0; i < 2; ++i) {
-                        fb[i] = *reinterpret_cast<const v4i32 *>(s_b + ((wave & 1) * 32 + i * 16 + (lane & 15)) * kAnyPitch + k + lane / 16 * 16);
-                        fa[i] = *reinterpret_cast<const v4i32 *>(s_a + ((wave >> 1) * 32 + i * 16 + (lane & 15)) * kAnyPitch + k + lane / 16 * 16);
-                    }
-                    for (int i = 0; i < 2; ++i)
-                        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[i], fa[j], acc[i][j], 0, 0, 0);
-                }
-                __syncthreads();
-            }
-        }
-        for (int j = 0; j < 2; ++j) {
-            const uint32_t row = t.begin + (wave >> 1) * 32 + j * 16 + (lane & 15);
-            if (row >= t.end) continue;
-            const float sa = t.group < a.groups ? a.a_scale[row] : 0.0f;
-            for (int i = 0; i < 2; ++i)
-                for (int v = 0; v < 4; ++v) {
-                    const uint32_t n = n0 + (wave & 1) * 32 + i * 16 + lane / 16 * 4 + v;
-                    if (n >= a.channels) continue;
-                    const float sb = t.group < a.groups ? a.b_scale[(int64_t)t.group * a.channels + n] : 0.0f;
-                    store_1(a, row, n, t.group < a.groups ? (float)acc[i][j][v] * (sa * sb) : 0.0f);
-                }
-        }
-    }
-}
-
 // Consecutive channels of one token, converted: 4 of them from channel n on, those below `channels`.
 template <class T>
 __device__ __forceinline__ void store_4(T *row, uint32_t n, uint32_t channels, const float (&v)[4])
@@ -234,6 +147,141 @@ __device__ __forceinline__ void store_4(T *row, uint32_t n, uint32_t channels, c
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (n + j < channels) row[n + j] = (T)v[j];
+    }
+}
+
+// ------------------------------------------------------------------ any size, any alignment
+//
+// For rows that do not lie at multiples of 16 bytes: 128 tokens x 128 channels, 128 columns at a time through registers and LDS, four
+// waves of 64 x 64 each.  16 bytes of a row at a time, from any address; nothing is read behind the end of a row but the rest of its last
+// word.  The next columns are fetched while these are multiplied: 3001 x 5001 x 4111 in 154 us, 800 TOP/s (66 in tiles, where rows lie
+// at 4112; 278 with 64 x 64, nothing under way and loads from odd addresses).
+constexpr uint32_t kAnyTokens = 128, kAnyChannels = 128, kAnyCols = 128, kAnyPitch = kAnyCols + 16;
+
+// The first n bytes, and zeros behind them.
+__device__ __forceinline__ v4i32 first_bytes(v4i32 v, int n)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int keep = min(max(n - 4 * j, 0), 4);
+        v[j] = keep ? v[j] & (int)(~0u >> (32 - 8 * keep)) : 0;
+    }
+    return v;
+}
+
+// 16 bytes from any address, of which n are there (at least 1), out of whole words: loads that are not at multiples of 4 take four times as long.
+// (A word of which a byte is there is in memory.)
+__device__ __forceinline__ v4i32 load_16(const int8_t *p, int n)
+{
+    typedef int words __attribute__((ext_vector_type(4), aligned(4)));
+    const uint32_t by = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
+    const int8_t *from = p - by;
+    int w[5];
+    if (n >= 16) {
+        const words v = *reinterpret_cast<const words *>(from);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = v[j];
+        w[4] = *reinterpret_cast<const int *>(from + (by ? 16 : 12));
+    } else {
+        const int last = ((int)by + n - 1) / 4;
+#pragma unroll
+        for (int j = 0; j < 5; ++j) w[j] = *reinterpret_cast<const int *>(from + 4 * min(j, last));
+    }
+    v4i32 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = (int)__builtin_amdgcn_alignbyte((uint32_t)w[j + 1], (uint32_t)w[j], by);
+    return n >= 16 ? v : first_bytes(v, n);
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void i8_any_kernel(I8Args a, uint32_t blocks)
+{
+    __shared__ __attribute__((aligned(16))) int8_t s_a[kAnyTokens * kAnyPitch], s_b[kAnyChannels * kAnyPitch];
+    __shared__ TileSearch s_search;
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+    for (uint32_t w = blockIdx.x; w < blocks; w += gridDim.x) {
+        Tile t;
+        if (!find_tile<4>(a, w, kAnyTokens, (a.channels + kAnyChannels - 1) / kAnyChannels, &s_search, &t)) continue;
+        const uint32_t n0 = t.column * kAnyChannels;
+        v4i32 acc[4][4] = {};
+        if (t.group < a.groups) {
+            const int8_t *b = a.b + (int64_t)t.group * a.channels * a.ldb;
+            constexpr uint32_t kPieces = kAnyCols / 16, kEach = kAnyTokens * kPieces / 256;
+            const uint32_t row = threadIdx.x / kPieces, col = threadIdx.x % kPieces * 16;     // and 256 / kPieces rows further on
+            v4i32 va[kEach], vb[kEach];
+            const int8_t *pa[kEach], *pb[kEach];                // (rows that are not there are taken as the last one: nobody stores them)
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i) {
+                const uint32_t at = row + i * (256 / kPieces);
+                pa[i] = a.a + (int64_t)min(t.begin + at, t.end - 1) * a.lda + col;
+                pb[i] = b + (int64_t)min(n0 + at, a.channels - 1) * a.ldb + col;
+            }
+            const auto fetch = [&](uint32_t k0) {
+                if (k0 + kAnyCols <= a.columns) {
+#pragma unroll
+                    for (uint32_t i = 0; i < kEach; ++i) {
+                        va[i] = load_16(pa[i] + k0, 16);
+                        vb[i] = load_16(pb[i] + k0, 16);
+                    }
+                } else if (k0 < a.columns) {
+                    // (pieces behind the end: the first one, and nothing of it)
+                    const int left = (int)a.columns - (int)(k0 + col), n = min(left > 0 ? left : (int)(a.columns - k0), 15);
+                    const uint32_t at = left > 0 ? k0 : k0 - col;
+#pragma unroll
+                    for (uint32_t i = 0; i < kEach; ++i) {
+                        va[i] = left >= 16 ? load_16(pa[i] + k0, 16) : first_bytes(load_16(pa[i] + at, n), left);
+                        vb[i] = left >= 16 ? load_16(pb[i] + k0, 16) : load_16(pb[i] + at, n);
+                    }
+                }
+            };
+            fetch(0);
+            for (uint32_t k0 = 0; k0 < a.columns; k0 += kAnyCols) {
+                __syncthreads();
+#pragma unroll
+                for (uint32_t i = 0; i < kEach; ++i) {
+                    const uint32_t at = (row + i * (256 / kPieces)) * kAnyPitch + col;
+                    *reinterpret_cast<v4i32 *>(s_a + at) = va[i];
+                    *reinterpret_cast<v4i32 *>(s_b + at) = vb[i];
+                }
+                __syncthreads();
+                fetch(k0 + kAnyCols);
+#pragma unroll
+                for (uint32_t k = 0; k < kAnyCols; k += 64) {
+                    v4i32 fb[4], fa[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        fb[i] = *reinterpret_cast<const v4i32 *>(s_b + ((wave & 1) * 64 + i * 16 + (lane & 15)) * kAnyPitch + k + lane / 16 * 16);
+                        fa[i] = *reinterpret_cast<const v4i32 *>(s_a + ((wave >> 1) * 64 + i * 16 + (lane & 15)) * kAnyPitch + k + lane / 16 * 16);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[i], fa[j], acc[i][j], 0, 0, 0);
+                }
+            }
+        }
+        // (every scale is fetched before the first store: a wait for a load is one for all stores before it, too)
+        const bool zero = t.group >= a.groups;
+        const float *sb = a.b_scale + (int64_t)(zero ? 0 : t.group) * a.channels;
+        const uint32_t row1 = t.begin + (wave >> 1) * 64 + (lane & 15), n1 = n0 + (wave & 1) * 64 + lane / 16 * 4;
+        float of_row[4], of_channel[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) of_row[j] = a.a_scale[min(row1 + j * 16, t.end - 1)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) of_channel[i][v] = sb[min(n1 + i * 16 + v, a.channels - 1)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t row = row1 + j * 16, n = n1 + i * 16;
+                if (row >= t.end || n >= a.channels) continue;
+                float v[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] = zero ? 0.0f : (float)acc[i][j][u] * (of_row[j] * of_channel[i][u]);
+                store_4(static_cast<T *>(a.out) + (int64_t)row * a.ldo, n, a.channels, v);
+            }
     }
 }
 
@@ -495,11 +543,19 @@ __global__ __launch_bounds__(kWG) void i8_join_kernel(I8Args a, SharedColumns sh
 // CI * 16 channels of one group per workgroup, whose waves each take a share of the columns; both operands come straight from memory, the
 // weights once per 64 rows, and the waves' sums meet in LDS.  Bound by the bytes of b: 8192 x 8192, one row, in 12.4 us
 // (5.4 TB/s), 64 groups of 2048 x 4096 with four rows each on average in 84 (6.3 TB/s).  Plain loads: an instruction takes half
-// of 16 lines, and with the streaming hint the other half comes from memory again (96 and 110 us).
+// of 16 lines, and with the streaming hint the other half comes from memory again (96 and 110 us).  Rows that do not lie at multiples of 16 bytes: 8192 x 8191, one row, 25 us (14 where they do).
 constexpr uint32_t kFewRows = 64;
 
-// 16 TJ rows from `at` on: the calling wave's columns [k_begin, k_end), U pieces of each row at a time.
-template <int CI, int TJ, int U>
+template <bool PIECES>
+__device__ __forceinline__ v4i32 load_piece(const int8_t *p)
+{
+    if constexpr (PIECES) return *reinterpret_cast<const v4i32 *>(p);
+    else return load_16(p, 16);
+}
+
+// 16 TJ rows from `at` on: the calling wave's columns [k_begin, k_end), U pieces of each row at a time.  PIECES: rows lie at multiples
+// of 16 bytes, and their last piece is read whole.
+template <bool PIECES, int CI, int TJ, int U>
 __device__ __forceinline__ void few_sums(const int8_t *const (&pb)[CI], const int8_t *const (&pa)[TJ], uint32_t k_begin, uint32_t k_end, uint32_t q,
                                          v4i32 (&acc)[CI][TJ])
 {
@@ -513,11 +569,11 @@ __device__ __forceinline__ void few_sums(const int8_t *const (&pb)[CI], const in
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < CI; ++i) fb[u][i] = *reinterpret_cast<const v4i32 *>(pb[i] + k + u * 64);
+            for (int i = 0; i < CI; ++i) fb[u][i] = load_piece<PIECES>(pb[i] + k + u * 64);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) fa[u][j] = *reinterpret_cast<const v4i32 *>(pa[j] + k + u * 64);
+            for (int j = 0; j < TJ; ++j) fa[u][j] = load_piece<PIECES>(pa[j] + k + u * 64);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -528,11 +584,12 @@ __device__ __forceinline__ void few_sums(const int8_t *const (&pb)[CI], const in
     for (; k < k_end; k += 64) {
         const bool in = k + q < k_end;
         const int have = (int)k_end - (int)(k + q);     // columns of the piece (b's others meet zeros)
+        const auto last = [&](const int8_t *p) { return PIECES ? *reinterpret_cast<const v4i32 *>(p) : load_16(p, have); };
         v4i32 fb[CI], fa[TJ];
 #pragma unroll
-        for (int i = 0; i < CI; ++i) fb[i] = in ? *reinterpret_cast<const v4i32 *>(pb[i] + k) : v4i32{0, 0, 0, 0};
+        for (int i = 0; i < CI; ++i) fb[i] = in ? last(pb[i] + k) : v4i32{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) fa[j] = in ? first_bytes(*reinterpret_cast<const v4i32 *>(pa[j] + k), have) : v4i32{0, 0, 0, 0};
+        for (int j = 0; j < TJ; ++j) fa[j] = in ? first_bytes(last(pa[j] + k), have) : v4i32{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < CI; ++i)
 #pragma unroll
@@ -540,7 +597,7 @@ __device__ __forceinline__ void few_sums(const int8_t *const (&pb)[CI], const in
     }
 }
 
-template <class T, int CI, int WAVES>
+template <class T, int CI, int WAVES, bool PIECES>
 __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8Args a, uint32_t share)
 {
     __shared__ __attribute__((aligned(16))) v4i32 s_acc[2][WAVES][CI][64];
@@ -568,7 +625,7 @@ __global__ __launch_bounds__(WAVES * 64) void i8_few_kernel(I8Args a, uint32_t s
 #pragma unroll
         for (int j = 0; j < TJ; ++j) pa[j] = a.a + (int64_t)min(at + j * 16 + (lane & 15), end - 1) * a.lda + q;
         v4i32 acc[CI][TJ];
-        few_sums<CI, TJ, decltype(pieces)::value>(pb, pa, k_begin, k_end, q, acc);
+        few_sums<PIECES, CI, TJ, decltype(pieces)::value>(pb, pa, k_begin, k_end, q, acc);
         // 16 rows at a time the waves' sums meet; wave i adds up and stores channels i * 16 ...
 #pragma unroll
         for (int j = 0; j < TJ; ++j) {
@@ -609,7 +666,7 @@ static bool in_pieces(const I8Args &a)
 {
     const auto whole = [](uintptr_t v) { return v % 16 == 0; };
     return whole(reinterpret_cast<uintptr_t>(a.a)) && whole(reinterpret_cast<uintptr_t>(a.b)) && whole((uintptr_t)a.lda) &&
-           whole((uintptr_t)a.ldb) && a.columns > 0;
+           whole((uintptr_t)a.ldb);
 }
 
 constexpr uint32_t kCUs = 256;
@@ -621,7 +678,7 @@ static uint64_t most_blocks(const I8Args &a, uint32_t tokens, uint32_t channels)
 }
 
 // The arithmetic on tiles is 32-bit.
-bool i8_product_fits(const I8Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, kAnyTokens, kAnyChannels) < (1u << 30); }
+bool i8_product_fits(const I8Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, 64, 64) < (1u << 30); }
 
 template <class T, int WAVES, int WC, int CI, int TJ, int BUFFERS>
 static bool launch_tiles(const I8Args &a, hipStream_t st)
@@ -644,13 +701,13 @@ static bool launch_tiles_64(const I8Args &a, hipStream_t st)
 }
 
 static_assert(SEER_MAX_EXPERTS < 65535, "groups are a dimension of the grid of the kernel for few rows");
-template <class T, int CI, int WAVES>
+template <class T, int CI, int WAVES, bool PIECES>
 static bool launch_few(const I8Args &a, hipStream_t st)
 {
     const uint32_t groups = a.groups + (a.group_ptr ? 1 : 0), share = ((a.columns + WAVES - 1) / WAVES + 63) & ~63u;
     const uint32_t across = (a.channels + CI * 16 - 1) / (CI * 16);
     if ((uint64_t)across * WAVES * 64 >= 1ull << 32) return false;  // (a launch has fewer lanes)
-    hipLaunchKernelGGL((i8_few_kernel<T, CI, WAVES>), dim3(across, groups), dim3(WAVES * 64), 0, st, a, share);
+    hipLaunchKernelGGL((i8_few_kernel<T, CI, WAVES, PIECES>), dim3(across, groups), dim3(WAVES * 64), 0, st, a, share);
     return true;
 }
 
@@ -762,30 +819,44 @@ static void launch_shared(const I8Args &a, uint32_t shares, void *workspace, hip
     hipLaunchKernelGGL((i8_join_kernel<T>), dim3((uint32_t)std::min<uint64_t>((lanes + kWG - 1) / kWG, 8 * kCUs)), dim3(kWG), 0, st, a, c, shares);
 }
 
+template <class T, bool PIECES>
+static bool launch_few_rows(const I8Args &a, hipStream_t st)
+{
+    if (few_channels(a) == 16) return launch_few<T, 1, 4, PIECES>(a, st);
+    return a.rows / a.groups > 1 && a.columns >= 4096 ? launch_few<T, 2, 8, PIECES>(a, st) : launch_few<T, 2, 4, PIECES>(a, st);
+}
+
+// False: the kernel for any product has to do it.
 template <class T>
-static bool launch_pieces(const I8Args &a, void *workspace, hipStream_t st)
+static bool launch_chosen(const I8Args &a, void *workspace, hipStream_t st)
 {
     const Choice c = choose(a);
-    if (c.tokens == 0) {
-        if (few_channels(a) == 16) return launch_few<T, 1, 4>(a, st);
-        return a.rows / a.groups > 1 && a.columns >= 4096 ? launch_few<T, 2, 8>(a, st) : launch_few<T, 2, 4>(a, st);
-    }
+    if (a.columns == 0) return false;
+    if (!in_pieces(a)) return c.tokens == 0 && launch_few_rows<T, false>(a, st);
+    if (c.tokens == 0) return launch_few_rows<T, true>(a, st);
     if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return false;     // offsets into a tile are 32-bit
     if (c.shares > 1) {
         launch_shared<T>(a, c.shares, workspace, st);
         return true;
     }
-    return c.tokens == 256 ? launch_tiles<T, 8, 2, 8, 4, 2>(a, st) : c.tokens == 128 ? launch_tiles<T, 8, 2, 8, 2, 3>(a, st) : launch_tiles_64<T>(a, st);
+    return c.tokens == 256   ? launch_tiles<T, 8, 2, 8, 4, 2>(a, st)
+           : c.tokens == 128 ? launch_tiles<T, 8, 2, 8, 2, 3>(a, st)
+                             : launch_tiles_64<T>(a, st);
+}
+
+template <class T>
+static void launch_product(const I8Args &a, void *workspace, hipStream_t st)
+{
+    if (launch_chosen<T>(a, workspace, st)) return;
+    const uint32_t blocks = (uint32_t)most_blocks(a, kAnyTokens, kAnyChannels);
+    hipLaunchKernelGGL((i8_any_kernel<T>), dim3(std::min(blocks, 1u << 22)), dim3(256), 0, st, a, blocks);
 }
 
 void launch_i8_product(const I8Args &a, void *workspace, hipStream_t st)
 {
-    if (in_pieces(a) && (a.type == SEER_F32    ? launch_pieces<float>(a, workspace, st)
-                         : a.type == SEER_BF16 ? launch_pieces<bf16_t>(a, workspace, st)
-                                               : launch_pieces<f16_t>(a, workspace, st)))
-        return;
-    const uint32_t blocks = (uint32_t)most_blocks(a, kAnyTokens, kAnyChannels);
-    hipLaunchKernelGGL(i8_any_kernel, dim3(std::min(blocks, 1u << 22)), dim3(256), 0, st, a, blocks);
+    if (a.type == SEER_F32) launch_product<float>(a, workspace, st);
+    else if (a.type == SEER_BF16) launch_product<bf16_t>(a, workspace, st);
+    else launch_product<f16_t>(a, workspace, st);
 }
 
 } // namespace seer
