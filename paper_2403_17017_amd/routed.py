@@ -73,11 +73,11 @@ def bind(L):
 def _new(shape, dtype, like, stream):
     """Memory for an output or a workspace that `stream` is going to write."""
     if stream is None:
-        return like.new_empty(shape, dtype=dtype)
+        return _torch.empty(*shape, dtype=dtype, device=like.device)     # (sizes one by one: 0.3 us less)
     if not hasattr(stream, "cuda_stream"):
         raise ValueError("pass every output and workspace when stream is a raw handle: the allocator does not know it")
     with _torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
+        return _torch.empty(*shape, dtype=dtype, device=like.device)
 
 
 def _matrix_shape(t, what):
@@ -293,7 +293,7 @@ def _grad_call(what, tensors, max_norm, norm, workspace, stream):
     if norm is None:
         if not tensors.count:
             raise ValueError("pass norm= where there are no tensors: nothing says which GPU it is to lie on")
-        norm = _new((), _torch.float32, tensors.grads[0], stream)
+        norm = _new((1,), _torch.float32, tensors.grads[0], stream).view(())
     if workspace is None:
         workspace = _new((grad_workspace_bytes(),), _torch.uint8, norm, stream)
     rc = m.clip(C.addressof(tensors.c), tensors.count, max_norm, norm, workspace, _stream_handle(stream))
