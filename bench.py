@@ -70,7 +70,7 @@ def kernel_source_sha16():
     """Fingerprint of the device code of the sparse products (every file under csrc/ but those of the
     routed layer, which no sparse kernel includes): a profile summary taken from other sources is stale."""
     import hashlib
-    routed = ("dense.hiph", "dense_api.hip", "dense_launch.h", "grad_norm.hip", "i8_product.hip", "route.hip")
+    routed = ("dense.hiph", "dense_api.hip", "dense_launch.h", "grad_norm.hip", "i8_pieces.hiph", "i8_product.hip", "route.hip")
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2403_17017_amd", "csrc")
     for name in sorted(os.listdir(d)):

@@ -5,6 +5,7 @@
 // columns, so that a lane's results are consecutive channels of one token.
 #include "dense.hiph"
 #include "dense_launch.h"
+#include "i8_pieces.hiph"
 
 namespace seer {
 
@@ -213,24 +214,22 @@ __global__ __launch_bounds__(256) void i8_any_kernel(I8Args a, uint32_t blocks)
 #pragma unroll
             for (uint32_t i = 0; i < kEach; ++i) {
                 const uint32_t at = row + i * (256 / kPieces);
-                pa[i] = a.a + (int64_t)min(t.begin + at, t.end - 1) * a.lda + col;
-                pb[i] = b + (int64_t)min(n0 + at, a.channels - 1) * a.ldb + col;
+                pa[i] = a.a + (int64_t)min(t.begin + at, t.end - 1) * a.lda;
+                pb[i] = b + (int64_t)min(n0 + at, a.channels - 1) * a.ldb;
             }
             const auto fetch = [&](uint32_t k0) {
                 if (k0 + kAnyCols <= a.columns) {
 #pragma unroll
                     for (uint32_t i = 0; i < kEach; ++i) {
-                        va[i] = load_16(pa[i] + k0, 16);
-                        vb[i] = load_16(pb[i] + k0, 16);
+                        va[i] = load_16(pa[i] + (k0 + col), 16);
+                        vb[i] = load_16(pb[i] + (k0 + col), 16);
                     }
                 } else if (k0 < a.columns) {
-                    // (pieces behind the end: the first one, and nothing of it)
-                    const int left = (int)a.columns - (int)(k0 + col), n = min(left > 0 ? left : (int)(a.columns - k0), 15);
-                    const uint32_t at = left > 0 ? k0 : k0 - col;
+                    const RowPiece p = row_piece(k0, col, a.columns);       // (b's columns behind the end meet zeros)
 #pragma unroll
                     for (uint32_t i = 0; i < kEach; ++i) {
-                        va[i] = left >= 16 ? load_16(pa[i] + k0, 16) : first_bytes(load_16(pa[i] + at, n), left);
-                        vb[i] = left >= 16 ? load_16(pb[i] + k0, 16) : load_16(pb[i] + at, n);
+                        va[i] = first_bytes(load_16(pa[i] + p.from, p.have), p.keep);
+                        vb[i] = load_16(pb[i] + p.from, p.have);
                     }
                 }
             };
