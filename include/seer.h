@@ -604,6 +604,17 @@ int seer_i8_product(const seer_dense *a, const float *a_scale, const seer_dense 
                     size_t workspace_bytes, void *stream);
 size_t seer_i8_product_workspace_bytes(int64_t rows, int64_t channels, int64_t columns, int32_t groups);
 
+/* Which kernel seer_i8_product takes for these operands (by their sizes, and whether their rows lie at multiples of 16 bytes), or a
+ * negative seer_status.  Nothing is launched and nothing is read through a pointer.  All kernels give the same results. */
+typedef enum {
+    SEER_I8_NONE = 0,   /* nothing to compute                                              */
+    SEER_I8_ANY = 1,    /* tiles through registers, for rows at any address                */
+    SEER_I8_FEW = 2,    /* few rows to a group                                             */
+    SEER_I8_TILES = 3,  /* tiles straight into LDS                                         */
+    SEER_I8_SHARED = 4  /* the same with the columns shared out, in two launches           */
+} seer_i8_kernel;
+int seer_i8_product_kernel(const seer_dense *a, const seer_dense *b, const int32_t *group_ptr, int32_t groups);
+
 /* One of the many tensors whose gradient is clipped: n contiguous elements. */
 typedef struct {
     const void *grad; /* DEVICE */

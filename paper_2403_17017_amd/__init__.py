@@ -11,8 +11,8 @@ from .binding import (  # noqa: F401
     spmv_auto_workspace_bytes, spmv_prepared_workspace_bytes, spmv_workspace_bytes, strerror,
 )
 from .routed import (  # noqa: F401
-    I8_MAX_K, MAX_EXPERTS, GradTensors, Routing,
-    grad_workspace_bytes, i8_product_workspace_bytes, route_workspace_bytes,
+    I8_KERNELS, I8_MAX_K, MAX_EXPERTS, GradTensors, Routing,
+    grad_workspace_bytes, i8_product_kernel, i8_product_workspace_bytes, route_workspace_bytes,
     seer_grad_clip, seer_grad_norm, seer_i8_product, seer_i8_quantize,
     seer_route, seer_route_combine, seer_route_gather, seer_route_gather_i8, seer_route_grad,
 )

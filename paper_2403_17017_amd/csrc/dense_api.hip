@@ -228,8 +228,21 @@ int seer_i8_product(const seer_dense *a, const float *a_scale, const seer_dense 
     if (!i8_product_fits(p)) return SEER_ELIMIT;
     const size_t need = i8_workspace_bytes(p.rows, p.channels, p.columns, p.groups);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return SEER_EWORKSPACE;
-    launch_i8_product(p, workspace, on(stream));
+    launch_i8_product(p, i8_plan(p), workspace, on(stream));
     return done();
+}
+
+int seer_i8_product_kernel(const seer_dense *a, const seer_dense *b, const int32_t *group_ptr, int32_t groups)
+{
+    if (!a || !b || groups < 1 || (!group_ptr && groups != 1)) return SEER_EINVAL;
+    int rc;
+    if ((rc = check_dense(a, a->rows, a->cols, SEER_I8)) != SEER_OK || (rc = check_dense(b, b->rows, a->cols, SEER_I8)) != SEER_OK) return rc;
+    if (b->rows % groups != 0) return SEER_EINVAL;
+    if (a->cols > SEER_I8_MAX_K) return SEER_ELIMIT;
+    I8Args p{static_cast<const int8_t *>(a->data), static_cast<const int8_t *>(b->data), nullptr, nullptr, group_ptr, nullptr, a->ld, b->ld, 0,
+             (uint32_t)a->rows, (uint32_t)(b->rows / groups), (uint32_t)a->cols, (uint32_t)groups, SEER_F32};
+    if (!i8_product_fits(p)) return SEER_ELIMIT;
+    return p.rows == 0 || p.channels == 0 ? SEER_I8_NONE : i8_plan(p).kernel;
 }
 
 size_t seer_grad_workspace_bytes(void) { return grad_workspace_bytes(); }

@@ -36,9 +36,11 @@ struct I8Args {
     uint32_t rows, channels, columns, groups;
     int32_t type;
 };
+struct I8Plan { int32_t kernel /* seer_i8_kernel */; uint32_t tokens /* to a tile */, shares /* of the columns */; };
 bool i8_product_fits(const I8Args &a);
+I8Plan i8_plan(const I8Args &a);            // by sizes and by where the operands lie
 size_t i8_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t columns, uint32_t groups);
-void launch_i8_product(const I8Args &a, void *workspace, hipStream_t st);
+void launch_i8_product(const I8Args &a, const I8Plan &p, void *workspace, hipStream_t st);
 
 constexpr uint32_t kGradParts = 2048;       // partial sums of squares
 inline size_t grad_workspace_bytes() { return kGradParts * sizeof(double); }

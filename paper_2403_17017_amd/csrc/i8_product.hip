@@ -680,13 +680,11 @@ static uint64_t most_blocks(const I8Args &a, uint32_t tokens, uint32_t channels)
 bool i8_product_fits(const I8Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, 64, 64) < (1u << 30); }
 
 template <class T, int WAVES, int WC, int CI, int TJ, int BUFFERS>
-static bool launch_tiles(const I8Args &a, hipStream_t st)
+static void launch_tiles(const I8Args &a, hipStream_t st)
 {
     using Shape = TileShape<WAVES, WC, CI, TJ, BUFFERS>;
-    const uint64_t blocks = most_blocks(a, Shape::kTokens, kTileChannels);
-    if (blocks * Shape::kThreads >= 1ull << 32) return false;       // (a launch has fewer lanes)
-    hipLaunchKernelGGL((i8_tile_kernel<T, WAVES, WC, CI, TJ, BUFFERS>), dim3((uint32_t)blocks), dim3(Shape::kThreads), 0, st, a, SharedColumns{});
-    return true;
+    const uint32_t blocks = (uint32_t)most_blocks(a, Shape::kTokens, kTileChannels);
+    hipLaunchKernelGGL((i8_tile_kernel<T, WAVES, WC, CI, TJ, BUFFERS>), dim3(blocks), dim3(Shape::kThreads), 0, st, a, SharedColumns{});
 }
 
 // Tiles of 64 tokens have two buffers, which leaves room for two workgroups on a CU (32 x 4096 x 4096, mean 1013: 785 us; three, and one
@@ -694,20 +692,19 @@ static bool launch_tiles(const I8Args &a, hipStream_t st)
 static bool three_buffers(const I8Args &a, uint64_t blocks) { return blocks <= kCUs && a.columns > 2048; }
 
 template <class T>
-static bool launch_tiles_64(const I8Args &a, hipStream_t st)
+static void launch_tiles_64(const I8Args &a, hipStream_t st)
 {
-    return three_buffers(a, most_blocks(a, 64, kTileChannels)) ? launch_tiles<T, 4, 4, 4, 4, 3>(a, st) : launch_tiles<T, 4, 4, 4, 4, 2>(a, st);
+    if (three_buffers(a, most_blocks(a, 64, kTileChannels))) launch_tiles<T, 4, 4, 4, 4, 3>(a, st);
+    else launch_tiles<T, 4, 4, 4, 4, 2>(a, st);
 }
 
 static_assert(SEER_MAX_EXPERTS < 65535, "groups are a dimension of the grid of the kernel for few rows");
 template <class T, int CI, int WAVES, bool PIECES>
-static bool launch_few(const I8Args &a, hipStream_t st)
+static void launch_few(const I8Args &a, hipStream_t st)
 {
     const uint32_t groups = a.groups + (a.group_ptr ? 1 : 0), share = ((a.columns + WAVES - 1) / WAVES + 63) & ~63u;
     const uint32_t across = (a.channels + CI * 16 - 1) / (CI * 16);
-    if ((uint64_t)across * WAVES * 64 >= 1ull << 32) return false;  // (a launch has fewer lanes)
     hipLaunchKernelGGL((i8_few_kernel<T, CI, WAVES, PIECES>), dim3(across, groups), dim3(WAVES * 64), 0, st, a, share);
-    return true;
 }
 
 // Which kernel, and for how many shares of the columns: the one whose time by the following lines is the least.  They are fitted to 256
@@ -818,44 +815,60 @@ static void launch_shared(const I8Args &a, uint32_t shares, void *workspace, hip
     hipLaunchKernelGGL((i8_join_kernel<T>), dim3((uint32_t)std::min<uint64_t>((lanes + kWG - 1) / kWG, 8 * kCUs)), dim3(kWG), 0, st, a, c, shares);
 }
 
+static bool few_in_eights(const I8Args &a) { return few_channels(a) == 32 && a.rows / a.groups > 1 && a.columns >= 4096; }
+
 template <class T, bool PIECES>
-static bool launch_few_rows(const I8Args &a, hipStream_t st)
+static void launch_few_rows(const I8Args &a, hipStream_t st)
 {
-    if (few_channels(a) == 16) return launch_few<T, 1, 4, PIECES>(a, st);
-    return a.rows / a.groups > 1 && a.columns >= 4096 ? launch_few<T, 2, 8, PIECES>(a, st) : launch_few<T, 2, 4, PIECES>(a, st);
+    if (few_channels(a) == 16) launch_few<T, 1, 4, PIECES>(a, st);
+    else if (few_in_eights(a)) launch_few<T, 2, 8, PIECES>(a, st);
+    else launch_few<T, 2, 4, PIECES>(a, st);
 }
 
-// False: the kernel for any product has to do it.
-template <class T>
-static bool launch_chosen(const I8Args &a, void *workspace, hipStream_t st)
+// The kernel for a product: what choose() says, where the operands and a launch (fewer than 2^32 lanes) allow it.
+I8Plan i8_plan(const I8Args &a)
 {
     const Choice c = choose(a);
-    if (a.columns == 0) return false;
-    if (!in_pieces(a)) return c.tokens == 0 && launch_few_rows<T, false>(a, st);
-    if (c.tokens == 0) return launch_few_rows<T, true>(a, st);
-    if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return false;     // offsets into a tile are 32-bit
-    if (c.shares > 1) {
-        launch_shared<T>(a, c.shares, workspace, st);
-        return true;
+    const I8Plan any{SEER_I8_ANY, 0, 1};
+    if (a.columns == 0) return any;
+    if (c.tokens == 0) {
+        const uint64_t across = (a.channels + few_channels(a) - 1) / few_channels(a);
+        return across * (few_in_eights(a) ? 512 : 256) < 1ull << 32 ? I8Plan{SEER_I8_FEW, 0, 1} : any;
     }
-    return c.tokens == 256   ? launch_tiles<T, 8, 2, 8, 4, 2>(a, st)
-           : c.tokens == 128 ? launch_tiles<T, 8, 2, 8, 2, 3>(a, st)
-                             : launch_tiles_64<T>(a, st);
+    if (!in_pieces(a)) return any;
+    if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return any;       // offsets into a tile are 32-bit
+    if (c.shares > 1) return I8Plan{SEER_I8_SHARED, c.tokens, c.shares};
+    const uint64_t lanes = most_blocks(a, c.tokens, kTileChannels) * (c.tokens == 64 ? 256 : 512);
+    return lanes < 1ull << 32 ? I8Plan{SEER_I8_TILES, c.tokens, 1} : any;
 }
 
 template <class T>
-static void launch_product(const I8Args &a, void *workspace, hipStream_t st)
+static void launch_product(const I8Args &a, const I8Plan &p, void *workspace, hipStream_t st)
 {
-    if (launch_chosen<T>(a, workspace, st)) return;
-    const uint32_t blocks = (uint32_t)most_blocks(a, kAnyTokens, kAnyChannels);
-    hipLaunchKernelGGL((i8_any_kernel<T>), dim3(std::min(blocks, 1u << 22)), dim3(256), 0, st, a, blocks);
+    switch (p.kernel) {
+    case SEER_I8_FEW:
+        if (in_pieces(a)) launch_few_rows<T, true>(a, st);
+        else launch_few_rows<T, false>(a, st);
+        return;
+    case SEER_I8_TILES:
+        if (p.tokens == 256) launch_tiles<T, 8, 2, 8, 4, 2>(a, st);
+        else if (p.tokens == 128) launch_tiles<T, 8, 2, 8, 2, 3>(a, st);
+        else launch_tiles_64<T>(a, st);
+        return;
+    case SEER_I8_SHARED:
+        launch_shared<T>(a, p.shares, workspace, st);
+        return;
+    default:
+        const uint32_t blocks = (uint32_t)most_blocks(a, kAnyTokens, kAnyChannels);
+        hipLaunchKernelGGL((i8_any_kernel<T>), dim3(std::min(blocks, 1u << 22)), dim3(256), 0, st, a, blocks);
+    }
 }
 
-void launch_i8_product(const I8Args &a, void *workspace, hipStream_t st)
+void launch_i8_product(const I8Args &a, const I8Plan &p, void *workspace, hipStream_t st)
 {
-    if (a.type == SEER_F32) launch_product<float>(a, workspace, st);
-    else if (a.type == SEER_BF16) launch_product<bf16_t>(a, workspace, st);
-    else launch_product<f16_t>(a, workspace, st);
+    if (a.type == SEER_F32) launch_product<float>(a, p, workspace, st);
+    else if (a.type == SEER_BF16) launch_product<bf16_t>(a, p, workspace, st);
+    else launch_product<f16_t>(a, p, workspace, st);
 }
 
 } // namespace seer

@@ -63,6 +63,7 @@ def bind(L):
             ("seer_route_gather_i8", [routing, dense, dense, vp, vp], C.c_int),
             ("seer_i8_product", [dense, vp, dense, vp, vp, i32, dense, vp, sz, vp], C.c_int),
             ("seer_i8_product_workspace_bytes", [i64, i64, i64, i32], sz),
+            ("seer_i8_product_kernel", [dense, dense, vp, i32], C.c_int),
             ("seer_grad_norm", [C.POINTER(seer_grad), i32, vp, vp, sz, vp], C.c_int),
             ("seer_grad_clip", [C.POINTER(seer_grad), i32, C.c_float, vp, vp, sz, vp], C.c_int),
             ("seer_grad_workspace_bytes", [], sz)):
@@ -238,6 +239,22 @@ def seer_route_gather_i8(r: Routing, x, q=None, scale=None, stream=None):
 
 def i8_product_workspace_bytes(rows: int, channels: int, columns: int, groups: int = 1) -> int:
     return int(B.lib().seer_i8_product_workspace_bytes(rows, channels, columns, groups))
+
+
+I8_KERNELS = ("none", "any", "few", "tiles", "shared")
+
+
+def i8_product_kernel(a, b, group_ptr=None) -> str:
+    """Which kernel seer_i8_product takes for these operands, one of I8_KERNELS; nothing is launched."""
+    if b.dim() not in (2, 3):
+        raise ValueError("b is to be [groups, channels, columns]")
+    groups = b.shape[0] if b.dim() == 3 else 1
+    dense = lambda t, rows: C.byref(seer_dense(t.data_ptr(), rows, t.shape[-1], max(t.stride(-2) if rows > 1 else 0, t.shape[-1]), 3))
+    rc = B.lib().seer_i8_product_kernel(dense(a, a.shape[0]), dense(b, groups * b.shape[-2]),
+                                        group_ptr.data_ptr() if group_ptr is not None else None, groups)
+    if rc < 0:
+        raise SeerError(rc, "seer_i8_product_kernel")
+    return I8_KERNELS[rc]
 
 
 def seer_i8_product(a, a_scale, b, b_scale, out=None, group_ptr=None, dtype=None, workspace=None, stream=None):

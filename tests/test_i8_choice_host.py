@@ -1,0 +1,38 @@
+"""Which kernel an 8-bit product takes: the host-side query, by sizes and alignment alone."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2403_17017_amd as S
+from paper_2403_17017_amd import routed as R
+
+A, B_, P = 1 << 20, 1 << 30, 1 << 10      # addresses that nothing reads
+
+
+def kernel(rows, channels, columns, groups=1, ld=None, at=0, ptr=None):
+    ld = columns if ld is None else ld
+    a, b = R.seer_dense(A + at, rows, columns, ld, 3), R.seer_dense(B_ + at, groups * channels, columns, ld, 3)
+    rc = S.lib().seer_i8_product_kernel(C.byref(a), C.byref(b), P if groups > 1 else ptr, groups)
+    return S.I8_KERNELS[rc] if rc >= 0 else rc
+
+
+def test_kinds():
+    assert kernel(1, 8192, 8192) == "few" and kernel(1, 8192, 8192, at=1) == "few" and kernel(256, 2048, 4096, groups=64) == "few"
+    assert kernel(3000, 5000, 4096) == "tiles" and kernel(30000, 4096, 4096, groups=32) == "tiles" and kernel(3000, 5000, 4111, ld=4112) == "tiles"
+    assert kernel(300, 512, 8192) == "shared" and S.i8_product_workspace_bytes(300, 512, 8192) > 0
+    assert kernel(3000, 5000, 4096, at=4) == "any" and kernel(3000, 5000, 4111) == "any" and kernel(3000, 700, 100) == "any"
+    assert kernel(3000, 5000, 4096, ld=1 << 23) == "any"       # too far apart for 32-bit offsets into a tile
+    assert kernel(5, 6, 0) == "any"
+    assert kernel(0, 5, 64) == kernel(5, 0, 64) == "none"
+
+
+def test_refusals():
+    assert kernel(4, 8, 131072) == -6 and kernel(4, 8, 64, ld=63) == -1 and kernel(4, 8, 64, groups=0) == -1
+    a, b = R.seer_dense(A, 4, 64, 64, 3), R.seer_dense(B_, 9, 64, 64, 3)
+    f = S.lib().seer_i8_product_kernel
+    assert f(C.byref(a), C.byref(b), P, 2) == -1               # nine rows are not two matrices
+    assert f(C.byref(a), C.byref(b), None, 3) == -1 and f(None, C.byref(b), None, 1) == -1 and f(C.byref(a), None, None, 1) == -1
+    with pytest.raises(ValueError):
+        S.i8_product_kernel(torch.zeros(4, 64, dtype=torch.int8), torch.zeros(64, dtype=torch.int8))
+    assert S.i8_product_kernel(torch.zeros(4, 64, dtype=torch.int8), torch.zeros(2, 8, 64, dtype=torch.int8), torch.zeros(3, dtype=torch.int32)) == "few"
