@@ -597,7 +597,7 @@ int seer_route_gather_i8(const seer_routing *r, const seer_dense *x, const seer_
  * a_scale: DEVICE fp32 [a.rows].  b_scale: DEVICE fp32 [groups][channels].  group_ptr: DEVICE int32 [groups + 1],
  * non-decreasing from 0 (entries outside 0 .. a.rows are taken as the nearer end), an expert_ptr for
  * instance; NULL with groups == 1: all rows.
- * workspace: >= seer_i8_product_workspace_bytes(a.rows, out.cols, a.cols, groups) (may be 0). */
+ * workspace: >= seer_i8_product_workspace_bytes(a.rows, out.cols, a.cols, groups) (may be 0); for the kernel SEER_I8_SHARED, others use none. */
 #define SEER_I8_MAX_K 131071
 int seer_i8_product(const seer_dense *a, const float *a_scale, const seer_dense *b, const float *b_scale,
                     const int32_t *group_ptr, int32_t groups, const seer_dense *out, void *workspace,

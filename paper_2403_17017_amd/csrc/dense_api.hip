@@ -226,9 +226,10 @@ int seer_i8_product(const seer_dense *a, const float *a_scale, const seer_dense 
     I8Args p{static_cast<const int8_t *>(a->data), static_cast<const int8_t *>(b->data), a_scale, b_scale, group_ptr, out->data,
              a->ld, b->ld, out->ld, (uint32_t)a->rows, (uint32_t)out->cols, (uint32_t)a->cols, (uint32_t)groups, out->type};
     if (!i8_product_fits(p)) return SEER_ELIMIT;
-    const size_t need = i8_workspace_bytes(p.rows, p.channels, p.columns, p.groups);
+    const I8Plan plan = i8_plan(p);
+    const size_t need = plan.kernel == SEER_I8_SHARED ? i8_workspace_bytes(p.rows, p.channels, p.columns, p.groups) : 0;
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return SEER_EWORKSPACE;
-    launch_i8_product(p, i8_plan(p), workspace, on(stream));
+    launch_i8_product(p, plan, workspace, on(stream));
     return done();
 }
 

@@ -720,13 +720,16 @@ static void launch_few(const I8Args &a, hipStream_t st)
 // 2048 columns, 64 groups of 8: 29 and 26).
 static uint32_t few_channels(const I8Args &a) { return (uint64_t)((a.channels + 31) / 32) * a.groups < 128 ? 16 : 32; }
 
-static double few_cost(const I8Args &a)
+struct FewCost { double start, batch, rate /* thousand bytes a us */, read /* million */; };
+constexpr FewCost kFewPieces = {4, 1.2, 24, 5.8}, kFewWords = {4, 3, 15, 2.4};
+
+static double few_cost(const I8Args &a, const FewCost &c)
 {
     const double mean = a.rows / a.groups, channels = few_channels(a);
     const double workgroups = (double)((a.channels + few_channels(a) - 1) / few_channels(a)) * a.groups;
     const double rows = std::max((mean + channels) * workgroups / kCUs, (a.group_ptr ? 4 : 1) * mean + channels);
     const double batches = a.rows / a.groups / kFewRows;        // (behind the first)
-    return std::max(4 + 1.2 * batches + rows * a.columns / 24e3, (double)a.groups * a.channels * a.columns / 5.8e6);
+    return std::max(c.start + c.batch * batches + rows * a.columns / (1e3 * c.rate), (double)a.groups * a.channels * a.columns / (1e6 * c.read));
 }
 
 // Tiles: rounds of as many as there is room for, `round` each and `least` to `least + more` for a step of 64 columns by how many are at
@@ -759,12 +762,12 @@ static double tile_cost(const I8Args &a, const TileCost &c, uint32_t shares)
 //   512 x 8192:  34 34 34 36 and 15 17 18 20      2048 x 8192: 34 35 45 46 and 19 20 24 33
 //   8192 x 8192: 46 46 55 74 and 24 33 43 64      2048 x 2048: 12.5 12.7 13 14 and 13 16 25 27 (hence one)
 // and of groups (mean 66, 100, 160, 256): 10 x 256 x 6656: 37 39 41 41 and 17 18 20 21, 32 x 256 x 4096: 26 28 29 30 and 20 22 24 25.
-struct Choice { uint32_t tokens /* 0: few rows */, shares; };
+struct Choice { uint32_t tokens /* 0: few rows */, shares /* 0: tiles for any address */; };
 
 static Choice choose(const I8Args &a)
 {
     Choice best{0, 1};
-    double least = few_cost(a);
+    double least = few_cost(a, kFewPieces);
     const auto consider = [&](uint32_t tokens, uint32_t shares, double cost) {
         if (cost >= least) return;
         least = cost;
@@ -778,6 +781,21 @@ static Choice choose(const I8Args &a)
     const uint32_t most = (uint32_t)std::min<uint64_t>({kCUs * 2 / tiles, (uint64_t)a.columns / kTileCols / 6, 16});
     for (uint32_t n = 2; n <= most; ++n) consider(64, n, tile_cost(a, kCost64, n) + n * (8.0 * a.rows * a.channels) / 3e6 + 8);
     return best;
+}
+
+// Rows off multiples of 16 bytes: few rows, in realigned words, or the tiles for any address, two workgroups of which are on a CU.  Fitted
+// to 117 draws like those above with rows at odd addresses, both kernels timed: what is chosen takes 1 % longer than the better one
+// on average, 1.4 times at most.  Measured, us, any and few: 97 x 16 x 3089 40 and 23, 100 x 512 x 8190 105 and 62, 47 x 656 x 8946 140 and 36;
+// 500 x 130 x 4111 57 and 113, 3001 x 5001 x 4111 152 and 875, 17 x 186 x 2278, mean 85, longest 682 9.9 and 28.
+static bool few_words(const I8Args &a)
+{
+    const double steps = (a.columns + kAnyCols - 1) / kAnyCols;
+    const uint64_t across = (a.channels + kAnyChannels - 1) / kAnyChannels,
+                   down = a.group_ptr ? (uint64_t)a.rows / kAnyTokens + (a.groups + 1) / 2 : ((uint64_t)a.rows + kAnyTokens - 1) / kAnyTokens;
+    const uint64_t room = 2 * kCUs, rest = down * across % room;
+    const auto round = [&](double full) { return 6.6 + steps * (1.6 + 1.36 * full); };
+    const double any = (double)(down * across / room) * round(1) + (rest ? round((double)rest / room) : 0);
+    return few_cost(a, kFewWords) < std::max(any, (double)a.groups * a.channels * a.columns / 2.6e6);
 }
 
 static SharedColumns shared_columns(const I8Args &a, uint32_t shares, void *workspace)
@@ -825,18 +843,18 @@ static void launch_few_rows(const I8Args &a, hipStream_t st)
     else launch_few<T, 2, 4, PIECES>(a, st);
 }
 
-// The kernel for a product: what choose() says, where the operands and a launch (fewer than 2^32 lanes) allow it.
+// The kernel for a product: what takes least, where the operands and a launch (fewer than 2^32 lanes) allow it.
 I8Plan i8_plan(const I8Args &a)
 {
-    const Choice c = choose(a);
     const I8Plan any{SEER_I8_ANY, 0, 1};
     if (a.columns == 0) return any;
+    // (rows further apart than that: offsets into a tile are 32-bit)
+    const Choice c = in_pieces(a) && a.lda < (1 << 23) && a.ldb < (1 << 23) ? choose(a) : Choice{few_words(a) ? 0u : kAnyTokens, 0};
     if (c.tokens == 0) {
         const uint64_t across = (a.channels + few_channels(a) - 1) / few_channels(a);
         return across * (few_in_eights(a) ? 512 : 256) < 1ull << 32 ? I8Plan{SEER_I8_FEW, 0, 1} : any;
     }
-    if (!in_pieces(a)) return any;
-    if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return any;       // offsets into a tile are 32-bit
+    if (c.shares == 0) return any;
     if (c.shares > 1) return I8Plan{SEER_I8_SHARED, c.tokens, c.shares};
     const uint64_t lanes = most_blocks(a, c.tokens, kTileChannels) * (c.tokens == 64 ? 256 : 512);
     return lanes < 1ull << 32 ? I8Plan{SEER_I8_TILES, c.tokens, 1} : any;

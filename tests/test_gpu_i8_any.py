@@ -1,9 +1,12 @@
 """seer_i8_product where rows do not lie at multiples of 16 bytes, in sizes that go to the tiled kernel for any address."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2403_17017_amd as S
+from paper_2403_17017_amd import routed as R
 from tests.gpu_util import announce
 from tests.routed_util import TYPES, shifted, spread
 from tests.test_gpu_i8_product import check_product, i8
@@ -71,3 +74,20 @@ def test_groups_at_any_address(groups, kind):
         a, b = apart(i8(rng, M, K), "both", by), apart(i8(rng, G * N, K), "both", 4 - by).unflatten(0, (G, N))
         assert S.i8_product_kernel(a, b, torch.tensor(ptr, dtype=torch.int32)) == "any"
         check_product(a, b, ptr, kind, rng)
+
+
+@pytest.mark.parametrize("shape", [(97, 16, 3089), (500, 130, 4111), (100, 512, 8190)], ids=str)
+def test_long_columns_without_a_workspace(shape):
+    """Sizes at which aligned rows would need a workspace: neither kernel for others does."""
+    M, N, K = shape
+    announce(f"i8 any without a workspace {shape}")
+    rng = np.random.default_rng(K)
+    a, b = apart(i8(rng, M, K), "both", 1), apart(i8(rng, N, K), "both", 3)
+    assert S.i8_product_workspace_bytes(M, N, K) > 0 and S.i8_product_kernel(a, b) in ("any", "few")
+    check_product(a, b[None], None, "f32", rng)
+    out, ones = torch.full((M, N), float("nan"), device="cuda:0"), torch.ones(max(M, N), device="cuda:0")
+    d = lambda t, kind: C.byref(R.seer_dense(t.data_ptr(), t.shape[0], t.shape[1], t.stride(0), kind))
+    stream = torch.cuda.current_stream().cuda_stream
+    assert S.lib().seer_i8_product(d(a, 3), ones.data_ptr(), d(b, 3), ones.data_ptr(), None, 1, d(out, 0), None, 0, stream) == 0
+    want = a.cpu().to(torch.int32).numpy().astype(np.int64) @ b.cpu().to(torch.int32).numpy().astype(np.int64).T
+    assert np.array_equal(out.cpu().numpy(), want.astype(np.float32))

@@ -36,3 +36,14 @@ def test_refusals():
     with pytest.raises(ValueError):
         S.i8_product_kernel(torch.zeros(4, 64, dtype=torch.int8), torch.zeros(64, dtype=torch.int8))
     assert S.i8_product_kernel(torch.zeros(4, 64, dtype=torch.int8), torch.zeros(2, 8, 64, dtype=torch.int8), torch.zeros(3, dtype=torch.int32)) == "few"
+
+
+def test_rows_off_multiples_of_16_bytes_are_priced_by_their_own_kernels():
+    """Sizes at which the tiles for aligned rows would share the columns out, which nothing else does."""
+    for size in ((97, 16, 3089), (100, 512, 8190), (47, 656, 8946)):
+        assert kernel(*size) == "few", size            # on 1 to 6 workgroups of the tiles for any address, 40 to 140 us; few rows 23 to 62
+    assert kernel(500, 130, 4111) == "any"             # few rows 113 us, tiles 57
+    assert kernel(85 * 17, 186, 2278, groups=17, at=1) == "any"
+    # rows too far apart for the tiles: the same choice, without a workspace
+    assert kernel(97, 16, 3104, ld=1 << 23) == "few" and S.i8_product_workspace_bytes(97, 16, 3104) > 0
+
