@@ -379,11 +379,12 @@ __global__ __launch_bounds__(kWG) void route_grad_kernel(RouteRows r, const floa
     }
 }
 
-// q = x / scale to the nearest integer, the division rounded to fp32 first; |x| <= 127 scale.
+// q = x / scale to the nearest integer, the division rounded to fp32 first; |x| <= 127 scale.  0 for an infinite scale, too, where the
+// quotients of infinite elements are no numbers.
 __device__ __forceinline__ float quantised(float x, float scale)
 {
     const float v = rintf(x / scale);
-    return scale > 0 ? fminf(fmaxf(v, -127.0f), 127.0f) : 0.0f;
+    return scale > 0 && scale < __builtin_inff() ? fminf(fmaxf(v, -127.0f), 127.0f) : 0.0f;
 }
 
 // Quantisation, of a row of x at a time; routed: its copies go to the slots of its choices.  A lane takes 16 elements at a
