@@ -618,8 +618,8 @@ int seer_i8_product_kernel(const seer_dense *a, const seer_dense *b, const int32
 /* One of the many tensors whose gradient is clipped: n contiguous elements. */
 typedef struct {
     const void *grad; /* DEVICE */
-    void *out;        /* DEVICE: where the clipped gradient goes: grad itself, or memory apart from every grad.
-                         seer_grad_norm does not look at it                                       */
+    void *out;        /* DEVICE: where the clipped gradient goes: grad itself, or memory apart from every grad; apart from every other
+                         out, so a gradient that is clipped in place is listed once (SEER_EINVAL).  seer_grad_norm does not look at it */
     int64_t n;
     int32_t type;     /* SEER_F32, SEER_BF16 or SEER_F16, for both */
 } seer_grad;

@@ -1,6 +1,8 @@
 // C ABI of the routed layer and its training step: checks of arguments, then the launches.
 #include "dense_launch.h"
 
+#include <cstdlib>
+
 using namespace seer;
 
 namespace {
@@ -61,11 +63,33 @@ int done()
 
 hipStream_t on(void *stream) { return static_cast<hipStream_t>(stream); }
 
+// Memory that a call reads, or writes.
+struct Span {
+    Extent at;
+    bool written;
+};
+
+// True: nothing that is written is anything else's, too.  Looked through in the order of the addresses, which lists often come in.
+bool written_apart(Span *spans, size_t n)
+{
+    const auto before = [](const Span &a, const Span &b) { return a.at.begin < b.at.begin; };
+    if (!std::is_sorted(spans, spans + n, before)) std::sort(spans, spans + n, before);
+    uintptr_t any = 0, written = 0;             // where what came so far ends
+    for (size_t i = 0; i < n; ++i) {
+        const Span &s = spans[i];
+        if (s.at.begin < (s.written ? any : written)) return false;
+        any = std::max(any, s.at.end);
+        if (s.written) written = std::max(written, s.at.end);
+    }
+    return true;
+}
+
 // Clipped or not: every tensor is there, and has a type and room in the address space.
 int check_grads(const seer_grad *tensors, int32_t count, const float *norm, bool clip)
 {
     if (count < 0 || (count > 0 && !tensors) || bad_pointer(norm, 4)) return SEER_EINVAL;
     const Extent at_norm = extent(norm, 4);
+    size_t spans = 0;
     for (int32_t i = 0; i < count; ++i) {
         const seer_grad &t = tensors[i];
         if (t.n < 0 || t.n > INT64_MAX / 8 || !is_float(t.type)) return SEER_EINVAL;
@@ -74,9 +98,23 @@ int check_grads(const seer_grad *tensors, int32_t count, const float *norm, bool
         if (bad_pointer(t.grad, size) || overlap(extent(t.grad, (size_t)t.n * size), at_norm)) return SEER_EINVAL;
         if (!clip) continue;
         if (bad_pointer(t.out, size) || overlap(extent(t.out, (size_t)t.n * size), at_norm)) return SEER_EINVAL;
-        if (t.out != t.grad && overlap(extent(t.out, (size_t)t.n * size), extent(t.grad, (size_t)t.n * size))) return SEER_EINVAL;
+        spans += t.out == t.grad ? 1 : 2;
     }
-    return SEER_OK;
+    if (spans < 2) return SEER_OK;
+    // what is clipped lies apart from every other gradient and from what else is clipped
+    Span few[128], *list = spans <= sizeof few / sizeof *few ? few : static_cast<Span *>(std::malloc(spans * sizeof(Span)));
+    if (!list) return SEER_EINVAL;
+    size_t n = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const seer_grad &t = tensors[i];
+        if (t.n == 0) continue;
+        const size_t bytes = (size_t)t.n * size_of(t.type);
+        list[n++] = Span{extent(t.out, bytes), true};
+        if (t.out != t.grad) list[n++] = Span{extent(t.grad, bytes), false};
+    }
+    const bool apart = written_apart(list, n);
+    if (list != few) std::free(list);
+    return apart ? SEER_OK : SEER_EINVAL;
 }
 
 } // namespace
