@@ -511,7 +511,7 @@ int seer_model_host_ns(const seer_model *model, int32_t rows, int32_t cols, int3
  * transpose with a dense matrix.  The same rules as above hold: caller's memory, asynchronous on
  * `stream`, capturable, a status and no output on an error.  Contents (the entries of a routing
  * or of group offsets) are the caller's contract, as a matrix's are, where not said otherwise.
- * Outputs must not overlap inputs or one another (SEER_EINVAL) where not said otherwise. */
+ * Outputs must not overlap inputs or one another (SEER_EINVAL) where not said otherwise, nor may what a call needs of its workspace. */
 
 typedef enum {
     SEER_F32 = 0,

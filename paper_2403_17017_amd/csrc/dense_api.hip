@@ -84,20 +84,25 @@ bool written_apart(Span *spans, size_t n)
     return true;
 }
 
-// Clipped or not: every tensor is there, and has a type and room in the address space.
-int check_grads(const seer_grad *tensors, int32_t count, const float *norm, bool clip)
+// Clipped or not: every tensor is there, has a type and room in the address space, and lies apart from the norm and the workspace.
+int check_grads(const seer_grad *tensors, int32_t count, const float *norm, bool clip, void *workspace, size_t workspace_bytes)
 {
     if (count < 0 || (count > 0 && !tensors) || bad_pointer(norm, 4)) return SEER_EINVAL;
-    const Extent at_norm = extent(norm, 4);
+    const Extent at_norm = extent(norm, 4), at_ws = extent(workspace, workspace ? std::min(workspace_bytes, grad_workspace_bytes()) : 0);
+    const auto apart_from_both = [&](const void *p, size_t bytes) {
+        const Extent e = extent(p, bytes);
+        return !overlap(e, at_norm) && !overlap(e, at_ws);
+    };
+    if (overlap(at_norm, at_ws)) return SEER_EINVAL;
     size_t spans = 0;
     for (int32_t i = 0; i < count; ++i) {
         const seer_grad &t = tensors[i];
         if (t.n < 0 || t.n > INT64_MAX / 8 || !is_float(t.type)) return SEER_EINVAL;
         if (t.n == 0) continue;
         const size_t size = size_of(t.type);
-        if (bad_pointer(t.grad, size) || overlap(extent(t.grad, (size_t)t.n * size), at_norm)) return SEER_EINVAL;
+        if (bad_pointer(t.grad, size) || !apart_from_both(t.grad, (size_t)t.n * size)) return SEER_EINVAL;
         if (!clip) continue;
-        if (bad_pointer(t.out, size) || overlap(extent(t.out, (size_t)t.n * size), at_norm)) return SEER_EINVAL;
+        if (bad_pointer(t.out, size) || !apart_from_both(t.out, (size_t)t.n * size)) return SEER_EINVAL;
         spans += t.out == t.grad ? 1 : 2;
     }
     if (spans < 2) return SEER_OK;
@@ -143,6 +148,8 @@ int seer_route(const void *expert, int32_t index_type, const seer_routing *r, vo
         return SEER_EINVAL;
     const size_t need = route_workspace_bytes(count, (uint32_t)r->experts);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return SEER_EWORKSPACE;
+    const Extent ws = extent(workspace, need);
+    if (overlap(ws, in) || overlap(ws, ptr) || overlap(ws, order) || overlap(ws, slots)) return SEER_EINVAL;
     launch_route(expert, index_type == SEER_I64, count, (uint32_t)r->experts, r->expert_ptr, r->slot_choice, r->choice_slot,
                  workspace, on(stream));
     return done();
@@ -257,16 +264,20 @@ int seer_i8_product(const seer_dense *a, const float *a_scale, const seer_dense 
     if (a->cols > SEER_I8_MAX_K) return SEER_ELIMIT;
     if (a->rows == 0 || out->cols == 0) return SEER_OK;
     if (bad_pointer(a_scale, 4) || bad_pointer(b_scale, 4) || (group_ptr && bad_pointer(group_ptr, 4))) return SEER_EINVAL;
-    const Extent to = extent(out);
-    if (overlap(to, extent(a)) || overlap(to, extent(b)) || overlap(to, extent(a_scale, (size_t)a->rows * 4)) ||
-        overlap(to, extent(b_scale, (size_t)b->rows * 4)) || overlap(to, extent(group_ptr, group_ptr ? ((size_t)groups + 1) * 4 : 0)))
-        return SEER_EINVAL;
+    const Extent to = extent(out), ins[] = {extent(a), extent(b), extent(a_scale, (size_t)a->rows * 4), extent(b_scale, (size_t)b->rows * 4),
+                                            extent(group_ptr, group_ptr ? ((size_t)groups + 1) * 4 : 0)};
+    for (const Extent &in : ins)
+        if (overlap(to, in)) return SEER_EINVAL;
     I8Args p{static_cast<const int8_t *>(a->data), static_cast<const int8_t *>(b->data), a_scale, b_scale, group_ptr, out->data,
              a->ld, b->ld, out->ld, (uint32_t)a->rows, (uint32_t)out->cols, (uint32_t)a->cols, (uint32_t)groups, out->type};
     if (!i8_product_fits(p)) return SEER_ELIMIT;
     const I8Plan plan = i8_plan(p);
     const size_t need = plan.kernel == SEER_I8_SHARED ? i8_workspace_bytes(p.rows, p.channels, p.columns, p.groups) : 0;
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return SEER_EWORKSPACE;
+    const Extent ws = extent(workspace, need);
+    if (overlap(ws, to)) return SEER_EINVAL;
+    for (const Extent &in : ins)
+        if (overlap(ws, in)) return SEER_EINVAL;
     launch_i8_product(p, plan, workspace, on(stream));
     return done();
 }
@@ -288,7 +299,7 @@ size_t seer_grad_workspace_bytes(void) { return grad_workspace_bytes(); }
 
 int seer_grad_norm(const seer_grad *tensors, int32_t count, float *norm, void *workspace, size_t workspace_bytes, void *stream)
 {
-    const int rc = check_grads(tensors, count, norm, false);
+    const int rc = check_grads(tensors, count, norm, false, workspace, workspace_bytes);
     if (rc != SEER_OK) return rc;
     if (!workspace || !aligned16(workspace) || workspace_bytes < grad_workspace_bytes()) return SEER_EWORKSPACE;
     launch_grad_norm(tensors, count, norm, workspace, on(stream));
@@ -298,7 +309,7 @@ int seer_grad_norm(const seer_grad *tensors, int32_t count, float *norm, void *w
 int seer_grad_clip(const seer_grad *tensors, int32_t count, float max_norm, float *norm, void *workspace, size_t workspace_bytes,
                    void *stream)
 {
-    const int rc = check_grads(tensors, count, norm, true);
+    const int rc = check_grads(tensors, count, norm, true, workspace, workspace_bytes);
     if (rc != SEER_OK) return rc;
     if (!(max_norm >= 0.0f)) return SEER_EINVAL;
     if (!workspace || !aligned16(workspace) || workspace_bytes < grad_workspace_bytes()) return SEER_EWORKSPACE;
