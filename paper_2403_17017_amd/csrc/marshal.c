@@ -173,7 +173,7 @@ static int (*f_norm)(const seer_grad *, int32_t, float *, void *, size_t, void *
 static int (*f_clip)(const seer_grad *, int32_t, float, float *, void *, size_t, void *);
 
 static PyObject *s_shape, *s_stride, *s_dtype, *s_is_cuda, *s_is_contiguous, *s_tokens, *s_choices, *s_experts, *s_expert_ptr,
-    *s_slot_choice, *s_choice_slot;
+    *s_slot_choice, *s_choice_slot, *s_nbytes;
 static PyObject *types[6];                   /* torch's dtypes in the order of seer_type */
 
 static int refuse(PyObject *error, const char *what, const char *is)
@@ -288,11 +288,15 @@ static int routing_of(PyObject *r, int all, seer_routing *c)
     return 0;
 }
 
+/* A contiguous tensor of any type, as bytes; None: null. */
 static int space(PyObject *workspace, uint64_t *at, uint64_t *bytes)
 {
     *at = *bytes = 0;
     if (workspace == Py_None) return 0;
-    return address_of(workspace, at) || taken(PyObject_CallMethodNoArgs(workspace, s_numel), as_size, bytes) ? -1 : 0;
+    const int whole = truth(workspace, s_is_contiguous, 1), there = truth(workspace, s_is_cuda, 0);
+    if (whole < 0 || there < 0) return -1;
+    if (!whole || !there) return refuse(PyExc_ValueError, "the workspace", "is to be contiguous and on the GPU");
+    return address_of(workspace, at) || taken(PyObject_GetAttr(workspace, s_nbytes), as_size, bytes) ? -1 : 0;
 }
 
 static int given(Py_ssize_t n, Py_ssize_t want)
@@ -508,9 +512,9 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_numel = PyUnicode_InternFromString("numel");
     PyObject **const names[] = {&s_shape, &s_stride, &s_dtype, &s_is_cuda, &s_is_contiguous, &s_tokens, &s_choices, &s_experts, &s_expert_ptr,
-                                &s_slot_choice, &s_choice_slot};
+                                &s_slot_choice, &s_choice_slot, &s_nbytes};
     const char *const spelt[] = {"shape", "stride", "dtype", "is_cuda", "is_contiguous", "tokens", "choices", "experts", "expert_ptr",
-                                 "slot_choice", "choice_slot"};
+                                 "slot_choice", "choice_slot", "nbytes"};
     for (size_t i = 0; i < sizeof spelt / sizeof *spelt; ++i)
         if (!(*names[i] = PyUnicode_InternFromString(spelt[i]))) return NULL;
     if (!s_rows || !s_cols || !s_nnz || !s_row_ptr || !s_col_idx || !s_values || !s_data_ptr || !s_numel) return NULL;
