@@ -172,9 +172,10 @@ static int (*f_product)(const seer_dense *, const float *, const seer_dense *, c
 static int (*f_norm)(const seer_grad *, int32_t, float *, void *, size_t, void *);
 static int (*f_clip)(const seer_grad *, int32_t, float, float *, void *, size_t, void *);
 
-static PyObject *s_shape, *s_stride, *s_dtype, *s_is_cuda, *s_is_contiguous, *s_tokens, *s_choices, *s_experts, *s_expert_ptr,
+static PyObject *s_shape, *s_stride, *s_dtype, *s_get_device, *s_is_contiguous, *s_tokens, *s_choices, *s_experts, *s_expert_ptr,
     *s_slot_choice, *s_choice_slot, *s_nbytes;
 static PyObject *types[6];                   /* torch's dtypes in the order of seer_type */
+static PyObject *current_device;             /* what gives the number of the current GPU */
 
 static int refuse(PyObject *error, const char *what, const char *is)
 {
@@ -182,10 +183,10 @@ static int refuse(PyObject *error, const char *what, const char *is)
     return -1;
 }
 
-/* Truth of an attribute (call: of what it returns). */
-static int truth(PyObject *t, PyObject *name, int call)
+/* Truth of what a method returns. */
+static int truth(PyObject *t, PyObject *name)
 {
-    PyObject *v = call ? PyObject_CallMethodNoArgs(t, name) : PyObject_GetAttr(t, name);
+    PyObject *v = PyObject_CallMethodNoArgs(t, name);
     if (!v) return -1;
     const int is = PyObject_IsTrue(v);
     Py_DECREF(v);
@@ -220,15 +221,43 @@ static int numbers(PyObject *tuple, int64_t out[3])
     return n;
 }
 
-static int on_gpu(PyObject *t, const char *what)
+/* The GPU that a tensor is on (-1: none), or -2. */
+static int gpu_of(PyObject *t)
 {
-    const int is = truth(t, s_is_cuda, 0);
-    if (is < 0) return -1;
-    return is ? 0 : refuse(PyExc_ValueError, what, "is not on a GPU");
+    uint64_t n;
+    if (taken(PyObject_CallMethodNoArgs(t, s_get_device), as_size, &n)) return -2;
+    return (int32_t)n < 0 ? -1 : (int32_t)n;
+}
+
+/* *gpu: that of the call's tensors so far, -1 before the first; all are on the same one. */
+static int same_gpu(int at, const char *what, int *gpu)
+{
+    if (*gpu < 0) *gpu = at;
+    if (at == *gpu) return 0;
+    PyErr_Format(PyExc_ValueError, "%s is on GPU %d and another tensor of the call on GPU %d", what, at, *gpu);
+    return -1;
+}
+
+static int on_gpu(PyObject *t, const char *what, int *gpu)
+{
+    const int at = gpu_of(t);
+    if (at == -2) return -1;
+    return at < 0 ? refuse(PyExc_ValueError, what, "is not on a GPU") : same_gpu(at, what, gpu);
+}
+
+/* The library launches on the current GPU. */
+static int is_current(int gpu)
+{
+    uint64_t now;
+    if (gpu < 0) return 0;
+    if (taken(PyObject_CallNoArgs(current_device), as_size, &now)) return -1;
+    if ((int32_t)now == gpu) return 0;
+    PyErr_Format(PyExc_ValueError, "the tensors are on GPU %d and the current one is %d", gpu, (int)(int32_t)now);
+    return -1;
 }
 
 /* A 2-D tensor (deep: or a 3-D one, matrices one behind the other, *groups of them) as rows; ld as the library counts it. */
-static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer_dense *d)
+static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer_dense *d, int *gpu)
 {
     int64_t n[3], by[3];
     const int dims = numbers(PyObject_GetAttr(t, s_shape), n);
@@ -241,7 +270,7 @@ static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer
     }
     if (n[2] > 1 && by[2] != 1 && n[0] > 0 && n[1] > 0) return refuse(PyExc_ValueError, what, "is to be a matrix with contiguous rows");
     if (n[0] > 1 && n[1] > 1 && by[0] != n[1] * by[1]) return refuse(PyExc_ValueError, what, "is to have its matrices one behind the other");
-    if (on_gpu(t, what)) return -1;
+    if (on_gpu(t, what, gpu)) return -1;
     uint64_t at;
     if ((d->type = type_of(t, what)) < 0 || address_of(t, &at)) return -1;
     d->data = (void *)(uintptr_t)at;
@@ -253,7 +282,7 @@ static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer
 }
 
 /* A contiguous tensor of n elements of a type; None: null. */
-static int vector(PyObject *t, const char *what, int type, int64_t n, uint64_t *at)
+static int vector(PyObject *t, const char *what, int type, int64_t n, uint64_t *at, int *gpu)
 {
     *at = 0;
     if (t == Py_None) return 0;
@@ -262,22 +291,32 @@ static int vector(PyObject *t, const char *what, int type, int64_t n, uint64_t *
     if (!d) return -1;
     const int same = d == types[type];
     Py_DECREF(d);
-    const int whole = truth(t, s_is_contiguous, 1), there = truth(t, s_is_cuda, 0);
-    if (whole < 0 || there < 0 || taken(PyObject_CallMethodNoArgs(t, s_numel), as_size, &count)) return -1;
-    if (!same || !whole || !there || (int64_t)count != n) {
+    const int whole = truth(t, s_is_contiguous), there = gpu_of(t);
+    if (whole < 0 || there == -2 || taken(PyObject_CallMethodNoArgs(t, s_numel), as_size, &count)) return -1;
+    if (!same || !whole || there < 0 || (int64_t)count != n) {
         PyErr_Format(PyExc_ValueError, "%s is to be a contiguous %S tensor of %lld elements on the GPU", what, types[type], (long long)n);
         return -1;
     }
-    return address_of(t, at);
+    return same_gpu(there, what, gpu) || address_of(t, at) ? -1 : 0;
+}
+
+/* An array of a routing. */
+static int array_attr(PyObject *r, PyObject *name, const char *what, uint64_t *at, int *gpu)
+{
+    PyObject *t = PyObject_GetAttr(r, name);
+    if (!t) return -1;
+    const int rc = on_gpu(t, what, gpu) || address_of(t, at) ? -1 : 0;
+    Py_DECREF(t);
+    return rc;
 }
 
 /* all: with the order of the slots; else only choice_slot, which is all that rows go by. */
-static int routing_of(PyObject *r, int all, seer_routing *c)
+static int routing_of(PyObject *r, int all, seer_routing *c, int *gpu)
 {
     uint64_t tokens, choices, experts, ptr = 0, order = 0, slots;
     if (size_attr(r, s_tokens, &tokens) || size_attr(r, s_choices, &choices) || size_attr(r, s_experts, &experts) ||
-        address_attr(r, s_choice_slot, &slots) ||
-        (all && (address_attr(r, s_expert_ptr, &ptr) || address_attr(r, s_slot_choice, &order))))
+        array_attr(r, s_choice_slot, "choice_slot", &slots, gpu) ||
+        (all && (array_attr(r, s_expert_ptr, "expert_ptr", &ptr, gpu) || array_attr(r, s_slot_choice, "slot_choice", &order, gpu))))
         return -1;
     c->tokens = (int32_t)tokens;
     c->choices = (int32_t)choices;
@@ -289,13 +328,14 @@ static int routing_of(PyObject *r, int all, seer_routing *c)
 }
 
 /* A contiguous tensor of any type, as bytes; None: null. */
-static int space(PyObject *workspace, uint64_t *at, uint64_t *bytes)
+static int space(PyObject *workspace, uint64_t *at, uint64_t *bytes, int *gpu)
 {
     *at = *bytes = 0;
     if (workspace == Py_None) return 0;
-    const int whole = truth(workspace, s_is_contiguous, 1), there = truth(workspace, s_is_cuda, 0);
-    if (whole < 0 || there < 0) return -1;
-    if (!whole || !there) return refuse(PyExc_ValueError, "the workspace", "is to be contiguous and on the GPU");
+    const int whole = truth(workspace, s_is_contiguous), there = gpu_of(workspace);
+    if (whole < 0 || there == -2) return -1;
+    if (!whole || there < 0) return refuse(PyExc_ValueError, "the workspace", "is to be contiguous and on the GPU");
+    if (same_gpu(there, "the workspace", gpu)) return -1;
     return address_of(workspace, at) || taken(PyObject_GetAttr(workspace, s_nbytes), as_size, bytes) ? -1 : 0;
 }
 
@@ -317,9 +357,11 @@ static PyObject *m_route(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     seer_routing r;
     uint64_t at, ws, bytes, stream;
-    if (given(n, 4) || routing_of(a[1], 1, &r)) return NULL;
+    int gpu = -1;
+    if (given(n, 4) || routing_of(a[1], 1, &r, &gpu)) return NULL;
     const int type = type_of(a[0], "expert");
-    if (type < 0 || vector(a[0], "expert", type, (int64_t)r.tokens * r.choices, &at) || space(a[2], &ws, &bytes) || as_size(a[3], &stream))
+    if (type < 0 || vector(a[0], "expert", type, (int64_t)r.tokens * r.choices, &at, &gpu) || space(a[2], &ws, &bytes, &gpu) ||
+        as_size(a[3], &stream) || is_current(gpu))
         return NULL;
     ASYNC(f_route(P(const void *, at), type, &r, P(void *, ws), (size_t)bytes, P(void *, stream)));
 }
@@ -328,8 +370,9 @@ static PyObject *m_route(PyObject *self, PyObject *const *a, Py_ssize_t n)
 static int rows_parse(PyObject *const *a, Py_ssize_t n, const char *first, const char *second, seer_routing *r, seer_dense *x,
                       seer_dense *y, uint64_t *weight, uint64_t *stream)
 {
-    return given(n, 5) || routing_of(a[0], 0, r) || matrix(a[1], first, 0, NULL, x) || matrix(a[2], second, 0, NULL, y) ||
-           vector(a[3], "weight", SEER_F32, (int64_t)r->tokens * r->choices, weight) || as_size(a[4], stream);
+    int gpu = -1;
+    return given(n, 5) || routing_of(a[0], 0, r, &gpu) || matrix(a[1], first, 0, NULL, x, &gpu) || matrix(a[2], second, 0, NULL, y, &gpu) ||
+           vector(a[3], "weight", SEER_F32, (int64_t)r->tokens * r->choices, weight, &gpu) || as_size(a[4], stream) || is_current(gpu);
 }
 
 static PyObject *m_gather(PyObject *self, PyObject *const *a, Py_ssize_t n)
@@ -356,9 +399,12 @@ static PyObject *m_grad(PyObject *self, PyObject *const *a, Py_ssize_t n)
     seer_routing r;
     seer_dense dy, z, dz;
     uint64_t weight, dweight, stream;
-    if (given(n, 7) || routing_of(a[0], 0, &r) || matrix(a[1], "dy", 0, NULL, &dy) || (a[2] != Py_None && matrix(a[2], "z", 0, NULL, &z)) ||
-        vector(a[3], "weight", SEER_F32, (int64_t)r.tokens * r.choices, &weight) || (a[4] != Py_None && matrix(a[4], "dz", 0, NULL, &dz)) ||
-        vector(a[5], "dweight", SEER_F32, (int64_t)r.tokens * r.choices, &dweight) || as_size(a[6], &stream))
+    int gpu = -1;
+    if (given(n, 7) || routing_of(a[0], 0, &r, &gpu) || matrix(a[1], "dy", 0, NULL, &dy, &gpu) ||
+        (a[2] != Py_None && matrix(a[2], "z", 0, NULL, &z, &gpu)) ||
+        vector(a[3], "weight", SEER_F32, (int64_t)r.tokens * r.choices, &weight, &gpu) ||
+        (a[4] != Py_None && matrix(a[4], "dz", 0, NULL, &dz, &gpu)) ||
+        vector(a[5], "dweight", SEER_F32, (int64_t)r.tokens * r.choices, &dweight, &gpu) || as_size(a[6], &stream) || is_current(gpu))
         return NULL;
     ASYNC(f_grad(&r, &dy, a[2] != Py_None ? &z : NULL, P(const float *, weight), a[4] != Py_None ? &dz : NULL, P(float *, dweight),
                  P(void *, stream)));
@@ -371,8 +417,9 @@ static PyObject *m_quantize(PyObject *self, PyObject *const *a, Py_ssize_t n)
     seer_dense x, q;
     uint64_t scale, stream;
     const int routed = n == 5 && a[0] != Py_None;
-    if (given(n, 5) || (routed && routing_of(a[0], 0, &r)) || matrix(a[1], "x", 0, NULL, &x) || matrix(a[2], "q", 0, NULL, &q) ||
-        vector(a[3], "scale", SEER_F32, routed ? (int64_t)r.tokens * r.choices : x.rows, &scale) || as_size(a[4], &stream))
+    int gpu = -1;
+    if (given(n, 5) || (routed && routing_of(a[0], 0, &r, &gpu)) || matrix(a[1], "x", 0, NULL, &x, &gpu) || matrix(a[2], "q", 0, NULL, &q, &gpu) ||
+        vector(a[3], "scale", SEER_F32, routed ? (int64_t)r.tokens * r.choices : x.rows, &scale, &gpu) || as_size(a[4], &stream) || is_current(gpu))
         return NULL;
     ASYNC(routed ? f_gather_i8(&r, &x, &q, P(float *, scale), P(void *, stream)) : f_quantize(&x, &q, P(float *, scale), P(void *, stream)));
 }
@@ -383,25 +430,28 @@ static PyObject *m_product(PyObject *self, PyObject *const *v, Py_ssize_t n)
     seer_dense a, b, out;
     int32_t groups;
     uint64_t sa, sb, ptr, ws, bytes, stream;
-    if (given(n, 8) || matrix(v[0], "a", 0, NULL, &a) || vector(v[1], "a_scale", SEER_F32, a.rows, &sa) || matrix(v[2], "b", 1, &groups, &b) ||
-        vector(v[3], "b_scale", SEER_F32, b.rows, &sb) || vector(v[4], "group_ptr", SEER_I32, (int64_t)groups + 1, &ptr) ||
-        matrix(v[5], "out", 0, NULL, &out) || space(v[6], &ws, &bytes) || as_size(v[7], &stream))
+    int gpu = -1;
+    if (given(n, 8) || matrix(v[0], "a", 0, NULL, &a, &gpu) || vector(v[1], "a_scale", SEER_F32, a.rows, &sa, &gpu) ||
+        matrix(v[2], "b", 1, &groups, &b, &gpu) || vector(v[3], "b_scale", SEER_F32, b.rows, &sb, &gpu) ||
+        vector(v[4], "group_ptr", SEER_I32, (int64_t)groups + 1, &ptr, &gpu) || matrix(v[5], "out", 0, NULL, &out, &gpu) ||
+        space(v[6], &ws, &bytes, &gpu) || as_size(v[7], &stream) || is_current(gpu))
         return NULL;
     ASYNC(f_product(&a, P(const float *, sa), &b, P(const float *, sb), P(const int32_t *, ptr), groups, &out, P(void *, ws), (size_t)bytes,
                     P(void *, stream)));
 }
 
 /* One tensor of a list of gradients. */
-static int gradient(PyObject *t, uint64_t *at, uint64_t *n, int *type)
+static int gradient(PyObject *t, uint64_t *at, uint64_t *n, int *type, int *gpu)
 {
-    const int there = truth(t, s_is_cuda, 0), whole = there < 0 ? -1 : truth(t, s_is_contiguous, 1);
+    const int there = gpu_of(t), whole = there == -2 ? -1 : truth(t, s_is_contiguous);
     if (whole < 0) return -1;
-    if (!there || !whole) return refuse(PyExc_ValueError, "gradients and outputs", "are to be contiguous and on the GPU");
+    if (there < 0 || !whole) return refuse(PyExc_ValueError, "gradients and outputs", "are to be contiguous and on the GPU");
+    if (same_gpu(there, "a gradient or output", gpu)) return -1;
     if ((*type = type_of(t, "a gradient")) < 0) return -1;
     return address_of(t, at) || taken(PyObject_CallMethodNoArgs(t, s_numel), as_size, n) ? -1 : 0;
 }
 
-/* (list of gradients, list of outputs or None, address of the seer_grad array to fill, its length) */
+/* (list of gradients, list of outputs or None, address of the seer_grad array to fill, its length): the GPU that they are on, or -1 */
 static PyObject *m_grads(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     uint64_t list, count;
@@ -412,6 +462,7 @@ static PyObject *m_grads(PyObject *self, PyObject *const *a, Py_ssize_t n)
         return NULL;
     }
     seer_grad *const out = P(seer_grad *, list);
+    int gpu = -1;
     for (uint64_t i = 0; i < count; ++i) {
         if ((uint64_t)PyList_GET_SIZE(a[0]) != count || (apart && (uint64_t)PyList_GET_SIZE(a[1]) != count)) {
             PyErr_SetString(PyExc_ValueError, "as many outputs as gradients are wanted");
@@ -422,8 +473,8 @@ static PyObject *m_grads(PyObject *self, PyObject *const *a, Py_ssize_t n)
         PyObject *g = PyList_GET_ITEM(a[0], (Py_ssize_t)i), *o = apart ? PyList_GET_ITEM(a[1], (Py_ssize_t)i) : g;
         Py_INCREF(g);
         Py_INCREF(o);
-        int rc = gradient(g, &at, &elems, &type);
-        if (!rc && apart) rc = gradient(o, &to, &room, &as);
+        int rc = gradient(g, &at, &elems, &type, &gpu);
+        if (!rc && apart) rc = gradient(o, &to, &room, &as, &gpu);
         else to = at, room = elems, as = type;
         if (!rc && (as != type || room != elems)) rc = refuse(PyExc_ValueError, "an output", "is to have its gradient's type and size");
         if (!rc && type > SEER_F16) {
@@ -438,16 +489,16 @@ static PyObject *m_grads(PyObject *self, PyObject *const *a, Py_ssize_t n)
         out[i].n = (int64_t)elems;
         out[i].type = type;
     }
-    Py_RETURN_NONE;
+    return PyLong_FromLong(gpu);
 }
 
-/* (address of the seer_grad array, count, max_norm or None, norm, workspace, stream) */
+/* (address of the seer_grad array, count, max_norm or None, norm, workspace, stream, what m_grads returned) */
 static PyObject *m_clip(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
-    uint64_t list, count, norm, ws, bytes, stream;
-    if (given(n, 6) || as_size(a[0], &list) || as_size(a[1], &count) || vector(a[3], "norm", SEER_F32, 1, &norm) || space(a[4], &ws, &bytes) ||
-        as_size(a[5], &stream))
-        return NULL;
+    uint64_t list, count, norm, ws, bytes, stream, tensors;
+    if (given(n, 7) || as_size(a[0], &list) || as_size(a[1], &count) || as_size(a[5], &stream) || as_size(a[6], &tensors)) return NULL;
+    int gpu = (int32_t)tensors;
+    if (vector(a[3], "norm", SEER_F32, 1, &norm, &gpu) || space(a[4], &ws, &bytes, &gpu) || is_current(gpu)) return NULL;
     const int clip = a[2] != Py_None;
     const double most = clip ? PyFloat_AsDouble(a[2]) : 0;
     if (PyErr_Occurred()) return NULL;
@@ -458,8 +509,9 @@ static PyObject *m_clip(PyObject *self, PyObject *const *a, Py_ssize_t n)
 static PyObject *m_bind_routed(PyObject *self, PyObject *args)
 {
     unsigned long long f[9];
-    PyObject *t[6];
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKOOOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, t, t + 1, t + 2, t + 3, t + 4, t + 5))
+    PyObject *t[6], *device;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKOOOOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, &device, t, t + 1, t + 2, t + 3, t + 4,
+                          t + 5))
         return NULL;
     f_route = P(int (*)(const void *, int32_t, const seer_routing *, void *, size_t, void *), f[0]);
     f_gather = P(int (*)(const seer_routing *, const seer_dense *, const float *, const seer_dense *, void *), f[1]);
@@ -471,6 +523,8 @@ static PyObject *m_bind_routed(PyObject *self, PyObject *args)
                           void *, size_t, void *), f[6]);
     f_norm = P(int (*)(const seer_grad *, int32_t, float *, void *, size_t, void *), f[7]);
     f_clip = P(int (*)(const seer_grad *, int32_t, float, float *, void *, size_t, void *), f[8]);
+    Py_INCREF(device);
+    Py_XSETREF(current_device, device);
     for (int i = 0; i < 6; ++i) {
         Py_INCREF(t[i]);
         Py_XSETREF(types[i], t[i]);
@@ -486,7 +540,7 @@ static PyMethodDef methods[] = {
      "spmv_model(model address, A, x, y, workspace, stream) -> (status, path, kernel id)"},
     {"spmv_prepared", (PyCFunction)(void (*)(void))m_prepared, METH_FASTCALL,
      "spmv_prepared(plan address, A, x, y, workspace, stream) -> status"},
-    {"bind_routed", m_bind_routed, METH_VARARGS, "bind_routed(addresses of the routed layer's functions, torch's dtypes)"},
+    {"bind_routed", m_bind_routed, METH_VARARGS, "bind_routed(addresses of the routed layer's functions, what gives the current GPU, torch's dtypes)"},
     {"route", (PyCFunction)(void (*)(void))m_route, METH_FASTCALL, "route(expert, routing, workspace, stream) -> status"},
     {"gather", (PyCFunction)(void (*)(void))m_gather, METH_FASTCALL, "gather(routing, x, out, weight, stream) -> status"},
     {"combine", (PyCFunction)(void (*)(void))m_combine, METH_FASTCALL, "combine(routing, z, y, weight, stream) -> status"},
@@ -494,8 +548,8 @@ static PyMethodDef methods[] = {
     {"quantize", (PyCFunction)(void (*)(void))m_quantize, METH_FASTCALL, "quantize(routing, x, q, scale, stream) -> status"},
     {"product", (PyCFunction)(void (*)(void))m_product, METH_FASTCALL,
      "product(a, a_scale, b, b_scale, group_ptr, out, workspace, stream) -> status"},
-    {"grads", (PyCFunction)(void (*)(void))m_grads, METH_FASTCALL, "grads(gradients, outputs or None, list address, count)"},
-    {"clip", (PyCFunction)(void (*)(void))m_clip, METH_FASTCALL, "clip(list address, count, max_norm, norm, workspace, stream) -> status"},
+    {"grads", (PyCFunction)(void (*)(void))m_grads, METH_FASTCALL, "grads(gradients, outputs or None, list address, count) -> GPU"},
+    {"clip", (PyCFunction)(void (*)(void))m_clip, METH_FASTCALL, "clip(list address, count, max_norm, norm, workspace, stream, GPU) -> status"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the asynchronous calls", -1,
@@ -511,9 +565,9 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_values = PyUnicode_InternFromString("values");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_numel = PyUnicode_InternFromString("numel");
-    PyObject **const names[] = {&s_shape, &s_stride, &s_dtype, &s_is_cuda, &s_is_contiguous, &s_tokens, &s_choices, &s_experts, &s_expert_ptr,
+    PyObject **const names[] = {&s_shape, &s_stride, &s_dtype, &s_get_device, &s_is_contiguous, &s_tokens, &s_choices, &s_experts, &s_expert_ptr,
                                 &s_slot_choice, &s_choice_slot, &s_nbytes};
-    const char *const spelt[] = {"shape", "stride", "dtype", "is_cuda", "is_contiguous", "tokens", "choices", "experts", "expert_ptr",
+    const char *const spelt[] = {"shape", "stride", "dtype", "get_device", "is_contiguous", "tokens", "choices", "experts", "expert_ptr",
                                  "slot_choice", "choice_slot", "nbytes"};
     for (size_t i = 0; i < sizeof spelt / sizeof *spelt; ++i)
         if (!(*names[i] = PyUnicode_InternFromString(spelt[i]))) return NULL;

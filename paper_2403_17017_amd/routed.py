@@ -3,7 +3,7 @@ experts and back with their gradients, products of 8-bit integers, the norm over
 
 The same manner as the calls on sparse matrices (binding.py): argument marshalling only, the work is the
 library's.  Outputs may be handed in or are allocated here (on the call's stream); a matrix is a 2-D tensor
-whose rows are contiguous.
+whose rows are contiguous.  A call's tensors are all on the current GPU (ValueError).
 """
 from __future__ import annotations
 
@@ -44,9 +44,21 @@ def _ready():
         L, m = B.lib(), B._marshal
         m.bind_routed(*(C.cast(f, C.c_void_p).value for f in (
             L.seer_route, L.seer_route_gather, L.seer_route_combine, L.seer_route_grad, L.seer_i8_quantize, L.seer_route_gather_i8,
-            L.seer_i8_product, L.seer_grad_norm, L.seer_grad_clip)), *ids)
+            L.seer_i8_product, L.seer_grad_norm, L.seer_grad_clip)), _current_device, *ids)
         _types, _torch = ids, torch
     return B._marshal
+
+
+def _current_device() -> int:
+    """The number of the GPU that calls run on (the first one, before torch has looked for them)."""
+    return _torch._C._cuda_getDevice() if _torch.cuda._initialized else 0
+
+
+def _handle(stream) -> int:
+    """As _stream_handle; a torch stream is one of the current GPU's."""
+    if stream is not None and hasattr(stream, "cuda_stream") and stream.device_index != _current_device():
+        raise ValueError(f"the stream is GPU {stream.device_index}'s and the current one is {_current_device()}")
+    return _stream_handle(stream)
 
 
 def bind(L):
@@ -145,7 +157,7 @@ def seer_route(expert, experts: int, routing: Routing = None, workspace=None, st
         workspace = room if workspace is None else workspace
     elif (routing.tokens, routing.choices, routing.experts) != (tokens, choices, experts):
         raise ValueError("routing has other sizes")
-    h = _stream_handle(stream)
+    h = _handle(stream)
     rc = m.route(expert, routing, workspace, h)
     if rc == EWORKSPACE and workspace is None:
         workspace = _new((route_workspace_bytes(tokens, choices, experts),), _torch.uint8, expert, stream)
@@ -160,7 +172,7 @@ def seer_route_gather(r: Routing, x, out=None, weight=None, stream=None):
     m = _ready()
     if out is None:
         out = _new((r.tokens * r.choices, _matrix_shape(x, "x")[1]), x.dtype, x, stream)
-    rc = m.gather(r, x, out, weight, _stream_handle(stream))
+    rc = m.gather(r, x, out, weight, _handle(stream))
     if rc:
         raise SeerError(rc, "seer_route_gather")
     return out
@@ -171,7 +183,7 @@ def seer_route_combine(r: Routing, z, y=None, weight=None, stream=None):
     m = _ready()
     if y is None:
         y = _new((r.tokens, _matrix_shape(z, "z")[1]), z.dtype, z, stream)
-    rc = m.combine(r, z, y, weight, _stream_handle(stream))
+    rc = m.combine(r, z, y, weight, _handle(stream))
     if rc:
         raise SeerError(rc, "seer_route_combine")
     return y
@@ -184,7 +196,7 @@ def seer_route_grad(r: Routing, dy, z, weight=None, dz=None, dweight=None, strea
         dz = _new((r.tokens * r.choices, _matrix_shape(dy, "dy")[1]), dy.dtype, dy, stream)
     if dweight is None and need_dweight:
         dweight = _new((r.tokens, r.choices), _torch.float32, dy, stream)
-    rc = m.grad(r, dy, z, weight, dz, dweight, _stream_handle(stream))
+    rc = m.grad(r, dy, z, weight, dz, dweight, _handle(stream))
     if rc:
         raise SeerError(rc, "seer_route_grad")
     return dz, dweight
@@ -214,7 +226,7 @@ def seer_i8_quantize(x, q=None, scale=None, stream=None):
         _room_for_pieces(q, cols)
     if scale is None:
         scale = _new((rows,), _torch.float32, x, stream)
-    rc = m.quantize(None, x, q, scale, _stream_handle(stream))
+    rc = m.quantize(None, x, q, scale, _handle(stream))
     if rc:
         raise SeerError(rc, "seer_i8_quantize")
     return q, scale
@@ -231,7 +243,7 @@ def seer_route_gather_i8(r: Routing, x, q=None, scale=None, stream=None):
         _room_for_pieces(q, cols)
     if scale is None:
         scale = _new((rows,), _torch.float32, x, stream)
-    rc = m.quantize(r, x, q, scale, _stream_handle(stream))
+    rc = m.quantize(r, x, q, scale, _handle(stream))
     if rc:
         raise SeerError(rc, "seer_route_gather_i8")
     return q, scale
@@ -275,7 +287,7 @@ def seer_i8_product(a, a_scale, b, b_scale, out=None, group_ptr=None, dtype=None
         out = _new((rows, channels), dtype or _torch.bfloat16, a, stream)
     elif dtype is not None and out.dtype != dtype:
         raise TypeError(f"out is {out.dtype}, not {dtype}")
-    h = _stream_handle(stream)
+    h = _handle(stream)
     rc = m.product(a, a_scale, b, b_scale, group_ptr, out, workspace, h)
     if rc == EWORKSPACE and workspace is None:
         workspace = _new((i8_product_workspace_bytes(rows, channels, columns, groups),), _torch.uint8, a, stream)
@@ -300,7 +312,7 @@ class GradTensors:
         if self.outs is not None and len(self.outs) != self.count:
             raise ValueError("as many outputs as gradients are wanted")
         self.c = (seer_grad * max(self.count, 1))()
-        m.grads(self.grads, self.outs, C.addressof(self.c), self.count)
+        self.gpu = m.grads(self.grads, self.outs, C.addressof(self.c), self.count)      # that they are on; -1: there are none
 
 
 def _grad_call(what, tensors, max_norm, norm, workspace, stream):
@@ -313,7 +325,7 @@ def _grad_call(what, tensors, max_norm, norm, workspace, stream):
         norm = _new((1,), _torch.float32, tensors.grads[0], stream).view(())
     if workspace is None:
         workspace = _new((grad_workspace_bytes(),), _torch.uint8, norm, stream)
-    rc = m.clip(C.addressof(tensors.c), tensors.count, max_norm, norm, workspace, _stream_handle(stream))
+    rc = m.clip(C.addressof(tensors.c), tensors.count, max_norm, norm, workspace, _handle(stream), tensors.gpu)
     if rc:
         raise SeerError(rc, what)
     return norm
