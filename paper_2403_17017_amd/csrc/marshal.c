@@ -172,10 +172,11 @@ static int (*f_product)(const seer_dense *, const float *, const seer_dense *, c
 static int (*f_norm)(const seer_grad *, int32_t, float *, void *, size_t, void *);
 static int (*f_clip)(const seer_grad *, int32_t, float, float *, void *, size_t, void *);
 
-static PyObject *s_shape, *s_stride, *s_dtype, *s_get_device, *s_is_contiguous, *s_tokens, *s_choices, *s_experts, *s_expert_ptr,
+static PyObject *s_shape, *s_stride, *s_dtype, *s_get_device, *s_requires_grad, *s_is_contiguous, *s_tokens, *s_choices, *s_experts, *s_expert_ptr,
     *s_slot_choice, *s_choice_slot, *s_nbytes;
 static PyObject *types[6];                   /* torch's dtypes in the order of seer_type */
 static PyObject *current_device;             /* what gives the number of the current GPU */
+static PyObject *grad_enabled;               /* what says whether torch records a history */
 
 static int refuse(PyObject *error, const char *what, const char *is)
 {
@@ -256,6 +257,23 @@ static int is_current(int gpu)
     return -1;
 }
 
+/* A history that torch is recording would end here without a word. */
+static int no_history(PyObject *t, const char *what)
+{
+    PyObject *v = PyObject_GetAttr(t, s_requires_grad);
+    if (!v) return -1;
+    const int wanted = PyObject_IsTrue(v);
+    Py_DECREF(v);
+    if (wanted <= 0) return wanted;
+    v = PyObject_CallNoArgs(grad_enabled);
+    if (!v) return -1;
+    const int on = PyObject_IsTrue(v);
+    Py_DECREF(v);
+    return on <= 0 ? on
+                   : refuse(PyExc_RuntimeError, what, "requires grad, and this call keeps no history: its gradients are calls of their own. Call it "
+                                                      "in the forward of a torch.autograd.Function, under torch.no_grad(), or with detached tensors");
+}
+
 /* A 2-D tensor (deep: or a 3-D one, matrices one behind the other, *groups of them) as rows; ld as the library counts it. */
 static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer_dense *d, int *gpu)
 {
@@ -272,7 +290,7 @@ static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer
     if (n[0] > 1 && n[1] > 1 && by[0] != n[1] * by[1]) return refuse(PyExc_ValueError, what, "is to have its matrices one behind the other");
     if (on_gpu(t, what, gpu)) return -1;
     uint64_t at;
-    if ((d->type = type_of(t, what)) < 0 || address_of(t, &at)) return -1;
+    if ((d->type = type_of(t, what)) < 0 || (d->type <= SEER_F16 && no_history(t, what)) || address_of(t, &at)) return -1;
     d->data = (void *)(uintptr_t)at;
     d->rows = n[0] * n[1];
     d->cols = n[2];
@@ -297,7 +315,7 @@ static int vector(PyObject *t, const char *what, int type, int64_t n, uint64_t *
         PyErr_Format(PyExc_ValueError, "%s is to be a contiguous %S tensor of %lld elements on the GPU", what, types[type], (long long)n);
         return -1;
     }
-    return same_gpu(there, what, gpu) || address_of(t, at) ? -1 : 0;
+    return same_gpu(there, what, gpu) || (type == SEER_F32 && no_history(t, what)) || address_of(t, at) ? -1 : 0;
 }
 
 /* An array of a routing. */
@@ -509,9 +527,9 @@ static PyObject *m_clip(PyObject *self, PyObject *const *a, Py_ssize_t n)
 static PyObject *m_bind_routed(PyObject *self, PyObject *args)
 {
     unsigned long long f[9];
-    PyObject *t[6], *device;
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKOOOOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, &device, t, t + 1, t + 2, t + 3, t + 4,
-                          t + 5))
+    PyObject *t[6], *device, *grad;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKOOOOOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, &device, &grad, t, t + 1, t + 2,
+                          t + 3, t + 4, t + 5))
         return NULL;
     f_route = P(int (*)(const void *, int32_t, const seer_routing *, void *, size_t, void *), f[0]);
     f_gather = P(int (*)(const seer_routing *, const seer_dense *, const float *, const seer_dense *, void *), f[1]);
@@ -523,6 +541,8 @@ static PyObject *m_bind_routed(PyObject *self, PyObject *args)
                           void *, size_t, void *), f[6]);
     f_norm = P(int (*)(const seer_grad *, int32_t, float *, void *, size_t, void *), f[7]);
     f_clip = P(int (*)(const seer_grad *, int32_t, float, float *, void *, size_t, void *), f[8]);
+    Py_INCREF(grad);
+    Py_XSETREF(grad_enabled, grad);
     Py_INCREF(device);
     Py_XSETREF(current_device, device);
     for (int i = 0; i < 6; ++i) {
@@ -540,7 +560,7 @@ static PyMethodDef methods[] = {
      "spmv_model(model address, A, x, y, workspace, stream) -> (status, path, kernel id)"},
     {"spmv_prepared", (PyCFunction)(void (*)(void))m_prepared, METH_FASTCALL,
      "spmv_prepared(plan address, A, x, y, workspace, stream) -> status"},
-    {"bind_routed", m_bind_routed, METH_VARARGS, "bind_routed(addresses of the routed layer's functions, what gives the current GPU, torch's dtypes)"},
+    {"bind_routed", m_bind_routed, METH_VARARGS, "bind_routed(addresses of the routed layer's functions, what gives the current GPU, and whether a history is recorded, torch's dtypes)"},
     {"route", (PyCFunction)(void (*)(void))m_route, METH_FASTCALL, "route(expert, routing, workspace, stream) -> status"},
     {"gather", (PyCFunction)(void (*)(void))m_gather, METH_FASTCALL, "gather(routing, x, out, weight, stream) -> status"},
     {"combine", (PyCFunction)(void (*)(void))m_combine, METH_FASTCALL, "combine(routing, z, y, weight, stream) -> status"},
@@ -565,9 +585,9 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_values = PyUnicode_InternFromString("values");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_numel = PyUnicode_InternFromString("numel");
-    PyObject **const names[] = {&s_shape, &s_stride, &s_dtype, &s_get_device, &s_is_contiguous, &s_tokens, &s_choices, &s_experts, &s_expert_ptr,
+    PyObject **const names[] = {&s_shape, &s_stride, &s_dtype, &s_get_device, &s_requires_grad, &s_is_contiguous, &s_tokens, &s_choices, &s_experts, &s_expert_ptr,
                                 &s_slot_choice, &s_choice_slot, &s_nbytes};
-    const char *const spelt[] = {"shape", "stride", "dtype", "get_device", "is_contiguous", "tokens", "choices", "experts", "expert_ptr",
+    const char *const spelt[] = {"shape", "stride", "dtype", "get_device", "requires_grad", "is_contiguous", "tokens", "choices", "experts", "expert_ptr",
                                  "slot_choice", "choice_slot", "nbytes"};
     for (size_t i = 0; i < sizeof spelt / sizeof *spelt; ++i)
         if (!(*names[i] = PyUnicode_InternFromString(spelt[i]))) return NULL;

@@ -4,6 +4,8 @@ experts and back with their gradients, products of 8-bit integers, the norm over
 The same manner as the calls on sparse matrices (binding.py): argument marshalling only, the work is the
 library's.  Outputs may be handed in or are allocated here (on the call's stream); a matrix is a 2-D tensor
 whose rows are contiguous.  A call's tensors are all on the current GPU (ValueError).
+No call keeps a history: a tensor that requires grad is refused while torch records one (RuntimeError); the gradients are calls
+of their own, for the backward of a torch.autograd.Function, say.
 """
 from __future__ import annotations
 
@@ -44,7 +46,7 @@ def _ready():
         L, m = B.lib(), B._marshal
         m.bind_routed(*(C.cast(f, C.c_void_p).value for f in (
             L.seer_route, L.seer_route_gather, L.seer_route_combine, L.seer_route_grad, L.seer_i8_quantize, L.seer_route_gather_i8,
-            L.seer_i8_product, L.seer_grad_norm, L.seer_grad_clip)), _current_device, *ids)
+            L.seer_i8_product, L.seer_grad_norm, L.seer_grad_clip)), _current_device, torch.is_grad_enabled, *ids)
         _types, _torch = ids, torch
     return B._marshal
 
