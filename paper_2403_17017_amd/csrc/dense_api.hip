@@ -209,6 +209,13 @@ int seer_route_grad(const seer_routing *r, const seer_dense *dy, const seer_dens
     return done();
 }
 
+// What a quantisation writes to q: the columns that are set to zero belong to it, too, also behind its last row.
+static Extent quantised_extent(const seer_dense *q)
+{
+    if (q->rows == 0) return {0, 0};
+    return extent(q->data, (size_t)((q->rows - 1) * q->ld + std::min<int64_t>(q->ld, (q->cols + 15) & ~(int64_t)15)));
+}
+
 // q and scale of `rows` rows, and their input.
 static int check_quantized(const seer_dense *x, const seer_dense *q, const float *scale, int64_t rows)
 {
@@ -216,9 +223,7 @@ static int check_quantized(const seer_dense *x, const seer_dense *q, const float
     const int rc = check_dense(q, rows, x->cols, SEER_I8);
     if (rc != SEER_OK) return rc;
     if (rows > 0 && bad_pointer(scale, 4)) return SEER_EINVAL;
-    // the columns that are set to zero belong to q, too, but behind its last row
-    const Extent qe = rows > 0 ? extent(q->data, (size_t)((rows - 1) * q->ld + std::min<int64_t>(q->ld, (x->cols + 15) & ~(int64_t)15)))
-                               : Extent{0, 0}, se = extent(scale, (size_t)rows * 4);
+    const Extent qe = quantised_extent(q), se = extent(scale, (size_t)rows * 4);
     if (overlap(qe, se) || overlap(qe, extent(x)) || overlap(se, extent(x))) return SEER_EINVAL;
     return SEER_OK;
 }
@@ -242,7 +247,7 @@ int seer_route_gather_i8(const seer_routing *r, const seer_dense *x, const seer_
     if ((rc = check_dense(x, r->tokens, x->cols, -1)) != SEER_OK || (rc = check_quantized(x, q, scale, count)) != SEER_OK) return rc;
     if (count == 0) return SEER_OK;
     const Extent slots = extent(r->choice_slot, (size_t)count * 4);
-    if (overlap(slots, extent(q)) || overlap(slots, extent(scale, (size_t)count * 4))) return SEER_EINVAL;
+    if (overlap(slots, quantised_extent(q)) || overlap(slots, extent(scale, (size_t)count * 4))) return SEER_EINVAL;
     launch_quantize(rows_of(r, x->cols), *x, *q, scale, on(stream));
     return done();
 }
