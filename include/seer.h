@@ -590,7 +590,7 @@ int seer_route_gather_i8(const seer_routing *r, const seer_dense *x, const seer_
  *   out[i][n] = a_scale[i] * b_scale[g][n] * sum_k a[i][k] * b[g][n][k]
  * for the rows i of group g, group_ptr[g] <= i < group_ptr[g + 1]; rows from group_ptr[groups] on are set to zero.
  * The sums are exact (32-bit integers: at most SEER_I8_MAX_K columns, else SEER_ELIMIT, as for more than SEER_MAX_EXPERTS
- * groups, or 2^30 or more tiles of 64 rows of one group by 64 channels).
+ * groups, or 2^30 or more tiles of 128 rows of one group by 128 channels).
  * a: SEER_I8.  b: SEER_I8 with groups * channels rows, the channels of group 0 first, and a's columns.  Fastest where data and
  * ld of both are multiples of 16; rows are then read in whole aligned pieces of 16 bytes, whatever lies behind their last column.
  * out: a's rows, `channels` = out's columns; SEER_F32, SEER_BF16 or SEER_F16.

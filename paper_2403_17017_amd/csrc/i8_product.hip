@@ -330,9 +330,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || BUFFERS == 2 ? 2 : 1) voi
     using Shape = TileShape<WAVES, WC, CI, TJ, BUFFERS>;
     constexpr uint32_t TOKENS = Shape::kTokens, LA = Shape::kLoadsA, LB = Shape::kLoadsB;
     // (arrays of their own: the compiler knows that loads into one are nothing to reads from another)
-    static_assert(BUFFERS >= 2 && BUFFERS <= 4, "");
-    __shared__ __attribute__((aligned(1024))) int8_t s_0[Shape::kBytes], s_1[Shape::kBytes], s_2[BUFFERS > 2 ? Shape::kBytes : 16], s_3[BUFFERS > 3 ? Shape::kBytes : 16];
-    int8_t *const buffer[4] = {s_0, s_1, BUFFERS > 2 ? s_2 : s_0, BUFFERS > 3 ? s_3 : s_0};
+    static_assert(BUFFERS == 2 || BUFFERS == 3, "");
+    __shared__ __attribute__((aligned(1024))) int8_t s_0[Shape::kBytes], s_1[Shape::kBytes], s_2[BUFFERS > 2 ? Shape::kBytes : 16];
+    int8_t *const buffer[3] = {s_0, s_1, BUFFERS > 2 ? s_2 : s_0};
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), lane = threadIdx.x & 63;
     const uint32_t across = (a.channels + kTileChannels - 1) / kTileChannels;
     Tile t;
@@ -488,7 +488,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || BUFFERS == 2 ? 2 : 1) voi
         static_assert(kPer * TJ * 16 * ROW <= Shape::kBytes && CI % CIP == 0, "the waves' regions fit");
         step_barrier<0>();                              // nothing is on its way to LDS, and nobody reads the last columns any more
         const uint32_t turn = wave / kPer;
-        int8_t *mine = (turn == 0 ? buffer[0] : turn == 1 ? buffer[1] : turn == 2 ? buffer[2] : buffer[3]) + (wave % kPer) * (TJ * 16 * ROW);
+        int8_t *mine = (turn == 0 ? buffer[0] : turn == 1 ? buffer[1] : buffer[2]) + (wave % kPer) * (TJ * 16 * ROW);
 #pragma unroll
         for (int first = 0; first < CI; first += CIP) {
 #pragma unroll
@@ -676,8 +676,8 @@ static uint64_t most_blocks(const I8Args &a, uint32_t tokens, uint32_t channels)
     return (most_tiles(a, tokens) * ((a.channels + channels - 1) / channels) + kXCD - 1) / kXCD * kXCD;
 }
 
-// The arithmetic on tiles is 32-bit.
-bool i8_product_fits(const I8Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, 64, 64) < (1u << 30); }
+// The arithmetic on tiles is 32-bit; of the tiles for any address, which no other kernel's launches outnumber (i8_plan), there are the most.
+bool i8_product_fits(const I8Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, kAnyTokens, kAnyChannels) < (1u << 30); }
 
 template <class T, int WAVES, int WC, int CI, int TJ, int BUFFERS>
 static void launch_tiles(const I8Args &a, hipStream_t st)

@@ -47,3 +47,9 @@ def test_rows_off_multiples_of_16_bytes_are_priced_by_their_own_kernels():
     # rows too far apart for the tiles: the same choice, without a workspace
     assert kernel(97, 16, 3104, ld=1 << 23) == "few" and S.i8_product_workspace_bytes(97, 16, 3104) > 0
 
+
+
+def test_most_tiles():
+    """2^30 tiles of 128 rows by 128 channels are too many for 32-bit numbers of tiles."""
+    assert kernel(1 << 22, 1 << 22, 1) == -6 and kernel((1 << 22) - 1024, (1 << 22) - 1024, 1) in S.I8_KERNELS
+    assert kernel(1 << 20, 1 << 19, 1, groups=4096) == -1 and kernel(4, 8, 1, groups=4097) == -6
