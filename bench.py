@@ -66,18 +66,38 @@ def load_model():
     return S.Model(t), {}, "hand-written default (no trained model file)"
 
 
-def kernel_source_sha16():
-    """Fingerprint of the device code of the sparse products (every file under csrc/ but those of the
-    routed layer, which no sparse kernel includes): a profile summary taken from other sources is stale."""
+#: The device code of the routed layer, which no sparse kernel includes; common.hiph is part of both.
+ROUTED_SOURCES = ("dense.hiph", "dense_api.hip", "dense_launch.h", "grad_norm.hip", "i8_pieces.hiph", "i8_product.hip", "route.hip")
+
+
+def _sha16(wanted):
     import hashlib
-    routed = ("dense.hiph", "dense_api.hip", "dense_launch.h", "grad_norm.hip", "i8_pieces.hiph", "i8_product.hip", "route.hip")
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2403_17017_amd", "csrc")
     for name in sorted(os.listdir(d)):
-        if name.endswith((".hip", ".hiph", ".h")) and name not in routed:
+        if name.endswith((".hip", ".hiph", ".h")) and wanted(name):
             with open(os.path.join(d, name), "rb") as fh:
                 h.update(name.encode() + b"\0" + fh.read())
     return h.hexdigest()[:16]
+
+
+def kernel_source_sha16():
+    """Fingerprint of the device code of the sparse products (every file under csrc/ but those of the
+    routed layer): a profile summary taken from other sources is stale."""
+    return _sha16(lambda name: name not in ROUTED_SOURCES)
+
+
+def routed_source_sha16():
+    """The same of the routed layer's."""
+    return _sha16(lambda name: name in ROUTED_SOURCES or name == "common.hiph")
+
+
+def routed_profile(path=None):
+    """Whether the committed summary of the routed layer's kernels was taken from the sources as they are."""
+    path = path or os.path.join(ROOT, "profiles", "kernel_trace_routed.txt")
+    if not os.path.exists(path):
+        return {"file": None, "stale": None}
+    return {"file": os.path.relpath(path, ROOT), "stale": _read_summary(path).get("source_sha16") != routed_source_sha16()}
 
 
 def _read_summary(path):
@@ -638,6 +658,7 @@ def main():
                     "product_us_on_gpu_timeline": round(g, 2),
                     "n_products_best_direct_kernel_us": round(n_it * best_direct, 1)}
         del warm
+        extras["routed_profile"] = routed_profile()
         extras["stream_copy_ceiling_gbps"] = round(stream_copy_ceiling(), 1)
         extras["read_ceiling_gbps"] = round(stream_read_ceiling(), 1)
         # warm, like the ceiling probe (which re-reads one set of buffers)
