@@ -709,8 +709,8 @@ static void launch_few(const I8Args &a, hipStream_t st)
 
 // Which kernel, and for how many shares of the columns: the one whose time by the following lines is the least.  They are fitted to 256
 // draws (one matrix, or 3 to 64 with rows to a group 1, 1 / sqrt(rank) or 1 / rank; 4 to 6000 rows to a group; 128 to 16 384 channels; 256 to
-// 11 000 columns; weights from memory, not from a cache), of which each kernel was timed: what is chosen takes
-// 2 % longer than the best one on average.
+// 11 000 columns; weights from memory, not from a cache), of which each kernel was timed.  Of 256 other draws, whose times are
+// kept in profiles/i8_kernel_times.csv, what is chosen takes 3 % longer than the best one on average, 1.6 times at most.
 //
 // Few rows: a workgroup reads its group's rows and its channels at some 24 GB/s, and so does a CU that has several.  Where lengths
 // differ, a group may be four times as long as the mean.  (1 x 2960 x 1424, 88 rows: few rows 9.5 us, tiles 16;
@@ -720,8 +720,8 @@ static void launch_few(const I8Args &a, hipStream_t st)
 // 2048 columns, 64 groups of 8: 29 and 26).
 static uint32_t few_channels(const I8Args &a) { return (uint64_t)((a.channels + 31) / 32) * a.groups < 128 ? 16 : 32; }
 
-struct FewCost { double start, batch, rate /* thousand bytes a us */, read /* million */; };
-constexpr FewCost kFewPieces = {4, 1.2, 24, 5.8}, kFewWords = {4, 3, 15, 2.4};
+struct FewCost { double start, batch, each /* 64 rows of a workgroup, where a CU has several */, rate /* thousand bytes a us */, read /* million */; };
+constexpr FewCost kFewPieces = {4, 1.2, 0, 24, 5.8}, kFewWords = {3.5, 1.6, 1.2, 16, 2.1};
 
 static double few_cost(const I8Args &a, const FewCost &c)
 {
@@ -729,7 +729,7 @@ static double few_cost(const I8Args &a, const FewCost &c)
     const double workgroups = (double)((a.channels + few_channels(a) - 1) / few_channels(a)) * a.groups;
     const double rows = std::max((mean + channels) * workgroups / kCUs, (a.group_ptr ? 4 : 1) * mean + channels);
     const double batches = a.rows / a.groups / kFewRows;        // (behind the first)
-    return std::max(c.start + c.batch * batches + rows * a.columns / (1e3 * c.rate), (double)a.groups * a.channels * a.columns / (1e6 * c.read));
+    return std::max(c.start + c.batch * batches + c.each * (batches + 1) * workgroups / kCUs + rows * a.columns / (1e3 * c.rate), (double)a.groups * a.channels * a.columns / (1e6 * c.read));
 }
 
 // Tiles: rounds of as many as there is room for, `round` each and `least` to `least + more` for a step of 64 columns by how many are at
@@ -784,9 +784,10 @@ static Choice choose(const I8Args &a)
 }
 
 // Rows off multiples of 16 bytes: few rows, in realigned words, or the tiles for any address, two workgroups of which are on a CU.  Fitted
-// to 117 draws like those above with rows at odd addresses, both kernels timed: what is chosen takes 1 % longer than the better one
-// on average, 1.4 times at most.  Measured, us, any and few: 97 x 16 x 3089 40 and 23, 100 x 512 x 8190 105 and 62, 47 x 656 x 8946 140 and 36;
-// 500 x 130 x 4111 57 and 113, 3001 x 5001 x 4111 152 and 875, 17 x 186 x 2278, mean 85, longest 682 9.9 and 28.
+// to 373 draws like those above with rows at odd addresses, both kernels timed (the same file): what is chosen takes 1.4 % longer than the better
+// one on average, 1.6 times at most.  Measured, us, any and few: 97 x 16 x 3089 40 and 23, 100 x 512 x 8190 105 and 62, 47 x 656 x 8946 140 and 36;
+// 500 x 130 x 4111 57 and 113, 3001 x 5001 x 4111 152 and 875, 17 x 186 x 2278, mean 85, longest 682 9.9 and 28, 39 x 2168 x 123,
+// mean 165, 33 and 89.
 static bool few_words(const I8Args &a)
 {
     const double steps = (a.columns + kAnyCols - 1) / kAnyCols;

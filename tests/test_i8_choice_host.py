@@ -1,6 +1,9 @@
 """Which kernel an 8-bit product takes: the host-side query, by sizes and alignment alone."""
+import csv
 import ctypes as C
+import os
 
+import numpy as np
 import pytest
 import torch
 
@@ -53,3 +56,33 @@ def test_most_tiles():
     """2^30 tiles of 128 rows by 128 channels are too many for 32-bit numbers of tiles."""
     assert kernel(1 << 22, 1 << 22, 1) == -6 and kernel((1 << 22) - 1024, (1 << 22) - 1024, 1) in S.I8_KERNELS
     assert kernel(1 << 20, 1 << 19, 1, groups=4096) == -1 and kernel(4, 8, 1, groups=4097) == -6
+
+
+def test_many_short_rows_off_multiples_of_16_bytes():
+    """Thousands of workgroups of few columns each cost few rows more than their bytes."""
+    for size, groups in (((6435, 2168, 123), 39), ((21850, 2984, 111), 46), ((2968, 13736, 86), 7)):
+        assert kernel(*size, groups=groups, at=1) == "any", size       # 33, 107 and 66 us; few rows 89, 261 and 143
+
+
+def measured(where):
+    import bench
+    with open(os.path.join(bench.ROOT, "profiles", "i8_kernel_times.csv")) as f:
+        rows = list(csv.DictReader(line for line in f if not line.startswith("#")))
+    for r in (r for r in rows if r["rows_at"] == where):
+        times = {k: float(r[k]) for k in ("any", "few", "tiles_64", "tiles_128", "tiles_256", "shared", "chosen") if r[k]}
+        yield kernel(int(r["rows"]), int(r["channels"]), int(r["columns"]), groups=int(r["groups"]), at=where == "odd"), r["kernel"], times
+
+
+def test_choice_on_measured_draws_at_odd_addresses():
+    lost = [times[k] / min(times.values()) for k, _, times in measured("odd") if k in times]
+    assert len(lost) > 350
+    assert np.exp(np.mean(np.log(lost))) < 1.02 and max(lost) < 1.7
+
+
+def test_choice_on_measured_draws():
+    """The times of the kernel that was chosen when they were taken; it is of the same kind now."""
+    lost = []
+    for now, then, times in measured("aligned"):
+        assert now == then
+        lost.append(times.pop("chosen") / min(times.values()))
+    assert len(lost) == 256 and np.exp(np.mean(np.log(lost))) < 1.04 and max(lost) < 1.7
