@@ -2,7 +2,8 @@
 // rows; the work is cut into chunks of equal size whatever tensor they belong to.  Where the tensors lie travels in
 // the kernel arguments, as many as fit 4 KB at a time.  Bound by bytes: every gradient is read for the norm and, since that has to be
 // known first, once more; the second pass goes backwards, so that it begins with what the first has left in the last-level cache.
-// A billion bf16 in 291 tensors: 320 us for the norm (6.2 TB/s, a read's rate), 730 for the scaling (5.5 TB/s), two launches each.
+// A billion bf16 in 291 tensors: 335 us for the norm (6.0 TB/s, near a read's rate), 717 for the scaling into a bucket (5.6 TB/s), 735 in place,
+// two launches each; in place with nothing to scale 90, for a walk over the chunks that reads the first of each workgroup.
 #include "dense.hiph"
 #include "dense_launch.h"
 

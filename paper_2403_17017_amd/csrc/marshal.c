@@ -172,10 +172,10 @@ static int (*f_product)(const seer_dense *, const float *, const seer_dense *, c
 static int (*f_norm)(const seer_grad *, int32_t, float *, void *, size_t, void *);
 static int (*f_clip)(const seer_grad *, int32_t, float, float *, void *, size_t, void *);
 
-static PyObject *s_shape, *s_stride, *s_dtype, *s_get_device, *s_requires_grad, *s_is_contiguous, *s_tokens, *s_choices, *s_experts, *s_expert_ptr,
+static PyObject *s_shape, *s_stride, *s_dtype, *s_get_device, *s_initialized, *s_get_current, *s_requires_grad, *s_is_contiguous, *s_tokens, *s_choices, *s_experts, *s_expert_ptr,
     *s_slot_choice, *s_choice_slot, *s_nbytes;
 static PyObject *types[6];                   /* torch's dtypes in the order of seer_type */
-static PyObject *current_device;             /* what gives the number of the current GPU */
+static PyObject *t_c, *t_cuda;               /* torch._C and torch.cuda, which know the current GPU */
 static PyObject *grad_enabled;               /* what says whether torch records a history */
 
 static int refuse(PyObject *error, const char *what, const char *is)
@@ -246,12 +246,16 @@ static int on_gpu(PyObject *t, const char *what, int *gpu)
     return at < 0 ? refuse(PyExc_ValueError, what, "is not on a GPU") : same_gpu(at, what, gpu);
 }
 
-/* The library launches on the current GPU. */
+/* The library launches on the current GPU (the first one, before torch has looked for them). */
 static int is_current(int gpu)
 {
-    uint64_t now;
+    uint64_t now = 0;
     if (gpu < 0) return 0;
-    if (taken(PyObject_CallNoArgs(current_device), as_size, &now)) return -1;
+    PyObject *known = PyObject_GetAttr(t_cuda, s_initialized);
+    if (!known) return -1;
+    const int ask = PyObject_IsTrue(known);
+    Py_DECREF(known);
+    if (ask < 0 || (ask && taken(PyObject_CallMethodNoArgs(t_c, s_get_current), as_size, &now))) return -1;
     if ((int32_t)now == gpu) return 0;
     PyErr_Format(PyExc_ValueError, "the tensors are on GPU %d and the current one is %d", gpu, (int)(int32_t)now);
     return -1;
@@ -527,8 +531,8 @@ static PyObject *m_clip(PyObject *self, PyObject *const *a, Py_ssize_t n)
 static PyObject *m_bind_routed(PyObject *self, PyObject *args)
 {
     unsigned long long f[9];
-    PyObject *t[6], *device, *grad;
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKOOOOOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, &device, &grad, t, t + 1, t + 2,
+    PyObject *t[6], *c, *cuda, *grad;
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKOOOOOOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, f + 7, f + 8, &c, &cuda, &grad, t, t + 1, t + 2,
                           t + 3, t + 4, t + 5))
         return NULL;
     f_route = P(int (*)(const void *, int32_t, const seer_routing *, void *, size_t, void *), f[0]);
@@ -543,8 +547,10 @@ static PyObject *m_bind_routed(PyObject *self, PyObject *args)
     f_clip = P(int (*)(const seer_grad *, int32_t, float, float *, void *, size_t, void *), f[8]);
     Py_INCREF(grad);
     Py_XSETREF(grad_enabled, grad);
-    Py_INCREF(device);
-    Py_XSETREF(current_device, device);
+    Py_INCREF(c);
+    Py_XSETREF(t_c, c);
+    Py_INCREF(cuda);
+    Py_XSETREF(t_cuda, cuda);
     for (int i = 0; i < 6; ++i) {
         Py_INCREF(t[i]);
         Py_XSETREF(types[i], t[i]);
@@ -560,7 +566,7 @@ static PyMethodDef methods[] = {
      "spmv_model(model address, A, x, y, workspace, stream) -> (status, path, kernel id)"},
     {"spmv_prepared", (PyCFunction)(void (*)(void))m_prepared, METH_FASTCALL,
      "spmv_prepared(plan address, A, x, y, workspace, stream) -> status"},
-    {"bind_routed", m_bind_routed, METH_VARARGS, "bind_routed(addresses of the routed layer's functions, what gives the current GPU, and whether a history is recorded, torch's dtypes)"},
+    {"bind_routed", m_bind_routed, METH_VARARGS, "bind_routed(addresses of the routed layer's functions, torch._C, torch.cuda, whether a history is recorded, torch's dtypes)"},
     {"route", (PyCFunction)(void (*)(void))m_route, METH_FASTCALL, "route(expert, routing, workspace, stream) -> status"},
     {"gather", (PyCFunction)(void (*)(void))m_gather, METH_FASTCALL, "gather(routing, x, out, weight, stream) -> status"},
     {"combine", (PyCFunction)(void (*)(void))m_combine, METH_FASTCALL, "combine(routing, z, y, weight, stream) -> status"},
@@ -585,9 +591,9 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_values = PyUnicode_InternFromString("values");
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_numel = PyUnicode_InternFromString("numel");
-    PyObject **const names[] = {&s_shape, &s_stride, &s_dtype, &s_get_device, &s_requires_grad, &s_is_contiguous, &s_tokens, &s_choices, &s_experts, &s_expert_ptr,
+    PyObject **const names[] = {&s_shape, &s_stride, &s_dtype, &s_get_device, &s_initialized, &s_get_current, &s_requires_grad, &s_is_contiguous, &s_tokens, &s_choices, &s_experts, &s_expert_ptr,
                                 &s_slot_choice, &s_choice_slot, &s_nbytes};
-    const char *const spelt[] = {"shape", "stride", "dtype", "get_device", "requires_grad", "is_contiguous", "tokens", "choices", "experts", "expert_ptr",
+    const char *const spelt[] = {"shape", "stride", "dtype", "get_device", "_initialized", "_cuda_getDevice", "requires_grad", "is_contiguous", "tokens", "choices", "experts", "expert_ptr",
                                  "slot_choice", "choice_slot", "nbytes"};
     for (size_t i = 0; i < sizeof spelt / sizeof *spelt; ++i)
         if (!(*names[i] = PyUnicode_InternFromString(spelt[i]))) return NULL;

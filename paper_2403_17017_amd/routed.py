@@ -46,20 +46,15 @@ def _ready():
         L, m = B.lib(), B._marshal
         m.bind_routed(*(C.cast(f, C.c_void_p).value for f in (
             L.seer_route, L.seer_route_gather, L.seer_route_combine, L.seer_route_grad, L.seer_i8_quantize, L.seer_route_gather_i8,
-            L.seer_i8_product, L.seer_grad_norm, L.seer_grad_clip)), _current_device, torch.is_grad_enabled, *ids)
+            L.seer_i8_product, L.seer_grad_norm, L.seer_grad_clip)), torch._C, torch.cuda, torch.is_grad_enabled, *ids)
         _types, _torch = ids, torch
     return B._marshal
 
 
-def _current_device() -> int:
-    """The number of the GPU that calls run on (the first one, before torch has looked for them)."""
-    return _torch._C._cuda_getDevice() if _torch.cuda._initialized else 0
-
-
 def _handle(stream) -> int:
     """As _stream_handle; a torch stream is one of the current GPU's."""
-    if stream is not None and hasattr(stream, "cuda_stream") and stream.device_index != _current_device():
-        raise ValueError(f"the stream is GPU {stream.device_index}'s and the current one is {_current_device()}")
+    if stream is not None and hasattr(stream, "cuda_stream") and stream.device_index != _torch._C._cuda_getDevice():
+        raise ValueError(f"the stream is GPU {stream.device_index}'s and the current one is {_torch._C._cuda_getDevice()}")
     return _stream_handle(stream)
 
 
