@@ -67,7 +67,8 @@ def load_model():
 
 
 #: The device code of the routed layer, which no sparse kernel includes; common.hiph is part of both.
-ROUTED_SOURCES = ("dense.hiph", "dense_api.hip", "dense_launch.h", "grad_norm.hip", "i8_pieces.hiph", "i8_product.hip", "route.hip")
+ROUTED_SOURCES = ("choose.hip", "dense.hiph", "dense_api.hip", "dense_checks.h", "dense_launch.h", "embed.hip", "grad_norm.hip", "i8_pieces.hiph",
+                  "i8_product.hip", "mx4.hip", "ragged.hiph", "route.hip", "token_api.hip")
 
 
 def _sha16(wanted):

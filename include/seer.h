@@ -22,7 +22,7 @@
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All
  *     device work is enqueued on it.  seer_spmv, seer_spmv_auto, seer_spmv_model and
  *     seer_spmv_prepared return without waiting, and so do all calls of a routed layer (seer_route to
- *     seer_grad_clip); seer_features, seer_spmv_prepare and seer_spmv_plan wait for their own result because they return host values.
+ *     seer_embed_grad); seer_features, seer_spmv_prepare and seer_spmv_plan wait for their own result because they return host values.
  *   - Every call returns SEER_OK (0) or a negative seer_status; on error no output
  *     is written.  Nothing throws or aborts.  Matrix contents (monotone row_ptr,
  *     column range) are NOT validated: they are the caller's contract.
@@ -55,8 +55,8 @@ typedef enum {
     SEER_EWORKSPACE = -4, /* workspace missing, misaligned or too small               */
     SEER_EHIP = -5,       /* a HIP runtime call failed; see seer_last_hip_error()     */
     SEER_ELIMIT = -6      /* seer_spmv_auto_static: the matrix needs more scratch than
-                             the library's built-in array holds; seer_route, seer_i8_product:
-                             more experts or columns than they take                     */
+                             the library's built-in array holds; calls of a routed layer:
+                             more experts, choices or columns than they take            */
 } seer_status;
 
 /* Kernel ids: the CSR rows of Table II ("load balancing schedules"), in its order. */
@@ -615,6 +615,34 @@ typedef enum {
 } seer_i8_kernel;
 int seer_i8_product_kernel(const seer_dense *a, const seer_dense *b, const int32_t *group_ptr, int32_t groups);
 
+/* Rows in 4-bit floating point: 32 consecutive values are a block of 16 bytes, two to a byte, the first in the lower half, and share a
+ * scale.  A value is a sign (bit 3) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 2 to 0), times 2^(scale byte - 127); a block whose scale byte is
+ * 255 is NaN throughout.  Row i: blocks of 16 bytes from data + i * ld on, scale bytes from scale + i * scale_ld on, ceil(cols / 32) of both.
+ * The values of the last block behind the last column are zeros.  data: DEVICE, a multiple of 16, and ld, too, where there is more than one
+ * row.  rows and cols below 2^31. */
+typedef struct {
+    void *data;
+    void *scale;
+    int64_t rows, cols, ld, scale_ld; /* ld and scale_ld in bytes */
+} seer_mx4;
+
+/* Rows in 4 bits: a block's scale is 2^(floor(log2 of its largest magnitude) - 2), at least 2^-127, and every value is divided by it (exactly)
+ * and taken to the nearest, ties to the even code; more than 6 becomes 6.  A block with an infinity or a NaN has scale byte 255 and
+ * codes 0.  q has x's rows and columns; x is SEER_F32, SEER_BF16 or SEER_F16. */
+int seer_mx4_quantize(const seer_dense *x, const seer_mx4 *q, void *stream);
+
+/* seer_route_gather without weights into 4 bits: q has tokens * choices rows; rows of slots that are no expert's are 0 with scale bytes 0. */
+int seer_route_gather_mx4(const seer_routing *r, const seer_dense *x, const seer_mx4 *q, void *stream);
+
+/* Products of rows in 4 bits: out[i][n] = sum_k a[i][k] * b[g][n][k] for the rows i of group g, group_ptr[g] <= i < group_ptr[g + 1];
+ * rows from group_ptr[groups] on are set to zero.  Products are exact, sums are in fp32, the same on every run, rounded to out's type
+ * once.  b has groups * channels rows, the channels of group 0 first, and a's columns; out: a's rows, `channels` = out's columns;
+ * SEER_F32, SEER_BF16 or SEER_F16.  group_ptr as in seer_i8_product.  SEER_ELIMIT for more than SEER_MAX_EXPERTS groups, or 2^30 or
+ * more tiles of 128 rows of one group by 128 channels. */
+int seer_mx4_product(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups, const seer_dense *out,
+                     void *workspace, size_t workspace_bytes, void *stream);
+size_t seer_mx4_product_workspace_bytes(int64_t rows, int64_t channels, int64_t columns, int32_t groups);
+
 /* One of the many tensors whose gradient is clipped: n contiguous elements. */
 typedef struct {
     const void *grad; /* DEVICE */
@@ -636,6 +664,55 @@ size_t seer_grad_workspace_bytes(void);
  * makes c 0 or NaN: norm says so.  max_norm >= 0 (SEER_EINVAL). */
 int seer_grad_clip(const seer_grad *tensors, int32_t count, float max_norm, float *norm, void *workspace,
                    size_t workspace_bytes, void *stream);
+
+/* How experts are chosen from a router's logits. */
+typedef enum { SEER_SOFTMAX = 0, SEER_SIGMOID = 1 } seer_score;
+#define SEER_MAX_CHOICES 64
+#define SEER_MAX_EXPERT_GROUPS 64
+typedef struct {
+    int32_t choices;     /* of each token: 1 .. SEER_MAX_CHOICES, and no more than there are experts in best_groups groups */
+    int32_t score;       /* seer_score */
+    int32_t groups;      /* the experts in that many runs of equal length, 1 .. SEER_MAX_EXPERT_GROUPS; 1: no groups       */
+    int32_t best_groups; /* choices come from that many groups, 1 .. groups                                                */
+    int32_t group_best;  /* a group counts as much as its best key (1), or as the sum of its two best scores, with the
+                            bias if there is one (2); as its one where it has one                                          */
+    int32_t renormalise; /* nonzero: the scores chosen are divided by their sum                                            */
+    float factor;        /* and multiplied by this, which is finite                                                        */
+} seer_choice;
+
+/* The experts of every token and their weights.  With s = softmax(logits[t]) or the sigmoids, an expert's key is s + bias, or, without a
+ * bias, its logit, which is in the same order.  Of the best_groups groups that count most the `choices` experts with the largest
+ * keys are chosen, the largest first: expert[t][k], and weight[t][k] = factor * s, divided by the sum of the chosen s if
+ * renormalise (without loss where every s is too small for fp32).  Keys and groups' sums are compared as 64-bit numbers hold them, ties go
+ * to the lower number, a NaN counts as the largest.  An expert whose logit, or bias, is -infinity is not chosen; where there are not
+ * enough others, expert is -1 (nobody's to seer_route) with weight 0.  A softmax over a NaN or +infinity is NaN throughout.
+ * logits: [tokens][experts], SEER_F32, SEER_BF16 or SEER_F16, at most SEER_MAX_EXPERTS columns (SEER_ELIMIT).  bias: DEVICE
+ * fp32 [experts], or NULL.  expert: DEVICE int32 [tokens][choices].  weight: DEVICE fp32 [tokens][choices]. */
+int seer_route_choose(const seer_dense *logits, const float *bias, const seer_choice *how, int32_t *expert,
+                      float *weight, void *stream);
+
+/* The gradient of seer_route_choose's weights in the logits, for that of its output, dweight (DEVICE fp32 [tokens][choices]); what is
+ * chosen counts as given, so no bias is wanted.  Renormalised, with w' = weight / factor (of the chosen logits alone): for the k-th choice
+ * factor * w'_k * (dweight_k - sum_j w'_j dweight_j), times 1 - s for sigmoids.  Else factor * s_k (1 - s_k) dweight_k for
+ * sigmoids, and factor * s_e * ([e chosen] dweight_e - sum_k s_k dweight_k) for every e of a softmax.  All other entries are 0.
+ * expert: DEVICE int32 [tokens][choices], any in any order; an entry outside [0, experts), or with a logit of -infinity, is no choice,
+ * one that comes twice is two.  dlogits: the shape and type of logits, computed in fp32 or more, rounded once. */
+int seer_route_choose_grad(const seer_dense *logits, const seer_choice *how, const int32_t *expert, const float *dweight,
+                           const seer_dense *dlogits, void *stream);
+
+/* Rows of a table by token: out[t] = scale * table[token[t]] (a product in fp32, rounded once; scale 1 copies bit by bit), and
+ * a row of zeros for a token outside [0, table->rows) (-1 for padding, say).  token: DEVICE [out->rows], of index_type SEER_I32 or
+ * SEER_I64.  out: the columns and type of table; SEER_F32, SEER_BF16 or SEER_F16. */
+int seer_embed(const void *token, int32_t index_type, const seer_dense *table, float scale, const seer_dense *out,
+               void *stream);
+
+/* The gradient of seer_embed in the table: dtable[v] = scale * sum over the t with token[t] == v of dy[t], and zeros for rows that are
+ * no token's; accumulate nonzero: dtable[v] += that, and those rows are neither read nor written.  The tokens are sorted, and sums
+ * are in fp32, in an order that the tokens alone decide; one rounding.  dy: a row for each of its dy->rows tokens.
+ * dtable: dy's type or SEER_F32.  workspace: >= seer_embed_grad_workspace_bytes(dy->rows, dtable->rows, dy->cols). */
+int seer_embed_grad(const void *token, int32_t index_type, const seer_dense *dy, float scale, int32_t accumulate,
+                    const seer_dense *dtable, void *workspace, size_t workspace_bytes, void *stream);
+size_t seer_embed_grad_workspace_bytes(int64_t tokens, int64_t rows, int64_t columns);
 
 int seer_num_kernels(void);
 const char *seer_kernel_name(int kernel_id); /* "CSR,TM" ...; NULL if out of range  */

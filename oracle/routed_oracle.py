@@ -79,3 +79,48 @@ def grad_norm(grads):
 
 def clip_factor(norm, max_norm):
     return min(1.0, max_norm / (norm + 1e-6))
+
+
+MX4_VALUES = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6])
+
+
+def mx4_quantize(x):
+    """(codes [rows, 16 * blocks], two to a byte, the first in the lower half; scale bytes [rows, blocks]) of float64 rows."""
+    rows, cols = x.shape
+    blocks = -(-cols // 32)
+    wide = np.zeros((rows, blocks * 32))
+    wide[:, :cols] = x
+    codes, scale = np.zeros((rows, blocks * 32), np.uint8), np.zeros((rows, blocks), np.uint8)
+    for i in range(rows):
+        for b in range(blocks):
+            v = wide[i, 32 * b: 32 * b + 32]
+            top = np.abs(v).max()
+            if not np.isfinite(top):
+                scale[i, b] = 255
+                continue
+            e = max(int(np.frexp(top)[1]) - 3, -127) if top > 0 else -127
+            scale[i, b] = e + 127
+            off = np.abs(np.abs(v)[:, None] * 2.0 ** -e - MX4_VALUES[None, :8])
+            off[:, 1::2] *= 1 + 1e-12                                # the even code of two that are as near
+            codes[i, 32 * b: 32 * b + 32] = off.argmin(1) + 8 * np.signbit(v)
+    return codes[:, 0::2] | codes[:, 1::2] << 4, scale
+
+
+def mx4_values(codes, scale):
+    """float64 [rows, 32 * blocks]."""
+    codes = np.asarray(codes)
+    v = np.empty((*codes.shape[:-1], 2 * codes.shape[-1]))
+    v[..., 0::2], v[..., 1::2] = MX4_VALUES[codes & 15], MX4_VALUES[codes >> 4]
+    by = np.where(np.asarray(scale) == 255, np.nan, 2.0 ** (np.asarray(scale, np.float64) - 127))
+    return v * np.repeat(by, 32, axis=-1)
+
+
+def mx4_product(a, b, group_ptr=None):
+    """(float64 [rows, channels], the sum of the magnitudes) of values a [rows, k] and b [groups, channels, k]."""
+    rows, groups = a.shape[0], b.shape[0]
+    ptr = [0, rows] if group_ptr is None else np.clip(np.asarray(group_ptr, np.int64), 0, rows)
+    out, size = np.zeros((rows, b.shape[1])), np.zeros((rows, b.shape[1]))
+    for g in range(groups):
+        i = slice(int(ptr[g]), int(ptr[g + 1]))
+        out[i], size[i] = a[i] @ b[g].T, np.abs(a[i]) @ np.abs(b[g]).T
+    return out, size

@@ -171,8 +171,9 @@ def lib():
         L.seer_strerror.argtypes = [C.c_int]
         L.seer_strerror.restype = C.c_char_p
         L.seer_last_hip_error.restype = C.c_int
-        from .routed import bind
-        bind(L)
+        from . import embedding, mx4, routed, router
+        for part in (routed, router, mx4, embedding):
+            part.bind(L)
         _bind_marshal(L)
         _lib = L
     return _lib

@@ -1,67 +1,11 @@
 // C ABI of the routed layer and its training step: checks of arguments, then the launches.
-#include "dense_launch.h"
+#include "dense_checks.h"
 
 #include <cstdlib>
 
 using namespace seer;
 
 namespace {
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool is_float(int type) { return type == SEER_F32 || type == SEER_BF16 || type == SEER_F16; }
-size_t size_of(int type) { return type == SEER_F32 ? 4 : type == SEER_I8 ? 1 : 2; }
-
-// Bytes from `begin` to `end`; nothing if there are no elements.
-struct Extent {
-    uintptr_t begin, end;
-};
-Extent extent(const void *p, size_t bytes)
-{
-    const uintptr_t b = reinterpret_cast<uintptr_t>(p);
-    return {b, b + bytes};
-}
-Extent extent(const seer_dense *m)
-{
-    if (m->rows == 0 || m->cols == 0) return {0, 0};
-    return extent(m->data, (size_t)((m->rows - 1) * m->ld + m->cols) * size_of(m->type));
-}
-bool overlap(Extent a, Extent b) { return a.begin < b.end && b.begin < a.end; }
-
-bool bad_pointer(const void *p, size_t multiple) { return !p || reinterpret_cast<uintptr_t>(p) % multiple != 0; }
-
-// A dense matrix of the expected size; type -1: one of the floating types.
-int check_dense(const seer_dense *m, int64_t rows, int64_t cols, int type)
-{
-    if (!m || m->rows != rows || m->cols != cols || m->ld < cols) return SEER_EINVAL;
-    if (rows < 0 || cols < 0 || rows > INT32_MAX || cols > INT32_MAX) return SEER_EINVAL;
-    if (type < 0 ? !is_float(m->type) : m->type != type) return SEER_EINVAL;
-    // (the byte extent has to fit an address)
-    if (rows > 0 && m->ld > (INT64_MAX / 8) / rows) return SEER_EINVAL;
-    if (rows > 0 && cols > 0 && bad_pointer(m->data, size_of(m->type))) return SEER_EINVAL;
-    return SEER_OK;
-}
-
-int check_routing(const seer_routing *r, bool entries)
-{
-    if (!r || r->tokens < 0 || r->choices < 1 || r->experts < 1) return SEER_EINVAL;
-    if (r->experts > SEER_MAX_EXPERTS) return SEER_ELIMIT;
-    if ((int64_t)r->tokens * r->choices > INT32_MAX) return SEER_EINVAL;
-    if (entries && r->tokens > 0 && bad_pointer(r->choice_slot, 4)) return SEER_EINVAL;
-    return SEER_OK;
-}
-
-RouteRows rows_of(const seer_routing *r, int64_t cols)
-{
-    return RouteRows{r->choice_slot, (uint32_t)r->tokens, (uint32_t)r->choices, (uint32_t)cols};
-}
-
-int done()
-{
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? SEER_OK : hip_fail(e);
-}
-
-hipStream_t on(void *stream) { return static_cast<hipStream_t>(stream); }
 
 // Memory that a call reads, or writes.
 struct Span {
@@ -298,6 +242,88 @@ int seer_i8_product_kernel(const seer_dense *a, const seer_dense *b, const int32
              (uint32_t)a->rows, (uint32_t)(b->rows / groups), (uint32_t)a->cols, (uint32_t)groups, SEER_F32};
     if (!i8_product_fits(p)) return SEER_ELIMIT;
     return p.rows == 0 || p.channels == 0 ? SEER_I8_NONE : i8_plan(p).kernel;
+}
+
+// Rows of 4-bit values: their blocks are whole and lie at multiples of 16 bytes.
+static int check_mx4(const seer_mx4 *m, int64_t rows, int64_t cols)
+{
+    if (!m || m->rows != rows || m->cols != cols || rows < 0 || cols < 0 || rows > INT32_MAX || cols > INT32_MAX) return SEER_EINVAL;
+    const int64_t blocks = (cols + 31) / 32;
+    if (m->ld < 16 * blocks || (rows > 1 && cols > 0 && m->ld % 16 != 0) || m->scale_ld < blocks) return SEER_EINVAL;
+    if (rows > 0 && (m->ld > (INT64_MAX / 8) / rows || m->scale_ld > (INT64_MAX / 8) / rows)) return SEER_EINVAL;
+    if (rows > 0 && cols > 0 && (bad_pointer(m->data, 16) || !m->scale)) return SEER_EINVAL;
+    return SEER_OK;
+}
+static Extent codes_extent(const seer_mx4 *m)
+{
+    if (m->rows == 0 || m->cols == 0) return {0, 0};
+    return extent(m->data, (size_t)((m->rows - 1) * m->ld + (m->cols + 31) / 32 * 16));
+}
+static Extent scales_extent(const seer_mx4 *m)
+{
+    if (m->rows == 0 || m->cols == 0) return {0, 0};
+    return extent(m->scale, (size_t)((m->rows - 1) * m->scale_ld + (m->cols + 31) / 32));
+}
+
+static int quantize_mx4(const RouteRows &r, const seer_dense *x, const seer_mx4 *q, int64_t rows, Extent slots, void *stream)
+{
+    int rc;
+    if ((rc = check_dense(x, r.tokens, x->cols, -1)) != SEER_OK || (rc = check_mx4(q, rows, x->cols)) != SEER_OK) return rc;
+    if (rows == 0 || x->cols == 0) return SEER_OK;
+    const Extent codes = codes_extent(q), scales = scales_extent(q), in = extent(x);
+    if (overlap(codes, scales) || overlap(codes, in) || overlap(scales, in) || overlap(codes, slots) || overlap(scales, slots)) return SEER_EINVAL;
+    launch_mx4_quantize(r, *x, *q, on(stream));
+    return done();
+}
+
+int seer_mx4_quantize(const seer_dense *x, const seer_mx4 *q, void *stream)
+{
+    if (!x || x->rows < 0 || x->rows > INT32_MAX) return SEER_EINVAL;
+    return quantize_mx4(RouteRows{nullptr, (uint32_t)x->rows, 1, (uint32_t)x->cols}, x, q, x->rows, Extent{0, 0}, stream);
+}
+
+int seer_route_gather_mx4(const seer_routing *r, const seer_dense *x, const seer_mx4 *q, void *stream)
+{
+    const int rc = check_routing(r, true);
+    if (rc != SEER_OK) return rc;
+    if (!x) return SEER_EINVAL;
+    const int64_t count = (int64_t)r->tokens * r->choices;
+    return quantize_mx4(rows_of(r, x->cols), x, q, count, extent(r->choice_slot, (size_t)count * 4), stream);
+}
+
+size_t seer_mx4_product_workspace_bytes(int64_t rows, int64_t channels, int64_t columns, int32_t groups)
+{
+    if (rows < 0 || channels < 0 || columns < 0 || groups < 1 || rows > INT32_MAX || channels > INT32_MAX || columns > INT32_MAX) return 0;
+    return mx4_workspace_bytes((uint32_t)rows, (uint32_t)channels, (uint32_t)((columns + 31) / 32), (uint32_t)groups);
+}
+
+int seer_mx4_product(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups, const seer_dense *out, void *workspace,
+                     size_t workspace_bytes, void *stream)
+{
+    if (!a || !b || !out || groups < 1 || (!group_ptr && groups != 1)) return SEER_EINVAL;
+    int rc;
+    if ((rc = check_mx4(a, a->rows, a->cols)) != SEER_OK || (rc = check_dense(out, a->rows, out->cols, -1)) != SEER_OK) return rc;
+    if (out->cols > INT32_MAX / groups) return SEER_EINVAL;
+    if ((rc = check_mx4(b, (int64_t)groups * out->cols, a->cols)) != SEER_OK) return rc;
+    if (groups > SEER_MAX_EXPERTS) return SEER_ELIMIT;
+    if (a->rows == 0 || out->cols == 0) return SEER_OK;
+    if (group_ptr && bad_pointer(group_ptr, 4)) return SEER_EINVAL;
+    const Extent to = extent(out), ins[] = {codes_extent(a), codes_extent(b), scales_extent(a), scales_extent(b),
+                                            extent(group_ptr, group_ptr ? ((size_t)groups + 1) * 4 : 0)};
+    for (const Extent &in : ins)
+        if (overlap(to, in)) return SEER_EINVAL;
+    const auto bytes = [](const void *p) { return static_cast<const uint8_t *>(p); };
+    const Mx4Args p{bytes(a->data), bytes(b->data), bytes(a->scale), bytes(b->scale), group_ptr, out->data, a->ld, b->ld, a->scale_ld, b->scale_ld, out->ld,
+                    (uint32_t)a->rows, (uint32_t)out->cols, (uint32_t)((a->cols + 31) / 32), (uint32_t)groups, out->type};
+    if (!mx4_product_fits(p)) return SEER_ELIMIT;
+    const size_t need = mx4_workspace_bytes(p.rows, p.channels, p.blocks, p.groups);
+    if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return SEER_EWORKSPACE;
+    const Extent ws = extent(workspace, need);
+    if (overlap(ws, to)) return SEER_EINVAL;
+    for (const Extent &in : ins)
+        if (overlap(ws, in)) return SEER_EINVAL;
+    launch_mx4_product(p, workspace, on(stream));
+    return done();
 }
 
 size_t seer_grad_workspace_bytes(void) { return grad_workspace_bytes(); }

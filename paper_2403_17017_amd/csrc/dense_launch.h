@@ -42,9 +42,32 @@ I8Plan i8_plan(const I8Args &a);            // by sizes and by where the operand
 size_t i8_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t columns, uint32_t groups);
 void launch_i8_product(const I8Args &a, const I8Plan &p, void *workspace, hipStream_t st);
 
+struct Mx4Args {
+    const uint8_t *a, *b, *a_scale, *b_scale;
+    const int32_t *group_ptr;               // null: one group of all rows
+    void *out;
+    int64_t lda, ldb, ldsa, ldsb, ldo;      // bytes, and elements of out
+    uint32_t rows, channels, blocks, groups;
+    int32_t type;
+};
+void launch_mx4_quantize(const RouteRows &r, const seer_dense &x, const seer_mx4 &q, hipStream_t st);
+bool mx4_product_fits(const Mx4Args &a);
+size_t mx4_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t blocks, uint32_t groups);
+void launch_mx4_product(const Mx4Args &a, void *workspace, hipStream_t st);
+
 constexpr uint32_t kGradParts = 2048;       // partial sums of squares
 inline size_t grad_workspace_bytes() { return kGradParts * sizeof(double); }
 void launch_grad_norm(const seer_grad *tensors, int32_t count, float *norm, void *workspace, hipStream_t st);
 void launch_grad_clip(const seer_grad *tensors, int32_t count, float max_norm, float *norm, void *workspace, hipStream_t st);
+
+void launch_choose(const seer_dense &logits, const float *bias, const seer_choice &how, int32_t *expert, float *weight, hipStream_t st);
+void launch_choose_grad(const seer_dense &logits, const seer_choice &how, const int32_t *expert, const float *dweight,
+                        const seer_dense &dlogits, hipStream_t st);
+
+void launch_embed(const void *token, bool wide /* 64-bit entries */, uint32_t tokens, const seer_dense &table, float scale,
+                  const seer_dense &out, hipStream_t st);
+size_t embed_grad_workspace_bytes(uint32_t count, uint32_t rows, uint32_t cols);
+void launch_embed_grad(const void *token, bool wide, const seer_dense &dy, float scale, bool accumulate, const seer_dense &dtable,
+                       void *workspace, hipStream_t st);
 
 } // namespace seer

@@ -6,150 +6,9 @@
 #include "dense.hiph"
 #include "dense_launch.h"
 #include "i8_pieces.hiph"
+#include "ragged.hiph"
 
 namespace seer {
-
-typedef int v4i32 __attribute__((ext_vector_type(4)));
-
-// A tile: the rows of group `group` from `begin` to `end`, and which of the `across` tiles beside one another.  Group number
-// `groups` stands for the rows behind the last one.
-struct Tile { uint32_t group, begin, end, column; };
-
-__device__ __forceinline__ uint32_t group_begin(const I8Args &a, uint32_t g)
-{
-    if (g > a.groups) return a.rows;
-    if (!a.group_ptr) return g ? a.rows : 0;
-    const int32_t p = a.group_ptr[g];
-    return p < 0 ? 0 : min((uint32_t)p, a.rows);
-}
-
-// The last group that begins at or before a row; `groups`: none's.
-__device__ __forceinline__ uint32_t group_of(const I8Args &a, uint32_t row)
-{
-    uint32_t low = 0, high = a.groups + 1;
-    if (!a.group_ptr) return 0;
-    while (low + 1 < high) {
-        const uint32_t mid = (low + high) / 2;
-        if (group_begin(a, mid) <= row) low = mid;
-        else high = mid;
-    }
-    return low;
-}
-
-// What a lane knows of group g: its rows, and the tiles that they take.
-struct GroupTiles { uint32_t from, to, tiles; };
-
-__device__ __forceinline__ GroupTiles group_tiles(const I8Args &a, uint32_t g, uint32_t tokens)
-{
-    GroupTiles t;
-    t.from = group_begin(a, min(g, a.groups + 1));
-    t.to = group_begin(a, min(g + 1, a.groups + 1));
-    t.tiles = t.to > t.from ? (t.to - t.from + tokens - 1) / tokens : 0;
-    return t;
-}
-
-// Tiles lie in the order of the groups; in a group, kPanel rows of tiles make a panel that is gone through column by
-// column, so that workgroups that run at the same time on an XCD share rows of both matrices in its L2, and every XCD has as
-// many of the tiles that there are (of 32 groups and 32768 rows of 4096 x 4096: 780 us when they were dealt out by row
-// of tiles among those that there may be, 685 us so).
-constexpr uint32_t kPanel = 4;
-
-__device__ __forceinline__ Tile tile_in_group(uint32_t group, uint32_t from, uint32_t to, uint32_t local, uint32_t tokens, uint32_t across)
-{
-    const uint32_t down = (to - from + tokens - 1) / tokens, panel = local / (kPanel * across), rest = local % (kPanel * across);
-    const uint32_t height = min(kPanel, down - panel * kPanel), row = panel * kPanel + rest % height;
-    Tile t;
-    t.group = group;
-    t.begin = from + row * tokens;
-    t.end = min(to, t.begin + tokens);
-    t.column = rest / height;
-    return t;
-}
-
-// The tile of workgroup `block` among the tiles there are: as many for each XCD.  False: there is none.  All WAVES waves of the
-// workgroup take part, a group to a lane; the result is uniform.  s: LDS of the workgroup, free again after the next barrier.
-struct TileSearch { uint32_t sum[16], found[4]; };
-
-template <uint32_t WAVES>
-__device__ __forceinline__ bool find_tile(const I8Args &a, uint32_t block, uint32_t tokens, uint32_t across, TileSearch *s, Tile *t)
-{
-    if (!a.group_ptr) {
-        const uint32_t all = (a.rows + tokens - 1) / tokens * across, w = tile_of_block(block, all, 1);
-        if (w >= all) return false;
-        *t = tile_in_group(0, 0, a.rows, w, tokens, across);
-        return true;
-    }
-    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    // tiles of the groups from `at` up to the lane's and with it; `all`: of all WAVES * 64 groups
-    const auto prefix = [&](uint32_t tiles, uint32_t *all) {
-        uint32_t sum = tiles;
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t other = __shfl_up(sum, d, 64);
-            if ((int)lane >= d) sum += other;
-        }
-        __syncthreads();
-        if (lane == 63) s->sum[wave] = sum;
-        __syncthreads();
-        *all = 0;
-#pragma unroll
-        for (uint32_t w = 0; w < WAVES; ++w) {
-            if (w < wave) sum += s->sum[w];
-            *all += s->sum[w];
-        }
-        return sum;
-    };
-    constexpr uint32_t kAtOnce = WAVES * 64;
-    uint32_t all = 0, before = 0, sum = 0, here = 0;
-    GroupTiles g;
-    for (uint32_t at = 0; at <= a.groups; at += kAtOnce) {
-        g = group_tiles(a, at + threadIdx.x, tokens);
-        sum = prefix(g.tiles, &here);
-        all += here;
-    }
-    const uint32_t w = tile_of_block(block, all * across, 1);
-    if (w >= all * across) return false;
-    for (uint32_t at = 0; at <= a.groups; at += kAtOnce) {
-        if (a.groups >= kAtOnce) {                  // (else they are known)
-            g = group_tiles(a, at + threadIdx.x, tokens);
-            sum = prefix(g.tiles, &here);
-        }
-        const uint32_t last = (before + sum) * across, first = last - g.tiles * across;
-        if (first <= w && w < last) {               // one lane of the workgroup
-            s->found[0] = at + threadIdx.x;
-            s->found[1] = g.from;
-            s->found[2] = g.to;
-            s->found[3] = w - first;
-        }
-        before += here;
-    }
-    __syncthreads();
-    const auto uniform = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
-    *t = tile_in_group(uniform(s->found[0]), uniform(s->found[1]), uniform(s->found[2]), uniform(s->found[3]), tokens, across);
-    return true;
-}
-
-// Rows of tiles of `tokens` rows that any division of the rows into groups needs.
-static uint64_t most_tiles(const I8Args &a, uint32_t tokens)
-{
-    return a.group_ptr ? (uint64_t)a.rows / tokens + std::min(a.groups + 1, a.rows) : ((uint64_t)a.rows + tokens - 1) / tokens;
-}
-
-// Consecutive channels of one token, converted: 4 of them from channel n on, those below `channels`.
-template <class T>
-__device__ __forceinline__ void store_4(T *row, uint32_t n, uint32_t channels, const float (&v)[4])
-{
-    typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    if (n + 4 <= channels) {
-        vec o;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = (T)v[j];
-        *reinterpret_cast<vec *>(row + n) = o;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (n + j < channels) row[n + j] = (T)v[j];
-    }
-}
 
 // ------------------------------------------------------------------ any size, any alignment
 //
@@ -298,8 +157,6 @@ __global__ __launch_bounds__(256) void i8_any_kernel(I8Args a, uint32_t blocks)
 // go on to their next tile (the registers for that spill).
 constexpr uint32_t kTileChannels = 256, kTileCols = 64, kLineCols = 2 * kTileCols;
 
-typedef __attribute__((address_space(3))) int8_t lds_byte;
-
 // WC x WAVES / WC waves, each of CI * 16 channels x TJ * 16 tokens; `BUFFERS` of two steps each.
 template <int WAVES, int WC, int CI, int TJ, int BUFFERS>
 struct TileShape {
@@ -314,13 +171,6 @@ struct TileShape {
 // The columns shared out: workgroups of share `s` multiply columns s * share ... and leave sums of 32-bit integers,
 // [shares][rows][pitch], which i8_join_kernel adds up and scales.
 struct SharedColumns { int32_t *sums; uint32_t blocks, share, pitch; };
-
-// Waits until all but the last `LOADS` of the wave's loads have arrived and its LDS reads are through, then for the other waves.
-template <uint32_t LOADS>
-__device__ __forceinline__ void step_barrier()
-{
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
-}
 
 template <class T, int WAVES, int WC, int CI, int TJ, int BUFFERS>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || BUFFERS == 2 ? 2 : 1) void i8_tile_kernel(I8Args a, SharedColumns shared)
@@ -666,14 +516,6 @@ static bool in_pieces(const I8Args &a)
     const auto whole = [](uintptr_t v) { return v % 16 == 0; };
     return whole(reinterpret_cast<uintptr_t>(a.a)) && whole(reinterpret_cast<uintptr_t>(a.b)) && whole((uintptr_t)a.lda) &&
            whole((uintptr_t)a.ldb);
-}
-
-constexpr uint32_t kCUs = 256;
-
-// Workgroups for the tiles that there may be.
-static uint64_t most_blocks(const I8Args &a, uint32_t tokens, uint32_t channels)
-{
-    return (most_tiles(a, tokens) * ((a.channels + channels - 1) / channels) + kXCD - 1) / kXCD * kXCD;
 }
 
 // The arithmetic on tiles is 32-bit; of the tiles for any address, which no other kernel's launches outnumber (i8_plan), there are the most.

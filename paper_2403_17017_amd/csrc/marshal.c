@@ -279,7 +279,7 @@ static int no_history(PyObject *t, const char *what)
 }
 
 /* A 2-D tensor (deep: or a 3-D one, matrices one behind the other, *groups of them) as rows; ld as the library counts it. */
-static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer_dense *d, int *gpu)
+static int rows_of(PyObject *t, const char *what, int deep, int32_t *groups, int64_t *rows, int64_t *cols, int64_t *ld)
 {
     int64_t n[3], by[3];
     const int dims = numbers(PyObject_GetAttr(t, s_shape), n);
@@ -292,14 +292,19 @@ static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer
     }
     if (n[2] > 1 && by[2] != 1 && n[0] > 0 && n[1] > 0) return refuse(PyExc_ValueError, what, "is to be a matrix with contiguous rows");
     if (n[0] > 1 && n[1] > 1 && by[0] != n[1] * by[1]) return refuse(PyExc_ValueError, what, "is to have its matrices one behind the other");
-    if (on_gpu(t, what, gpu)) return -1;
+    *rows = n[0] * n[1];
+    *cols = n[2];
+    *ld = n[1] > 1 ? by[1] : n[0] > 1 ? by[0] : by[1] > n[2] ? by[1] : n[2];
+    if (groups) *groups = (int32_t)n[0];
+    return 0;
+}
+
+static int matrix(PyObject *t, const char *what, int deep, int32_t *groups, seer_dense *d, int *gpu)
+{
     uint64_t at;
+    if (rows_of(t, what, deep, groups, &d->rows, &d->cols, &d->ld) || on_gpu(t, what, gpu)) return -1;
     if ((d->type = type_of(t, what)) < 0 || (d->type <= SEER_F16 && no_history(t, what)) || address_of(t, &at)) return -1;
     d->data = (void *)(uintptr_t)at;
-    d->rows = n[0] * n[1];
-    d->cols = n[2];
-    d->ld = n[1] > 1 ? by[1] : n[0] > 1 ? by[0] : by[1] > n[2] ? by[1] : n[2];
-    if (groups) *groups = (int32_t)n[0];
     return 0;
 }
 
@@ -558,6 +563,174 @@ static PyObject *m_bind_routed(PyObject *self, PyObject *args)
     Py_RETURN_NONE;
 }
 
+/* ---- what a routed layer is fed by: the router's choice (router.py) and the embedding of tokens (embedding.py) */
+
+static int (*f_choose)(const seer_dense *, const float *, const seer_choice *, int32_t *, float *, void *);
+static int (*f_choose_grad)(const seer_dense *, const seer_choice *, const int32_t *, const float *, const seer_dense *, void *);
+static int (*f_embed)(const void *, int32_t, const seer_dense *, float, const seer_dense *, void *);
+static int (*f_embed_grad)(const void *, int32_t, const seer_dense *, float, int32_t, const seer_dense *, void *, size_t, void *);
+
+/* (logits, bias or None, address of the seer_choice, expert, weight, stream) */
+static PyObject *m_choose(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_dense logits;
+    uint64_t bias, how, expert, weight, stream;
+    int gpu = -1;
+    if (given(n, 6) || as_size(a[2], &how) || matrix(a[0], "logits", 0, NULL, &logits, &gpu)) return NULL;
+    const int64_t count = logits.rows * P(const seer_choice *, how)->choices;
+    if (vector(a[1], "bias", SEER_F32, logits.cols, &bias, &gpu) || vector(a[3], "expert", SEER_I32, count, &expert, &gpu) ||
+        vector(a[4], "weight", SEER_F32, count, &weight, &gpu) || as_size(a[5], &stream) || is_current(gpu))
+        return NULL;
+    ASYNC(f_choose(&logits, P(const float *, bias), P(const seer_choice *, how), P(int32_t *, expert), P(float *, weight), P(void *, stream)));
+}
+
+/* (logits, address of the seer_choice, expert, dweight, dlogits, stream) */
+static PyObject *m_choose_grad(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_dense logits, dlogits;
+    uint64_t how, expert, dweight, stream;
+    int gpu = -1;
+    if (given(n, 6) || as_size(a[1], &how) || matrix(a[0], "logits", 0, NULL, &logits, &gpu)) return NULL;
+    const int64_t count = logits.rows * P(const seer_choice *, how)->choices;
+    if (vector(a[2], "expert", SEER_I32, count, &expert, &gpu) || vector(a[3], "dweight", SEER_F32, count, &dweight, &gpu) ||
+        matrix(a[4], "dlogits", 0, NULL, &dlogits, &gpu) || as_size(a[5], &stream) || is_current(gpu))
+        return NULL;
+    ASYNC(f_choose_grad(&logits, P(const seer_choice *, how), P(const int32_t *, expert), P(const float *, dweight), &dlogits, P(void *, stream)));
+}
+
+static int number(PyObject *o, float *out)
+{
+    const double v = PyFloat_AsDouble(o);
+    *out = (float)v;
+    return v == -1.0 && PyErr_Occurred() ? -1 : 0;
+}
+
+/* Tokens, of a type that the library knows or refuses. */
+static int tokens_of(PyObject *t, int64_t n, uint64_t *at, int *type, int *gpu)
+{
+    return (*type = type_of(t, "token")) < 0 || vector(t, "token", *type, n, at, gpu) ? -1 : 0;
+}
+
+/* (token, table, scale, out, stream) */
+static PyObject *m_embed(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_dense table, out;
+    uint64_t token, stream;
+    float scale;
+    int gpu = -1, type;
+    if (given(n, 5) || matrix(a[1], "table", 0, NULL, &table, &gpu) || number(a[2], &scale) || matrix(a[3], "out", 0, NULL, &out, &gpu) ||
+        tokens_of(a[0], out.rows, &token, &type, &gpu) || as_size(a[4], &stream) || is_current(gpu))
+        return NULL;
+    ASYNC(f_embed(P(const void *, token), type, &table, scale, &out, P(void *, stream)));
+}
+
+/* (token, dy, scale, accumulate, dtable, workspace or None, stream) */
+static PyObject *m_embed_grad(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_dense dy, dtable;
+    uint64_t token, ws, bytes, stream;
+    float scale;
+    int gpu = -1, type;
+    if (given(n, 7) || matrix(a[1], "dy", 0, NULL, &dy, &gpu) || number(a[2], &scale) || matrix(a[4], "dtable", 0, NULL, &dtable, &gpu) ||
+        tokens_of(a[0], dy.rows, &token, &type, &gpu) || space(a[5], &ws, &bytes, &gpu) || as_size(a[6], &stream) || is_current(gpu))
+        return NULL;
+    const int add = PyObject_IsTrue(a[3]);
+    if (add < 0) return NULL;
+    ASYNC(f_embed_grad(P(const void *, token), type, &dy, scale, add, &dtable, P(void *, ws), (size_t)bytes, P(void *, stream)));
+}
+
+static PyObject *m_bind_tokens(PyObject *self, PyObject *args)
+{
+    unsigned long long f[4];
+    if (!PyArg_ParseTuple(args, "KKKK", f, f + 1, f + 2, f + 3)) return NULL;
+    f_choose = P(int (*)(const seer_dense *, const float *, const seer_choice *, int32_t *, float *, void *), f[0]);
+    f_choose_grad = P(int (*)(const seer_dense *, const seer_choice *, const int32_t *, const float *, const seer_dense *, void *), f[1]);
+    f_embed = P(int (*)(const void *, int32_t, const seer_dense *, float, const seer_dense *, void *), f[2]);
+    f_embed_grad = P(int (*)(const void *, int32_t, const seer_dense *, float, int32_t, const seer_dense *, void *, size_t, void *), f[3]);
+    Py_RETURN_NONE;
+}
+
+/* ---- rows in 4-bit floating point (mx4.py) */
+
+static int (*f_mx4_quantize)(const seer_dense *, const seer_mx4 *, void *);
+static int (*f_gather_mx4)(const seer_routing *, const seer_dense *, const seer_mx4 *, void *);
+static int (*f_mx4_product)(const seer_mx4 *, const seer_mx4 *, const int32_t *, int32_t, const seer_dense *, void *, size_t, void *);
+static PyObject *type_u8;
+
+static int bytes_of(PyObject *t, const char *what, int deep, int32_t *groups, int64_t *rows, int64_t *cols, int64_t *ld, void **data, int *gpu)
+{
+    uint64_t at;
+    PyObject *d = PyObject_GetAttr(t, s_dtype);
+    if (!d) return -1;
+    Py_DECREF(d);                            /* (torch keeps its types) */
+    if (d != type_u8) return refuse(PyExc_TypeError, what, "is to be a uint8 tensor");
+    if (rows_of(t, what, deep, groups, rows, cols, ld) || on_gpu(t, what, gpu) || address_of(t, &at)) return -1;
+    *data = (void *)(uintptr_t)at;
+    return 0;
+}
+
+/* Codes, 16 bytes to a block, and a scale byte for each; all blocks count as whole. */
+static int blocks_of(PyObject *q, const char *q_what, PyObject *scale, const char *scale_what, int deep, int32_t *groups, seer_mx4 *m, int *gpu)
+{
+    int32_t scale_groups;
+    int64_t rows, bytes, blocks;
+    if (bytes_of(q, q_what, deep, groups, &m->rows, &bytes, &m->ld, &m->data, gpu) ||
+        bytes_of(scale, scale_what, deep, &scale_groups, &rows, &blocks, &m->scale_ld, &m->scale, gpu))
+        return -1;
+    if (rows != m->rows || bytes != 16 * blocks || (groups && scale_groups != *groups))
+        return refuse(PyExc_ValueError, scale_what, "is to have a byte for every 16 bytes of the codes");
+    m->cols = 32 * blocks;
+    return 0;
+}
+
+/* (routing or None, x, q, scale, stream) */
+static PyObject *m_mx4_quantize(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    seer_routing r;
+    seer_dense x;
+    seer_mx4 q;
+    uint64_t stream;
+    const int routed = n == 5 && a[0] != Py_None;
+    int gpu = -1;
+    if (given(n, 5) || (routed && routing_of(a[0], 0, &r, &gpu)) || matrix(a[1], "x", 0, NULL, &x, &gpu) ||
+        blocks_of(a[2], "q", a[3], "scale", 0, NULL, &q, &gpu) || as_size(a[4], &stream) || is_current(gpu))
+        return NULL;
+    if (q.cols / 32 != (x.cols + 31) / 32) {
+        refuse(PyExc_ValueError, "q", "is to have 16 bytes for every 32 columns of x");
+        return NULL;
+    }
+    q.cols = x.cols;
+    ASYNC(routed ? f_gather_mx4(&r, &x, &q, P(void *, stream)) : f_mx4_quantize(&x, &q, P(void *, stream)));
+}
+
+/* (a, a_scale, b, b_scale, group_ptr or None, out, workspace or None, stream) */
+static PyObject *m_mx4_product(PyObject *self, PyObject *const *v, Py_ssize_t n)
+{
+    seer_mx4 a, b;
+    seer_dense out;
+    int32_t groups;
+    uint64_t ptr, ws, bytes, stream;
+    int gpu = -1;
+    if (given(n, 8) || blocks_of(v[0], "a", v[1], "a_scale", 0, NULL, &a, &gpu) || blocks_of(v[2], "b", v[3], "b_scale", 1, &groups, &b, &gpu) ||
+        vector(v[4], "group_ptr", SEER_I32, (int64_t)groups + 1, &ptr, &gpu) || matrix(v[5], "out", 0, NULL, &out, &gpu) ||
+        space(v[6], &ws, &bytes, &gpu) || as_size(v[7], &stream) || is_current(gpu))
+        return NULL;
+    ASYNC(f_mx4_product(&a, &b, P(const int32_t *, ptr), groups, &out, P(void *, ws), (size_t)bytes, P(void *, stream)));
+}
+
+static PyObject *m_bind_mx4(PyObject *self, PyObject *args)
+{
+    unsigned long long f[3];
+    PyObject *u8;
+    if (!PyArg_ParseTuple(args, "KKKO", f, f + 1, f + 2, &u8)) return NULL;
+    f_mx4_quantize = P(int (*)(const seer_dense *, const seer_mx4 *, void *), f[0]);
+    f_gather_mx4 = P(int (*)(const seer_routing *, const seer_dense *, const seer_mx4 *, void *), f[1]);
+    f_mx4_product = P(int (*)(const seer_mx4 *, const seer_mx4 *, const int32_t *, int32_t, const seer_dense *, void *, size_t, void *), f[2]);
+    Py_INCREF(u8);
+    Py_XSETREF(type_u8, u8);
+    Py_RETURN_NONE;
+}
+
 static PyMethodDef methods[] = {
     {"bind", m_bind, METH_VARARGS, "bind(spmv, spmv_auto, spmv_model, spmv_prepared): addresses of the library's functions"},
     {"spmv", (PyCFunction)(void (*)(void))m_spmv, METH_FASTCALL, "spmv(kernel_id, A, x, y, workspace, stream) -> status"},
@@ -576,6 +749,17 @@ static PyMethodDef methods[] = {
      "product(a, a_scale, b, b_scale, group_ptr, out, workspace, stream) -> status"},
     {"grads", (PyCFunction)(void (*)(void))m_grads, METH_FASTCALL, "grads(gradients, outputs or None, list address, count) -> GPU"},
     {"clip", (PyCFunction)(void (*)(void))m_clip, METH_FASTCALL, "clip(list address, count, max_norm, norm, workspace, stream, GPU) -> status"},
+    {"bind_tokens", m_bind_tokens, METH_VARARGS, "bind_tokens(addresses of seer_route_choose, seer_route_choose_grad, seer_embed, seer_embed_grad)"},
+    {"choose", (PyCFunction)(void (*)(void))m_choose, METH_FASTCALL, "choose(logits, bias or None, choice address, expert, weight, stream) -> status"},
+    {"choose_grad", (PyCFunction)(void (*)(void))m_choose_grad, METH_FASTCALL,
+     "choose_grad(logits, choice address, expert, dweight, dlogits, stream) -> status"},
+    {"embed", (PyCFunction)(void (*)(void))m_embed, METH_FASTCALL, "embed(token, table, scale, out, stream) -> status"},
+    {"embed_grad", (PyCFunction)(void (*)(void))m_embed_grad, METH_FASTCALL,
+     "embed_grad(token, dy, scale, accumulate, dtable, workspace, stream) -> status"},
+    {"bind_mx4", m_bind_mx4, METH_VARARGS, "bind_mx4(addresses of seer_mx4_quantize, seer_route_gather_mx4, seer_mx4_product, torch.uint8)"},
+    {"mx4_quantize", (PyCFunction)(void (*)(void))m_mx4_quantize, METH_FASTCALL, "mx4_quantize(routing or None, x, q, scale, stream) -> status"},
+    {"mx4_product", (PyCFunction)(void (*)(void))m_mx4_product, METH_FASTCALL,
+     "mx4_product(a, a_scale, b, b_scale, group_ptr, out, workspace, stream) -> status"},
     {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the asynchronous calls", -1,

@@ -68,34 +68,6 @@ __device__ void place_choices(const I *expert, uint32_t begin, uint32_t end, uin
     }
 }
 
-// Exclusive prefix sum over v[0 .. n) in LDS by the whole workgroup, the total in v[n].
-__device__ void scan_lds(uint32_t *v, uint32_t n, uint32_t *s_wave)
-{
-    const uint32_t threads = blockDim.x, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    uint32_t carry = 0;
-    for (uint32_t at = 0; at < n; at += threads) {
-        const uint32_t i = at + threadIdx.x;
-        const uint32_t mine = i < n ? v[i] : 0;
-        uint32_t sum = mine;
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t other = __shfl_up(sum, d, 64);
-            if ((int)lane >= d) sum += other;
-        }
-        if (lane == 63) s_wave[wave] = sum;
-        __syncthreads();
-        uint32_t before = carry, all = 0;
-        for (uint32_t w = 0; w < threads / 64; ++w) {
-            if (w < wave) before += s_wave[w];
-            all += s_wave[w];
-        }
-        if (i < n) v[i] = before + sum - mine;
-        carry += all;
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) v[n] = carry;
-    __syncthreads();
-}
-
 struct SortArgs {
     const void *expert;
     uint32_t count, experts, per_wave, groups;
@@ -577,14 +549,6 @@ __global__ __launch_bounds__(kWG) void quantize_kernel(RouteRows r, const T *__r
 }
 
 // ------------------------------------------------------------------ launches
-
-template <class F>
-static void by_type(int type, F f)
-{
-    if (type == SEER_F32) f((float *)nullptr);
-    else if (type == SEER_BF16) f((bf16_t *)nullptr);
-    else f((f16_t *)nullptr);
-}
 
 // Rows that begin on multiples of 16 bytes are streamed; the pieces of others share lines, which have to stay for the second one.
 // (1031 rows of 1023 floats, two choices each, gradient: 6.9 us, 9.0 streamed.)

@@ -47,6 +47,8 @@ def _ready():
         m.bind_routed(*(C.cast(f, C.c_void_p).value for f in (
             L.seer_route, L.seer_route_gather, L.seer_route_combine, L.seer_route_grad, L.seer_i8_quantize, L.seer_route_gather_i8,
             L.seer_i8_product, L.seer_grad_norm, L.seer_grad_clip)), torch._C, torch.cuda, torch.is_grad_enabled, *ids)
+        m.bind_tokens(*(C.cast(f, C.c_void_p).value for f in (L.seer_route_choose, L.seer_route_choose_grad, L.seer_embed, L.seer_embed_grad)))
+        m.bind_mx4(*(C.cast(f, C.c_void_p).value for f in (L.seer_mx4_quantize, L.seer_route_gather_mx4, L.seer_mx4_product)), torch.uint8)
         _types, _torch = ids, torch
     return B._marshal
 
