@@ -52,104 +52,361 @@ __device__ __forceinline__ double chosen_share(const seer_choice &how, float x, 
     return in ? s / sum : 0.0;
 }
 
-// One wave to a token, lane l has the experts l, 64 + l, ...
+// The choice of one token by a whole wave, in 64 bits; lane l has the experts l, 64 + l, ...  s_key: LDS of the wave, [experts], with groups.
+template <class T, int PER>
+__device__ __noinline__ void choose_exactly(const T *logits, int64_t ld, uint32_t t, uint32_t experts, const float *bias, const seer_choice &how, int32_t *expert,
+                               float *weight, uint64_t *s_key)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    const bool grouped = how.best_groups < how.groups;
+    const T *row = logits + (int64_t)t * ld;
+    float x[PER];
+    uint64_t key[PER];
+    double most = -INFINITY, all = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const uint32_t e = i * 64 + lane;
+        x[i] = e < experts ? logit(row, e) : -INFINITY;
+        most = x[i] != x[i] || x[i] > most ? (double)x[i] : most;
+    }
+    const bool scored = bias || (grouped && how.group_best == 2) || !how.renormalise;
+    if (how.score == SEER_SOFTMAX && scored) {
+        most = wave_max(most);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (x[i] != -INFINITY) all += exp((double)x[i] - most);
+        all = wave_sum(all);
+    }
+    const auto score = [&](float v) { return how.score == SEER_SIGMOID ? sigmoid((double)v) : exp((double)v - most) / all; };
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const uint32_t e = i * 64 + lane;
+        const float b = bias && e < experts ? bias[e] : 0.0f;
+        key[i] = x[i] == -INFINITY || b == -INFINITY ? 0 : key_of(bias ? score(x[i]) + (double)b : (double)x[i]);
+    }
+    if (grouped) {
+        uint64_t *mine = s_key;
+        const uint32_t length = experts / how.groups;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t e = i * 64 + lane;
+            if (e < experts) mine[e] = key[i] == 0 || how.group_best == 1 || bias ? key[i] : key_of(score(x[i]));
+        }
+        __builtin_amdgcn_wave_barrier();
+        uint64_t best = 0, second = 0;
+        if (lane < (uint32_t)how.groups) {
+            for (uint32_t j = 0; j < length; ++j) {
+                const uint64_t k = mine[lane * length + j];
+                second = max(second, min(best, k));
+                best = max(best, k);
+            }
+            if (how.group_best == 2 && second) best = key_of((best == ~0ull ? NAN : of_key(best)) + (second == ~0ull ? NAN : of_key(second)));
+        }
+        uint32_t rank = 0;
+        for (uint32_t g = 0; g < (uint32_t)how.groups; ++g) {
+            const uint64_t other = __shfl(best, (int)g, 64);
+            rank += other > best || (other == best && g < lane);
+        }
+        const uint64_t open = __ballot(lane < (uint32_t)how.groups && rank < (uint32_t)how.best_groups);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t e = i * 64 + lane;
+            if (e < experts && !(open >> (e / length) & 1)) key[i] = 0;
+        }
+    }
+    int32_t chosen = -1;                            // of the lane's number
+    for (int k = 0; k < how.choices; ++k) {
+        uint64_t best = 0;
+        uint32_t at = ~0u;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (key[i] > best) {
+                best = key[i];
+                at = i * 64 + lane;
+            }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint64_t other = __shfl_xor(best, d, 64);
+            const uint32_t there = __shfl_xor(at, d, 64);
+            if (other > best || (other == best && there < at)) {
+                best = other;
+                at = there;
+            }
+        }
+        if (best == 0) break;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (at == i * 64 + lane) key[i] = 0;
+        if ((int)lane == k) chosen = (int32_t)at;
+    }
+    double share = chosen_share(how, chosen >= 0 ? logit(row, (uint32_t)chosen) : 0.0f, chosen >= 0, most, all);
+    if (all != all && chosen >= 0) share = all;             // (what makes a softmax NaN need not be among the chosen)
+    if ((int)lane < how.choices) {
+        const size_t to = (size_t)t * how.choices + lane;
+        expert[to] = chosen;
+        weight[to] = (float)((double)how.factor * share);
+    }
+}
+
 template <class T, int PER>
 __global__ __launch_bounds__(kWG) void choose_kernel(const T *__restrict__ logits, int64_t ld, uint32_t tokens, uint32_t experts,
                                                      const float *__restrict__ bias, seer_choice how, int32_t *__restrict__ expert,
                                                      float *__restrict__ weight)
 {
     extern __shared__ __attribute__((aligned(16))) uint64_t s_key[];          // [waves][experts], with groups
-    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-    const bool grouped = how.best_groups < how.groups;
-    for (uint32_t t = blockIdx.x * (kWG / kWave) + wave; t < tokens; t += gridDim.x * (kWG / kWave)) {
-        const T *row = logits + (int64_t)t * ld;
+    const uint32_t wave = threadIdx.x / 64;
+    for (uint32_t t = blockIdx.x * (kWG / kWave) + wave; t < tokens; t += gridDim.x * (kWG / kWave))
+        choose_exactly<T, PER>(logits, ld, t, experts, bias, how, expert, weight, s_key + (size_t)wave * experts);
+}
+
+// ------------------------------------------------------------------ four tokens to a wave
+//
+// 16 lanes to a token, a lane with PER consecutive experts; keys in 32 bits, with bounds on what they may be off by.  A token whose choice the
+// bounds leave open is chosen again by the whole wave, in 64 bits.
+//
+// A key travels with its expert in one word: the 24 upper bits of the number that has the key's order, and 255 less the
+// expert's number; the next best is the largest word below the last one.  Keys that are made of scores are taken less the largest of them, so
+// that what is cut off is 2^-15 of the distance from the best.  The bounds on a score: of a sigmoid, 2^-21 (an exponential with an error
+// of 2^-23 and 1.5 |x| 2^-24 of itself, times s (1 - s), where s (1 - s) |x| < 0.23; a sum and a reciprocal, 1.5 * 2^-23); of a softmax, 2^-18 of
+// the largest (such exponentials, s |x - max| < 0.4 max s, a sum of 256 in 20 steps, a reciprocal and a product).  A bias adds 2^-24 of the key.
+// Without a bias keys are logits, and exact.
+constexpr uint32_t kRowBlocks = 1024 /* as many as there is room for; a wave then goes on to other tokens */;
+constexpr uint32_t kRowLanes = 16, kFastChoices = 15, kFastExperts = 256;
+constexpr float kSigmoidError = 0x1p-21f, kSoftmaxError = 0x1p-18f, kCut = 0x1p-15f;
+
+// The other lanes of 16: fold with the same result in all of them.
+template <int CTRL>
+__device__ __forceinline__ uint32_t row_move(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+template <int CTRL>
+__device__ __forceinline__ float row_move(float v) { return dpp_f<CTRL>(v); }
+template <class V, class F>
+__device__ __forceinline__ V row_fold(V v, F f)
+{
+    v = f(v, row_move<0xB1>(v));
+    v = f(v, row_move<0x4E>(v));
+    v = f(v, row_move<0x141>(v));
+    return f(v, row_move<0x140>(v));
+}
+__device__ __forceinline__ float row_sum(float v)
+{
+    return row_fold(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float row_max(float v)
+{
+    return row_fold(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+__device__ __forceinline__ uint32_t word_of(float key)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, key + 0.0f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float of_word(uint32_t w)
+{
+    return __builtin_bit_cast(float, w >> 31 ? w & 0x7fffffffu : ~w);
+}
+
+// f with the 15 other lanes' values in turn, and from which lane they are.
+template <int N = 1, class F>
+__device__ __forceinline__ void other_lanes(F f)
+{
+    if constexpr (N < (int)kRowLanes) {
+        f(std::integral_constant<int, 0x120 + N>{}, (threadIdx.x - N) & (kRowLanes - 1));
+        other_lanes<N + 1>(f);
+    }
+}
+
+__device__ __forceinline__ float fast_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
+
+// The weights of the experts chosen for a token, one to a lane of 16: as chosen_share.
+__device__ __forceinline__ float row_share(const seer_choice &how, float x, bool in, float most, float all)
+{
+    if (!how.renormalise) return !in ? 0.0f : how.score == SEER_SIGMOID ? fast_sigmoid(x) : __expf(x - most) * __builtin_amdgcn_rcpf(all);
+    float top = row_max(in ? x : -INFINITY), s;
+    if (how.score == SEER_SIGMOID) {
+        top = fminf(top, 0.0f);
+        s = x > 0 ? fast_sigmoid(x) : __expf(x - top) * __builtin_amdgcn_rcpf(1.0f + __expf(x));
+    } else
+        s = __expf(x - top);
+    s = in ? s : 0.0f;
+    const float sum = row_sum(s);
+    return in ? s * __builtin_amdgcn_rcpf(sum) : 0.0f;
+}
+
+// per: the experts of a lane; VEC: rows are read 4 elements at a time.  group_lanes: lanes to a group, 0 without groups.
+template <class T, int PER, bool VEC, bool BIAS>
+__global__ __launch_bounds__(kWG, 4) void choose_rows_kernel(const T *__restrict__ logits, int64_t ld, uint32_t tokens, uint32_t experts, uint32_t per,
+                                                          uint32_t group_lanes, const float *__restrict__ bias, seer_choice how,
+                                                          int32_t *__restrict__ expert, float *__restrict__ weight)
+{
+    extern __shared__ __attribute__((aligned(16))) uint64_t s_key[];          // [waves][experts], with groups
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63, l = lane & (kRowLanes - 1);
+    const bool two = group_lanes && how.group_best == 2;
+    const auto bits = [](float v) { return __builtin_bit_cast(uint32_t, v); };
+    float b[BIAS ? PER : 1];
+    if constexpr (BIAS) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) b[i] = bias[min(l * per + i, experts - 1)];
+    }
+    for (uint32_t t0 = (blockIdx.x * (kWG / kWave) + wave) * 4; t0 < tokens; t0 += gridDim.x * kWG / kRowLanes) {
+        const uint32_t t = t0 + lane / kRowLanes;
+        const T *row = logits + (int64_t)min(t, tokens - 1) * ld;
         float x[PER];
-        uint64_t key[PER];
-        double most = -INFINITY, all = 0;
+        if constexpr (VEC) {
+            typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const uint32_t e = i * 64 + lane;
-            x[i] = e < experts ? logit(row, e) : -INFINITY;
-            most = x[i] != x[i] || x[i] > most ? (double)x[i] : most;
-        }
-        const bool scored = bias || (grouped && how.group_best == 2) || !how.renormalise;
-        if (how.score == SEER_SOFTMAX && scored) {
-            most = wave_max(most);
+            for (int i = 0; i < PER; i += 4) {
+                const uint32_t e = l * per + i;
+                const bool in = e < experts && (uint32_t)i < per;
+                four v = {};
+                if (in) v = *reinterpret_cast<const four *>(row + e);
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (x[i] != -INFINITY) all += exp((double)x[i] - most);
-            all = wave_sum(all);
-        }
-        const auto score = [&](float v) { return how.score == SEER_SIGMOID ? sigmoid((double)v) : exp((double)v - most) / all; };
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const uint32_t e = i * 64 + lane;
-            const float b = bias && e < experts ? bias[e] : 0.0f;
-            key[i] = x[i] == -INFINITY || b == -INFINITY ? 0 : key_of(bias ? score(x[i]) + (double)b : (double)x[i]);
-        }
-        if (grouped) {
-            uint64_t *mine = s_key + (size_t)wave * experts;
-            const uint32_t length = experts / how.groups;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint32_t e = i * 64 + lane;
-                if (e < experts) mine[e] = key[i] == 0 || how.group_best == 1 || bias ? key[i] : key_of(score(x[i]));
+                for (int j = 0; j < 4; ++j) x[i + j] = in ? (float)v[j] : -INFINITY;
             }
-            __builtin_amdgcn_wave_barrier();
-            uint64_t best = 0, second = 0;
-            if (lane < (uint32_t)how.groups) {
-                for (uint32_t j = 0; j < length; ++j) {
-                    const uint64_t k = mine[lane * length + j];
-                    second = max(second, min(best, k));
-                    best = max(best, k);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) x[i] = l * per + i < experts && (uint32_t)i < per ? (float)row[l * per + i] : -INFINITY;
+        }
+        // keys: scores with the bias, or logits; -infinity is not to be chosen
+        float key[PER], most = -INFINITY, all = 0, score_error = kSigmoidError, by = 0;
+        if (how.score == SEER_SOFTMAX && (BIAS || two || !how.renormalise)) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) most = fmaxf(most, x[i]);
+            most = row_max(most);
+            most = most == -INFINITY ? 0 : most;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) all += __expf(x[i] - most);
+            all = row_sum(all);
+            by = all > 0 ? __builtin_amdgcn_rcpf(all) : 0;
+            score_error = kSoftmaxError * by;
+        }
+        const auto score = [&](float v) { return how.score == SEER_SIGMOID ? fast_sigmoid(v) : __expf(v - most) * by; };
+        if constexpr (BIAS) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) key[i] = x[i] == -INFINITY ? x[i] : score(x[i]) + b[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) key[i] = x[i];
+        }
+        // another number that is not finite leaves the token to 64 bits
+        bool unsure = all != all, open = true;
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) top = max(top, bits(key[i]) & 0x7fffffffu);
+        if (__ballot(top >= 0x7f800000u)) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) unsure = unsure || (bits(key[i]) != 0xff800000u && (bits(key[i]) & 0x7fffffffu) >= 0x7f800000u);
+        }
+        if (group_lanes) {
+            float first = -INFINITY, second = -INFINITY;
+            if (BIAS || !two) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    second = __builtin_amdgcn_fmed3f(first, second, key[i]);
+                    first = fmaxf(first, key[i]);
                 }
-                if (how.group_best == 2 && second) best = key_of((best == ~0ull ? NAN : of_key(best)) + (second == ~0ull ? NAN : of_key(second)));
-            }
-            uint32_t rank = 0;
-            for (uint32_t g = 0; g < (uint32_t)how.groups; ++g) {
-                const uint64_t other = __shfl(best, (int)g, 64);
-                rank += other > best || (other == best && g < lane);
-            }
-            const uint64_t open = __ballot(lane < (uint32_t)how.groups && rank < (uint32_t)how.best_groups);
-            __builtin_amdgcn_wave_barrier();
+            } else {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint32_t e = i * 64 + lane;
-                if (e < experts && !(open >> (e / length) & 1)) key[i] = 0;
-            }
-        }
-        int32_t chosen = -1;                            // of the lane's number
-        for (int k = 0; k < how.choices; ++k) {
-            uint64_t best = 0;
-            uint32_t at = ~0u;
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (key[i] > best) {
-                    best = key[i];
-                    at = i * 64 + lane;
-                }
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint64_t other = __shfl_xor(best, d, 64);
-                const uint32_t there = __shfl_xor(at, d, 64);
-                if (other > best || (other == best && there < at)) {
-                    best = other;
-                    at = there;
+                for (int i = 0; i < PER; ++i) {
+                    const float v = x[i] == -INFINITY ? x[i] : score(x[i]);
+                    second = __builtin_amdgcn_fmed3f(first, second, v);
+                    first = fmaxf(first, v);
                 }
             }
-            if (best == 0) break;
+            const auto meet = [&](float f, float sec) {
+                second = fmaxf(fminf(first, f), fmaxf(second, sec));
+                first = fmaxf(first, f);
+            };
+            if (group_lanes > 1) meet(row_move<0xB1>(first), row_move<0xB1>(second));
+            if (group_lanes > 2) meet(row_move<0x4E>(first), row_move<0x4E>(second));
+            if (group_lanes > 4) meet(row_move<0x141>(first), row_move<0x141>(second));
+            float worth = first;
+            if (two && second != -INFINITY) worth += second;
+            worth = fmaxf(worth, -0x1.fffffep127f);         // (a group with none is behind all others)
+            const uint32_t room = (uint32_t)how.best_groups * group_lanes;          // in lanes, as the counts
+            uint32_t above = 0;
+            if (BIAS || two) {
+                const float size = row_max(first == -INFINITY ? 0.0f : fmaxf(fabsf(first), second == -INFINITY ? 0.0f : fabsf(second)));
+                const float near = 4 * score_error + size * 0x1p-21f;
+                uint32_t not_below = 0;
+                other_lanes([&](auto ctrl, uint32_t) {
+                    const float gap = row_move<decltype(ctrl)::value>(worth) - worth;
+                    above += gap > near;
+                    not_below += gap >= -near;
+                });
+                open = above < room;
+                // (the own group's other lanes are level with it)
+                unsure = unsure || (open && not_below - (group_lanes - 1) >= room);
+            } else {
+                const uint32_t mine = l & ~(group_lanes - 1);
+                other_lanes([&](auto ctrl, uint32_t from) {
+                    const float other = row_move<decltype(ctrl)::value>(worth);
+                    above += other > worth || (other == worth && from < mine);
+                });
+                open = above < room;
+            }
+        }
+        uint32_t word[PER], none;
+        const uint32_t kept = open ? ~255u : 0;
+        float size = 0;
+        if constexpr (BIAS) {
+            float best = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (at == i * 64 + lane) key[i] = 0;
-            if ((int)lane == k) chosen = (int32_t)at;
+            for (int i = 0; i < PER; ++i) best = fmaxf(best, key[i]);
+            best = row_max(open ? best : -INFINITY);
+            best = best == -INFINITY ? 0 : best;
+            // (what is below the best in an open group; what is above it is in a closed one)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) word[i] = (~bits(fmaxf(best - key[i], 0.0f)) & kept) | (255 - (l * per + i));
+            size = fabsf(best) + 2;
+            none = ~0x7f800000u;                            // an infinite distance, or less
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) word[i] = (word_of(key[i]) & kept) | (255 - (l * per + i));
+            none = ~0xff800000u;                            // -infinity
         }
-        double share = chosen_share(how, chosen >= 0 ? logit(row, (uint32_t)chosen) : 0.0f, chosen >= 0, most, all);
-        if (all != all && chosen >= 0) share = all;             // (what makes a softmax NaN need not be among the chosen)
-        if ((int)lane < how.choices) {
-            const size_t to = (size_t)t * how.choices + lane;
-            expert[to] = chosen;
-            weight[to] = (float)((double)how.factor * share);
+        uint32_t last = 0, mine = 0;                        // lane k takes the k-th word
+        for (int k = 0; k <= how.choices; ++k) {
+            uint32_t next = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) next = max(next, word[i] - last);
+            next = row_fold(next, [](uint32_t a, uint32_t c) { return max(a, c); }) + last;
+            // (nothing below the last word: what comes out is that word or one above it)
+            if (next <= none || (k > 0 && (last == 0 || next >= last))) next = 0;
+            mine = (int)l == k ? next : mine;
+            last = next;
         }
+        const bool in = mine != 0 && (int)l < how.choices;
+        const uint32_t at = min(255 - (mine & 255), experts - 1);
+        const float xl = mine ? (float)row[at] : 0.0f;
+        {
+            const uint32_t after = row_move<0x101>(mine);   // of the next lane
+            const float xa = row_move<0x101>(xl);
+            const bool border = (int)l == how.choices - 1;
+            bool sure;
+            if constexpr (BIAS) {
+                const float bl = mine ? bias[at] : 0.0f, ba = row_move<0x101>(bl);
+                const float here = __builtin_bit_cast(float, ~mine & ~255u), there = __builtin_bit_cast(float, ~after & ~255u);      // distances from the best
+                sure = there - here > 2 * score_error + size * 0x1p-22f + kCut * there || (!border && xl == xa && bl == ba);
+            } else
+                sure = mine >> 8 != after >> 8 || (border ? sizeof(T) == 2 : xl >= xa);
+            unsure = unsure || (in && after && !sure);
+        }
+        const float share = row_share(how, xl, in, most, all);
+        const uint64_t again = __ballot(unsure);
+        if (t < tokens && (int)l < how.choices && !(again >> (lane & 48) & 0xffff)) {
+            const size_t to = (size_t)t * how.choices + l;
+            expert[to] = in ? (int32_t)at : -1;
+            weight[to] = how.factor * share;
+        }
+        if (__builtin_expect(again != 0, 0))
+            for (uint32_t i = 0; i < 4; ++i)
+                if ((again >> (i * kRowLanes) & 0xffff) && t0 + i < tokens)
+                    choose_exactly<T, (PER + 3) / 4>(logits, ld, t0 + i, experts, bias, how, expert, weight, s_key + (size_t)wave * experts);
     }
 }
 
@@ -212,9 +469,108 @@ __global__ __launch_bounds__(kWG) void choose_grad_kernel(const T *__restrict__ 
     }
 }
 
+// Four tokens to a wave: the chosen experts' gradients, one to a lane of 16, are put into a row of zeros in LDS, from where the row goes out
+// whole, four elements at a time.  UNITS of these to a lane.
+template <class T, int UNITS, bool WHOLE>
+__global__ __launch_bounds__(kWG) void choose_grad_rows_kernel(const T *__restrict__ logits, int64_t ld, uint32_t tokens, uint32_t experts,
+                                                               seer_choice how, const int32_t *__restrict__ expert,
+                                                               const float *__restrict__ dweight, T *__restrict__ dlogits, int64_t ldd)
+{
+    constexpr uint32_t ROW = UNITS * kRowLanes * 4;
+    __shared__ __attribute__((aligned(16))) float s_row[kWG / kRowLanes][ROW];
+    const uint32_t lane = threadIdx.x & 63, l = lane & (kRowLanes - 1);
+    float *mine = s_row[threadIdx.x / kRowLanes];
+    for (uint32_t t0 = blockIdx.x * (kWG / kRowLanes); t0 < tokens; t0 += gridDim.x * (kWG / kRowLanes)) {
+        const uint32_t t = min(t0 + threadIdx.x / kRowLanes, tokens - 1);
+        const T *row = logits + (int64_t)t * ld;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) *reinterpret_cast<v4f *>(mine + (u * kRowLanes + l) * 4) = v4f{0, 0, 0, 0};
+        float p[WHOLE ? UNITS * 4 : 1], most = -INFINITY, all = 0;
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int i = 0; i < UNITS * 4; ++i) {
+                const uint32_t e = (i / 4 * kRowLanes + l) * 4 + i % 4;
+                p[i] = e < experts ? (float)row[e] : -INFINITY;
+                most = p[i] != p[i] ? p[i] : fmaxf(most, p[i]);
+            }
+            most = row_max(most);
+#pragma unroll
+            for (int i = 0; i < UNITS * 4; ++i) all += p[i] = p[i] == -INFINITY ? 0.0f : __expf(p[i] - most);
+            all = row_sum(all);
+        }
+        int32_t e = -1;
+        float x = 0, dw = 0;
+        if ((int)l < how.choices) {
+            e = expert[(size_t)t * how.choices + l];
+            if (e >= 0 && e < (int32_t)experts) {
+                x = (float)row[e];
+                dw = dweight[(size_t)t * how.choices + l];
+            } else e = -1;
+            if (x == -INFINITY) e = -1;
+        }
+        const bool in = e >= 0;
+        const float share = row_share(how, x, in, most, all), part = in ? share * dw : 0.0f, sum = row_sum(part);
+        float g = how.renormalise ? part - share * sum : part;
+        if (how.score == SEER_SIGMOID) g *= fast_sigmoid(-x);
+        g = in ? how.factor * g : 0.0f;
+        // an expert that comes more than once: its first lane adds up
+        float of_expert = g;
+        bool first = in;
+        other_lanes([&](auto ctrl, uint32_t from) {
+            constexpr int CTRL = decltype(ctrl)::value;
+            const bool same = (int32_t)row_move<CTRL>((uint32_t)e) == e;
+            const float other = row_move<CTRL>(g);
+            of_expert += same ? other : 0.0f;
+            first = first && !(same && from < l);
+        });
+        __builtin_amdgcn_wave_barrier();            // (a wave's LDS accesses are served in order)
+        if (first) mine[e] = of_expert;
+        __builtin_amdgcn_wave_barrier();
+        const float off = how.factor * sum * __builtin_amdgcn_rcpf(all);
+        const bool any = (__ballot(in) >> (lane & 48) & 0xffff) != 0;
+        if (t0 + threadIdx.x / kRowLanes < tokens) {
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                const uint32_t at = (u * kRowLanes + l) * 4;
+                if (at >= experts) continue;
+                const v4f v = *reinterpret_cast<const v4f *>(mine + at);
+                float d[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[j] = WHOLE && any ? v[j] - p[WHOLE ? u * 4 + j : 0] * off : v[j];
+                T *to = dlogits + (int64_t)t * ldd + at;
+                if (at + 4 <= experts) {
+                    typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+                    four o;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[j] = (T)d[j];
+                    *reinterpret_cast<four *>(to) = o;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (at + j < experts) to[j] = (T)d[j];
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
 // ------------------------------------------------------------------ launches
 
 static dim3 token_grid(uint32_t tokens) { return dim3(std::min((tokens + kWG / kWave - 1) / (kWG / kWave), 1u << 20)); }
+
+// How a wave takes four tokens: the experts of a lane and the lanes of a group, which are whole and begin with a group's first.  per 0: it does not.
+struct RowShape { uint32_t per, group_lanes; };
+
+static RowShape row_shape(uint32_t experts, const seer_choice &how)
+{
+    if (experts > kFastExperts || how.choices > (int32_t)kFastChoices) return RowShape{0, 0};
+    if (how.best_groups == how.groups) return RowShape{(experts + kRowLanes - 1) / kRowLanes, 0};
+    const uint32_t groups = (uint32_t)how.groups, length = experts / groups;
+    for (uint32_t lanes = 8; lanes; lanes /= 2)
+        if (groups * lanes <= kRowLanes && length % lanes == 0 && length / lanes <= kFastExperts / kRowLanes) return RowShape{length / lanes, lanes};
+    return RowShape{0, 0};
+}
 
 void launch_choose(const seer_dense &logits, const float *bias, const seer_choice &how, int32_t *expert, float *weight, hipStream_t st)
 {
@@ -227,6 +583,26 @@ void launch_choose(const seer_dense &logits, const float *bias, const seer_choic
                                logits.ld, tokens, experts, bias, how, expert, weight);
         };
         using std::integral_constant;
+        const RowShape r = row_shape(experts, how);
+        if (r.per) {
+            const bool vec = r.per % 4 == 0 && experts % 4 == 0;
+            const auto rows = [&](auto per, auto vectors) {
+                const auto go = [&](auto with_bias) {
+                    hipLaunchKernelGGL((choose_rows_kernel<T, decltype(per)::value, decltype(vectors)::value, decltype(with_bias)::value>),
+                                       dim3(std::min((tokens + kWG / kRowLanes - 1) / (kWG / kRowLanes), kRowBlocks)), dim3(kWG), lds, st,
+                                       static_cast<const T *>(logits.data), logits.ld, tokens, experts, r.per, r.group_lanes, bias, how, expert, weight);
+                };
+                if (bias) go(std::true_type{});
+                else go(std::false_type{});
+            };
+            const auto of_width = [&](auto per) { vec ? rows(per, std::true_type{}) : rows(per, std::false_type{}); };
+            if (r.per == 1) rows(integral_constant<int, 1>{}, std::false_type{});
+            else if (r.per <= 4) of_width(integral_constant<int, 4>{});
+            else if (r.per <= 8) of_width(integral_constant<int, 8>{});
+            else if (r.per <= 12) of_width(integral_constant<int, 12>{});
+            else of_width(integral_constant<int, 16>{});
+            return;
+        }
         if (experts <= 64) launch(integral_constant<int, 1>{});
         else if (experts <= 128) launch(integral_constant<int, 2>{});
         else if (experts <= 256) launch(integral_constant<int, 4>{});
@@ -241,6 +617,24 @@ void launch_choose_grad(const seer_dense &logits, const seer_choice &how, const 
 {
     by_type(logits.type, [&](auto *of) {
         using T = std::remove_pointer_t<decltype(of)>;
+        const uint32_t tokens = (uint32_t)logits.rows, experts = (uint32_t)logits.cols;
+        if (experts <= kFastExperts && how.choices <= (int32_t)kRowLanes) {
+            const bool whole = how.score == SEER_SOFTMAX && !how.renormalise;
+            const auto rows = [&](auto units) {
+                const auto go = [&](auto all) {
+                    hipLaunchKernelGGL((choose_grad_rows_kernel<T, decltype(units)::value, decltype(all)::value>),
+                                       dim3(std::min((tokens + kWG / kRowLanes - 1) / (kWG / kRowLanes), 1u << 20)), dim3(kWG), 0, st,
+                                       static_cast<const T *>(logits.data), logits.ld, tokens, experts, how, expert, dweight,
+                                       static_cast<T *>(dlogits.data), dlogits.ld);
+                };
+                if (whole) go(std::true_type{});
+                else go(std::false_type{});
+            };
+            if (experts <= 64) rows(std::integral_constant<int, 1>{});
+            else if (experts <= 128) rows(std::integral_constant<int, 2>{});
+            else rows(std::integral_constant<int, 4>{});
+            return;
+        }
         hipLaunchKernelGGL((choose_grad_kernel<T>), token_grid((uint32_t)logits.rows), dim3(kWG), 0, st, static_cast<const T *>(logits.data), logits.ld,
                            (uint32_t)logits.rows, (uint32_t)logits.cols, how, expert, dweight, static_cast<T *>(dlogits.data), dlogits.ld);
     });
