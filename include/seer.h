@@ -638,10 +638,22 @@ int seer_route_gather_mx4(const seer_routing *r, const seer_dense *x, const seer
  * rows from group_ptr[groups] on are set to zero.  Products are exact, sums are in fp32, the same on every run, rounded to out's type
  * once.  b has groups * channels rows, the channels of group 0 first, and a's columns; out: a's rows, `channels` = out's columns;
  * SEER_F32, SEER_BF16 or SEER_F16.  group_ptr as in seer_i8_product.  SEER_ELIMIT for more than SEER_MAX_EXPERTS groups, or 2^30 or
- * more tiles of 128 rows of one group by 128 channels. */
+ * more tiles of 128 rows of one group by 128 channels.
+ * workspace: >= seer_mx4_product_workspace_bytes(a.rows, out.cols, a.cols, groups) (may be 0); for the kernel SEER_MX4_SHARED, others use none. */
 int seer_mx4_product(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups, const seer_dense *out,
                      void *workspace, size_t workspace_bytes, void *stream);
 size_t seer_mx4_product_workspace_bytes(int64_t rows, int64_t channels, int64_t columns, int32_t groups);
+
+/* Which kernel seer_mx4_product takes for these operands (by their sizes and the distances of their rows), or a negative seer_status.  Nothing is
+ * launched and nothing is read through a pointer. */
+typedef enum {
+    SEER_MX4_NONE = 0,   /* nothing to compute                                              */
+    SEER_MX4_ANY = 1,    /* rows of 8 MiB or more                                           */
+    SEER_MX4_FEW = 2,    /* few rows to a group                                             */
+    SEER_MX4_TILES = 3,  /* tiles straight into LDS                                         */
+    SEER_MX4_SHARED = 4  /* the same with the columns shared out, in two launches           */
+} seer_mx4_kernel;
+int seer_mx4_product_kernel(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups);
 
 /* One of the many tensors whose gradient is clipped: n contiguous elements. */
 typedef struct {

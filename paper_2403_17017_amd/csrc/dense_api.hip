@@ -316,14 +316,27 @@ int seer_mx4_product(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_
     const Mx4Args p{bytes(a->data), bytes(b->data), bytes(a->scale), bytes(b->scale), group_ptr, out->data, a->ld, b->ld, a->scale_ld, b->scale_ld, out->ld,
                     (uint32_t)a->rows, (uint32_t)out->cols, (uint32_t)((a->cols + 31) / 32), (uint32_t)groups, out->type};
     if (!mx4_product_fits(p)) return SEER_ELIMIT;
-    const size_t need = mx4_workspace_bytes(p.rows, p.channels, p.blocks, p.groups);
+    const Mx4Plan plan = mx4_plan(p);
+    const size_t need = plan.kernel == SEER_MX4_SHARED ? mx4_workspace_bytes(p.rows, p.channels, p.blocks, p.groups) : 0;
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return SEER_EWORKSPACE;
     const Extent ws = extent(workspace, need);
     if (overlap(ws, to)) return SEER_EINVAL;
     for (const Extent &in : ins)
         if (overlap(ws, in)) return SEER_EINVAL;
-    launch_mx4_product(p, workspace, on(stream));
+    launch_mx4_product(p, plan, workspace, on(stream));
     return done();
+}
+
+int seer_mx4_product_kernel(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups)
+{
+    if (!a || !b || groups < 1 || (!group_ptr && groups != 1)) return SEER_EINVAL;
+    int rc;
+    if ((rc = check_mx4(a, a->rows, a->cols)) != SEER_OK || (rc = check_mx4(b, b->rows, a->cols)) != SEER_OK) return rc;
+    if (b->rows % groups != 0) return SEER_EINVAL;
+    const Mx4Args p{nullptr, nullptr, nullptr, nullptr, group_ptr, nullptr, a->ld, b->ld, a->scale_ld, b->scale_ld, 0,
+                    (uint32_t)a->rows, (uint32_t)(b->rows / groups), (uint32_t)((a->cols + 31) / 32), (uint32_t)groups, SEER_F32};
+    if (!mx4_product_fits(p)) return SEER_ELIMIT;
+    return p.rows == 0 || p.channels == 0 ? SEER_MX4_NONE : mx4_plan(p).kernel;
 }
 
 size_t seer_grad_workspace_bytes(void) { return grad_workspace_bytes(); }

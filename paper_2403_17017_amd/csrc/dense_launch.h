@@ -52,8 +52,10 @@ struct Mx4Args {
 };
 void launch_mx4_quantize(const RouteRows &r, const seer_dense &x, const seer_mx4 &q, hipStream_t st);
 bool mx4_product_fits(const Mx4Args &a);
+struct Mx4Plan { int32_t kernel /* seer_mx4_kernel */; uint32_t tokens /* to a tile */, shares /* of the columns */; };
+Mx4Plan mx4_plan(const Mx4Args &a);         // by sizes and distances of rows
 size_t mx4_workspace_bytes(uint32_t rows, uint32_t channels, uint32_t blocks, uint32_t groups);
-void launch_mx4_product(const Mx4Args &a, void *workspace, hipStream_t st);
+void launch_mx4_product(const Mx4Args &a, const Mx4Plan &p, void *workspace, hipStream_t st);
 
 constexpr uint32_t kGradParts = 2048;       // partial sums of squares
 inline size_t grad_workspace_bytes() { return kGradParts * sizeof(double); }

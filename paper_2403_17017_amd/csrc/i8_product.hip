@@ -18,41 +18,6 @@ namespace seer {
 // at 4112; 278 with 64 x 64, nothing under way and loads from odd addresses).
 constexpr uint32_t kAnyTokens = 128, kAnyChannels = 128, kAnyCols = 128, kAnyPitch = kAnyCols + 16;
 
-// The first n bytes, and zeros behind them.
-__device__ __forceinline__ v4i32 first_bytes(v4i32 v, int n)
-{
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int keep = min(max(n - 4 * j, 0), 4);
-        v[j] = keep ? v[j] & (int)(~0u >> (32 - 8 * keep)) : 0;
-    }
-    return v;
-}
-
-// 16 bytes from any address, of which n are there (at least 1), out of whole words: loads that are not at multiples of 4 take four times as long.
-// (A word of which a byte is there is in memory.)
-__device__ __forceinline__ v4i32 load_16(const int8_t *p, int n)
-{
-    typedef int words __attribute__((ext_vector_type(4), aligned(4)));
-    const uint32_t by = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
-    const int8_t *from = p - by;
-    int w[5];
-    if (n >= 16) {
-        const words v = *reinterpret_cast<const words *>(from);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = v[j];
-        w[4] = *reinterpret_cast<const int *>(from + (by ? 16 : 12));
-    } else {
-        const int last = ((int)by + n - 1) / 4;
-#pragma unroll
-        for (int j = 0; j < 5; ++j) w[j] = *reinterpret_cast<const int *>(from + 4 * min(j, last));
-    }
-    v4i32 v;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = (int)__builtin_amdgcn_alignbyte((uint32_t)w[j + 1], (uint32_t)w[j], by);
-    return n >= 16 ? v : first_bytes(v, n);
-}
-
 template <class T>
 __global__ __launch_bounds__(256) void i8_any_kernel(I8Args a, uint32_t blocks)
 {

@@ -24,6 +24,7 @@ def bind(L):
     dense, mx4, routing = C.POINTER(R.seer_dense), C.POINTER(seer_mx4), C.POINTER(R.seer_routing)
     for name, args, res in (("seer_mx4_quantize", [dense, mx4, vp], C.c_int), ("seer_route_gather_mx4", [routing, dense, mx4, vp], C.c_int),
                             ("seer_mx4_product", [mx4, mx4, vp, i32, dense, vp, sz, vp], C.c_int),
+                            ("seer_mx4_product_kernel", [mx4, mx4, vp, i32], C.c_int),
                             ("seer_mx4_product_workspace_bytes", [i64, i64, i64, i32], sz)):
         f = getattr(L, name)
         f.argtypes, f.restype = args, res
@@ -55,6 +56,21 @@ def seer_route_gather_mx4(r: R.Routing, x, q=None, scale=None, stream=None):
 
 def mx4_product_workspace_bytes(rows: int, channels: int, columns: int, groups: int = 1) -> int:
     return int(B.lib().seer_mx4_product_workspace_bytes(rows, channels, columns, groups))
+
+
+MX4_KERNELS = ("none", "any", "few", "tiles", "shared")
+
+
+def mx4_product_kernel(a, b, group_ptr=None) -> str:
+    """Which kernel seer_mx4_product takes for these codes, one of MX4_KERNELS; nothing is launched."""
+    if b.dim() not in (2, 3):
+        raise ValueError("b is to be [groups, channels, bytes]")
+    groups, blocks = b.shape[0] if b.dim() == 3 else 1, a.shape[-1] // 16
+    rows_of = lambda t, rows: C.byref(seer_mx4(t.data_ptr(), t.data_ptr(), rows, 32 * blocks, t.stride(-2) if rows > 1 else 16 * blocks, blocks))
+    rc = B.lib().seer_mx4_product_kernel(rows_of(a, a.shape[0]), rows_of(b, groups * b.shape[-2]), group_ptr.data_ptr() if group_ptr is not None else None, groups)
+    if rc < 0:
+        raise SeerError(rc, "seer_mx4_product_kernel")
+    return MX4_KERNELS[rc]
 
 
 def seer_mx4_product(a, a_scale, b, b_scale, out=None, group_ptr=None, dtype=None, workspace=None, stream=None):

@@ -247,3 +247,39 @@ def test_same_bits_and_captured():
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(out, run())
+
+
+KERNELS = [  # rows, channels, blocks, lengths of the groups, kernel
+    (0, 8, 4, None, "none"), (3, 130, 20, None, "few"), (40, 300, 40, [20, 0, 20], "few"), (3000, 1500, 8, None, "tiles"), (900, 600, 16, [500, 400], "tiles"),
+    (700, 3000, 33, None, "tiles"), (150, 3000, 64, None, "few"), (200, 512, 400, None, "shared"), (203, 260, 301, None, "shared"), (300, 260, 256, [180, 120], "shared"),
+]
+
+
+@pytest.mark.parametrize("case", KERNELS, ids=str)
+def test_every_kernel(case):
+    announce(f"mx4 kernel {case}")
+    rows, channels, blocks, lengths, kernel = case
+    rng = np.random.default_rng(rows)
+    more = 5 if lengths else 0
+    a, b = codes(rng, rows + more, blocks), codes(rng, len(lengths) if lengths else 1, channels, blocks)
+    ptr = None if lengths is None else np.concatenate([[0], np.cumsum(lengths)]).tolist()
+    assert S.mx4_product_kernel(a[0], b[0], None if ptr is None else torch.tensor(ptr, dtype=torch.int32, device="cuda:0")) == kernel
+    for kind in TYPES:
+        out = check_product(a, b, ptr, kind)
+        assert not more or not out[-more:].any()
+
+
+def test_rows_far_apart():
+    """8 MiB from row to row."""
+    rng = np.random.default_rng(6)
+    a, b = codes(rng, 3, 20), codes(rng, 1, 5, 20)
+    want = S.seer_mx4_product(*a, *b, dtype=torch.float32)
+    qa, qb = spread(a[0], 1 << 23, 0x77), spread(b[0][0], 1 << 23, 0x77)
+    assert S.mx4_product_kernel(qa, qb) == "any" and S.mx4_product_kernel(*[t[0] for t in (a, b)]) == "few"
+    check_product((qa, a[1]), (qb[None], b[1]), None, "f32")
+    out = torch.full((3, 9), 55.0, device="cuda:0")
+    S.seer_mx4_product(qa, a[1], qb, b[1][0], out=out[:, :5])
+    assert torch.allclose(out[:, :5], want, rtol=1e-5, atol=1e-4 * float(want.abs().max())) and bool((out[:, 5:] == 55).all())
+    ptr = torch.tensor([1, 2], dtype=torch.int32, device="cuda:0")
+    y = S.seer_mx4_product(qa, a[1], qb, b[1][0], group_ptr=ptr, dtype=torch.float32)
+    assert torch.equal(y[1], out[1, :5]) and not y[2].any()
