@@ -63,7 +63,7 @@ struct DigitArgs {
     Pairs from, to;         // from.row null: the tokens themselves
     uint32_t count, rows, per_wave, groups;
     int shift, bits;
-    uint32_t *counts;       // [groups][1 << bits], where there is more than one
+    uint32_t *counts;       // [groups][1 << bits]
 };
 
 template <class I>
@@ -82,22 +82,13 @@ __device__ __forceinline__ void place_digits(const DigitArgs &a, const I *token,
     __syncthreads();
     const uint32_t from = min(a.count, (group * kDigitWaves + wave) * a.per_wave), to = min(a.count, from + a.per_wave);
     for (uint32_t i = from + lane; i < to; i += 64) atomicAdd(&cnt[wave * buckets + (pair_row(a, token, i) >> a.shift & mask)], 1u);
-    if (a.groups > 1)
-        for (uint32_t i = threadIdx.x, all = a.groups * buckets; i < all; i += blockDim.x) {
-            const uint32_t n = a.counts[i];
-            if (n == 0) continue;
-            atomicAdd(&base[i & mask], n);
-            if (i >> a.bits < group) atomicAdd(&before[i & mask], n);
-        }
-    __syncthreads();
-    if (a.groups == 1) {
-        for (uint32_t k = threadIdx.x; k < buckets; k += blockDim.x) {
-            uint32_t sum = 0;
-            for (uint32_t w = 0; w < kDigitWaves; ++w) sum += cnt[w * buckets + k];
-            base[k] = sum;
-        }
-        __syncthreads();
+    for (uint32_t i = threadIdx.x, all = a.groups * buckets; i < all; i += blockDim.x) {
+        const uint32_t n = a.counts[i];
+        if (n == 0) continue;
+        atomicAdd(&base[i & mask], n);
+        if (i >> a.bits < group) atomicAdd(&before[i & mask], n);
     }
+    __syncthreads();
     scan_lds(base, buckets, s_wave);
     for (uint32_t k = threadIdx.x; k < buckets; k += blockDim.x) {
         uint32_t sum = base[k] + before[k];
@@ -128,10 +119,23 @@ __device__ __forceinline__ void place_digits(const DigitArgs &a, const I *token,
     }
 }
 
+// Where a row's places begin, plus one, and end; {0, ..} for rows that are no token's.
+struct Places { uint32_t first, end; };
+// Beside the first launch of a sort other workgroups clear these (rows 0: they were not asked for).
+struct Clear { Places *places; uint32_t rows; };
+constexpr uint32_t kClearRows = 8192;               // of a workgroup
+
+__device__ __forceinline__ void clear_places(const Clear &c, uint32_t block)
+{
+    for (uint32_t i = block * kClearRows + threadIdx.x, end = min(c.rows, (block + 1) * kClearRows); i < end; i += blockDim.x) c.places[i] = Places{0, 0};
+}
+__global__ __launch_bounds__(kDigitWaves * 64) void clear_places_kernel(Clear c) { clear_places(c, blockIdx.x); }
+
 template <class I>
-__global__ __launch_bounds__(kDigitWaves * 64) void count_digits_kernel(DigitArgs a, const I *__restrict__ token)
+__global__ __launch_bounds__(kDigitWaves * 64) void count_digits_kernel(DigitArgs a, const I *__restrict__ token, Clear clear)
 {
     __shared__ uint32_t s_cnt[1 << kDigitBits];
+    if (blockIdx.x >= a.groups) return clear_places(clear, blockIdx.x - a.groups);
     const uint32_t buckets = 1u << a.bits;
     for (uint32_t i = threadIdx.x; i < buckets; i += blockDim.x) s_cnt[i] = 0;
     __syncthreads();
@@ -149,18 +153,31 @@ __global__ __launch_bounds__(kDigitWaves * 64) void place_digits_kernel(DigitArg
     place_digits(a, token, blockIdx.x, lds, s_wave);
 }
 
-// All digits in one workgroup; pass p leaves its pairs in pairs[p & 1].
-struct PairBuffers { Pairs at[2]; };
+// Few tokens find their places by counting, 16 lanes to a token: the rows below its own, and its own row's tokens before it.  1031 tokens: 3.6 us
+// in one launch (sorted by digits in one workgroup 11).
+constexpr uint32_t kRankTokens = 4096, kRankLanes = 16;
+
 template <class I>
-__global__ __launch_bounds__(kDigitWaves * 64) void sort_pairs_kernel(DigitArgs a, const I *__restrict__ token, PairBuffers pairs, int passes)
+__global__ __launch_bounds__(kWG) void rank_pairs_kernel(const I *__restrict__ token, uint32_t count, uint32_t rows, Pairs to, uint32_t blocks, Clear clear)
 {
-    extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
-    __shared__ uint32_t s_wave[kDigitWaves];
-    for (int p = 0; p < passes; ++p, a.shift += a.bits) {
-        if (p) a.from = pairs.at[(p - 1) & 1];
-        a.to = pairs.at[p & 1];
-        place_digits(a, token, 0, lds, s_wave);
-        __syncthreads();
+    __shared__ __attribute__((aligned(16))) uint32_t s_row[kRankTokens];
+    if (blockIdx.x >= blocks) return clear_places(clear, blockIdx.x - blocks);
+    const uint32_t padded = (count + 3) & ~3u;
+    for (uint32_t i = threadIdx.x; i < padded; i += kWG) s_row[i] = i < count ? row_of(token, i, rows) : ~0u;     // (behind all rows)
+    __syncthreads();
+    const uint32_t t = blockIdx.x * (kWG / kRankLanes) + threadIdx.x / kRankLanes, lane = threadIdx.x % kRankLanes;
+    const uint32_t row = s_row[min(t, count - 1)];
+    uint32_t before = 0;
+    for (uint32_t i = lane * 4; i < padded; i += kRankLanes * 4) {
+        const v4i k = *reinterpret_cast<const v4i *>(s_row + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) before += (uint32_t)k[j] < row || ((uint32_t)k[j] == row && i + j < t);
+    }
+#pragma unroll
+    for (uint32_t d = 1; d < kRankLanes; d <<= 1) before += (uint32_t)__shfl_xor((int)before, (int)d, kWave);
+    if (t < count && lane == 0) {
+        to.row[before] = row;
+        to.token[before] = t;
     }
 }
 
@@ -169,27 +186,18 @@ __global__ __launch_bounds__(kDigitWaves * 64) void sort_pairs_kernel(DigitArgs 
 // Every row of the table adds up its tokens' rows of dy in the order of the tokens.  Where a row has many, sums of kRun
 // consecutive places that are all its own are made beforehand, and of kRun such sums, each by a workgroup of its own; the row then
 // takes the largest pieces that lie in its range.  Bound by bytes.
-constexpr uint32_t kRun = 32;
-
-// Where a row's places begin, plus one, and end; {0, ..} for rows that are no token's.
-struct Places { uint32_t first, end; };
+constexpr uint32_t kRun = 16;
 
 struct GradArgs {
     Pairs sorted;
     Places *places;         // [rows]
-    float *run, *runs;      // sums of kRun places, and of kRun such sums, [count / kRun][cols] and [count / kRun^2][cols]
-    uint32_t count, rows, cols;
+    float *run, *runs;      // sums of kRun places, and of kRun such sums, [count / kRun][pitch] and [count / kRun^2][pitch]; runs may be null
+    uint32_t count, rows, cols, pitch;
     float scale;
 };
 
-__global__ __launch_bounds__(kWG) void clear_places_kernel(Places *places, uint32_t rows)
+__device__ __forceinline__ void mark_places(const GradArgs &a, uint32_t i)
 {
-    for (uint32_t i = blockIdx.x * kWG + threadIdx.x; i < rows; i += gridDim.x * kWG) places[i] = Places{0, 0};
-}
-
-__global__ __launch_bounds__(kWG) void mark_places_kernel(GradArgs a)
-{
-    const uint32_t i = blockIdx.x * kWG + threadIdx.x;
     if (i >= a.count) return;
     const uint32_t row = a.sorted.row[i];
     if (row >= a.rows) return;
@@ -202,14 +210,24 @@ template <class T>
 __device__ __forceinline__ void add_places(const GradArgs &a, const T *dy, int64_t ldy, uint32_t from, uint32_t to, uint32_t col, int n,
                                            float (&acc)[Unit<T>::kElems])
 {
-    constexpr int E = Unit<T>::kElems, AT_ONCE = 4;
-    for (uint32_t at = from; at < to; at += AT_ONCE) {
+    constexpr int E = Unit<T>::kElems, AT_ONCE = 16;
+    uint32_t at = from;
+    for (; at + AT_ONCE <= to; at += AT_ONCE) {
         Unit<T> u[AT_ONCE];
 #pragma unroll
-        for (uint32_t i = 0; i < AT_ONCE; ++i)
-            if (at + i < to) u[i] = load_some(dy + (int64_t)a.sorted.token[at + i] * ldy + col, n);
+        for (uint32_t i = 0; i < AT_ONCE; ++i) u[i] = load_some(dy + (int64_t)a.sorted.token[at + i] * ldy + col, n);
 #pragma unroll
         for (uint32_t i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+            for (int j = 0; j < E; ++j) acc[j] += (float)u[i].v[j];
+    }
+    if (at < to) {                                      // (the last one again, and not added)
+        Unit<T> u[AT_ONCE - 1];
+#pragma unroll
+        for (uint32_t i = 0; i < AT_ONCE - 1; ++i)
+            if (at + i < to) u[i] = load_some(dy + (int64_t)a.sorted.token[at + i] * ldy + col, n);
+#pragma unroll
+        for (uint32_t i = 0; i < AT_ONCE - 1; ++i)
             if (at + i < to) {
 #pragma unroll
                 for (int j = 0; j < E; ++j) acc[j] += (float)u[i].v[j];
@@ -219,36 +237,48 @@ __device__ __forceinline__ void add_places(const GradArgs &a, const T *dy, int64
 
 // acc += sums [from, to) of those made beforehand.
 template <int E>
-__device__ __forceinline__ void add_sums(const float *sums, uint32_t cols, uint32_t from, uint32_t to, uint32_t col, int n, float (&acc)[E])
+__device__ __forceinline__ void add_sums(const float *sums, uint32_t pitch, uint32_t from, uint32_t to, uint32_t col, float (&acc)[E])
 {
-    for (uint32_t at = from; at < to; ++at)
+    constexpr uint32_t AT_ONCE = 8;
+    for (uint32_t at = from; at < to; at += AT_ONCE) {
+        v4f u[AT_ONCE][E / 4];
 #pragma unroll
-        for (int j = 0; j < E; ++j) acc[j] += j < n ? sums[(size_t)at * cols + col + j] : 0.0f;
+        for (uint32_t i = 0; i < AT_ONCE; ++i)
+            if (at + i < to) {
+#pragma unroll
+                for (int j = 0; j < E / 4; ++j)
+                    if (col + 4 * j < pitch) u[i][j] = *reinterpret_cast<const v4f *>(sums + (size_t)(at + i) * pitch + col + 4 * j);
+            }
+#pragma unroll
+        for (uint32_t i = 0; i < AT_ONCE; ++i)
+            if (at + i < to) {
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+                    if (col + j / 4 * 4 < pitch) acc[j] += u[i][j / 4][j % 4];
+            }
+    }
 }
 
-// LEVEL 1: sums of kRun places that are one row's; 2: of kRun such sums.
+// LEVEL 1: sums of kRun places that are one row's, and, in the first workgroups, where each row's places are; 2: of kRun such sums.
 template <class T, int LANES, int LEVEL>
-__global__ __launch_bounds__(kWG) void run_kernel(GradArgs a, const T *__restrict__ dy, int64_t ldy)
+__global__ __launch_bounds__(kWG) void run_kernel(GradArgs a, const T *__restrict__ dy, int64_t ldy, uint32_t marking)
 {
     constexpr int E = Unit<T>::kElems;
-    constexpr uint32_t LENGTH = LEVEL == 1 ? kRun : kRun * kRun;
-    const uint32_t runs = a.count / LENGTH;
-    for (uint32_t b = blockIdx.y; b * (kWG / LANES) < runs; b += gridDim.y) {
-        const uint32_t r = b * (kWG / LANES) + row_in_block<LANES>();
-        if (r >= runs) continue;
-        const uint32_t row = a.sorted.row[r * LENGTH];
-        if (row >= a.rows || a.sorted.row[r * LENGTH + LENGTH - 1] != row) continue;
-        for (uint32_t col = (blockIdx.x * LANES + threadIdx.x % LANES) * E; col < a.cols; col += gridDim.x * LANES * E) {
-            const int n = (int)min((uint32_t)E, a.cols - col);
-            float acc[E] = {};
-            if constexpr (LEVEL == 1) add_places(a, dy, ldy, r * kRun, (r + 1) * kRun, col, n, acc);
-            else add_sums<E>(a.run, a.cols, r * kRun, (r + 1) * kRun, col, n, acc);
-            float *to = (LEVEL == 1 ? a.run : a.runs) + (size_t)r * a.cols + col;
+    constexpr uint32_t LENGTH = LEVEL == 1 ? kRun : kRun * kRun, ROWS = kWG / LANES;
+    if (LEVEL == 1 && blockIdx.x < marking) return mark_places(a, blockIdx.x * kWG + threadIdx.x);
+    const uint32_t runs = a.count / LENGTH, across = (a.cols + LANES * E - 1) / (LANES * E), block = blockIdx.x - marking;
+    const uint32_t r = block / across * ROWS + row_in_block<LANES>(), col = (block % across * LANES + threadIdx.x % LANES) * E;
+    if (r >= runs || col >= a.cols) return;
+    const uint32_t row = a.sorted.row[r * LENGTH];
+    if (row >= a.rows || a.sorted.row[r * LENGTH + LENGTH - 1] != row) return;
+    const int n = (int)min((uint32_t)E, a.cols - col);
+    float acc[E] = {};
+    if constexpr (LEVEL == 1) add_places(a, dy, ldy, r * kRun, (r + 1) * kRun, col, n, acc);
+    else add_sums<E>(a.run, a.pitch, r * kRun, (r + 1) * kRun, col, acc);
+    float *to = (LEVEL == 1 ? a.run : a.runs) + (size_t)r * a.pitch + col;
 #pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (j < n) to[j] = acc[j];
-        }
-    }
+    for (int j = 0; j < E; j += 4)
+        if (j < n) *reinterpret_cast<v4f *>(to + j) = v4f{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
 }
 
 // E results, rounded to the type of the output.
@@ -266,40 +296,106 @@ __device__ __forceinline__ void store_sums(O *p, const float (&v)[E], int n)
         }
 }
 
-// ADD: by place, the first of each row adds to it; else by row of the table.
-template <class T, class O, int LANES, bool ADD>
-__global__ __launch_bounds__(kWG) void embed_grad_kernel(GradArgs a, const T *__restrict__ dy, int64_t ldy, O *__restrict__ dtable, int64_t ldt)
+// The rows that are a token's: the first of a row's places is who adds up, LANES lanes to UNITS pieces of 16 bytes each (of dy), a row in as many
+// parts as that takes; plus what is there, with ADD.  Its loads wait for one another four deep, so what counts is how many rows are
+// under way, and how many of a row's places: 131 072 x 4096 bf16 with 28 000 rows of tokens, the whole call, 322 us with a workgroup to each row,
+// 286 with four pieces and four places at a time, 275 with two and eight; 50 000 x 1024 84 and 67, 8000 x 512 54 and 44.
+template <class T, class O, int LANES, int UNITS, bool ADD>
+__device__ __forceinline__ void sum_row(const GradArgs &a, const T *__restrict__ dy, int64_t ldy, O *__restrict__ dtable, int64_t ldt, uint32_t i, uint32_t part)
 {
     constexpr int E = Unit<T>::kElems;
-    const uint32_t items = ADD ? a.count : a.rows;
-    for (uint32_t b = blockIdx.y; b * (kWG / LANES) < items; b += gridDim.y) {
-        const uint32_t item = b * (kWG / LANES) + row_in_block<LANES>();
-        if (item >= items) continue;
-        const uint32_t row = ADD ? a.sorted.row[item] : item;
-        if (ADD && (row >= a.rows || (item > 0 && a.sorted.row[item - 1] == row))) continue;
-        const Places p = a.places[row];
-        const uint32_t first = p.first ? p.first - 1 : 0, end = p.first ? p.end : 0;
-        // whole runs of kRun, and of kRun of these, in the row's range
-        const uint32_t run0 = (first + kRun - 1) / kRun, run1 = end / kRun;
-        const uint32_t runs0 = (run0 + kRun - 1) / kRun, runs1 = run1 / kRun;
-        for (uint32_t col = (blockIdx.x * LANES + threadIdx.x % LANES) * E; col < a.cols; col += gridDim.x * LANES * E) {
-            const int n = (int)min((uint32_t)E, a.cols - col);
-            float acc[E] = {};
-            if (run0 >= run1) add_places(a, dy, ldy, first, end, col, n, acc);
-            else {
-                add_places(a, dy, ldy, first, run0 * kRun, col, n, acc);
-                if (runs0 >= runs1) add_sums<E>(a.run, a.cols, run0, run1, col, n, acc);
-                else {
-                    add_sums<E>(a.run, a.cols, run0, runs0 * kRun, col, n, acc);
-                    add_sums<E>(a.runs, a.cols, runs0, runs1, col, n, acc);
-                    add_sums<E>(a.run, a.cols, runs1 * kRun, run1, col, n, acc);
-                }
-                add_places(a, dy, ldy, run1 * kRun, end, col, n, acc);
-            }
-            O *to = dtable + (int64_t)row * ldt + col;
+    constexpr uint32_t AT_ONCE = 8;
+    const uint32_t row = a.sorted.row[i];
+    if (row >= a.rows || (i > 0 && a.sorted.row[i - 1] == row)) return;
+    const uint32_t end = a.places[row].end, col0 = (part * UNITS * LANES + threadIdx.x % LANES) * E;
+    O *to = dtable + (int64_t)row * ldt;
+    float acc[UNITS][E] = {};
+    Unit<O> held[ADD ? UNITS : 1][E / Unit<O>::kElems];
+    const auto have = [&](int u) { return (int)a.cols - (int)(col0 + u * LANES * E); };         // columns from piece u's first on
+    if constexpr (ADD) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) acc[j] = !p.first ? 0.0f : a.scale * acc[j] + (ADD && j < n ? (float)to[j] : 0.0f);
-            store_sums<O, E>(to, acc, n);
+        for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+            for (int j = 0; j < E; j += Unit<O>::kElems)
+                if (have(u) > j) held[u][j / Unit<O>::kElems] = load_some(to + col0 + u * LANES * E + j, have(u) - j);
+    }
+    const auto add = [&](uint32_t from, uint32_t upto) {
+        for (uint32_t at = from; at < upto; at += AT_ONCE) {
+            Unit<T> v[AT_ONCE][UNITS];
+#pragma unroll
+            for (uint32_t k = 0; k < AT_ONCE; ++k)
+                if (at + k < upto) {
+                    const T *y = dy + (int64_t)a.sorted.token[at + k] * ldy + col0;
+#pragma unroll
+                    for (int u = 0; u < UNITS; ++u)
+                        if (have(u) > 0) v[k][u] = load_some(y + u * LANES * E, have(u));
+                }
+#pragma unroll
+            for (uint32_t k = 0; k < AT_ONCE; ++k)
+                if (at + k < upto) {
+#pragma unroll
+                    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+                        for (int j = 0; j < E; ++j) acc[u][j] += (float)v[k][u].v[j];
+                }
+        }
+    };
+    // whole runs of kRun, and of kRun of these, in the row's range
+    const uint32_t run0 = (i + kRun - 1) / kRun, run1 = end / kRun;
+    const uint32_t runs0 = (run0 + kRun - 1) / kRun, runs1 = a.runs ? run1 / kRun : 0;
+    const auto sums = [&](const float *of, uint32_t from, uint32_t upto) {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) add_sums<E>(of, a.pitch, from, upto, col0 + u * LANES * E, acc[u]);
+    };
+    if (run0 >= run1) add(i, end);
+    else {
+        add(i, run0 * kRun);
+        if (runs0 >= runs1) sums(a.run, run0, run1);
+        else {
+            sums(a.run, run0, runs0 * kRun);
+            sums(a.runs, runs0, runs1);
+            sums(a.run, runs1 * kRun, run1);
+        }
+        add(run1 * kRun, end);
+    }
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        if (have(u) <= 0) continue;
+#pragma unroll
+        for (int j = 0; j < E; ++j) acc[u][j] = a.scale * acc[u][j] + (ADD ? (float)held[ADD ? u : 0][j / Unit<O>::kElems].v[j % Unit<O>::kElems] : 0.0f);
+        store_sums<O, E>(to + col0 + u * LANES * E, acc[u], have(u));
+    }
+}
+
+// The first `summing` workgroups; the others write zeros to rows that are no token's, kAhead rows at a time.
+// STREAM: whole rows lie at multiples of 16 bytes and leave the caches as they are written.
+constexpr uint32_t kAhead = 2;
+
+template <class T, class O, int LANES, int UNITS, bool ADD, bool STREAM>
+__global__ __launch_bounds__(kWG) void rows_kernel(GradArgs a, const T *__restrict__ dy, int64_t ldy, O *__restrict__ dtable, int64_t ldt, uint32_t summing)
+{
+    constexpr uint32_t ROWS = kWG / LANES;
+    if (blockIdx.x < summing) {
+        const uint32_t parts = (a.cols + UNITS * LANES * Unit<T>::kElems - 1) / (UNITS * LANES * Unit<T>::kElems);
+        const uint64_t items = (uint64_t)a.count * parts;
+        for (uint64_t w = (uint64_t)blockIdx.x * ROWS + row_in_block<LANES>(); w < items; w += (uint64_t)summing * ROWS)
+            sum_row<T, O, LANES, UNITS, ADD>(a, dy, ldy, dtable, ldt, (uint32_t)(w / parts), (uint32_t)(w % parts));
+        return;
+    }
+    constexpr int E = Unit<O>::kElems;
+    constexpr uint32_t ZLANES = LANES < kWave ? LANES : kWG, ZROWS = kWG / ZLANES;
+    const uint32_t lane = threadIdx.x % ZLANES;
+    for (uint32_t b = blockIdx.x - summing; b * ZROWS * kAhead < a.rows; b += gridDim.x - summing) {
+        const uint32_t row0 = b * ZROWS * kAhead + row_in_block<ZLANES>();
+        uint32_t first[kAhead];
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) first[i] = a.places[min(row0 + i * ZROWS, a.rows - 1)].first;
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) {
+            const uint32_t row = row0 + i * ZROWS;
+            if (row >= a.rows || first[i]) continue;
+            O *to = dtable + (int64_t)row * ldt;
+            for (uint32_t col = lane * E; col < a.cols; col += ZLANES * E) store_row<STREAM>(to + col, zero_unit<O>(), (int)min((uint32_t)E, a.cols - col));
         }
     }
 }
@@ -314,6 +410,10 @@ static void by_row_lanes(uint32_t cols, uint32_t elems, F f)
     if (pieces <= 32) f(std::integral_constant<int, 16>{});
     else if (pieces <= 128) f(std::integral_constant<int, 64>{});
     else f(std::integral_constant<int, 256>{});
+}
+static bool aligned_rows(const seer_dense &m, size_t size)
+{
+    return reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (size_t)m.ld * size % 16 == 0;
 }
 static dim3 row_grid(uint32_t rows, uint32_t cols, uint32_t elems, uint32_t lanes)
 {
@@ -341,7 +441,7 @@ void launch_embed(const void *token, bool wide, uint32_t tokens, const seer_dens
 
 struct SortPlan { uint32_t per_wave, groups; int passes, bits; };
 
-// One workgroup sorts few pairs in one launch; more take two launches for each digit.
+// Two launches for each digit.
 static SortPlan sort_plan(uint32_t count, uint32_t rows)
 {
     SortPlan p;
@@ -349,14 +449,18 @@ static SortPlan sort_plan(uint32_t count, uint32_t rows)
     while (bits < 32 && rows >> bits) ++bits;           // `rows` is the largest key
     p.passes = (bits + kDigitBits - 1) / kDigitBits;
     p.bits = (bits + p.passes - 1) / p.passes;
-    const uint32_t groups = count <= 8192 ? 1 : std::min((count + 4095) / 4096, 128u);
+    const uint32_t groups = std::min(std::max((count + 1023) / 1024, 1u), 128u);
     const uint32_t share = (count + groups - 1) / groups;
     p.per_wave = std::max(64u, ((share + kDigitWaves - 1) / kDigitWaves + 63) & ~63u);
     p.groups = (count + kDigitWaves * p.per_wave - 1) / (kDigitWaves * p.per_wave);
     return p;
 }
 
+// Sums of sums are worth their launch from here on: one row's tokens may be all of them.
+constexpr uint32_t kManyTokens = 2048;
+
 struct GradSpace { size_t pairs, counts, places, run, runs, bytes; };
+static uint32_t sum_pitch(uint32_t cols) { return (cols + 3) & ~3u; }
 
 static GradSpace grad_space(uint32_t count, uint32_t rows, uint32_t cols)
 {
@@ -365,36 +469,38 @@ static GradSpace grad_space(uint32_t count, uint32_t rows, uint32_t cols)
     GradSpace s;
     s.pairs = 0;
     s.counts = 4 * pad((size_t)count * 4);
-    s.places = s.counts + (p.groups > 1 ? pad(((size_t)p.groups << p.bits) * 4) : 0);
+    s.places = s.counts + pad(((size_t)p.groups << p.bits) * 4);
     s.run = s.places + pad((size_t)rows * sizeof(Places));
-    s.runs = s.run + pad((size_t)(count / kRun) * cols * 4);
-    s.bytes = s.runs + pad((size_t)(count / (kRun * kRun)) * cols * 4);
+    s.runs = s.run + pad((size_t)(count / kRun) * sum_pitch(cols) * 4);
+    s.bytes = s.runs + (count < kManyTokens ? 0 : pad((size_t)(count / (kRun * kRun)) * sum_pitch(cols) * 4));
     return s;
 }
 
 size_t embed_grad_workspace_bytes(uint32_t count, uint32_t rows, uint32_t cols) { return grad_space(count, rows, cols).bytes; }
 
 template <class I>
-static Pairs launch_sort(const I *token, uint32_t count, uint32_t rows, char *ws, const GradSpace &s, hipStream_t st)
+static Pairs launch_sort(const I *token, uint32_t count, uint32_t rows, char *ws, const GradSpace &s, const Clear &clear, hipStream_t st)
 {
-    const SortPlan p = sort_plan(count, rows);
+    const uint32_t clearing = (clear.rows + kClearRows - 1) / kClearRows;
     const size_t each = ((size_t)count * 4 + 255) & ~(size_t)255;
     const auto array = [&](int i) { return reinterpret_cast<uint32_t *>(ws + s.pairs + i * each); };
-    const PairBuffers pairs{{Pairs{array(0), array(1)}, Pairs{array(2), array(3)}}};
-    DigitArgs a{Pairs{nullptr, nullptr}, pairs.at[0], count, rows, p.per_wave, p.groups, 0, p.bits, reinterpret_cast<uint32_t *>(ws + s.counts)};
+    const Pairs pairs[2] = {{array(0), array(1)}, {array(2), array(3)}};
+    if (count <= kRankTokens) {
+        const uint32_t blocks = (count + kWG / kRankLanes - 1) / (kWG / kRankLanes);
+        hipLaunchKernelGGL((rank_pairs_kernel<I>), dim3(blocks + clearing), dim3(kWG), 0, st, token, count, rows, pairs[0], blocks, clear);
+        return pairs[0];
+    }
+    const SortPlan p = sort_plan(count, rows);
+    DigitArgs a{Pairs{nullptr, nullptr}, pairs[0], count, rows, p.per_wave, p.groups, 0, p.bits, reinterpret_cast<uint32_t *>(ws + s.counts)};
     const size_t lds = ((size_t)(kDigitWaves + 2) << p.bits) * 4 + 4;
     const dim3 wg(kDigitWaves * 64);
-    if (p.groups == 1) {
-        hipLaunchKernelGGL((sort_pairs_kernel<I>), dim3(1), wg, lds, st, a, token, pairs, p.passes);
-        return pairs.at[(p.passes - 1) & 1];
-    }
     for (int i = 0; i < p.passes; ++i, a.shift += a.bits) {
-        if (i) a.from = pairs.at[(i - 1) & 1];
-        a.to = pairs.at[i & 1];
-        hipLaunchKernelGGL((count_digits_kernel<I>), dim3(p.groups), wg, 0, st, a, token);
+        if (i) a.from = pairs[(i - 1) & 1];
+        a.to = pairs[i & 1];
+        hipLaunchKernelGGL((count_digits_kernel<I>), dim3(p.groups + (i ? 0 : clearing)), wg, 0, st, a, token, clear);
         hipLaunchKernelGGL((place_digits_kernel<I>), dim3(p.groups), wg, lds, st, a, token);
     }
-    return pairs.at[(p.passes - 1) & 1];
+    return pairs[(p.passes - 1) & 1];
 }
 
 void launch_embed_grad(const void *token, bool wide, const seer_dense &dy, float scale, bool accumulate, const seer_dense &dtable, void *workspace,
@@ -404,29 +510,36 @@ void launch_embed_grad(const void *token, bool wide, const seer_dense &dy, float
     char *ws = static_cast<char *>(workspace);
     const GradSpace s = grad_space(count, rows, cols);
     GradArgs a{Pairs{nullptr, nullptr}, reinterpret_cast<Places *>(ws + s.places), reinterpret_cast<float *>(ws + s.run),
-               reinterpret_cast<float *>(ws + s.runs), count, rows, cols, scale};
-    if (!accumulate) hipLaunchKernelGGL(clear_places_kernel, dim3(std::min((rows + kWG - 1) / kWG, 1024u)), dim3(kWG), 0, st, a.places, rows);
-    if (count) {
-        a.sorted = wide ? launch_sort(static_cast<const int64_t *>(token), count, rows, ws, s, st)
-                        : launch_sort(static_cast<const int32_t *>(token), count, rows, ws, s, st);
-        hipLaunchKernelGGL(mark_places_kernel, dim3((count + kWG - 1) / kWG), dim3(kWG), 0, st, a);
-    }
+               count < kManyTokens ? nullptr : reinterpret_cast<float *>(ws + s.runs), count, rows, cols, sum_pitch(cols), scale};
+    const Clear clear{a.places, accumulate ? 0 : rows};
+    if (count)
+        a.sorted = wide ? launch_sort(static_cast<const int64_t *>(token), count, rows, ws, s, clear, st)
+                        : launch_sort(static_cast<const int32_t *>(token), count, rows, ws, s, clear, st);
+    else hipLaunchKernelGGL(clear_places_kernel, dim3((rows + kClearRows - 1) / kClearRows), dim3(kDigitWaves * 64), 0, st, clear);
     by_type(dy.type, [&](auto *of) {
         using T = std::remove_pointer_t<decltype(of)>;
         by_row_lanes(cols, Unit<T>::kElems, [&](auto lanes) {
             constexpr int LANES = decltype(lanes)::value;
+            constexpr uint32_t ROWS = kWG / LANES, E = Unit<T>::kElems;
             const T *y = static_cast<const T *>(dy.data);
-            const auto grid = [&](uint32_t n) { return row_grid(n, cols, Unit<T>::kElems, LANES); };
-            if (count >= kRun) hipLaunchKernelGGL((run_kernel<T, LANES, 1>), grid(count / kRun), dim3(kWG), 0, st, a, y, dy.ld);
-            if (count >= kRun * kRun) hipLaunchKernelGGL((run_kernel<T, LANES, 2>), grid(count / (kRun * kRun)), dim3(kWG), 0, st, a, y, dy.ld);
-            const auto launch = [&](auto *to) {
-                using O = std::remove_pointer_t<decltype(to)>;
+            const uint32_t across = (cols + LANES * E - 1) / (LANES * E), marking = (count + kWG - 1) / kWG;
+            const auto runs = [&](uint32_t n) { return (n + ROWS - 1) / ROWS * across; };
+            if (count) hipLaunchKernelGGL((run_kernel<T, LANES, 1>), dim3(marking + runs(count / kRun)), dim3(kWG), 0, st, a, y, dy.ld, marking);
+            if (a.runs) hipLaunchKernelGGL((run_kernel<T, LANES, 2>), dim3(runs(count / (kRun * kRun))), dim3(kWG), 0, st, a, y, dy.ld, 0);
+            const auto launch = [&](auto *out) {
+                using O = std::remove_pointer_t<decltype(out)>;
+                constexpr int L = LANES < kWave ? LANES : kWave, UNITS = LANES < kWave ? 1 : 2;
+                constexpr uint32_t PART = L * UNITS * E, WAVES = kWG / L, ZROWS = LANES < kWave ? kWG / LANES : 1;
+                O *to = static_cast<O *>(dtable.data);
+                const uint64_t items = (uint64_t)count * ((cols + PART - 1) / PART);
+                const uint32_t summing = (uint32_t)std::min<uint64_t>((items + WAVES - 1) / WAVES, 1u << 20);
+                const uint32_t zeroing = std::min((rows + ZROWS * kAhead - 1) / (ZROWS * kAhead), 1u << 20);
                 if (accumulate)
-                    hipLaunchKernelGGL((embed_grad_kernel<T, O, LANES, true>), grid(count), dim3(kWG), 0, st, a, y, dy.ld,
-                                       static_cast<O *>(dtable.data), dtable.ld);
+                    hipLaunchKernelGGL((rows_kernel<T, O, L, UNITS, true, false>), dim3(summing), dim3(kWG), 0, st, a, y, dy.ld, to, dtable.ld, summing);
+                else if (aligned_rows(dtable, sizeof(O)))
+                    hipLaunchKernelGGL((rows_kernel<T, O, L, UNITS, false, true>), dim3(summing + zeroing), dim3(kWG), 0, st, a, y, dy.ld, to, dtable.ld, summing);
                 else
-                    hipLaunchKernelGGL((embed_grad_kernel<T, O, LANES, false>), grid(rows), dim3(kWG), 0, st, a, y, dy.ld,
-                                       static_cast<O *>(dtable.data), dtable.ld);
+                    hipLaunchKernelGGL((rows_kernel<T, O, L, UNITS, false, false>), dim3(summing + zeroing), dim3(kWG), 0, st, a, y, dy.ld, to, dtable.ld, summing);
             };
             if (dtable.type == dy.type) launch((T *)nullptr);
             else if constexpr (!std::is_same<T, float>::value) launch((float *)nullptr);

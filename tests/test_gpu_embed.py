@@ -145,9 +145,10 @@ def test_rows_and_columns_beyond_32_bits():
     out = S.seer_embed(far, table, scale=2.0)
     assert torch.equal(out, 2 * table[far])
     d = S.seer_embed_grad(far, out, dtable=table)
-    want = torch.zeros(V, device="cuda:0")
-    want.index_add_(0, far, out[:, 0].float())
-    assert torch.equal(d[:, 0].float(), want) and torch.equal(d[:, -1].float(), want)
+    for column in (0, -1):          # (which of two assignments to a row of the table stays may differ from column to column)
+        want = torch.zeros(V, device="cuda:0")
+        want.index_add_(0, far, out[:, column].float())
+        assert torch.equal(d[:, column].float(), want)
 
 
 def test_on_another_stream_and_captured():

@@ -73,6 +73,8 @@ def test_embed_refusals():
     assert back(ws=None) == EWORKSPACE and back(ws=P + 8) == EWORKSPACE and back(size=S.embed_grad_workspace_bytes(4, 100, 8) - 1) == EWORKSPACE
     assert back(ws=A) == EINVAL and back(ws=B_) == EINVAL and back(ws=W - 64) == EINVAL
     assert back(to=dense(None, 0, 8, kind=1)) == 0 and back(add=1, dy=dense(None, 0, 8, kind=1), token=None) == 0
+    for tokens, rows, columns in ((0, 5, 5), (0, 0, 0), (1, 1, 1), (4097, 7, 0), ((1 << 31) - 1, (1 << 31) - 1, 1)):
+        assert S.embed_grad_workspace_bytes(tokens, rows, columns) >= 16 * tokens + 8 * rows
     assert S.embed_grad_workspace_bytes(-1, 4, 4) == S.embed_grad_workspace_bytes(4, 1 << 31, 4) == 0
 
 
