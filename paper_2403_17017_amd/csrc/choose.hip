@@ -165,15 +165,15 @@ __global__ __launch_bounds__(kWG) void choose_kernel(const T *__restrict__ logit
 // 16 lanes to a token, a lane with PER consecutive experts; keys in 32 bits, with bounds on what they may be off by.  A token whose choice the
 // bounds leave open is chosen again by the whole wave, in 64 bits.
 //
-// A key travels with its expert in one word: the 24 upper bits of the number that has the key's order, and 255 less the
-// expert's number; the next best is the largest word below the last one.  Keys that are made of scores are taken less the largest of them, so
-// that what is cut off is 2^-15 of the distance from the best.  The bounds on a score: of a sigmoid, 2^-21 (an exponential with an error
+// A key travels with its expert in one word: the 24 upper bits (23 with more than 256 experts) of the number that has the key's order, and 255 less
+// the expert's number (511); the next best is the largest word below the last one.  Keys that are made of scores are taken less the largest of them, so
+// that what is cut off is 2^-15 (2^-14) of the distance from the best.  The bounds on a score: of a sigmoid, 2^-21 (an exponential with an error
 // of 2^-23 and 1.5 |x| 2^-24 of itself, times s (1 - s), where s (1 - s) |x| < 0.23; a sum and a reciprocal, 1.5 * 2^-23); of a softmax, 2^-18 of
-// the largest (such exponentials, s |x - max| < 0.4 max s, a sum of 256 in 20 steps, a reciprocal and a product).  A bias adds 2^-24 of the key.
+// the largest (such exponentials, s |x - max| < 0.4 max s, a sum of up to 512 in 36 steps, a reciprocal and a product).  A bias adds 2^-24 of the key.
 // Without a bias keys are logits, and exact.
 constexpr uint32_t kRowBlocks = 1024 /* as many as there is room for; a wave then goes on to other tokens */;
-constexpr uint32_t kRowLanes = 16, kFastChoices = 15, kFastExperts = 256;
-constexpr float kSigmoidError = 0x1p-21f, kSoftmaxError = 0x1p-18f, kCut = 0x1p-15f;
+constexpr uint32_t kRowLanes = 16, kFastChoices = 15, kFastExperts = 512;
+constexpr float kSigmoidError = 0x1p-21f, kSoftmaxError = 0x1p-18f;
 
 // The other lanes of 16: fold with the same result in all of them.
 template <int CTRL>
@@ -239,12 +239,14 @@ __device__ __forceinline__ float row_share(const seer_choice &how, float x, bool
 
 // per: the experts of a lane; VEC: rows are read 4 elements at a time.  group_lanes: lanes to a group, 0 without groups.
 template <class T, int PER, bool VEC, bool BIAS>
-__global__ __launch_bounds__(kWG, 4) void choose_rows_kernel(const T *__restrict__ logits, int64_t ld, uint32_t tokens, uint32_t experts, uint32_t per,
+__global__ __launch_bounds__(kWG, PER > 16 ? 2 : 4) void choose_rows_kernel(const T *__restrict__ logits, int64_t ld, uint32_t tokens, uint32_t experts, uint32_t per,
                                                           uint32_t group_lanes, const float *__restrict__ bias, seer_choice how,
                                                           int32_t *__restrict__ expert, float *__restrict__ weight)
 {
     extern __shared__ __attribute__((aligned(16))) uint64_t s_key[];          // [waves][experts], with groups
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x & 63, l = lane & (kRowLanes - 1);
+    constexpr uint32_t NUMBERS = PER > 16 ? 512 : 256, NUMBER = NUMBERS - 1;       // of experts; the bits of a word that hold one
+    constexpr float kCut = PER > 16 ? 0x1p-14f : 0x1p-15f;
     const bool two = group_lanes && how.group_best == 2;
     const auto bits = [](float v) { return __builtin_bit_cast(uint32_t, v); };
     float b[BIAS ? PER : 1];
@@ -351,7 +353,7 @@ __global__ __launch_bounds__(kWG, 4) void choose_rows_kernel(const T *__restrict
             }
         }
         uint32_t word[PER], none;
-        const uint32_t kept = open ? ~255u : 0;
+        const uint32_t kept = open ? ~NUMBER : 0;
         float size = 0;
         if constexpr (BIAS) {
             float best = -INFINITY;
@@ -361,13 +363,13 @@ __global__ __launch_bounds__(kWG, 4) void choose_rows_kernel(const T *__restrict
             best = best == -INFINITY ? 0 : best;
             // (what is below the best in an open group; what is above it is in a closed one)
 #pragma unroll
-            for (int i = 0; i < PER; ++i) word[i] = (~bits(fmaxf(best - key[i], 0.0f)) & kept) | (255 - (l * per + i));
+            for (int i = 0; i < PER; ++i) word[i] = (~bits(fmaxf(best - key[i], 0.0f)) & kept) | (NUMBER - (l * per + i));
             size = fabsf(best) + 2;
-            none = ~0x7f800000u;                            // an infinite distance, or less
+            none = ~0x7f800000u | NUMBER;                            // an infinite distance, or less
         } else {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) word[i] = (word_of(key[i]) & kept) | (255 - (l * per + i));
-            none = ~0xff800000u;                            // -infinity
+            for (int i = 0; i < PER; ++i) word[i] = (word_of(key[i]) & kept) | (NUMBER - (l * per + i));
+            none = ~0xff800000u | NUMBER;                            // -infinity
         }
         uint32_t last = 0, mine = 0;                        // lane k takes the k-th word
         for (int k = 0; k <= how.choices; ++k) {
@@ -381,7 +383,7 @@ __global__ __launch_bounds__(kWG, 4) void choose_rows_kernel(const T *__restrict
             last = next;
         }
         const bool in = mine != 0 && (int)l < how.choices;
-        const uint32_t at = min(255 - (mine & 255), experts - 1);
+        const uint32_t at = min(NUMBER - (mine & NUMBER), experts - 1);
         const float xl = mine ? (float)row[at] : 0.0f;
         {
             const uint32_t after = row_move<0x101>(mine);   // of the next lane
@@ -390,10 +392,10 @@ __global__ __launch_bounds__(kWG, 4) void choose_rows_kernel(const T *__restrict
             bool sure;
             if constexpr (BIAS) {
                 const float bl = mine ? bias[at] : 0.0f, ba = row_move<0x101>(bl);
-                const float here = __builtin_bit_cast(float, ~mine & ~255u), there = __builtin_bit_cast(float, ~after & ~255u);      // distances from the best
+                const float here = __builtin_bit_cast(float, ~mine & ~NUMBER), there = __builtin_bit_cast(float, ~after & ~NUMBER);      // distances from the best
                 sure = there - here > 2 * score_error + size * 0x1p-22f + kCut * there || (!border && xl == xa && bl == ba);
             } else
-                sure = mine >> 8 != after >> 8 || (border ? sizeof(T) == 2 : xl >= xa);
+                sure = mine / NUMBERS != after / NUMBERS || (border ? sizeof(T) == 2 : xl >= xa);
             unsure = unsure || (in && after && !sure);
         }
         const float share = row_share(how, xl, in, most, all);
@@ -600,7 +602,8 @@ void launch_choose(const seer_dense &logits, const float *bias, const seer_choic
             else if (r.per <= 4) of_width(integral_constant<int, 4>{});
             else if (r.per <= 8) of_width(integral_constant<int, 8>{});
             else if (r.per <= 12) of_width(integral_constant<int, 12>{});
-            else of_width(integral_constant<int, 16>{});
+            else if (r.per <= 16) of_width(integral_constant<int, 16>{});
+            else of_width(integral_constant<int, 32>{});
             return;
         }
         if (experts <= 64) launch(integral_constant<int, 1>{});
@@ -632,7 +635,8 @@ void launch_choose_grad(const seer_dense &logits, const seer_choice &how, const 
             };
             if (experts <= 64) rows(std::integral_constant<int, 1>{});
             else if (experts <= 128) rows(std::integral_constant<int, 2>{});
-            else rows(std::integral_constant<int, 4>{});
+            else if (experts <= 256) rows(std::integral_constant<int, 4>{});
+            else rows(std::integral_constant<int, 8>{});
             return;
         }
         hipLaunchKernelGGL((choose_grad_kernel<T>), token_grid((uint32_t)logits.rows), dim3(kWG), 0, st, static_cast<const T *>(logits.data), logits.ld,
