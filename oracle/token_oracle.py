@@ -17,9 +17,9 @@ def scores(logits, score):
         return np.exp(log_s), log_s
 
 
-def _before(a, b):
-    """Whether key a comes before key b: a NaN is above all."""
-    return (np.isnan(a) and not np.isnan(b)) or a > b
+def _ranked(keys):
+    """The numbers of a dictionary's keys: the largest value first, a NaN above all, ties to the lower number."""
+    return sorted(keys, key=lambda n: (not np.isnan(keys[n]), 0.0 if np.isnan(keys[n]) else -keys[n], n))
 
 
 def choose(logits, choices, score="softmax", bias=None, groups=1, best_groups=None, group_best=1, renormalise=True, factor=1.0):
@@ -43,14 +43,9 @@ def choose(logits, choices, score="softmax", bias=None, groups=1, best_groups=No
                 mine.sort(key=lambda v: (not np.isnan(v), -v if not np.isnan(v) else 0))
                 if mine:
                     worth[g] = mine[0] if group_best == 1 else sum(mine[:2])
-            order = []
-            for g in worth:
-                order.insert(next((i for i, o in enumerate(order) if _before(worth[g], worth[o])), len(order)), g)
-            there = [e for e in there if e // n in order[:best_groups]]
-        order = []
-        for e in there:
-            order.insert(next((i for i, o in enumerate(order) if _before(key[e], key[o])), len(order)), e)
-        mine = order[:choices]
+            best = _ranked(worth)[:best_groups]
+            there = [e for e in there if e // n in best]
+        mine = _ranked({e: key[e] for e in there})[:choices]
         expert[t, :len(mine)] = mine
         if not mine:
             continue

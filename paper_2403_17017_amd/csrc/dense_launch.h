@@ -1,4 +1,4 @@
-// Host-side declarations of the kernels over dense rows (routing, 8-bit products, gradient norms).
+// Host-side declarations of the kernels over dense rows (routing and its choice, products in 8 and 4 bits, embedding, gradient norms).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stddef.h>

@@ -24,7 +24,7 @@ __device__ __forceinline__ uint32_t row_in_block()
 
 // ------------------------------------------------------------------ lookup
 //
-// Bound by bytes: each row is read and written once.
+// Bound by bytes: each row is read and written once.  32 771 tokens, 131 072 x 4096 bf16: 84 us (537 MB, 6.4 TB/s).
 template <class T, class I, int LANES>
 __global__ __launch_bounds__(kWG) void embed_kernel(const I *__restrict__ token, uint32_t tokens, const T *__restrict__ table, int64_t ldt,
                                                     uint32_t rows, uint32_t cols, float scale, T *__restrict__ out, int64_t ldo)
@@ -153,8 +153,8 @@ __global__ __launch_bounds__(kDigitWaves * 64) void place_digits_kernel(DigitArg
     place_digits(a, token, blockIdx.x, lds, s_wave);
 }
 
-// Few tokens find their places by counting, 16 lanes to a token: the rows below its own, and its own row's tokens before it.  1031 tokens: 3.6 us
-// in one launch (sorted by digits in one workgroup 11).
+// Few tokens find their places by counting, 16 lanes to a token: the rows below its own, and its own row's tokens before it.  1031 tokens: 6.5 us
+// in one launch, sorted by digits in one workgroup 11.
 constexpr uint32_t kRankTokens = 4096, kRankLanes = 16;
 
 template <class I>
@@ -185,7 +185,8 @@ __global__ __launch_bounds__(kWG) void rank_pairs_kernel(const I *__restrict__ t
 //
 // Every row of the table adds up its tokens' rows of dy in the order of the tokens.  Where a row has many, sums of kRun
 // consecutive places that are all its own are made beforehand, and of kRun such sums, each by a workgroup of its own; the row then
-// takes the largest pieces that lie in its range.  Bound by bytes.
+// takes the largest pieces that lie in its range.  1031 tokens by a power law, 1023 fp32: 8.0 us for the sums made beforehand and 17.4 for the rows
+// with runs of 16, 13.2 and 23.4 with runs of 32.
 constexpr uint32_t kRun = 16;
 
 struct GradArgs {

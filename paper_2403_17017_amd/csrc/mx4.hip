@@ -14,7 +14,8 @@ typedef int v8i32 __attribute__((ext_vector_type(8)));
 
 // ------------------------------------------------------------------ quantisation
 //
-// Four lanes to a block, eight values each; the largest of a block decides its scale.
+// Four lanes to a block, eight values each; the largest of a block decides its scale.  Bound by bytes: 8192 rows of 4096 bf16 to four experts each
+// 28 us (138 MB, 4.9 TB/s).
 constexpr uint32_t kMxBlock = 32, kMxEach = 8;
 
 // Eight values as floats, of which n are there, zeros behind them.
@@ -156,6 +157,10 @@ __global__ __launch_bounds__(256) void mx4_any_kernel(Mx4Args a, uint32_t blocks
 // straight from memory into one of two LDS buffers, and from there, 4 blocks (a step) at a time, into registers while those before
 // are multiplied.  Scales come 16 blocks (a round of four steps) at a time through registers, a row to a thread, which puts the bytes in
 // the order that the matrix instructions take them in: one word of a lane has the bytes of its block in each of the four steps.
+// 8192 x 8192 x 8192: 281 us, 3.9 PFLOP/s (zeros 234; matrix instructions alone 6.4 on random codes, at the card's power).  A step takes
+// 0.96 us where they would take 0.67; without its loads 0.79.  A tile's first loads and last stores add some 12 us, which nothing
+// hides: 32 groups of 4096 x 4096, mean 1013, 390 us.  Slower: wave tiles of 128 x 128 in 512 registers (the same product 420, 448 before
+// scales were realigned late), registers for the next channels' codes besides (spilled).
 constexpr uint32_t kTileChannels = 256, kStepBlocks = 4, kRoundSteps = 4, kLineBytes = 128;
 
 // WC x WAVES / WC waves, each of CI * 16 channels x TJ * 16 tokens.
@@ -429,7 +434,9 @@ __global__ __launch_bounds__(kWG) void mx4_join_kernel(Mx4Args a, Mx4Shared shar
 // ------------------------------------------------------------------ few rows to a group
 //
 // CI * 16 channels of one group per workgroup, whose waves each take a share of the columns; both operands come straight from memory, the
-// weights once per 64 rows, and the waves' sums meet in LDS.  Bound by the bytes of b.
+// weights once per 64 rows, and the waves' sums meet in LDS.  Bound by the bytes of b: 8192 x 8192, one row, 9.6 us (3.7 TB/s), 64 groups of
+// 2048 x 4096 with four rows each on average 62 (4.6 TB/s).  32 channels to a workgroup: 14.8 us for the one row with its quantisation
+// (16: 15.7), 61.8 for the groups (67.2), but 2 % slower over 300 draws; eight waves 15.0 and 99.9.
 constexpr uint32_t kMxFewRows = 64, kRoundBlocks = kRoundSteps * kStepBlocks;
 
 // 16 TJ rows: the calling wave's blocks [k, k_end), R rounds of 16 at a time.  Pointers are those of the lane's rows, of codes with the lane's
@@ -586,8 +593,14 @@ static void launch_tiles(const Mx4Args &a, hipStream_t st)
                        0, st, a, Mx4Shared{});
 }
 
-// Which kernel: the one whose time by the following lines (us) is the least.
-constexpr double kJoinCost = 5;
+// Which kernel: the one whose time by the following lines (us) is the least.  They are fitted to 300 draws (one matrix, or 2 to 64 with rows to a group
+// 1, 1 / sqrt(rank) or 1 / rank; 128 to 12 288 channels and 256 to 12 288 columns; weights from memory) of which each kernel was
+// timed.  Of 220 other draws, whose times are kept in profiles/mx4_kernel_times.csv, what is chosen takes 2.4 % longer than the best one on average,
+// 1.47 times at most.  Measured, us, few rows, tiles of 64, of 128 and of 256 tokens: 1848 x 1856, 41 rows 5.4, 11, 11 and 14; 11 976 x 7872,
+// 16 rows 20, 61, 56 and 59; 8944 x 1536, 82 rows 13, 11, 12 and 14; 46 groups of 456 x 10 912, mean 142, 239, 152, 86 and 110; 43 of
+// 6088 x 1792, mean 168, 516, 175, 146 and 113.  Columns shared between two and four workgroups (tiles of 64, one share): 6520 x 6304,
+// 19 rows 32 and 22 (48), 2936 x 3296, 44 rows 17 and 13 (20).
+constexpr double kJoinCost = 5;     // the second launch; and 1 us for every 3 MB of sums written and read
 
 static double few_cost(const Mx4Args &a)
 {

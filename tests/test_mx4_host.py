@@ -104,3 +104,45 @@ def test_oracle_pins():
     assert scale.ravel().tolist() == [255, 255, 0, 0] and not codes.any()
     out, size = O.mx4_product(np.array([[1.0, -2], [3, 4], [5, 6]]), np.array([[[1.0, 1]], [[0, 1]]]), [0, 1, 2])
     assert out.ravel().tolist() == [-1, 4, 0] and size.ravel().tolist() == [3, 4, 0]
+
+
+def kernel(rows, channels, columns, groups=1, ld=None, ptr=None):
+    f = lambda at, n: C.byref(M.seer_mx4(at, at + 4096, n, columns, ld or 16 * -(-columns // 32), -(-columns // 32)))
+    rc = S.lib().seer_mx4_product_kernel(f(A, rows), f(1 << 30, groups * channels), P if groups > 1 else ptr, groups)
+    return S.MX4_KERNELS[rc] if rc >= 0 else rc
+
+
+def test_kernels():
+    assert kernel(1, 8192, 8192) == "few" and kernel(256, 2048, 4096, groups=64) == "few" and kernel(5, 6, 0) == "few"
+    assert kernel(3001, 5001, 4111) == "tiles" and kernel(32768, 4096, 4096, groups=32) == "tiles"
+    assert kernel(300, 512, 8192) == "shared" and S.mx4_product_workspace_bytes(300, 512, 8192) > 0
+    assert kernel(3000, 5000, 4096, ld=1 << 23) == kernel(1, 5000, 4096, ld=1 << 23) == "any"      # too far apart for 32-bit offsets into a tile
+    assert kernel(0, 5, 64) == kernel(5, 0, 64) == "none"
+    # 2^30 tiles of 128 rows by 128 channels are too many for 32-bit numbers of tiles
+    assert kernel(1 << 22, 1 << 22, 32) == -6 and kernel((1 << 22) - 1024, (1 << 22) - 1024, 32) in S.MX4_KERNELS
+    assert kernel(4, 8, 64, groups=4097) == -6 and kernel(4, 8, 64, groups=0) == -1 and kernel(4, 8, 64, ld=24) == -1
+
+
+def test_kernel_query_refusals():
+    f = S.lib().seer_mx4_product_kernel
+    assert f(None, mx4(B_, W, 8, 64), None, 1) == -1 and f(mx4(A, W, 4, 64), None, None, 1) == -1 and f(mx4(A, W, 4, 64), mx4(B_, W, 9, 64), P, 2) == -1
+    assert f(mx4(A, W, 4, 64), mx4(B_, W, 8, 64), None, 2) == -1 and f(mx4(A, W, 4, 64), mx4(B_, W, 8, 96), None, 1) == -1
+    with pytest.raises(ValueError):
+        S.mx4_product_kernel(torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(64, dtype=torch.uint8))
+    assert S.mx4_product_kernel(torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(2, 8, 64, dtype=torch.uint8), torch.zeros(3, dtype=torch.int32)) == "few"
+
+
+def test_what_is_chosen_is_near_the_best():
+    """Of 220 drawn sizes with every kernel timed."""
+    import csv
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "profiles", "mx4_kernel_times.csv")
+    with open(path) as f:
+        rows = list(csv.DictReader(line for line in f if not line.startswith("#")))
+    assert len(rows) == 220
+    over = []
+    for r in rows:
+        times = {k: float(r[k]) for k in ("few", "tiles_64", "tiles_128", "tiles_256", "shared") if float(r[k]) > 0}
+        kind = kernel(int(r["rows"]), int(r["channels"]), int(r["columns"]), int(r["groups"]))
+        over.append(min(t for k, t in times.items() if k.startswith(kind)) / min(times.values()))
+    assert np.mean(over) < 1.03 and max(over) < 1.6
