@@ -275,3 +275,26 @@ def test_on_another_stream_and_captured():
         want = [*S.seer_route_choose(x, how, bias=bias)]
         want.append(S.seer_route_choose_grad(x, how, want[0], dw))
         assert all(torch.equal(a, b) for a, b in zip(want, out))
+
+
+@pytest.mark.parametrize("how", [dict(score="sigmoid", groups=8, best_groups=4, group_best=2), dict(score="softmax", renormalise=False), dict(score="softmax", groups=4, best_groups=2)], ids=str)
+@pytest.mark.parametrize("E", [64, 256, 512])
+def test_many_tokens_choose_as_64_bits_do(E, how):
+    """40 000 tokens: experts equal to those of the definition, borders that 32 bits leave open among them."""
+    announce(f"40 000 tokens of {E} {how}")
+    g = torch.Generator(device="cuda:0").manual_seed(E)
+    x = torch.randn(40000, E, generator=g, device="cuda:0") * 1.5
+    bias = torch.round(torch.randn(E, generator=g, device="cuda:0") * 20) * 1e-3 if how["score"] == "sigmoid" else None
+    e, _ = S.seer_route_choose(x, S.Choice(8, **how), bias=bias)
+    d = x.double()
+    s = torch.sigmoid(d) if how["score"] == "sigmoid" else torch.softmax(d, 1)
+    key = d if bias is None else s + bias.double()
+    if how.get("groups", 1) > 1:
+        G = how["groups"]
+        top = torch.sort(key.view(-1, G, E // G), dim=2, descending=True).values
+        worth = top[:, :, :2].sum(2) if how.get("group_best") == 2 else top[:, :, 0]
+        best = torch.sort(worth, dim=1, descending=True, stable=True).indices[:, : how["best_groups"]]
+        shut = torch.ones(40000, G, dtype=torch.bool, device="cuda:0").scatter_(1, best, False)
+        key = key.masked_fill(shut.repeat_interleave(E // G, 1), -float("inf"))
+    want = torch.sort(key, dim=1, descending=True, stable=True).indices[:, :8]
+    assert torch.equal(e.long(), want)

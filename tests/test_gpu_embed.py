@@ -178,3 +178,21 @@ def test_on_another_stream_and_captured():
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(out[0], S.seer_embed(token, table, scale=3.0)) and torch.equal(out[1], S.seer_embed_grad(token, dy, 500, scale=3.0))
+
+
+@pytest.mark.parametrize("V", [3, 5000, 1500000])
+def test_more_tokens_than_one_pass_of_workgroups(V):
+    """300 000 tokens, a third of them one row's: shares of the sort longer than a wave, and sums of sums of sums."""
+    announce(f"300 000 tokens of {V}")
+    g = torch.Generator(device="cuda:0").manual_seed(6)
+    token = torch.randint(-1, V, (300000,), generator=g, device="cuda:0")
+    token[torch.rand(300000, generator=g, device="cuda:0") < 0.33] = 1
+    dy = torch.randn(300000, 8, generator=g, device="cuda:0")
+    got = S.seer_embed_grad(token, dy, V, scale=0.5)
+    known = token >= 0
+    at, rows = token[known], dy[known].double()
+    want = torch.zeros(V, 8, dtype=torch.float64, device="cuda:0").index_add_(0, at, rows) * 0.5
+    size = torch.zeros(V, 8, dtype=torch.float64, device="cuda:0").index_add_(0, at, rows.abs()) * 0.5
+    # runs of 16, of these 16, and what is left: no element goes through more than 16 + 16 + 2^17 / 256 + 62 additions
+    assert bool(((got - want).abs() <= U32 * 700 * size + U32 * want.abs()).all())
+    assert torch.equal(got, S.seer_embed_grad(token.int(), dy, V, scale=0.5))
