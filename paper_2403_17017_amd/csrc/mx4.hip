@@ -232,14 +232,15 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : 1) void mx4_tile_kerne
             const uint32_t row = (i * WAVES + wave) * 8 + lane / 8;
             at_b[i] = row < chans ? row * ldb + piece : kNowhere;
         }
+        // (an offset is held against the range less the line's, which lines fetched behind the last one must not turn below zero)
         const auto fetch = [&](uint32_t line, int8_t *lds) {
-            const uint32_t k0 = line * kLineBytes, nowhere = k0 + piece < bytes ? 0 : kNowhere;
+            const uint32_t k0 = line * kLineBytes, nowhere = k0 + piece < bytes ? 0 : kNowhere, at = min(k0, bytes);
 #pragma unroll
             for (uint32_t i = 0; i < LA; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte *)(lds + (i * WAVES + wave) * 1024), 16, (int)(at_a[i] | nowhere), (int)k0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte *)(lds + (i * WAVES + wave) * 1024), 16, (int)(at_a[i] | nowhere), (int)at, 0, 0);
 #pragma unroll
             for (uint32_t i = 0; i < LB; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte *)(lds + TOKENS * kLineBytes + (i * WAVES + wave) * 1024), 16, (int)(at_b[i] | nowhere), (int)k0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte *)(lds + TOKENS * kLineBytes + (i * WAVES + wave) * 1024), 16, (int)(at_b[i] | nowhere), (int)at, 0, 0);
         };
         // the scales of a thread's rows (those that are not there: the last one's), 16 blocks of round r
         const int8_t *from_scale[Shape::kScaleRows];

@@ -283,3 +283,13 @@ def test_rows_far_apart():
     ptr = torch.tensor([1, 2], dtype=torch.int32, device="cuda:0")
     y = S.seer_mx4_product(qa, a[1], qb, b[1][0], group_ptr=ptr, dtype=torch.float32)
     assert torch.equal(y[1], out[1, :5]) and not y[2].any()
+
+
+@pytest.mark.parametrize("blocks", [1, 7, 8, 9, 16, 17, 40])
+def test_tiles_that_end_in_one_row_and_one_channel(blocks):
+    """Lines are fetched behind the columns' end, of a range that is one row long."""
+    announce(f"mx4 2817 x 1537 x {blocks} blocks")
+    rng = np.random.default_rng(blocks)
+    a, b = codes(rng, 2817, blocks), codes(rng, 1, 1537, blocks)
+    assert S.mx4_product_kernel(a[0], b[0]) == "tiles"
+    check_product(a, b, None, "f32")
