@@ -193,14 +193,15 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 || BUFFERS == 2 ? 2 : 1) voi
             at_b[i] = row < chans ? row * ldb + piece : kNowhere;
         }
         const uint32_t steps = (a.columns + kTileCols - 1) / kTileCols;
+        // (an offset is held against the range less the line's, which lines fetched behind the last one must not turn below zero)
         const auto fetch = [&](uint32_t line, int8_t *lds) {
-            const uint32_t k0 = line * kLineCols, nowhere = k0 + piece < a.columns ? 0 : kNowhere;
+            const uint32_t k0 = line * kLineCols, nowhere = k0 + piece < a.columns ? 0 : kNowhere, at = min(k0, readable);
 #pragma unroll
             for (uint32_t i = 0; i < LA; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte *)(lds + (i * WAVES + wave) * 1024), 16, (int)(at_a[i] | nowhere), (int)k0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte *)(lds + (i * WAVES + wave) * 1024), 16, (int)(at_a[i] | nowhere), (int)at, 0, 0);
 #pragma unroll
             for (uint32_t i = 0; i < LB; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte *)(lds + TOKENS * kLineCols + (i * WAVES + wave) * 1024), 16, (int)(at_b[i] | nowhere), (int)k0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte *)(lds + TOKENS * kLineCols + (i * WAVES + wave) * 1024), 16, (int)(at_b[i] | nowhere), (int)at, 0, 0);
         };
         // a lane's place in the first and the second 64 columns
         const uint32_t own = (lane & 15) * kLineCols;

@@ -362,3 +362,13 @@ def test_shared_columns_with_a_workspace_of_the_callers():
         S.seer_i8_product(a, sa, b, sb, workspace=ws[: need - 1])
     ptr = torch.tensor([0, M], dtype=torch.int32, device="cuda:0")
     assert torch.equal(S.seer_i8_product(a, sa, b, sb, group_ptr=ptr), want)
+
+
+@pytest.mark.parametrize("K", [16, 112, 128, 144, 256, 272, 640])
+def test_tiles_that_end_in_one_row_and_one_channel(K):
+    """Lines are fetched behind the columns' end, of a range that is one row long."""
+    announce(f"i8 2817 x 1537 x {K}")
+    rng = np.random.default_rng(K)
+    a, b = i8(rng, 2817, K), i8(rng, 1, 1537, K)
+    assert S.i8_product_kernel(a, b) == "tiles"
+    check_product(a, b, None, "f32", rng)
