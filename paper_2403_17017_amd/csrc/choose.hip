@@ -176,6 +176,7 @@ __global__ __launch_bounds__(kWG) void choose_kernel(const T *__restrict__ logit
 // bits; the logits alone are read in 13), softmax without either 32; 16 411 of 160 in bf16, 8 groups 11.
 constexpr uint32_t kRowBlocks = 1024 /* as many as there is room for; a wave then goes on to other tokens */;
 constexpr uint32_t kRowLanes = 16, kFastChoices = 15, kFastExperts = 512;
+constexpr float kFar = 0x1p100f;    // above it sums of two keys, and distances from the best one, may be infinite in 32 bits
 constexpr float kSigmoidError = 0x1p-21f, kSoftmaxError = 0x1p-18f;
 
 // The other lanes of 16: fold with the same result in all of them.
@@ -331,6 +332,7 @@ __global__ __launch_bounds__(kWG, PER > 16 ? 2 : 4) void choose_rows_kernel(cons
             if (group_lanes > 4) meet(row_move<0x141>(first), row_move<0x141>(second));
             float worth = first;
             if (two && second != -INFINITY) worth += second;
+            unsure = unsure || worth > kFar;
             worth = fmaxf(worth, -0x1.fffffep127f);         // (a group with none is behind all others)
             const uint32_t room = (uint32_t)how.best_groups * group_lanes;          // in lanes, as the counts
             uint32_t above = 0;
@@ -364,6 +366,7 @@ __global__ __launch_bounds__(kWG, PER > 16 ? 2 : 4) void choose_rows_kernel(cons
             for (int i = 0; i < PER; ++i) best = fmaxf(best, key[i]);
             best = row_max(open ? best : -INFINITY);
             best = best == -INFINITY ? 0 : best;
+            unsure = unsure || best > kFar;
             // (what is below the best in an open group; what is above it is in a closed one)
 #pragma unroll
             for (int i = 0; i < PER; ++i) word[i] = (~bits(fmaxf(best - key[i], 0.0f)) & kept) | (NUMBER - (l * per + i));

@@ -298,3 +298,24 @@ def test_many_tokens_choose_as_64_bits_do(E, how):
         key = key.masked_fill(shut.repeat_interleave(E // G, 1), -float("inf"))
     want = torch.sort(key, dim=1, descending=True, stable=True).indices[:, :8]
     assert torch.equal(e.long(), want)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("groups", [(1, 1, 1), (4, 2, 1), (4, 2, 2)], ids=str)
+@pytest.mark.parametrize("E", [16, 64, 384])
+def test_biases_at_the_ends_of_the_range(E, groups, score):
+    """The lowest number as a mask, and sums and distances of two biases that 32 bits do not hold."""
+    announce(f"choose biases {E} {groups} {score}")
+    rng = np.random.default_rng(E)
+    far = float(np.finfo(np.float32).max)
+    x = rng.standard_normal((9, E)) * 2
+    masked = np.where(rng.random(E) < 0.6, -far, rng.standard_normal(E) * 0.1)
+    high = np.where(rng.random(E) < 0.3, far, 0.9 * far)
+    both = rng.choice([-far, -0.75 * far, 0.0, 0.75 * far, far], E)
+    one = np.full(E, -far)
+    one[E // 3] = far
+    two = rng.standard_normal(E) * 0.1
+    two[[1, 2, E // 2, E // 2 + 1, E - 1, E - 2]] = [0.6 * far, 0.6 * far, 0.8 * far, 0.8 * far, 0.9 * far, 0.9 * far]
+    for bias in (masked, high, both, one, two, -high):
+        G, best, of = groups
+        check(x, "f32", 4, rng, bias.astype(np.float32), grad=False, score=score, groups=G, best_groups=best, group_best=of)
