@@ -330,13 +330,13 @@ __global__ __launch_bounds__(kWG, PER > 16 ? 2 : 4) void choose_rows_kernel(cons
             if (group_lanes > 1) meet(row_move<0xB1>(first), row_move<0xB1>(second));
             if (group_lanes > 2) meet(row_move<0x4E>(first), row_move<0x4E>(second));
             if (group_lanes > 4) meet(row_move<0x141>(first), row_move<0x141>(second));
-            float worth = first;
-            if (two && second != -INFINITY) worth += second;
-            unsure = unsure || worth > kFar;
-            worth = fmaxf(worth, -0x1.fffffep127f);         // (a group with none is behind all others)
             const uint32_t room = (uint32_t)how.best_groups * group_lanes;          // in lanes, as the counts
             uint32_t above = 0;
             if (BIAS || two) {
+                float worth = first;
+                if (two && second != -INFINITY) worth += second;
+                unsure = unsure || worth > kFar;
+                worth = fmaxf(worth, -0x1.fffffep127f);     // (with a group that has none at the border, 64 bits decide)
                 const float size = row_max(first == -INFINITY ? 0.0f : fmaxf(fabsf(first), second == -INFINITY ? 0.0f : fabsf(second)));
                 const float near = 4 * score_error + size * 0x1p-21f;
                 uint32_t not_below = 0;
@@ -349,10 +349,11 @@ __global__ __launch_bounds__(kWG, PER > 16 ? 2 : 4) void choose_rows_kernel(cons
                 // (the own group's other lanes are level with it)
                 unsure = unsure || (open && not_below - (group_lanes - 1) >= room);
             } else {
+                // exact: a group with none is -infinity, behind the lowest number
                 const uint32_t mine = l & ~(group_lanes - 1);
                 other_lanes([&](auto ctrl, uint32_t from) {
-                    const float other = row_move<decltype(ctrl)::value>(worth);
-                    above += other > worth || (other == worth && from < mine);
+                    const float other = row_move<decltype(ctrl)::value>(first);
+                    above += other > first || (other == first && from < mine);
                 });
                 open = above < room;
             }

@@ -319,3 +319,25 @@ def test_biases_at_the_ends_of_the_range(E, groups, score):
     for bias in (masked, high, both, one, two, -high):
         G, best, of = groups
         check(x, "f32", 4, rng, bias.astype(np.float32), grad=False, score=score, groups=G, best_groups=best, group_best=of)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("groups", [(2, 1, 1), (4, 2, 1), (4, 3, 1), (4, 2, 2)], ids=str)
+@pytest.mark.parametrize("E", [16, 64, 384, 600])
+def test_lowest_logits_beside_groups_with_none(E, groups, score):
+    """Experts held back by fp32's lowest number are there, those with minus infinity are not: a group of the first kind comes before one of the second."""
+    announce(f"choose lowest {E} {groups} {score}")
+    rng = np.random.default_rng(E)
+    G, best, of = groups
+    n, lowest = E // G, float(np.finfo(np.float32).min)
+    x = rng.standard_normal((2 * G + 2, E))
+    for g in range(G):
+        x[g, :] = lowest
+        x[g, g * n: (g + 1) * n] = -np.inf                       # one group has none
+        x[G + g, :] = -np.inf
+        x[G + g, g * n: (g + 1) * n] = lowest                    # all but one have none
+    x[2 * G, :n] = -np.inf
+    x[2 * G, n:] = np.where(np.arange(E - n) % 3, lowest, -np.inf)
+    x[2 * G + 1] = lowest
+    for bias in (None, np.zeros(E)):
+        check(x, "f32", min(3, n), rng, bias, grad=False, score=score, groups=G, best_groups=best, group_best=of)
