@@ -706,7 +706,8 @@ int seer_route_choose(const seer_dense *logits, const float *bias, const seer_ch
 /* The gradient of seer_route_choose's weights in the logits, for that of its output, dweight (DEVICE fp32 [tokens][choices]); what is
  * chosen counts as given, so no bias is wanted.  Renormalised, with w' = weight / factor (of the chosen logits alone): for the k-th choice
  * factor * w'_k * (dweight_k - sum_j w'_j dweight_j), times 1 - s for sigmoids.  Else factor * s_k (1 - s_k) dweight_k for
- * sigmoids, and factor * s_e * ([e chosen] dweight_e - sum_k s_k dweight_k) for every e of a softmax.  All other entries are 0.
+ * sigmoids, and factor * s_e * ([e chosen] dweight_e - sum_k s_k dweight_k) for every e of a softmax.  All other entries are
+ * 0, and so are those of logits of -infinity, whatever dweight is.
  * expert: DEVICE int32 [tokens][choices], any in any order; an entry outside [0, experts), or with a logit of -infinity, is no choice,
  * one that comes twice is two.  dlogits: the shape and type of logits, computed in fp32 or more, rounded once. */
 int seer_route_choose_grad(const seer_dense *logits, const seer_choice *how, const int32_t *expert, const float *dweight,

@@ -504,7 +504,7 @@ __global__ __launch_bounds__(kWG) void choose_grad_rows_kernel(const T *__restri
             }
             most = row_max(most);
 #pragma unroll
-            for (int i = 0; i < UNITS * 4; ++i) all += p[i] = p[i] == -INFINITY ? 0.0f : __expf(p[i] - most);
+            for (int i = 0; i < UNITS * 4; ++i) all += p[i] = p[i] == -INFINITY ? -0.0f : __expf(p[i] - most);      // (-0: masked)
             all = row_sum(all);
         }
         int32_t e = -1;
@@ -545,7 +545,10 @@ __global__ __launch_bounds__(kWG) void choose_grad_rows_kernel(const T *__restri
                 const v4f v = *reinterpret_cast<const v4f *>(mine + at);
                 float d[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) d[j] = WHOLE && any ? v[j] - p[WHOLE ? u * 4 + j : 0] * off : v[j];
+                for (int j = 0; j < 4; ++j) {
+                    const float s = p[WHOLE ? u * 4 + j : 0];
+                    d[j] = WHOLE && any && __builtin_bit_cast(uint32_t, s) != 1u << 31 ? v[j] - s * off : v[j];
+                }
                 T *to = dlogits + (int64_t)t * ldd + at;
                 if (at + 4 <= experts) {
                     typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));

@@ -341,3 +341,23 @@ def test_lowest_logits_beside_groups_with_none(E, groups, score):
     x[2 * G + 1] = lowest
     for bias in (None, np.zeros(E)):
         check(x, "f32", min(3, n), rng, bias, grad=False, score=score, groups=G, best_groups=best, group_best=of)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renormalise", [True, False])
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("E", [8, 64, 300, 600])
+def test_gradient_of_masked_logits_is_zero(E, kind, renormalise, score):
+    """Whatever the others' gradients are: NaN, infinite, or of a row with a NaN in it."""
+    announce(f"choose_grad masked {E} {kind} {renormalise} {score}")
+    rng = np.random.default_rng(E)
+    x = rng.standard_normal((7, E))
+    masked = rng.random((7, E)) < 0.4
+    masked[:, :3], masked[:, 3] = False, True
+    x[masked] = -np.inf
+    x[1, 0], x[2, 1] = np.nan, np.inf
+    expert = np.tile([0, 1, 3], (7, 1)).astype(np.int32)
+    dw = rng.standard_normal((7, 3)).astype(np.float32)
+    dw[3, 0], dw[4, 1], dw[5, 0] = np.inf, np.nan, -np.inf
+    d = host(S.seer_route_choose_grad(rounded(x, kind), S.Choice(3, score=score, renormalise=renormalise), torch.from_numpy(expert).cuda(), torch.from_numpy(dw).cuda()))
+    assert not d[masked].any() and np.isfinite(d[[0, 6]]).all() and np.isnan(d[1]).any()
