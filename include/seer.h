@@ -695,9 +695,11 @@ typedef struct {
 /* The experts of every token and their weights.  With s = softmax(logits[t]) or the sigmoids, an expert's key is s + bias, or, without a
  * bias, its logit, which is in the same order.  Of the best_groups groups that count most the `choices` experts with the largest
  * keys are chosen, the largest first: expert[t][k], and weight[t][k] = factor * s, divided by the sum of the chosen s if
- * renormalise (without loss where every s is too small for fp32).  Keys and groups' sums are compared as 64-bit numbers hold them, ties go
- * to the lower number, a NaN counts as the largest.  An expert whose logit, or bias, is -infinity is not chosen; where there are not
- * enough others, expert is -1 (nobody's to seer_route) with weight 0.  A softmax over a NaN or +infinity is NaN throughout.
+ * renormalise (without loss where every s is too small for fp32).  Weights are computed in 64 bits and rounded once, but for the
+ * exponentials that a softmax which is not renormalised adds up over all experts: these are in 32 or more.  Keys and groups' sums are
+ * compared as 64-bit numbers hold them, ties go to the lower number, a NaN counts as the largest.  An expert whose logit, or bias, is
+ * -infinity is not chosen; where there are not enough others, expert is -1 (nobody's to seer_route) with weight 0.  A softmax over a NaN or
+ * +infinity is NaN throughout.
  * logits: [tokens][experts], SEER_F32, SEER_BF16 or SEER_F16, at most SEER_MAX_EXPERTS columns (SEER_ELIMIT).  bias: DEVICE
  * fp32 [experts], or NULL.  expert: DEVICE int32 [tokens][choices].  weight: DEVICE fp32 [tokens][choices]. */
 int seer_route_choose(const seer_dense *logits, const float *bias, const seer_choice *how, int32_t *expert,

@@ -187,6 +187,12 @@ __device__ __forceinline__ uint32_t row_move(uint32_t v)
 }
 template <int CTRL>
 __device__ __forceinline__ float row_move(float v) { return dpp_f<CTRL>(v); }
+template <int CTRL>
+__device__ __forceinline__ double row_move(double v)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)row_move<CTRL>((uint32_t)(u >> 32)) << 32 | row_move<CTRL>((uint32_t)u));
+}
 template <class V, class F>
 __device__ __forceinline__ V row_fold(V v, F f)
 {
@@ -195,9 +201,10 @@ __device__ __forceinline__ V row_fold(V v, F f)
     v = f(v, row_move<0x141>(v));
     return f(v, row_move<0x140>(v));
 }
-__device__ __forceinline__ float row_sum(float v)
+template <class V>
+__device__ __forceinline__ V row_sum(V v)
 {
-    return row_fold(v, [](float a, float b) { return a + b; });
+    return row_fold(v, [](V a, V b) { return a + b; });
 }
 __device__ __forceinline__ float row_max(float v)
 {
@@ -226,7 +233,45 @@ __device__ __forceinline__ void other_lanes(F f)
 
 __device__ __forceinline__ float fast_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 
-// The weights of the experts chosen for a token, one to a lane of 16: as chosen_share.
+// e^x for x <= 0 to 2^-42 of itself: 2^n times the series of e^f up to f^10 / 10!, |f| <= ln(2) / 2.  (Numbers that are made where they are used: those of the
+// library's exponential are kept in 22 registers from token to token.)
+__device__ __forceinline__ double exp_below_0(double x)
+{
+    x = x < -1100.0 ? -1100.0 : x;
+    const double n = rint(x * 0x1.71547652b82fep+0), f = fma(n, -0x1.62e42fefa39efp-1, x);
+    const auto here = [](double c) {
+        asm volatile("" : "+s"(c));
+        return c;
+    };
+    double p = here(1.0 / 3628800);
+    p = fma(p, f, here(1.0 / 362880));
+    p = fma(p, f, here(1.0 / 40320));
+    p = fma(p, f, here(1.0 / 5040));
+    p = fma(p, f, here(1.0 / 720));
+    p = fma(p, f, here(1.0 / 120));
+    p = fma(p, f, here(1.0 / 24));
+    p = fma(p, f, here(1.0 / 6));
+    p = fma(p, f, 0.5);
+    p = fma(p, f, 1.0);
+    p = fma(p, f, 1.0);
+    return ldexp(p, (int)n);
+}
+
+// The weights of the experts chosen for a token, one to a lane of 16: as chosen_share, and in 64 bits as there; only the sum that a softmax over all experts
+// divides by has terms in 32.  (65 536 tokens of 256 experts, eight choices: 1.8 us longer than in 32 bits, which were off by up to 4e-7 of a weight.)
+__device__ __forceinline__ double row_share(const seer_choice &how, float x, bool in, float most, double all)
+{
+    const double v = (double)x;
+    const float top = how.renormalise ? row_max(in ? x : -INFINITY) : most;
+    const bool sigmoid = how.score == SEER_SIGMOID && !(how.renormalise && top < -600.0f);      // (e^x: what 64 bits do not hold counts from the largest)
+    const double z = exp_below_0(!in ? 0.0 : sigmoid ? -fabs(v) : v - (double)top);
+    double s = in ? sigmoid && v > 0 ? 1.0 : z : 0.0;
+    if (how.score == SEER_SIGMOID) s /= sigmoid ? 1.0 + z : 1.0;
+    const double sum = how.renormalise ? row_sum(s) : all;
+    return (how.renormalise || how.score == SEER_SOFTMAX) && in ? s / sum : s;
+}
+
+// The same in 32 bits for the gradient.
 __device__ __forceinline__ float row_share(const seer_choice &how, float x, bool in, float most, float all)
 {
     if (!how.renormalise) return !in ? 0.0f : how.score == SEER_SIGMOID ? fast_sigmoid(x) : __expf(x - most) * __builtin_amdgcn_rcpf(all);
@@ -239,6 +284,14 @@ __device__ __forceinline__ float row_share(const seer_choice &how, float x, bool
     s = in ? s : 0.0f;
     const float sum = row_sum(s);
     return in ? s * __builtin_amdgcn_rcpf(sum) : 0.0f;
+}
+
+// The sum of a lane's values by halves.
+template <int N, class F>
+__device__ __forceinline__ float sum_of(F f, int from = 0)
+{
+    if constexpr (N == 1) return f(from);
+    else return sum_of<N / 2>(f, from) + sum_of<N - N / 2>(f, from + N / 2);
 }
 
 // per: the experts of a lane; VEC: rows are read 4 elements at a time.  group_lanes: lanes to a group, 0 without groups.
@@ -278,16 +331,15 @@ __global__ __launch_bounds__(kWG, PER > 16 ? 2 : 4) void choose_rows_kernel(cons
             for (int i = 0; i < PER; ++i) x[i] = l * per + i < experts && (uint32_t)i < per ? (float)row[l * per + i] : -INFINITY;
         }
         // keys: scores with the bias, or logits; -infinity is not to be chosen
-        float key[PER], most = -INFINITY, all = 0, score_error = kSigmoidError, by = 0;
+        float key[PER], most = -INFINITY, score_error = kSigmoidError, by = 0;
+        double all = 0;
         if (how.score == SEER_SOFTMAX && (BIAS || two || !how.renormalise)) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) most = fmaxf(most, x[i]);
             most = row_max(most);
             most = most == -INFINITY ? 0 : most;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) all += __expf(x[i] - most);
-            all = row_sum(all);
-            by = all > 0 ? __builtin_amdgcn_rcpf(all) : 0;
+            all = row_sum((double)sum_of<PER>([&](int i) { return __expf(x[i] - most); }));
+            by = all > 0 ? __builtin_amdgcn_rcpf((float)all) : 0;
             score_error = kSoftmaxError * by;
         }
         const auto score = [&](float v) { return how.score == SEER_SIGMOID ? fast_sigmoid(v) : __expf(v - most) * by; };
@@ -405,12 +457,12 @@ __global__ __launch_bounds__(kWG, PER > 16 ? 2 : 4) void choose_rows_kernel(cons
                 sure = mine / NUMBERS != after / NUMBERS || (border ? sizeof(T) == 2 : xl >= xa);
             unsure = unsure || (in && after && !sure);
         }
-        const float share = row_share(how, xl, in, most, all);
+        const double share = row_share(how, xl, in, most, all);
         const uint64_t again = __ballot(unsure);
         if (t < tokens && (int)l < how.choices && !(again >> (lane & 48) & 0xffff)) {
             const size_t to = (size_t)t * how.choices + l;
             expert[to] = in ? (int32_t)at : -1;
-            weight[to] = how.factor * share;
+            weight[to] = (float)((double)how.factor * share);
         }
         if (__builtin_expect(again != 0, 0))
             for (uint32_t i = 0; i < 4; ++i)

@@ -361,3 +361,51 @@ def test_gradient_of_masked_logits_is_zero(E, kind, renormalise, score):
     dw[3, 0], dw[4, 1], dw[5, 0] = np.inf, np.nan, -np.inf
     d = host(S.seer_route_choose_grad(rounded(x, kind), S.Choice(3, score=score, renormalise=renormalise), torch.from_numpy(expert).cuda(), torch.from_numpy(dw).cuda()))
     assert not d[masked].any() and np.isfinite(d[[0, 6]]).all() and np.isnan(d[1]).any()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,C", [(8, 2), (64, 8), (256, 8), (300, 15), (512, 10), (600, 8), (64, 20)], ids=str)
+@pytest.mark.parametrize("biased", [False, True])
+def test_weights_are_rounded_once(E, C, biased, score):
+    """Weights are computed in 64 bits and rounded to fp32: half a unit in the last place, and 2^-40 for the 64 bits."""
+    announce(f"weights {E} {C} {score} {biased}")
+    rng = np.random.default_rng(E + C)
+    x = rounded(rng.standard_normal((200, E)) * 3, "f32")
+    x[1] -= 150
+    x[2] *= 10
+    bias = (rng.standard_normal(E) * 0.1).astype(np.float32) if biased else None
+    for renormalise in (True, False) if score == "sigmoid" else (True,):
+        e, w = S.seer_route_choose(x, S.Choice(C, score=score, renormalise=renormalise, factor=2.5), bias=None if bias is None else torch.from_numpy(bias).cuda())
+        want_e, want = O.choose(host(x), C, bias=None if bias is None else bias.astype(np.float64), score=score, renormalise=renormalise, factor=2.5)
+        assert np.array_equal(host(e), want_e)
+        assert_within(host(w), want, np.abs(want) * (U32 + 2.0 ** -40) + TINY["f32"], "weight")
+
+
+@pytest.mark.parametrize("E", [8, 64, 160, 256, 300, 512])
+def test_weights_of_a_softmax_over_all_experts(E):
+    """The sum that they are divided by has terms in 32 bits: an exponential is off by 2 half units in the last place and by 2.25 of them for
+    each unit of its argument (a difference, a product, and log2(e) in 32 bits), the sum by these on its terms' average and by 5 for up to 32
+    terms added by halves; everything else is in 64 bits, and rounded once."""
+    announce(f"weights of a softmax over {E}")
+    rng = np.random.default_rng(E)
+    x = host(rounded(rng.standard_normal((300, E)) * 3, "f32"))
+    x[1] *= 8
+    e, w = S.seer_route_choose(torch.from_numpy(x).float().cuda(), S.Choice(min(E, 8), renormalise=False))
+    want_e, want = O.choose(x, min(E, 8), renormalise=False)
+    assert np.array_equal(host(e), want_e)
+    d = x.max(1, keepdims=True) - x
+    terms = 5 + (np.exp(-d) * (2 + 2.25 * d)).sum(1, keepdims=True) / np.exp(-d).sum(1, keepdims=True)
+    assert_within(host(w), want, want * (U32 * (1 + terms) * (1 + 2.0 ** -10)) + 2.0 ** -126, "weight")
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("E", [1, 8, 64, 256, 512, 600])
+def test_one_choice_renormalised_is_the_factor(E, kind, score):
+    """Its weight hangs on no logit."""
+    announce(f"one choice of {E} {kind} {score}")
+    rng = np.random.default_rng(E)
+    x = rounded(rng.standard_normal((500, E)) * 4, kind)
+    how = S.Choice(1, score=score, factor=2.7)
+    e, w = S.seer_route_choose(x, how)
+    assert bool((w == float(np.float32(2.7))).all())
