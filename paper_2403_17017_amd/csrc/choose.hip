@@ -271,7 +271,7 @@ __device__ __forceinline__ double row_share(const seer_choice &how, float x, boo
     return (how.renormalise || how.score == SEER_SOFTMAX) && in ? s / sum : s;
 }
 
-// The same in 32 bits for the gradient.
+// The same in 32 bits for the gradient.  (A quotient of its own: one choice is 1.)
 __device__ __forceinline__ float row_share(const seer_choice &how, float x, bool in, float most, float all)
 {
     if (!how.renormalise) return !in ? 0.0f : how.score == SEER_SIGMOID ? fast_sigmoid(x) : __expf(x - most) * __builtin_amdgcn_rcpf(all);
@@ -283,7 +283,7 @@ __device__ __forceinline__ float row_share(const seer_choice &how, float x, bool
         s = __expf(x - top);
     s = in ? s : 0.0f;
     const float sum = row_sum(s);
-    return in ? s * __builtin_amdgcn_rcpf(sum) : 0.0f;
+    return in ? s / sum : 0.0f;
 }
 
 // The sum of a lane's values by halves.

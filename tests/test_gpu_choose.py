@@ -402,10 +402,11 @@ def test_weights_of_a_softmax_over_all_experts(E):
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("E", [1, 8, 64, 256, 512, 600])
 def test_one_choice_renormalised_is_the_factor(E, kind, score):
-    """Its weight hangs on no logit."""
+    """Its weight hangs on no logit, so its gradient is 0."""
     announce(f"one choice of {E} {kind} {score}")
     rng = np.random.default_rng(E)
     x = rounded(rng.standard_normal((500, E)) * 4, kind)
     how = S.Choice(1, score=score, factor=2.7)
     e, w = S.seer_route_choose(x, how)
     assert bool((w == float(np.float32(2.7))).all())
+    assert not S.seer_route_choose_grad(x, how, e, torch.from_numpy(rng.standard_normal((500, 1)).astype(np.float32)).cuda()).any()
