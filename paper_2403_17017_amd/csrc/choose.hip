@@ -388,8 +388,10 @@ __global__ __launch_bounds__(kWG, PER > 16 ? 2 : 4) void choose_rows_kernel(cons
                 float worth = first;
                 if (two && second != -INFINITY) worth += second;
                 unsure = unsure || worth > kFar;
-                worth = fmaxf(worth, -0x1.fffffep127f);     // (with a group that has none at the border, 64 bits decide)
-                const float size = row_max(first == -INFINITY ? 0.0f : fmaxf(fabsf(first), second == -INFINITY ? 0.0f : fabsf(second)));
+                // a group with none stays at -infinity, behind sums that are
+                const bool there = first != -INFINITY;
+                if (there) worth = fmaxf(worth, -0x1.fffffep127f);
+                const float size = row_max(there ? fmaxf(fabsf(first), second == -INFINITY ? 0.0f : fabsf(second)) : 0.0f);
                 const float near = 4 * score_error + size * 0x1p-21f;
                 uint32_t not_below = 0;
                 other_lanes([&](auto ctrl, uint32_t) {
@@ -398,8 +400,8 @@ __global__ __launch_bounds__(kWG, PER > 16 ? 2 : 4) void choose_rows_kernel(cons
                     not_below += gap >= -near;
                 });
                 open = above < room;
-                // (the own group's other lanes are level with it)
-                unsure = unsure || (open && not_below - (group_lanes - 1) >= room);
+                // (the own group's other lanes are level with it; whether a group with none is open is nothing to the choice)
+                unsure = unsure || (there && open && not_below - (group_lanes - 1) >= room);
             } else {
                 // exact: a group with none is -infinity, behind the lowest number
                 const uint32_t mine = l & ~(group_lanes - 1);

@@ -410,3 +410,23 @@ def test_one_choice_renormalised_is_the_factor(E, kind, score):
     e, w = S.seer_route_choose(x, how)
     assert bool((w == float(np.float32(2.7))).all())
     assert not S.seer_route_choose_grad(x, how, e, torch.from_numpy(rng.standard_normal((500, 1)).astype(np.float32)).cuda()).any()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("groups", [(2, 1, 2), (4, 3, 1), (8, 4, 2), (16, 5, 2)], ids=str)
+@pytest.mark.parametrize("E", [16, 64, 256, 384])
+def test_groups_with_none_beside_sums_of_any_size(E, groups, score):
+    """Padding, fewer groups in service than are kept, one more, and groups whose two best have a sum below all numbers in 32 bits."""
+    announce(f"choose padding {E} {groups} {score}")
+    rng = np.random.default_rng(E)
+    G, best, of = groups
+    n, far = E // G, float(np.finfo(np.float32).max)
+    x = rng.standard_normal((60, E)) * 2
+    x[rng.random(60) < 0.2] = -np.inf
+    for t in range(20):                                          # t + 1 groups of the row are in service
+        keep = rng.permutation(G)[: t % G + 1]
+        x[t] = np.where(np.isin(np.arange(E) // n, keep), x[t], -np.inf)
+    low = -far * rng.choice([0.4, 0.7, 0.9, 1.0], E)
+    some = np.where(rng.random(E) < 0.5, low, rng.standard_normal(E) * 0.1)
+    for bias in (rng.standard_normal(E) * 0.1, low, some, np.zeros(E)) + ((None,) if of == 2 else ()):
+        check(x, "f32", min(4, n), rng, None if bias is None else bias.astype(np.float32), grad=False, score=score, groups=G, best_groups=best, group_best=of)
