@@ -655,6 +655,10 @@ typedef enum {
 } seer_mx4_kernel;
 int seer_mx4_product_kernel(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups);
 
+/* The same, with how many rows a tile has (64, 128 or 256; 0 without tiles) and between how many workgroups the columns of each are
+ * shared out (1 but for SEER_MX4_SHARED), in *tokens and *shares, HOST; either may be NULL.  Nothing is written on error. */
+int seer_mx4_product_plan(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups, int32_t *tokens, int32_t *shares);
+
 /* One of the many tensors whose gradient is clipped: n contiguous elements. */
 typedef struct {
     const void *grad; /* DEVICE */

@@ -18,5 +18,5 @@ from .routed import (  # noqa: F401
     seer_route, seer_route_combine, seer_route_gather, seer_route_gather_i8, seer_route_grad,
 )
 from .router import MAX_CHOICES, MAX_EXPERT_GROUPS, Choice, seer_route_choose, seer_route_choose_grad  # noqa: F401
-from .mx4 import MX4_KERNELS, mx4_product_kernel, mx4_product_workspace_bytes, seer_mx4_product, seer_mx4_quantize, seer_route_gather_mx4  # noqa: F401
+from .mx4 import MX4_KERNELS, mx4_product_kernel, mx4_product_plan, mx4_product_workspace_bytes, seer_mx4_product, seer_mx4_quantize, seer_route_gather_mx4  # noqa: F401
 from .embedding import embed_grad_workspace_bytes, seer_embed, seer_embed_grad  # noqa: F401

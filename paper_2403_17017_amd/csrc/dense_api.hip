@@ -327,7 +327,7 @@ int seer_mx4_product(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_
     return done();
 }
 
-int seer_mx4_product_kernel(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups)
+int seer_mx4_product_plan(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups, int32_t *tokens, int32_t *shares)
 {
     if (!a || !b || groups < 1 || (!group_ptr && groups != 1)) return SEER_EINVAL;
     int rc;
@@ -336,7 +336,15 @@ int seer_mx4_product_kernel(const seer_mx4 *a, const seer_mx4 *b, const int32_t 
     const Mx4Args p{nullptr, nullptr, nullptr, nullptr, group_ptr, nullptr, a->ld, b->ld, a->scale_ld, b->scale_ld, 0,
                     (uint32_t)a->rows, (uint32_t)(b->rows / groups), (uint32_t)((a->cols + 31) / 32), (uint32_t)groups, SEER_F32};
     if (!mx4_product_fits(p)) return SEER_ELIMIT;
-    return p.rows == 0 || p.channels == 0 ? SEER_MX4_NONE : mx4_plan(p).kernel;
+    const Mx4Plan plan = p.rows == 0 || p.channels == 0 ? Mx4Plan{SEER_MX4_NONE, 0, 1} : mx4_plan(p);
+    if (tokens) *tokens = (int32_t)plan.tokens;
+    if (shares) *shares = (int32_t)plan.shares;
+    return plan.kernel;
+}
+
+int seer_mx4_product_kernel(const seer_mx4 *a, const seer_mx4 *b, const int32_t *group_ptr, int32_t groups)
+{
+    return seer_mx4_product_plan(a, b, group_ptr, groups, nullptr, nullptr);
 }
 
 size_t seer_grad_workspace_bytes(void) { return grad_workspace_bytes(); }

@@ -630,6 +630,13 @@ static Mx4Shared shared_columns(const Mx4Args &a, uint32_t shares, void *workspa
     return Mx4Shared{static_cast<float *>(workspace), (uint32_t)most_blocks(a, 64, kTileChannels), (rounds + shares - 1) / shares * kRoundBlocks, (a.channels + 3) & ~3u};
 }
 
+// How many of `shares` are left when each is whole rounds.
+static uint32_t whole_shares(uint32_t blocks, uint32_t shares)
+{
+    const uint32_t rounds = (blocks + kRoundBlocks - 1) / kRoundBlocks, each = (rounds + shares - 1) / shares;
+    return (rounds + each - 1) / each;
+}
+
 struct Mx4Choice { uint32_t tokens /* 0: few rows */, shares; };
 
 static Mx4Choice choose(const Mx4Args &a)
@@ -673,7 +680,7 @@ Mx4Plan mx4_plan(const Mx4Args &a)
     if (a.lda >= (1 << 23) || a.ldb >= (1 << 23)) return any;
     const Mx4Choice c = choose(a);
     if (c.tokens == 0) return (uint64_t)((a.channels + 15) / 16) * 256 < 1ull << 32 ? Mx4Plan{SEER_MX4_FEW, 0, 1} : any;
-    if (c.shares > 1) return Mx4Plan{SEER_MX4_SHARED, c.tokens, c.shares};
+    if (c.shares > 1) return Mx4Plan{SEER_MX4_SHARED, c.tokens, whole_shares(a.blocks, c.shares)};
     return most_blocks(a, c.tokens, kTileChannels) * (c.tokens == 64 ? 256 : 512) < 1ull << 32 ? Mx4Plan{SEER_MX4_TILES, c.tokens, 1} : any;
 }
 
@@ -696,10 +703,9 @@ void launch_mx4_product(const Mx4Args &a, const Mx4Plan &p, void *workspace, hip
             return;
         case SEER_MX4_SHARED: {
             const Mx4Shared c = shared_columns(a, p.shares, workspace);
-            const uint32_t shares = (a.blocks + c.share - 1) / c.share;
-            hipLaunchKernelGGL((mx4_tile_kernel<float, 4, 4, 4, 4, true>), dim3(c.blocks * shares), dim3(256), 0, st, a, c);
+            hipLaunchKernelGGL((mx4_tile_kernel<float, 4, 4, 4, 4, true>), dim3(c.blocks * p.shares), dim3(256), 0, st, a, c);
             const uint64_t lanes = (uint64_t)a.rows * (c.pitch / 4);
-            hipLaunchKernelGGL((mx4_join_kernel<T>), dim3((uint32_t)std::min<uint64_t>((lanes + kWG - 1) / kWG, 8 * kCUs)), dim3(kWG), 0, st, a, c, shares);
+            hipLaunchKernelGGL((mx4_join_kernel<T>), dim3((uint32_t)std::min<uint64_t>((lanes + kWG - 1) / kWG, 8 * kCUs)), dim3(kWG), 0, st, a, c, p.shares);
             return;
         }
         default: {

@@ -25,6 +25,7 @@ def bind(L):
     for name, args, res in (("seer_mx4_quantize", [dense, mx4, vp], C.c_int), ("seer_route_gather_mx4", [routing, dense, mx4, vp], C.c_int),
                             ("seer_mx4_product", [mx4, mx4, vp, i32, dense, vp, sz, vp], C.c_int),
                             ("seer_mx4_product_kernel", [mx4, mx4, vp, i32], C.c_int),
+                            ("seer_mx4_product_plan", [mx4, mx4, vp, i32, C.POINTER(i32), C.POINTER(i32)], C.c_int),
                             ("seer_mx4_product_workspace_bytes", [i64, i64, i64, i32], sz)):
         f = getattr(L, name)
         f.argtypes, f.restype = args, res
@@ -61,16 +62,24 @@ def mx4_product_workspace_bytes(rows: int, channels: int, columns: int, groups: 
 MX4_KERNELS = ("none", "any", "few", "tiles", "shared")
 
 
-def mx4_product_kernel(a, b, group_ptr=None) -> str:
-    """Which kernel seer_mx4_product takes for these codes, one of MX4_KERNELS; nothing is launched."""
+def mx4_product_plan(a, b, group_ptr=None):
+    """(kernel, tokens, shares) that seer_mx4_product takes for these codes: one of MX4_KERNELS, the rows of a tile (0 without tiles), and
+    between how many workgroups a tile's columns are shared out; nothing is launched."""
     if b.dim() not in (2, 3):
         raise ValueError("b is to be [groups, channels, bytes]")
     groups, blocks = b.shape[0] if b.dim() == 3 else 1, a.shape[-1] // 16
     rows_of = lambda t, rows: C.byref(seer_mx4(t.data_ptr(), t.data_ptr(), rows, 32 * blocks, t.stride(-2) if rows > 1 else 16 * blocks, blocks))
-    rc = B.lib().seer_mx4_product_kernel(rows_of(a, a.shape[0]), rows_of(b, groups * b.shape[-2]), group_ptr.data_ptr() if group_ptr is not None else None, groups)
+    tokens, shares = C.c_int32(), C.c_int32()
+    rc = B.lib().seer_mx4_product_plan(rows_of(a, a.shape[0]), rows_of(b, groups * b.shape[-2]), group_ptr.data_ptr() if group_ptr is not None else None, groups,
+                                       C.byref(tokens), C.byref(shares))
     if rc < 0:
-        raise SeerError(rc, "seer_mx4_product_kernel")
-    return MX4_KERNELS[rc]
+        raise SeerError(rc, "seer_mx4_product_plan")
+    return MX4_KERNELS[rc], tokens.value, shares.value
+
+
+def mx4_product_kernel(a, b, group_ptr=None) -> str:
+    """Which kernel seer_mx4_product takes for these codes, one of MX4_KERNELS; nothing is launched."""
+    return mx4_product_plan(a, b, group_ptr)[0]
 
 
 def seer_mx4_product(a, a_scale, b, b_scale, out=None, group_ptr=None, dtype=None, workspace=None, stream=None):

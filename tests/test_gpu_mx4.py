@@ -293,3 +293,96 @@ def test_tiles_that_end_in_one_row_and_one_channel(blocks):
     a, b = codes(rng, 2817, blocks), codes(rng, 1, 1537, blocks)
     assert S.mx4_product_kernel(a[0], b[0]) == "tiles"
     check_product(a, b, None, "f32")
+
+
+def codes_here(seed, *shape, spread_of_scales=4):
+    """The same as codes, made on the GPU."""
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    q = torch.randint(0, 256, (*shape[:-1], 16 * shape[-1]), generator=g, device="cuda:0", dtype=torch.uint8)
+    return q, torch.randint(127 - spread_of_scales, 127 + spread_of_scales, shape, generator=g, device="cuda:0", dtype=torch.uint8)
+
+
+def values_here(q, s):
+    """What codes and scales stand for, fp64 on the GPU."""
+    table = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device="cuda:0")
+    two = torch.stack([q & 15, q >> 4], dim=-1).flatten(-2).long()
+    v = table[two & 7] * (1 - 2 * (two >> 3)) * torch.exp2(s.double() - 127).repeat_interleave(32, dim=-1)
+    return v.masked_fill((s == 255).repeat_interleave(32, dim=-1), float("nan"))
+
+
+TILES = [  # rows of a tile; rows, channels of one matrix; groups, rows behind them, channels
+    (64, (1153, 2305), ([300, 2, 0, 700, 17, 257], 7, 1537)),
+    (128, (2817, 1537), ([900, 0, 1, 257, 255, 2000, 256], 7, 1100)),
+    (256, (4097, 2305), ([1, 255, 0, 256, 257, 1500, 3000], 7, 2305)),
+]
+
+
+def tiled(tokens, sizes, grouped, blocks, seed):
+    """(a, b, group_ptr or None, bounds of the groups, rows behind them) of a case of TILES, which takes tiles of `tokens` rows."""
+    lengths, more, channels = ([sizes[0][0]], 0, sizes[0][1]) if not grouped else sizes[1]
+    upto = np.concatenate([[0], np.cumsum(lengths)]).tolist()
+    a, b = codes_here(seed, upto[-1] + more, blocks), codes_here(seed + 1, len(lengths), channels, blocks)
+    ptr = torch.tensor(upto, dtype=torch.int32, device="cuda:0") if grouped else None
+    assert S.mx4_product_plan(a[0], b[0], ptr) == ("tiles", tokens, 1)
+    return a, b, ptr, upto, more
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("blocks", [1, 4, 5, 16, 17, 33, 129])
+@pytest.mark.parametrize("grouped", [False, True], ids=["one", "groups"])
+@pytest.mark.parametrize("tokens,one,groups", TILES, ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_tiles_of_every_size(tokens, one, groups, grouped, blocks, kind):
+    """Against a product in fp64 on the GPU, with the bound of check_product."""
+    announce(f"mx4 tiles of {tokens}, {'groups' if grouped else 'one'}, {blocks} blocks, {kind}")
+    a, b, ptr, upto, more = tiled(tokens, (one, groups), grouped, blocks, blocks)
+    out = torch.full((a[0].shape[0], b[0].shape[1]), float("nan"), dtype=TYPES[kind], device="cuda:0")
+    S.seer_mx4_product(*a, *b, group_ptr=ptr, out=out)
+    left = values_here(*a)
+    for g in range(len(upto) - 1):
+        rows, right = slice(upto[g], upto[g + 1]), values_here(b[0][g], b[1][g]).t().contiguous()
+        want, size = left[rows] @ right, left[rows].abs() @ right.abs()
+        off = 2 * U32 * (a[0].shape[1] // 64 + 18) * size
+        off = off + (want.abs() + off) * ROUND[kind] + TINY[kind]
+        ok = (out[rows].double() - want).abs() <= off
+        if kind == "f16":
+            ok |= want.abs() > 65000                                 # beyond its range
+        assert bool(ok.all()), (g, int((~ok).sum()))
+    assert not out[upto[-1]:].any()
+
+
+@pytest.mark.parametrize("blocks", [1, 4, 5, 17, 130])
+@pytest.mark.parametrize("grouped", [False, True], ids=["one", "groups"])
+@pytest.mark.parametrize("tokens,one,groups", TILES, ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_nan_blocks_stay_in_their_rows_of_tiles(tokens, one, groups, grouped, blocks):
+    """In the last row and the first of a group, in a tile's last channel and the next one's first."""
+    announce(f"mx4 NaN, tiles of {tokens}, {'groups' if grouped else 'one'}, {blocks} blocks")
+    a, b, ptr, upto, more = tiled(tokens, (one, groups), grouped, blocks, blocks)
+    last = len(upto) - 2                                             # the last group; its neighbours are to stay as they are
+    rows, channels = sorted({0, upto[last], upto[-1] - 1, upto[-1] - tokens}), [0, 255, 256, b[0].shape[1] - 1]
+    a[1][rows, blocks - 1] = 255
+    b[1][last, channels, 0] = 255
+    if more:
+        a[1][upto[-1]:] = 255                                        # nobody's rows
+    nan = S.seer_mx4_product(*a, *b, group_ptr=ptr, dtype=torch.float32).isnan()
+    want = torch.zeros_like(nan)
+    want[rows] = True
+    want[upto[last]: upto[-1], channels] = True
+    assert torch.equal(nan, want)
+
+
+@pytest.mark.parametrize("blocks", [3, 6, 64, 129])
+@pytest.mark.parametrize("grouped", [False, True], ids=["one", "groups"])
+@pytest.mark.parametrize("tokens,one,groups", TILES, ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_strides_and_odd_addresses_of_tiles(tokens, one, groups, grouped, blocks):
+    """Codes further apart, scale bytes at any address and results further apart give the same bits; what lies between is left alone."""
+    announce(f"mx4 strides, tiles of {tokens}, {'groups' if grouped else 'one'}, {blocks} blocks")
+    a, b, ptr, upto, more = tiled(tokens, (one, groups), grouped, blocks, blocks)
+    G, N = b[0].shape[:2]
+    want = S.seer_mx4_product(*a, *b, group_ptr=ptr, dtype=torch.float32)
+    qa, qb = spread(a[0], 16 * blocks + 16, 0x77), spread(b[0].view(G * N, -1), 16 * blocks + 48, 0x77)
+    for by in (0, 1, 2, 3, 7):
+        sa, sb = spread(shifted(a[1], by), blocks + by, 255), spread(shifted(b[1].view(G * N, -1), 1 + by), blocks + 2 * by + 1, 255)
+        out = torch.full((a[0].shape[0], N + 14), 55.0, device="cuda:0")
+        S.seer_mx4_product(qa, sa, qb.as_strided((G, N, 16 * blocks), (N * qb.stride(0), qb.stride(0), 1)), sb.as_strided((G, N, blocks), (N * sb.stride(0), sb.stride(0), 1)),
+                           group_ptr=ptr, out=out[:, :N])
+        assert torch.equal(out[:, :N], want) and bool((out[:, N:] == 55).all())

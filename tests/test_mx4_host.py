@@ -146,3 +146,59 @@ def test_what_is_chosen_is_near_the_best():
         kind = kernel(int(r["rows"]), int(r["channels"]), int(r["columns"]), int(r["groups"]))
         over.append(min(t for k, t in times.items() if k.startswith(kind)) / min(times.values()))
     assert np.mean(over) < 1.03 and max(over) < 1.6
+
+
+def plan(rows, channels, columns, groups=1):
+    f = lambda at, n: C.byref(M.seer_mx4(at, at + 4096, n, columns, 16 * -(-columns // 32), -(-columns // 32)))
+    tokens, shares = C.c_int32(-7), C.c_int32(-7)
+    rc = S.lib().seer_mx4_product_plan(f(A, rows), f(1 << 30, groups * channels), P if groups > 1 else None, groups, C.byref(tokens), C.byref(shares))
+    return (S.MX4_KERNELS[rc] if rc >= 0 else rc), tokens.value, shares.value
+
+
+def test_plans():
+    assert plan(1, 8192, 8192) == ("few", 0, 1) and plan(0, 5, 64) == ("none", 0, 1) and plan(5, 6, 0) == ("few", 0, 1)
+    assert plan(1000, 3001, 4096) == ("tiles", 64, 1) and plan(2817, 1537, 4096) == ("tiles", 128, 1) and plan(3001, 5001, 4111) == ("tiles", 256, 1)
+    assert plan(32768, 4096, 4096, 32) == ("tiles", 256, 1)
+    kind, tokens, shares = plan(300, 512, 8192)
+    assert kind == "shared" and tokens == 64 and shares > 1 and shares * 300 * 512 * 4 <= S.mx4_product_workspace_bytes(300, 512, 8192)
+    assert plan(1 << 22, 1 << 22, 32) == (-6, -7, -7) and plan(4, 8, 64, 4097) == (-6, -7, -7)      # nothing is written on error
+    f = S.lib().seer_mx4_product_plan
+    assert f(mx4(A, W, 2817, 64), mx4(B_, W, 1537, 64), None, 1, None, None) == S.MX4_KERNELS.index("tiles")
+    assert f(None, mx4(B_, W, 8, 64), None, 1, None, None) == -1 and f(mx4(A, W, 4, 64), mx4(B_, W, 9, 64), P, 2, None, None) == -1
+    assert S.mx4_product_plan(torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(2, 8, 64, dtype=torch.uint8), torch.zeros(3, dtype=torch.int32)) == ("few", 0, 1)
+    with pytest.raises(ValueError):
+        S.mx4_product_plan(torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(64, dtype=torch.uint8))
+
+
+def test_shares_are_whole_rounds():
+    """No share of the columns is empty, and each but the last has as many rounds of 16 blocks."""
+    seen = set()
+    for rows in (70, 130, 200, 300):
+        for channels in (256, 300, 512, 700):
+            for blocks in range(33, 700, 13):
+                kind, tokens, shares = plan(rows, channels, 32 * blocks)
+                if kind == "shared":
+                    rounds = -(-blocks // 16)
+                    each = -(-rounds // shares)
+                    assert (shares - 1) * each < rounds <= shares * each
+                    seen.add(shares)
+    assert len(seen) > 3
+
+
+def test_tiles_that_are_chosen_are_near_the_best():
+    """Of the 220 sizes the very tiles that are planned, and as many shares as are planned where those were timed."""
+    import csv
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "profiles", "mx4_kernel_times.csv")
+    with open(path) as f:
+        rows = list(csv.DictReader(line for line in f if not line.startswith("#")))
+    over, kinds = [], set()
+    for r in rows:
+        times = {k: float(r[k]) for k in ("few", "tiles_64", "tiles_128", "tiles_256", "shared") if float(r[k]) > 0}
+        kind, tokens, shares = plan(int(r["rows"]), int(r["channels"]), int(r["columns"]), int(r["groups"]))
+        kinds.add((kind, tokens))
+        # (of shares the best are timed; another number of them counts with what the library's choice took)
+        took = times[f"tiles_{tokens}"] if kind == "tiles" else times["few"] if kind == "few" else times["shared"] if shares == int(r["shares"]) else float(r["chosen"])
+        over.append(took / min(times.values()))
+    assert kinds == {("few", 0), ("tiles", 64), ("tiles", 128), ("tiles", 256), ("shared", 64)}
+    assert np.mean(over) < 1.03 and max(over) < 1.6
