@@ -196,3 +196,18 @@ def test_more_tokens_than_one_pass_of_workgroups(V):
     # runs of 16, of these 16, and what is left: no element goes through more than 16 + 16 + 2^17 / 256 + 62 additions
     assert bool(((got - want).abs() <= U32 * 700 * size + U32 * want.abs()).all())
     assert torch.equal(got, S.seer_embed_grad(token.int(), dy, V, scale=0.5))
+
+
+@pytest.mark.parametrize("accumulate", [False, True], ids=["", "add"])
+@pytest.mark.parametrize("types", GRADS, ids=lambda t: f"{t[0]}-{t[1]}")
+@pytest.mark.parametrize("size", [(4097, 512, 24, 0.5), (9000, 1000, 16, 1), (5000, 1023, 130, 0), (9000, 1 << 18, 8, 0.8), (20000, (1 << 20) - 1, 4, 0)], ids=str)
+def test_gradient_by_digits_of_ten_bits(size, types, accumulate):
+    """More than 4096 tokens of tables of 512 to 1023 rows, and of 2^18 to 2^20 - 1: places are counted in 1024 buckets a wave."""
+    T, V, D, skew = size
+    announce(f"embed_grad ten bits {size} {types} {accumulate}")
+    rng = np.random.default_rng(T + V)
+    p = np.arange(1, V + 1) ** -float(skew)
+    token = rng.choice(V, size=T, p=p / p.sum())
+    token[rng.random(T) < 0.05] = -1
+    token[5], token[6], token[7] = V, V - 1, 0
+    check_grad(token, rounded(rng.standard_normal((T, D)), types[0]), V, *types, scale=0.3, accumulate=accumulate, index="i32" if T % 3 else "i64")
