@@ -430,3 +430,33 @@ def test_groups_with_none_beside_sums_of_any_size(E, groups, score):
     some = np.where(rng.random(E) < 0.5, low, rng.standard_normal(E) * 0.1)
     for bias in (rng.standard_normal(E) * 0.1, low, some, np.zeros(E)) + ((None,) if of == 2 else ()):
         check(x, "f32", min(4, n), rng, None if bias is None else bias.astype(np.float32), grad=False, score=score, groups=G, best_groups=best, group_best=of)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("how", [dict(score="sigmoid"), dict(score="softmax", renormalise=False, bias=True), dict(score="sigmoid", groups=4, best_groups=2, group_best=2, bias=True),
+                                 dict(score="softmax", groups=8, best_groups=3)], ids=str)
+@pytest.mark.parametrize("E", [64, 192, 256, 512])
+def test_strides_and_odd_addresses_of_four_at_a_time(E, how, kind):
+    """Numbers of experts that rows are read four elements at a time for, at every address that an element can have."""
+    announce(f"choose strides {E} {how} {kind}")
+    rng = np.random.default_rng(E)
+    how = dict(how)
+    bias = torch.from_numpy((rng.standard_normal(E) * 0.1).astype(np.float32)).cuda() if how.pop("bias", False) else None
+    case = S.Choice(5, **how)
+    x = rounded(rng.standard_normal((37, E)), kind)
+    e, w = S.seer_route_choose(x, case, bias=bias)
+    want, _ = O.choose(host(x), 5, bias=None if bias is None else host(bias), **how)
+    assert np.array_equal(host(e), want)
+    dw = torch.from_numpy(rng.standard_normal((37, 5)).astype(np.float32)).cuda()
+    d = S.seer_route_choose_grad(x, case, e, dw)
+    for ld in (E, E + 1, E + 13):
+        for by in (0, 1, 2, 3):
+            room = torch.full((37 * ld + by,), float("nan"), dtype=x.dtype, device="cuda:0")
+            other = room[by:].view(37, ld)[:, :E]
+            other.copy_(x)
+            e2, w2 = S.seer_route_choose(other, case, bias=bias)
+            assert torch.equal(e, e2) and torch.equal(w, w2)
+            to = torch.full((37 * ld + by,), 55.0, dtype=x.dtype, device="cuda:0")
+            to_rows = to[by:].view(37, ld)
+            assert torch.equal(S.seer_route_choose_grad(other, case, e, dw, dlogits=to_rows[:, :E]), d)
+            assert bool((to_rows[:, E:] == 55).all()) and bool((to[:by] == 55).all())
