@@ -715,7 +715,8 @@ int seer_route_choose(const seer_dense *logits, const float *bias, const seer_ch
  * sigmoids, and factor * s_e * ([e chosen] dweight_e - sum_k s_k dweight_k) for every e of a softmax.  All other entries are
  * 0, and so are those of logits of -infinity, whatever dweight is.
  * expert: DEVICE int32 [tokens][choices], any in any order; an entry outside [0, experts), or with a logit of -infinity, is no choice,
- * one that comes twice is two.  dlogits: the shape and type of logits, computed in fp32 or more, rounded once. */
+ * one that comes twice is two.  dlogits: the shape and type of logits; computed in 64 bits, in 32 or more where a softmax over all experts or
+ * an expert that comes twice adds up. */
 int seer_route_choose_grad(const seer_dense *logits, const seer_choice *how, const int32_t *expert, const float *dweight,
                            const seer_dense *dlogits, void *stream);
 

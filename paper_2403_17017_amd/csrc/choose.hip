@@ -259,31 +259,21 @@ __device__ __forceinline__ double exp_below_0(double x)
 
 // The weights of the experts chosen for a token, one to a lane of 16: as chosen_share, and in 64 bits as there; only the sum that a softmax over all experts
 // divides by has terms in 32.  (65 536 tokens of 256 experts, eight choices: 1.8 us longer than in 32 bits, which were off by up to 4e-7 of a weight.)
-__device__ __forceinline__ double row_share(const seer_choice &how, float x, bool in, float most, double all)
+// rest: 1 less a sigmoid's score, for its gradient.
+__device__ __forceinline__ double row_share(const seer_choice &how, float x, bool in, float most, double all, double *rest = nullptr)
 {
     const double v = (double)x;
     const float top = how.renormalise ? row_max(in ? x : -INFINITY) : most;
     const bool sigmoid = how.score == SEER_SIGMOID && !(how.renormalise && top < -600.0f);      // (e^x: what 64 bits do not hold counts from the largest)
     const double z = exp_below_0(!in ? 0.0 : sigmoid ? -fabs(v) : v - (double)top);
     double s = in ? sigmoid && v > 0 ? 1.0 : z : 0.0;
-    if (how.score == SEER_SIGMOID) s /= sigmoid ? 1.0 + z : 1.0;
+    if (how.score == SEER_SIGMOID) {
+        const double q = sigmoid ? 1.0 / (1.0 + z) : 1.0;
+        s *= q;
+        if (rest) *rest = sigmoid && v > 0 ? z * q : q;
+    }
     const double sum = how.renormalise ? row_sum(s) : all;
     return (how.renormalise || how.score == SEER_SOFTMAX) && in ? s / sum : s;
-}
-
-// The same in 32 bits for the gradient.  (A quotient of its own: one choice is 1.)
-__device__ __forceinline__ float row_share(const seer_choice &how, float x, bool in, float most, float all)
-{
-    if (!how.renormalise) return !in ? 0.0f : how.score == SEER_SIGMOID ? fast_sigmoid(x) : __expf(x - most) * __builtin_amdgcn_rcpf(all);
-    float top = row_max(in ? x : -INFINITY), s;
-    if (how.score == SEER_SIGMOID) {
-        top = fminf(top, 0.0f);
-        s = x > 0 ? fast_sigmoid(x) : __expf(x - top) * __builtin_amdgcn_rcpf(1.0f + __expf(x));
-    } else
-        s = __expf(x - top);
-    s = in ? s : 0.0f;
-    const float sum = row_sum(s);
-    return in ? s / sum : 0.0f;
 }
 
 // The sum of a lane's values by halves.
@@ -548,7 +538,8 @@ __global__ __launch_bounds__(kWG) void choose_grad_rows_kernel(const T *__restri
         const T *row = logits + (int64_t)t * ld;
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) *reinterpret_cast<v4f *>(mine + (u * kRowLanes + l) * 4) = v4f{0, 0, 0, 0};
-        float p[WHOLE ? UNITS * 4 : 1], most = -INFINITY, all = 0;
+        float p[WHOLE ? UNITS * 4 : 1], most = -INFINITY;
+        double all = 0;
         if constexpr (WHOLE) {
 #pragma unroll
             for (int i = 0; i < UNITS * 4; ++i) {
@@ -558,8 +549,8 @@ __global__ __launch_bounds__(kWG) void choose_grad_rows_kernel(const T *__restri
             }
             most = row_max(most);
 #pragma unroll
-            for (int i = 0; i < UNITS * 4; ++i) all += p[i] = p[i] == -INFINITY ? -0.0f : __expf(p[i] - most);      // (-0: masked)
-            all = row_sum(all);
+            for (int i = 0; i < UNITS * 4; ++i) p[i] = p[i] == -INFINITY ? -0.0f : __expf(p[i] - most);       // (-0: masked)
+            all = row_sum((double)sum_of<UNITS * 4>([&](int i) { return p[i]; }));
         }
         int32_t e = -1;
         float x = 0, dw = 0;
@@ -572,10 +563,10 @@ __global__ __launch_bounds__(kWG) void choose_grad_rows_kernel(const T *__restri
             if (x == -INFINITY) e = -1;
         }
         const bool in = e >= 0;
-        const float share = row_share(how, x, in, most, all), part = in ? share * dw : 0.0f, sum = row_sum(part);
-        float g = how.renormalise ? part - share * sum : part;
-        if (how.score == SEER_SIGMOID) g *= fast_sigmoid(-x);
-        g = in ? how.factor * g : 0.0f;
+        double rest = 1;
+        const double share = row_share(how, x, in, most, all, &rest), part = in ? share * (double)dw : 0.0, sum = row_sum(part);
+        const double slope = (how.renormalise ? part - share * sum : part) * rest;
+        const float g = in ? (float)((double)how.factor * slope) : 0.0f;
         // an expert that comes more than once: its first lane adds up
         float of_expert = g;
         bool first = in;
@@ -589,7 +580,7 @@ __global__ __launch_bounds__(kWG) void choose_grad_rows_kernel(const T *__restri
         __builtin_amdgcn_wave_barrier();            // (a wave's LDS accesses are served in order)
         if (first) mine[e] = of_expert;
         __builtin_amdgcn_wave_barrier();
-        const float off = how.factor * sum * __builtin_amdgcn_rcpf(all);
+        const float off = WHOLE ? (float)((double)how.factor * sum / all) : 0.0f;
         const bool any = (__ballot(in) >> (lane & 48) & 0xffff) != 0;
         if (t0 + threadIdx.x / kRowLanes < tokens) {
 #pragma unroll

@@ -460,3 +460,21 @@ def test_strides_and_odd_addresses_of_four_at_a_time(E, how, kind):
             to_rows = to[by:].view(37, ld)
             assert torch.equal(S.seer_route_choose_grad(other, case, e, dw, dlogits=to_rows[:, :E]), d)
             assert bool((to_rows[:, E:] == 55).all()) and bool((to[:by] == 55).all())
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("score,renormalise", [("softmax", True), ("sigmoid", True), ("sigmoid", False)])
+@pytest.mark.parametrize("E,C", [(8, 2), (64, 8), (256, 8), (300, 15), (512, 16), (600, 8), (64, 20)], ids=str)
+def test_gradients_are_rounded_to_fp32_once(E, C, score, renormalise, kind):
+    """Computed in 64 bits (2^-40 of the magnitudes that cancel), taken to fp32 and to the type."""
+    announce(f"choose_grad rounding {E} {C} {score} {renormalise} {kind}")
+    rng = np.random.default_rng(E + C)
+    logits = rounded(rng.standard_normal((200, E)) * 3, kind)
+    logits[1] -= 150
+    x = host(logits)
+    expert = np.stack([rng.permutation(E)[:C] for _ in range(200)]).astype(np.int32)
+    dw = rng.standard_normal((200, C)).astype(np.float32)
+    d = S.seer_route_choose_grad(logits, S.Choice(C, score=score, renormalise=renormalise, factor=2.5), torch.from_numpy(expert).cuda(), torch.from_numpy(dw).cuda())
+    want, size = O.choose_grad(x, expert, dw.astype(np.float64), score=score, renormalise=renormalise, factor=2.5)
+    off = np.abs(want) * U32 + size * 2.0 ** -40 + TINY["f32"]
+    assert_within(host(d), want, off if kind == "f32" else off + (np.abs(want) + off) * ROUND[kind] + TINY[kind], "dlogits")
