@@ -484,7 +484,8 @@ static bool in_pieces(const I8Args &a)
            whole((uintptr_t)a.ldb);
 }
 
-// The arithmetic on tiles is 32-bit; of the tiles for any address, which no other kernel's launches outnumber (i8_plan), there are the most.
+// The arithmetic on tiles is 32-bit.  Of the tiles of 64 rows there may be twice as many as of these (up to 128 channels), so below 2^31, and a launch has
+// fewer than 2^24 of them (i8_plan).
 bool i8_product_fits(const I8Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, kAnyTokens, kAnyChannels) < (1u << 30); }
 
 template <class T, int WAVES, int WC, int CI, int TJ, int BUFFERS>

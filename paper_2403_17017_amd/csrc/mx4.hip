@@ -583,7 +583,8 @@ void launch_mx4_quantize(const RouteRows &rows, const seer_dense &x, const seer_
     });
 }
 
-// The arithmetic on tiles is 32-bit; of the tiles for any distance of rows, which no other kernel's launches outnumber (mx4_plan), there are the most.
+// The arithmetic on tiles is 32-bit.  Of the tiles of 64 rows there may be twice as many as of these (up to 128 channels), so below 2^31, and a launch has
+// fewer than 2^24 of them (mx4_plan).
 bool mx4_product_fits(const Mx4Args &a) { return a.groups <= SEER_MAX_EXPERTS && most_blocks(a, kMxTile, kMxTile) < (1u << 30); }
 
 template <class T, int WAVES, int WC, int CI, int TJ>
