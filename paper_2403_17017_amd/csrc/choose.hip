@@ -52,7 +52,7 @@ __device__ __forceinline__ double chosen_share(const seer_choice &how, float x, 
     return in ? s / sum : 0.0;
 }
 
-// The choice of one token by a whole wave, in 64 bits; lane l has the experts l, 64 + l, ...  16 384 tokens of 1024 experts 103 us.  s_key: LDS of the wave, [experts], with groups.
+// The choice of one token by a whole wave, in 64 bits; lane l has the experts l, 64 + l, ...  16 384 tokens of 1024 experts 102 us.  s_key: LDS of the wave, [experts], with groups.
 template <class T, int PER>
 __device__ __noinline__ void choose_exactly(const T *logits, int64_t ld, uint32_t t, uint32_t experts, const float *bias, const seer_choice &how, int32_t *expert,
                                float *weight, uint64_t *s_key)
@@ -169,11 +169,15 @@ __global__ __launch_bounds__(kWG) void choose_kernel(const T *__restrict__ logit
 // the expert's number (511); the next best is the largest word below the last one.  Keys that are made of scores are taken less the largest of them, so
 // that what is cut off is 2^-15 (2^-14) of the distance from the best.  The bounds on a score: of a sigmoid, 2^-21 (an exponential with an error
 // of 2^-23 and 1.5 |x| 2^-24 of itself, times s (1 - s), where s (1 - s) |x| < 0.23; a sum and a reciprocal, 1.5 * 2^-23); of a softmax, 2^-18 of
-// the largest (such exponentials, s |x - max| < 0.4 max s, a sum of up to 512 in 36 steps, a reciprocal and a product).  A bias adds 2^-24 of the key.
+// the largest (such exponentials, s |x - max| < 0.4 max s, a lane's sum by halves, in 64 bits from there, a reciprocal and a product).  A bias adds 2^-24 of the key.
 // Without a bias keys are logits, and exact.
 //
-// Bound by instructions: 65 536 tokens of 256 experts, eight choices, fp32: sigmoids, bias and 8 groups 55 us (190 with a wave to a token in 64
-// bits; the logits alone are read in 13), softmax without either 32; 16 411 of 160 in bf16, 8 groups 11.
+// Bound by instructions: 65 536 tokens of 256 experts, eight choices, fp32: sigmoids, bias and 8 groups 61 us (190 with a wave to a token in 64
+// bits; the logits alone are read in 13), softmax without either 29, over all experts 35; 16 411 of 160 in bf16, 8 groups 11 (46).
+//
+// As many experts and choices as the form holds (9 bits of a word number an expert, a lane of 16 takes a choice, one shows what comes next); there
+// it is still ahead.  16 384 tokens, softmax, this form and the other one: 64 experts, two choices 8.6 and 19, 15 choices 18 and 58; 256, 15 choices 21 and
+// 58; 512, 10 choices 27 and 57, 15 choices 39 and 76; one token of 512, 15 choices 5.5 and 15.  Behind, 16 choices of 512 take 80, 10 of 513 112.
 constexpr uint32_t kRowBlocks = 1024 /* as many as there is room for; a wave then goes on to other tokens */;
 constexpr uint32_t kRowLanes = 16, kFastChoices = 15, kFastExperts = 512;
 constexpr float kFar = 0x1p100f;    // above it sums of two keys, and distances from the best one, may be infinite in 32 bits
@@ -523,7 +527,8 @@ __global__ __launch_bounds__(kWG) void choose_grad_kernel(const T *__restrict__ 
 }
 
 // Four tokens to a wave: the chosen experts' gradients, one to a lane of 16, are put into a row of zeros in LDS, from where the row goes out
-// whole, four elements at a time.  UNITS of these to a lane.  Bound by bytes: 65 536 x 256 fp32 in 18 us (67 MB written), 100 with a wave to a token.
+// whole, four elements at a time.  UNITS of these to a lane.  Bound by bytes: 65 536 x 256 fp32 in 17 us (67 MB written), 91
+// with a wave to a token; WHOLE, which reads all logits, 27 (5.2 TB/s).  16 384 tokens, 16 choices of 512: 10 and 76, 10 choices of 513 57.
 template <class T, int UNITS, bool WHOLE>
 __global__ __launch_bounds__(kWG) void choose_grad_rows_kernel(const T *__restrict__ logits, int64_t ld, uint32_t tokens, uint32_t experts,
                                                                seer_choice how, const int32_t *__restrict__ expert,

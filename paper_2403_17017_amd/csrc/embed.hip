@@ -24,7 +24,8 @@ __device__ __forceinline__ uint32_t row_in_block()
 
 // ------------------------------------------------------------------ lookup
 //
-// Bound by bytes: each row is read and written once.  32 771 tokens, 131 072 x 4096 bf16: 84 us (537 MB, 6.4 TB/s).
+// Bound by bytes: each row is read and written once.  32 771 tokens, 131 072 x 4096 bf16: 87 us, 81 at least (268 MB written; of the rows, 11 000 different ones,
+// 162 MB come from memory: 4.9 to 5.3 TB/s).
 template <class T, class I, int LANES>
 __global__ __launch_bounds__(kWG) void embed_kernel(const I *__restrict__ token, uint32_t tokens, const T *__restrict__ table, int64_t ldt,
                                                     uint32_t rows, uint32_t cols, float scale, T *__restrict__ out, int64_t ldo)
@@ -153,8 +154,10 @@ __global__ __launch_bounds__(kDigitWaves * 64) void place_digits_kernel(DigitArg
     place_digits(a, token, blockIdx.x, lds, s_wave);
 }
 
-// Few tokens find their places by counting, 16 lanes to a token: the rows below its own, and its own row's tokens before it.  1031 tokens: 6.5 us
-// in one launch, sorted by digits in one workgroup 11.
+// Few tokens find their places by counting, 16 lanes to a token: the rows below its own, and its own row's tokens before it.  Every
+// token looks at all, so this grows with their square, but it is one launch.  The whole gradient, us, so and with the sort: 8009 x 1023 fp32, 1024 tokens 27 and 35, 3000
+// 40 and 42, 4096 47 and 45, 8192 66 and 49; 32 000 x 512 bf16, 1024 22 and 30, 4096 34 and 35, 6000 43 and 38; 131 072 x 64, 1024 18 and 28, 4096 33 and 35, 6000 39 and
+// 36.  Of a table whose rows are one digit the sort is two launches: 100 x 256, 1024 tokens 16 and 17, 2048 22 and 21, 4096 30 and 23.
 constexpr uint32_t kRankTokens = 4096, kRankLanes = 16;
 
 template <class I>
@@ -185,8 +188,8 @@ __global__ __launch_bounds__(kWG) void rank_pairs_kernel(const I *__restrict__ t
 //
 // Every row of the table adds up its tokens' rows of dy in the order of the tokens.  Where a row has many, sums of kRun
 // consecutive places that are all its own are made beforehand, and of kRun such sums, each by a workgroup of its own; the row then
-// takes the largest pieces that lie in its range.  1031 tokens by a power law, 1023 fp32: 8.0 us for the sums made beforehand and 17.4 for the rows
-// with runs of 16, 13.2 and 23.4 with runs of 32.
+// takes the largest pieces that lie in its range.  1031 tokens by a power law, 8009 x 1023 fp32, the whole
+// gradient: 26 us with runs of 16 (of which the sums made beforehand take 7.6 and the rows 13.4), 42 with runs of 32; 32 768 tokens, 131 072 x 4096 bf16, 287 and 290.
 constexpr uint32_t kRun = 16;
 
 struct GradArgs {
@@ -457,7 +460,9 @@ static SortPlan sort_plan(uint32_t count, uint32_t rows)
     return p;
 }
 
-// Sums of sums are worth their launch from here on: one row's tokens may be all of them.
+// Sums of sums are worth their launch from here on: one row's tokens may be all of them.  Without and with, us: all tokens of one row of 1024 bf16, 1024 tokens
+// 26 and 16, 2040 45 and 25, 4096 79 and 29; where no row has that many, the launch alone: 32 000 x 512, 1024 tokens 22.2 and 23.5, 2048 25.3 and 26.8, 8192 36 and
+// 39; 8009 x 1023 fp32 by a power law, 4096 42 and 47, 16 384 63 and 57.
 constexpr uint32_t kManyTokens = 2048;
 
 struct GradSpace { size_t pairs, counts, places, run, runs, bytes; };

@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kWG) void mx4_quantize_kernel(RouteRows r, const T 
 // ------------------------------------------------------------------ products
 //
 // For rows further apart than 32-bit offsets into a tile reach: 128 tokens x 128 channels, 8 blocks of columns at a time through registers and
-// LDS, four waves of 64 x 64 each, scales straight from memory.  8192 x 4 rows through 32 matrices of 4096 x 4096: 1500 us (tiles: 390).
+// LDS, four waves of 64 x 64 each, scales straight from memory.  8192 x 4 rows through 32 matrices of 4096 x 4096: 1500 us (tiles: 410).
 constexpr uint32_t kMxTile = 128, kMxLine = 128 /* bytes */, kMxPitch = kMxLine + 16;
 
 // 16 channels x 16 tokens x 128 columns: byte S of each scale word is the lane's.
@@ -157,10 +157,10 @@ __global__ __launch_bounds__(256) void mx4_any_kernel(Mx4Args a, uint32_t blocks
 // straight from memory into one of two LDS buffers, and from there, 4 blocks (a step) at a time, into registers while those before
 // are multiplied.  Scales come 16 blocks (a round of four steps) at a time through registers, a row to a thread, which puts the bytes in
 // the order that the matrix instructions take them in: one word of a lane has the bytes of its block in each of the four steps.
-// 8192 x 8192 x 8192: 281 us, 3.9 PFLOP/s (zeros 234; matrix instructions alone 6.4 on random codes, at the card's power).  A step takes
+// 8192 x 8192 x 8192: 281 to 300 us, 3.9 PFLOP/s at best (zeros 234; matrix instructions alone 6.4 on random codes, at the card's power).  A step takes
 // 0.96 us where they would take 0.67; without its loads 0.79.  A tile's first loads and last stores add some 12 us, which nothing
-// hides: 32 groups of 4096 x 4096, mean 1013, 390 us.  Slower: wave tiles of 128 x 128 in 512 registers (the same product 420, 448 before
-// scales were realigned late), registers for the next channels' codes besides (spilled).
+// hides: 32 groups of 4096 x 4096, mean 1013, 410 us (391 at least).  Slower: wave tiles of 128 x 128 in 512 registers (the same product 420 against 390
+// then, 448 before scales were realigned late), registers for the next channels' codes besides (spilled).
 constexpr uint32_t kTileChannels = 256, kStepBlocks = 4, kRoundSteps = 4, kLineBytes = 128;
 
 // WC x WAVES / WC waves, each of CI * 16 channels x TJ * 16 tokens.
@@ -435,8 +435,8 @@ __global__ __launch_bounds__(kWG) void mx4_join_kernel(Mx4Args a, Mx4Shared shar
 // ------------------------------------------------------------------ few rows to a group
 //
 // CI * 16 channels of one group per workgroup, whose waves each take a share of the columns; both operands come straight from memory, the
-// weights once per 64 rows, and the waves' sums meet in LDS.  Bound by the bytes of b: 8192 x 8192, one row, 9.6 us (3.7 TB/s), 64 groups of
-// 2048 x 4096 with four rows each on average 62 (4.6 TB/s).  32 channels to a workgroup: 14.8 us for the one row with its quantisation
+// weights once per 64 rows, and the waves' sums meet in LDS.  Bound by the bytes of b: 8192 x 8192, one row, 10.3 us (3.5 TB/s), 64 groups of
+// 2048 x 4096 with four rows each on average 63 (4.5 TB/s).  32 channels to a workgroup: 14.8 us for the one row with its quantisation
 // (16: 15.7), 61.8 for the groups (67.2), but 2 % slower over 300 draws; eight waves 15.0 and 99.9.
 constexpr uint32_t kMxFewRows = 64, kRoundBlocks = kRoundSteps * kStepBlocks;
 
