@@ -258,7 +258,7 @@ __device__ __forceinline__ double exp_below_0(double x)
     p = fma(p, f, 0.5);
     p = fma(p, f, 1.0);
     p = fma(p, f, 1.0);
-    return ldexp(p, (int)n);
+    return x != x ? x : ldexp(p, (int)n);               // (a NaN is no int)
 }
 
 // The weights of the experts chosen for a token, one to a lane of 16: as chosen_share, and in 64 bits as there; only the sum that a softmax over all experts
